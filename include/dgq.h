@@ -29,6 +29,10 @@
  *                          the quantized value tensor, the attention with a given
  *                          scale, self-attention over N keys, and the attention
  *                          product on V^'s integer codes by shifts and adds
+ *   dgq_kv_plan, dgq_kv_release, dgq_kv_store, dgq_kv_load, dgq_xattn_kv
+ *                          text keys and values of many requests kept in blocks of
+ *                          8-bit codes over the denoising steps, and the
+ *                          cross-attention to prompts of any lengths that reads them
  *
  * Conventions
  *   - Every tensor pointer is a DEVICE pointer unless the comment says "host".
@@ -36,7 +40,7 @@
  *     address aligned to 16 bytes (else DGQ_EALIGN).
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).
  *     The hot calls (quantize_act, linear and its variants, conv3x3_codes,
- *     quantize_value, the attentions) only enqueue work: they neither
+ *     quantize_value, the attentions, the kv calls) only enqueue work: they neither
  *     synchronise nor allocate.  The caller owns every tensor and
  *     keeps it alive until the stream has passed the call.
  *   - Return value: DGQ_OK or a negative dgq_status.  Nothing is enqueued when
@@ -533,6 +537,122 @@ int dgq_xattn_logq_intv(const float *q, const float *k, const uint8_t *v_codes,
                         const float *v_params, const float *key_bias, int32_t B, int32_t N,
                         int32_t H, int32_t d, int32_t nk, int32_t attn_bits, float *out,
                         float *scale_out, uint8_t *codes_dump, int32_t *acc_dump, void *stream);
+
+/*
+ * ---- keys and values of text kept in 8 bits, and the cross-attention that reads them ----
+ *
+ * A prompt's keys and values do not change over the denoising steps.  The calls below keep them in blocks of
+ * block_size rows ("slots"; 32, 64 or 128) that all requests of a server share, so that prompts of any lengths lie side
+ * by side, are written once and may be read by several requests (the unconditional prompt).  Request b names its blocks,
+ * in order, in row b of a table: int32 [B, width], its row r in slot r % block_size of block table[b][r / block_size].
+ * Everything a step needs stays on the device: lengths, tables and the list of free blocks are int32 tensors that
+ * kernels read and write, so a step can be captured in a graph with lengths that change between replays.
+ *
+ * What a kernel finds in these tensors is checked there, without an error: lengths below 0 count as 0 and above
+ * width * block_size as that, and a block index outside [0, n_blocks) is a block that is not there.
+ */
+typedef enum dgq_dtype { DGQ_F32 = 0, DGQ_F16 = 1, DGQ_BF16 = 2 } dgq_dtype;
+
+/* Requests that one planning call takes. */
+#define DGQ_KV_MAX_REQUESTS 4096
+
+/*
+ * Blocks and runs for new rows, on the device.  Request b holds lengths[b] rows and is to get new_rows[b] more, which lie
+ * at rows row_offsets[b] .. of the packed tensors that dgq_kv_store takes (requests in order, row_offsets the exclusive
+ * sums of new_rows; below 0 counts as 0).  A request is served if its lengths and new_rows are not negative, the table's
+ * row has room for all its rows, its rows lie within `rows`, and the free blocks reach for it and all before it; else it
+ * stays as it is.  With new_rows[b] = 0 it is served if the former hold.
+ *   rows         rows of the packed tensors (host; what counts[3] may not pass)
+ *   table        int32 [B, width]: entries of blocks that a request gets are written, no others
+ *   free_blocks  int32 [free_capacity], the first n_free[0] of them free; blocks are taken from the end, requests in
+ *                order, each one's in order.  The list itself is not changed
+ *   lengths_out [B], n_free_out [1]: the new state (not the buffers of lengths, new_rows and n_free)
+ *   row_offsets  int32 [B + 1]
+ *   runs         int32 [max_runs, 4], 16-byte aligned, max_runs >= rows / block_size + 2 B: one entry for every block that
+ *                gets rows, (block, first row in the packed tensors, first slot, rows), requests in order; (-1, 0, 0, 0)
+ *                behind them.  It is the rows' slot map with one entry a block, since a block's rows share a scale
+ *   counts       int32 [4]: runs, blocks taken, requests not served, row_offsets[B]
+ * 1 <= B <= DGQ_KV_MAX_REQUESTS, width * block_size < 2^31.  Enqueues on `stream`; neither synchronises nor allocates.
+ */
+int dgq_kv_plan(const int32_t *lengths, const int32_t *new_rows, int32_t B, int32_t block_size, int64_t rows,
+                int32_t *table, int32_t width, const int32_t *free_blocks, int32_t free_capacity,
+                const int32_t *n_free, int32_t *lengths_out, int32_t *n_free_out, int32_t *row_offsets,
+                int32_t *runs, int64_t max_runs, int32_t *counts, void *stream);
+
+/*
+ * The blocks of finished requests (done[b] != 0, u8 [B]) go to the end of the free list, requests in order, each one's
+ * blocks in order, and their lengths become 0.  free_blocks is written behind its first n_free[0] entries (what does not
+ * fit free_capacity is dropped).  lengths_out [B] and n_free_out [1] are not the buffers of lengths and n_free.  A block
+ * that several requests name goes back as often as it is named by a finished one: copy a row of the table only to
+ * requests that are not released themselves.  Enqueues on `stream`; neither synchronises nor allocates.
+ */
+int dgq_kv_release(const uint8_t *done, const int32_t *lengths, const int32_t *table, int32_t B, int32_t width,
+                   int32_t block_size, int32_t *free_blocks, int32_t free_capacity, const int32_t *n_free,
+                   int32_t *lengths_out, int32_t *n_free_out, void *stream);
+
+/*
+ * Bytes of a cache of n_blocks blocks of H heads of d dims (d a multiple of 8, at most 256); 0 for sizes that are not
+ * supported.  With S = block_size and e = d rounded up to a multiple of 16:
+ *   codes   u8 [n_blocks, H, S / 32, 64 e]: every tile of 32 slots holds K as [e / 16, 32 slots, 16 dims], then V as
+ *           [e dims, 2, 16], place i of half h being slot 4 h + i % 4 + 8 (i / 4 % 2) + 16 (i / 8).  A byte is the code
+ *           (-127 .. 127) + 128; dims from d on hold code 0
+ *   scales  fp32 [n_blocks, H, 2] behind them: of K, of V.  A row's value is code * scale, rounded once to fp32
+ * (the order in which the attention's lanes load operands of the matrix cores).  Nothing needs clearing.
+ */
+size_t dgq_kv_cache_bytes(int32_t n_blocks, int32_t block_size, int32_t H, int32_t d);
+
+/*
+ * Rows of K and V into the cache: every run puts its rows into slots slot .. slot + n - 1 of its block, K and V and every
+ * head with a scale of their own:
+ *   s = max |x| * (1/127) over the run's rows (0 if that is below 2^-96: such rows become zeros); a run that starts at a slot
+ *   above 0 continues the block: s = max(s, the block's scale), and the rows in front keep their values, code * old scale
+ *   code = clamp(rne(x * (1/s)), -127, 127)       (separate fp32 operations)
+ * Slots behind the run hold code 0 afterwards.  NaN or infinity in x makes the scale, and with it every value of the
+ * block and head, not finite.
+ *   k, v     [rows, H, d] of `dtype`, dims contiguous; row and head strides in elements, multiples of 16 bytes (so both may
+ *            be views of one projection's output), bases 16-byte aligned
+ *   runs     int32 [n_runs, 4] as dgq_kv_plan writes them, 16-byte aligned; entries with n < 1 or that point outside
+ *            the cache or the tensors are passed over.  No two runs of a call may name the same block
+ *   cache    dgq_kv_cache_bytes(...) bytes, 16-byte aligned
+ * Enqueues on `stream`; neither synchronises nor allocates.
+ */
+int dgq_kv_store(const void *k, const void *v, int32_t dtype, int64_t rows, int64_t k_row_stride,
+                 int64_t k_head_stride, int64_t v_row_stride, int64_t v_head_stride, const int32_t *runs,
+                 int64_t n_runs, void *cache, int32_t n_blocks, int32_t block_size, int32_t H, int32_t d, void *stream);
+
+/*
+ * The values that the cache holds: k, v [B, max_rows, H, d] of `dtype`, contiguous, 16-byte aligned; rows from a
+ * request's length on (and of blocks that are not there) are zeros.  What dgq_xattn_logq takes as k and v for a batch
+ * of one prompt length, and what moves a prompt elsewhere.  Enqueues on `stream`; neither synchronises nor allocates.
+ */
+int dgq_kv_load(const void *cache, int32_t n_blocks, int32_t block_size, int32_t H, int32_t d, const int32_t *table,
+                int32_t width, const int32_t *lengths, int32_t B, int32_t max_rows, int32_t dtype, void *k, void *v,
+                void *stream);
+
+/*
+ * Cross-attention to the cache: every query of request b against that request's rows,
+ *   L[i, j] = (q[i, h, :] . k[j, h / G, :]) / sqrt(d),  out[i, h, :] = sum_j softmax_j(L)[i, j] v[j, h / G, :],
+ * over j < lengths[b], with Hq = G H query heads to H cached ones.  A request without rows gives zeros.  Probabilities
+ * stay in fp32 precision (no codes): this is the attention of layers whose text is longer than dgq_xattn_logq takes, of
+ * several lengths in one batch, or kept in 8 bits.
+ *   q, out    [B, N, Hq, d] of `dtype` (q_offsets NULL: N queries for every request), or [N, Hq, d] with q_offsets int32
+ *             [B + 1] ascending: request b has rows q_offsets[b] .. q_offsets[b + 1] - 1; rows of no request keep what
+ *             out held.  dims contiguous; q's batch, row and head strides in elements, multiples of 16 bytes; out is
+ *             contiguous; both 16-byte aligned
+ *   lengths   int32 [B], table int32 [B, width]
+ *   workspace dgq_xattn_kv_workspace_bytes(...) bytes, 16-byte aligned (0 bytes: NULL): where few queries meet many rows
+ *             the rows are split over the chip and a second kernel joins the parts, which it holds
+ * fp32 queries count with 22 bits, fp16 and bf16 ones with all of theirs; probabilities are rounded to fp16 for 16-bit
+ * types and to 22 bits for fp32; sums are fp32.  A query with NaN or infinity gives NaN in its own row and head only.
+ * Hq a multiple of H, d a multiple of 8 up to 256 (DGQ_EUNSUPPORTED otherwise).  Enqueues on `stream`; neither
+ * synchronises nor allocates.
+ */
+size_t dgq_xattn_kv_workspace_bytes(int32_t B, int64_t N, int32_t packed, int32_t Hq, int32_t H, int32_t d,
+                                    int32_t width, int32_t block_size);
+int dgq_xattn_kv(const void *q, int32_t dtype, const int32_t *q_offsets, int64_t q_batch_stride, int64_t q_row_stride,
+                 int64_t q_head_stride, int32_t B, int64_t N, int32_t Hq, const void *cache, int32_t n_blocks,
+                 int32_t block_size, int32_t H, int32_t d, const int32_t *table, int32_t width,
+                 const int32_t *lengths, void *out, void *workspace, size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from collections import namedtuple
 from dataclasses import dataclass
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -93,6 +94,16 @@ def lib():
         L.dgq_selfattn_workspace_bytes.argtypes = [i32, i32, i32, i32]
         L.dgq_selfattn_workspace_bytes.restype = sz
         L.dgq_selfattn_logq.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, sz, vp]
+        L.dgq_kv_plan.argtypes = [vp, vp, i32, i32, i64, vp, i32, vp, i32, vp, vp, vp, vp, vp, i64, vp, vp]
+        L.dgq_kv_release.argtypes = [vp, vp, vp, i32, i32, i32, vp, i32, vp, vp, vp, vp]
+        L.dgq_kv_cache_bytes.argtypes = [i32, i32, i32, i32]
+        L.dgq_kv_cache_bytes.restype = sz
+        L.dgq_kv_store.argtypes = [vp, vp, i32, i64, i64, i64, i64, i64, vp, i64, vp, i32, i32, i32, i32, vp]
+        L.dgq_kv_load.argtypes = [vp, i32, i32, i32, i32, vp, i32, vp, i32, i32, i32, vp, vp, vp]
+        L.dgq_xattn_kv_workspace_bytes.argtypes = [i32, i64, i32, i32, i32, i32, i32, i32]
+        L.dgq_xattn_kv_workspace_bytes.restype = sz
+        L.dgq_xattn_kv.argtypes = [vp, i32, vp, i64, i64, i64, i32, i64, i32, vp, i32, i32, i32, i32, vp, i32, vp, vp, vp, sz,
+                                   vp]
         L.dgq_last_error.restype = C.c_char_p
         L.dgq_version.restype = C.c_int
         _lib = L
@@ -445,3 +456,70 @@ def dgq_xattn_logq_static(q, k, v, key_bias, attn_bits: int, scale_in, out=None,
     """Attention with a given prompt scale (one pass).  Returns (out, scale_out or None)."""
     return (_hot or _load_hot()).xattn_logq_static(q, k, v, key_bias, attn_bits, scale_in, out, scale_out,
                                                    codes_dump, stream)
+
+
+@dataclass
+class KVCache:
+    """Keys and values of text in 8 bits: n_blocks blocks of block_size rows, heads heads of d dims, in the uint8 device
+    tensor `data` of dgq_kv_cache_bytes() bytes (layout in include/dgq.h).  Nothing needs clearing."""
+    data: object
+    n_blocks: int
+    block_size: int
+    heads: int
+    d: int
+
+    @classmethod
+    def empty(cls, n_blocks: int, block_size: int, heads: int, d: int, device="cuda"):
+        import torch
+        nbytes = dgq_kv_cache_bytes(n_blocks, block_size, heads, d)
+        if nbytes == 0:
+            raise ValueError("no such cache: block_size is 32, 64 or 128, d a multiple of 8 up to 256")
+        return cls(torch.empty(nbytes, dtype=torch.uint8, device=device), n_blocks, block_size, heads, d)
+
+
+#: What dgq_kv_plan returns: the new lengths [B] and n_free [1], row_offsets [B + 1], runs [max_runs, 4], counts [4].
+KVPlan = namedtuple("KVPlan", "lengths n_free row_offsets runs counts")
+
+KV_MAX_REQUESTS = 4096
+
+
+def dgq_kv_cache_bytes(n_blocks: int, block_size: int, heads: int, d: int) -> int:
+    return int(lib().dgq_kv_cache_bytes(n_blocks, block_size, heads, d))
+
+
+def dgq_kv_plan(lengths, new_rows, table, free_blocks, n_free, block_size: int, rows: int, lengths_out=None,
+                n_free_out=None, row_offsets=None, runs=None, counts=None, stream=None) -> KVPlan:
+    """Blocks and runs for new_rows[b] more rows of every request (int32 device tensors; rows: of the packed K and V that
+    dgq_kv_store takes).  Fills new entries of `table` [B, width] and returns a KVPlan; what is passed is written into."""
+    return KVPlan(*(_hot or _load_hot()).kv_plan(lengths, new_rows, table, free_blocks, n_free, block_size, rows,
+                                                 lengths_out, n_free_out, row_offsets, runs, counts, stream))
+
+
+def dgq_kv_release(done, lengths, table, free_blocks, n_free, block_size: int, lengths_out=None, n_free_out=None,
+                   stream=None):
+    """Blocks of the requests with done[b] != 0 (uint8 [B]) back to the end of free_blocks.  Returns (lengths, n_free)."""
+    return (_hot or _load_hot()).kv_release(done, lengths, table, free_blocks, n_free, block_size, lengths_out,
+                                            n_free_out, stream)
+
+
+def dgq_kv_store(cache: KVCache, k, v, runs, stream=None):
+    """k, v [rows, heads, d] (fp32, fp16 or bf16; views with contiguous dims may be passed) into the cache by `runs`."""
+    (_hot or _load_hot()).kv_store(k, v, runs, cache.data, cache.n_blocks, cache.block_size, cache.heads, cache.d, stream)
+
+
+def dgq_kv_load(cache: KVCache, table, lengths, max_rows: int, dtype=None, k=None, v=None, stream=None):
+    """(k, v) [B, max_rows, heads, d] of `dtype` (fp32 by default) as the cache holds them; zeros behind a request's rows."""
+    return (_hot or _load_hot()).kv_load(cache.data, cache.n_blocks, cache.block_size, cache.heads, cache.d, table, lengths,
+                                         max_rows, dtype, k, v, stream)
+
+
+def dgq_xattn_kv_workspace_bytes(B, N, packed, Hq, heads, d, width, block_size) -> int:
+    return int(lib().dgq_xattn_kv_workspace_bytes(B, N, int(bool(packed)), Hq, heads, d, width, block_size))
+
+
+def dgq_xattn_kv(q, cache: KVCache, table, lengths, q_offsets=None, out=None, workspace=None, stream=None):
+    """Cross-attention of q [B, N, Hq, d], or packed q [rows, Hq, d] with q_offsets int32 [B + 1], to the first lengths[b]
+    rows of each request's blocks.  q: fp32, fp16 or bf16, dims contiguous; Hq a multiple of the cache's heads.  Returns
+    out, contiguous, of q's shape and type."""
+    return (_hot or _load_hot()).xattn_kv(q, cache.data, cache.n_blocks, cache.block_size, cache.heads, cache.d, table,
+                                          lengths, q_offsets, out, workspace, stream)

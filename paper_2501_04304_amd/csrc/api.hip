@@ -1256,3 +1256,154 @@ int dgq_quantize_value(const float *v, int32_t B, int32_t nk, int32_t H, int32_t
 }
 
 }  // extern "C"
+
+// ---- the 8-bit cache ----------------------------------------------------------------------------
+namespace {
+
+bool kv_sizes_ok(int32_t block_size, int32_t d) {
+    return (block_size == 32 || block_size == 64 || block_size == 128) && d >= 8 && d <= kKvMaxDim && d % 8 == 0;
+}
+
+int64_t kv_code_bytes(int32_t n_blocks, int32_t block_size, int32_t H, int32_t d) {
+    return (int64_t)n_blocks * H * kv_slice_bytes(block_size, d);
+}
+
+// The cache's parts behind one pointer; an error names the call.
+int kv_cache_of(const char *who, const void *cache, int32_t n_blocks, int32_t block_size, int32_t H, int32_t d, KvCache *out) {
+    const std::string name(who);
+    if (!cache) return fail(DGQ_EINVAL, name + ": null pointer");
+    if (n_blocks < 1 || H < 1) return fail(DGQ_EINVAL, name + ": empty cache");
+    if (!kv_sizes_ok(block_size, d))
+        return fail(DGQ_EUNSUPPORTED, name + ": needs block_size 32, 64 or 128 and d a multiple of 8 up to 256");
+    if (H > 65535) return fail(DGQ_EUNSUPPORTED, name + ": H above 65535");
+    if (!aligned16(cache)) return fail(DGQ_EALIGN, name + ": cache not 16-byte aligned");
+    uint8_t *codes = static_cast<uint8_t *>(const_cast<void *>(cache));
+    *out = {codes, reinterpret_cast<float *>(codes + kv_code_bytes(n_blocks, block_size, H, d)), n_blocks, block_size, H, d};
+    return DGQ_OK;
+}
+
+bool kv_dtype_ok(int32_t t) { return t == DGQ_F32 || t == DGQ_F16 || t == DGQ_BF16; }
+// strides that keep every row's 16-byte loads aligned
+bool kv_stride_ok(int64_t stride, int32_t dtype) { return stride >= 0 && stride % (dtype == DGQ_F32 ? 4 : 8) == 0; }
+
+int kv_table_ok(const char *who, int32_t B, int32_t width, int32_t block_size) {
+    if (B < 1 || width < 1) return fail(DGQ_EINVAL, std::string(who) + ": empty table");
+    if ((int64_t)width * block_size > INT32_MAX) return fail(DGQ_EUNSUPPORTED, std::string(who) + ": width * block_size above 2^31");
+    return DGQ_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int dgq_kv_plan(const int32_t *lengths, const int32_t *new_rows, int32_t B, int32_t block_size, int64_t rows,
+                int32_t *table, int32_t width, const int32_t *free_blocks, int32_t free_capacity,
+                const int32_t *n_free, int32_t *lengths_out, int32_t *n_free_out, int32_t *row_offsets,
+                int32_t *runs, int64_t max_runs, int32_t *counts, void *stream) {
+    if (!lengths || !new_rows || !table || !free_blocks || !n_free || !lengths_out || !n_free_out || !row_offsets || !runs || !counts)
+        return fail(DGQ_EINVAL, "dgq_kv_plan: null pointer");
+    if (block_size != 32 && block_size != 64 && block_size != 128)
+        return fail(DGQ_EUNSUPPORTED, "dgq_kv_plan: block_size must be 32, 64 or 128");
+    if (const int rc = kv_table_ok("dgq_kv_plan", B, width, block_size)) return rc;
+    if (B > kKvMaxRequests) return fail(DGQ_EUNSUPPORTED, "dgq_kv_plan: more than DGQ_KV_MAX_REQUESTS requests");
+    if (rows < 0 || free_capacity < 1) return fail(DGQ_EINVAL, "dgq_kv_plan: rows below 0 or no room in the free list");
+    if (rows > INT32_MAX || max_runs > INT32_MAX) return fail(DGQ_EUNSUPPORTED, "dgq_kv_plan: rows or max_runs above 2^31 - 1");
+    if (lengths_out == lengths || lengths_out == new_rows || n_free_out == n_free)
+        return fail(DGQ_EINVAL, "dgq_kv_plan: the new state needs buffers of its own");
+    if (max_runs < rows / block_size + 2 * (int64_t)B)
+        return fail(DGQ_ESHAPE, "dgq_kv_plan: max_runs below rows / block_size + 2 B");
+    if (!aligned16(runs)) return fail(DGQ_EALIGN, "dgq_kv_plan: runs not 16-byte aligned");
+    DGQ_HIP(launch_kv_plan(lengths, new_rows, B, block_size, rows, table, width, free_blocks, free_capacity, n_free, lengths_out,
+                           n_free_out, row_offsets, runs, (int32_t)max_runs, counts, static_cast<hipStream_t>(stream)));
+    return DGQ_OK;
+}
+
+int dgq_kv_release(const uint8_t *done, const int32_t *lengths, const int32_t *table, int32_t B, int32_t width,
+                   int32_t block_size, int32_t *free_blocks, int32_t free_capacity, const int32_t *n_free,
+                   int32_t *lengths_out, int32_t *n_free_out, void *stream) {
+    if (!done || !lengths || !table || !free_blocks || !n_free || !lengths_out || !n_free_out)
+        return fail(DGQ_EINVAL, "dgq_kv_release: null pointer");
+    if (block_size != 32 && block_size != 64 && block_size != 128)
+        return fail(DGQ_EUNSUPPORTED, "dgq_kv_release: block_size must be 32, 64 or 128");
+    if (const int rc = kv_table_ok("dgq_kv_release", B, width, block_size)) return rc;
+    if (B > kKvMaxRequests) return fail(DGQ_EUNSUPPORTED, "dgq_kv_release: more than DGQ_KV_MAX_REQUESTS requests");
+    if (free_capacity < 1) return fail(DGQ_EINVAL, "dgq_kv_release: no room in the free list");
+    if (lengths_out == lengths || n_free_out == n_free)
+        return fail(DGQ_EINVAL, "dgq_kv_release: the new state needs buffers of its own");
+    DGQ_HIP(launch_kv_release(done, lengths, table, B, width, block_size, free_blocks, free_capacity, n_free, lengths_out,
+                              n_free_out, static_cast<hipStream_t>(stream)));
+    return DGQ_OK;
+}
+
+size_t dgq_kv_cache_bytes(int32_t n_blocks, int32_t block_size, int32_t H, int32_t d) {
+    if (n_blocks < 1 || H < 1 || H > 65535 || !kv_sizes_ok(block_size, d)) return 0;
+    return (size_t)kv_code_bytes(n_blocks, block_size, H, d) + (size_t)n_blocks * H * 2 * sizeof(float);
+}
+
+int dgq_kv_store(const void *k, const void *v, int32_t dtype, int64_t rows, int64_t k_row_stride,
+                 int64_t k_head_stride, int64_t v_row_stride, int64_t v_head_stride, const int32_t *runs,
+                 int64_t n_runs, void *cache, int32_t n_blocks, int32_t block_size, int32_t H, int32_t d, void *stream) {
+    KvCache c;
+    if (const int rc = kv_cache_of("dgq_kv_store", cache, n_blocks, block_size, H, d, &c)) return rc;
+    if (!kv_dtype_ok(dtype)) return fail(DGQ_EINVAL, "dgq_kv_store: bad dtype");
+    if (rows < 0 || n_runs < 0) return fail(DGQ_EINVAL, "dgq_kv_store: sizes below 0");
+    if (rows == 0 || n_runs == 0) return DGQ_OK;
+    if (!k || !v || !runs) return fail(DGQ_EINVAL, "dgq_kv_store: null pointer");
+    if (rows > INT32_MAX || n_runs > INT32_MAX) return fail(DGQ_EUNSUPPORTED, "dgq_kv_store: rows or n_runs above 2^31 - 1");
+    if (!kv_stride_ok(k_row_stride, dtype) || !kv_stride_ok(k_head_stride, dtype) || !kv_stride_ok(v_row_stride, dtype) ||
+        !kv_stride_ok(v_head_stride, dtype))
+        return fail(DGQ_EALIGN, "dgq_kv_store: strides must be multiples of 16 bytes, not negative");
+    if (!aligned16(k) || !aligned16(v) || !aligned16(runs)) return fail(DGQ_EALIGN, "dgq_kv_store: tensor not 16-byte aligned");
+    DGQ_HIP(launch_kv_store(k, v, dtype, rows, k_row_stride, k_head_stride, v_row_stride, v_head_stride, runs, (int32_t)n_runs, c,
+                            static_cast<hipStream_t>(stream)));
+    return DGQ_OK;
+}
+
+int dgq_kv_load(const void *cache, int32_t n_blocks, int32_t block_size, int32_t H, int32_t d, const int32_t *table,
+                int32_t width, const int32_t *lengths, int32_t B, int32_t max_rows, int32_t dtype, void *k, void *v,
+                void *stream) {
+    KvCache c;
+    if (const int rc = kv_cache_of("dgq_kv_load", cache, n_blocks, block_size, H, d, &c)) return rc;
+    if (const int rc = kv_table_ok("dgq_kv_load", B, width, block_size)) return rc;
+    if (!kv_dtype_ok(dtype) || max_rows < 0) return fail(DGQ_EINVAL, "dgq_kv_load: bad dtype, or max_rows below 0");
+    if (max_rows == 0) return DGQ_OK;
+    if (!table || !lengths || !k || !v) return fail(DGQ_EINVAL, "dgq_kv_load: null pointer");
+    if (B > 65535) return fail(DGQ_EUNSUPPORTED, "dgq_kv_load: B above 65535");
+    if (!aligned16(k) || !aligned16(v)) return fail(DGQ_EALIGN, "dgq_kv_load: tensor not 16-byte aligned");
+    DGQ_HIP(launch_kv_load(c, table, width, lengths, B, max_rows, dtype, k, v, static_cast<hipStream_t>(stream)));
+    return DGQ_OK;
+}
+
+size_t dgq_xattn_kv_workspace_bytes(int32_t B, int64_t N, int32_t packed, int32_t Hq, int32_t H, int32_t d,
+                                    int32_t width, int32_t block_size) {
+    if (B < 1 || N < 1 || H < 1 || Hq < H || Hq % H || width < 1 || !kv_sizes_ok(block_size, d)) return 0;
+    return xattn_kv_workspace_bytes(B, packed ? N : (int64_t)B * N, packed != 0, Hq, H, d, (int64_t)width * block_size);
+}
+
+int dgq_xattn_kv(const void *q, int32_t dtype, const int32_t *q_offsets, int64_t q_batch_stride, int64_t q_row_stride,
+                 int64_t q_head_stride, int32_t B, int64_t N, int32_t Hq, const void *cache, int32_t n_blocks,
+                 int32_t block_size, int32_t H, int32_t d, const int32_t *table, int32_t width,
+                 const int32_t *lengths, void *out, void *workspace, size_t workspace_bytes, void *stream) {
+    KvCache c;
+    if (const int rc = kv_cache_of("dgq_xattn_kv", cache, n_blocks, block_size, H, d, &c)) return rc;
+    if (const int rc = kv_table_ok("dgq_xattn_kv", B, width, block_size)) return rc;
+    if (!kv_dtype_ok(dtype)) return fail(DGQ_EINVAL, "dgq_xattn_kv: bad dtype");
+    if (N < 0 || Hq < 1) return fail(DGQ_EINVAL, "dgq_xattn_kv: empty tensor");
+    if (Hq % H) return fail(DGQ_EUNSUPPORTED, "dgq_xattn_kv: query heads must be a multiple of the cached ones");
+    if (N == 0) return DGQ_OK;
+    if (!q || !table || !lengths || !out) return fail(DGQ_EINVAL, "dgq_xattn_kv: null pointer");
+    // the grid: at most one workgroup for every 8 rows of (query, head), and one a request and head more
+    if (N > INT32_MAX || (q_offsets ? N : N * B) > INT32_MAX / Hq || B > INT32_MAX / Hq)
+        return fail(DGQ_EUNSUPPORTED, "dgq_xattn_kv: more than 2^31 rows of queries and heads");
+    if (!kv_stride_ok(q_batch_stride, dtype) || !kv_stride_ok(q_row_stride, dtype) || !kv_stride_ok(q_head_stride, dtype))
+        return fail(DGQ_EALIGN, "dgq_xattn_kv: strides must be multiples of 16 bytes, not negative");
+    if (!aligned16(q) || !aligned16(out)) return fail(DGQ_EALIGN, "dgq_xattn_kv: tensor not 16-byte aligned");
+    const KvQueries in{q, q_offsets, q_batch_stride, q_row_stride, q_head_stride, dtype, B, (int32_t)N, Hq};
+    const size_t need = xattn_kv_workspace_bytes(B, in.rows(), q_offsets != nullptr, Hq, H, d, (int64_t)width * block_size);
+    if (need && (!workspace || workspace_bytes < need || !aligned16(workspace)))
+        return fail(DGQ_EWORKSPACE, "dgq_xattn_kv: workspace missing, too small or misaligned");
+    DGQ_HIP(launch_xattn_kv(in, c, table, width, lengths, out, workspace, static_cast<hipStream_t>(stream)));
+    return DGQ_OK;
+}
+
+}  // extern "C"

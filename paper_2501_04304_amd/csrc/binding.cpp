@@ -9,7 +9,9 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/hip/HIPGuard.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -433,6 +435,252 @@ PyObject *selfattn_logq(Args a) {
     return one(a[5], out);
 }
 
+// ---- the 8-bit cache ----
+
+// A call's device and stream: its tensors lie on one device, which is current while it runs; what it allocates belongs to
+// the stream that it enqueues on, so a workspace that is dropped on return is not handed out before that work is done.
+class Place {
+public:
+    Place(PyObject *stream, const at::Tensor &first)
+        : device_(first.device()), guard_(device_), on_(given(stream) ? external(stream) : c10::hip::getCurrentHIPStream(device_.index())) {}
+    void *stream() const { return stream_.stream(); }
+    void same(const at::Tensor &t, const char *name) const {
+        if (t.device() == device_) return;
+        PyErr_Format(PyExc_ValueError, "%s is on another device", name);
+        throw Raised();
+    }
+
+private:
+    c10::hip::HIPStream external(PyObject *stream) const {
+        return c10::hip::getStreamFromExternal(static_cast<hipStream_t>(stream_of(stream)), device_.index());
+    }
+    const c10::Device device_;
+    const c10::DeviceGuard guard_;
+    const c10::hip::HIPStreamGuard on_;
+    const c10::hip::HIPStream stream_ = c10::hip::getCurrentHIPStream(device_.index());
+};
+
+int32_t kv_dtype(at::ScalarType t) {
+    return t == at::kFloat ? DGQ_F32 : t == at::kHalf ? DGQ_F16 : t == at::kBFloat16 ? DGQ_BF16 : -1;
+}
+
+const at::Tensor &floats(PyObject *o, const char *name, int64_t dims) {
+    if (THPVariable_Check(o)) {
+        const at::Tensor &v = THPVariable_Unpack(o);
+        if (v.is_cuda() && kv_dtype(v.scalar_type()) >= 0) {
+            if (v.dim() != dims) {
+                PyErr_Format(PyExc_ValueError, "%s must have %lld dimensions", name, (long long)dims);
+                throw Raised();
+            }
+            if (v.numel() == 0 || v.size(-1) == 1 || v.stride(-1) == 1) return v;
+        }
+    }
+    PyErr_Format(PyExc_TypeError, "%s must be a CUDA tensor of float32, float16 or bfloat16 with contiguous dims", name);
+    throw Raised();
+}
+// the stride of a dimension of one entry says nothing
+int64_t step(const at::Tensor &t, int64_t dim) { return t.size(dim) > 1 ? t.stride(dim) : 0; }
+
+const at::Tensor &ints(PyObject *o, const char *name, std::initializer_list<int64_t> shape) {
+    const at::Tensor &t = tensor(o, at::kInt, name);
+    if (!shape_is(t, shape)) {
+        PyErr_Format(PyExc_ValueError, "%s has the wrong shape", name);
+        throw Raised();
+    }
+    return t;
+}
+at::Tensor ints_or_new(PyObject *o, const char *name, std::initializer_list<int64_t> shape, const Place &place, const at::Tensor &like) {
+    if (!given(o)) return empty(at::IntArrayRef(shape.begin(), shape.size()), at::kInt, like);
+    const at::Tensor &t = ints(o, name, shape);
+    place.same(t, name);
+    return t;
+}
+
+// The block table and what goes with it; B and width from its shape.
+struct KvTable {
+    const at::Tensor &table;
+    int32_t B = 0, width = 0;
+    explicit KvTable(PyObject *o) : table(tensor(o, at::kInt, "table")) {
+        if (table.dim() != 2 || table.size(0) > INT32_MAX || table.size(1) > INT32_MAX) raise_value("table must be [B, width]");
+        B = (int32_t)table.size(0), width = (int32_t)table.size(1);
+    }
+};
+
+// (data, n_blocks, block_size, heads, d) from a[0]
+struct KvCacheIn {
+    const at::Tensor &data;
+    int32_t n_blocks, block_size, heads, d;
+    explicit KvCacheIn(Args a)
+        : data(tensor(a[0], at::kByte, "cache.data")), n_blocks(integer32(a[1])), block_size(integer32(a[2])),
+          heads(integer32(a[3])), d(integer32(a[4])) {
+        holds(data, (int64_t)dgq_kv_cache_bytes(n_blocks, block_size, heads, d), "cache.data");
+    }
+};
+
+// (lengths, new_rows, table, free_blocks, n_free, block_size, rows, lengths_out, n_free_out, row_offsets, runs, counts, stream)
+PyObject *kv_plan(Args a) {
+    const KvTable t(a[2]);
+    const Place place(a[12], t.table);
+    const at::Tensor &lengths = ints(a[0], "lengths", {t.B}), &more = ints(a[1], "new_rows", {t.B});
+    const at::Tensor &list = tensor(a[3], at::kInt, "free_blocks"), &n_free = ints(a[4], "n_free", {1});
+    if (list.dim() != 1 || list.numel() > INT32_MAX) raise_value("free_blocks must be [capacity]");
+    place.same(lengths, "lengths"), place.same(more, "new_rows"), place.same(list, "free_blocks"), place.same(n_free, "n_free");
+    const int32_t S = integer32(a[5]);
+    const int64_t rows = integer(a[6]);
+    int64_t max_runs = 2 * (int64_t)t.B + (S > 0 && rows > 0 ? rows / S : 0);
+    if (given(a[10])) {
+        const at::Tensor &r = tensor(a[10], at::kInt, "runs");
+        if (r.dim() != 2 || r.size(1) != 4) raise_value("runs must be [max_runs, 4]");
+        max_runs = r.size(0);
+    }
+    if (max_runs > INT32_MAX) raise_value("rows is too large");
+    const at::Tensor lengths2 = ints_or_new(a[7], "lengths_out", {t.B}, place, lengths);
+    const at::Tensor n_free2 = ints_or_new(a[8], "n_free_out", {1}, place, lengths);
+    const at::Tensor offsets = ints_or_new(a[9], "row_offsets", {t.B + (int64_t)1}, place, lengths);
+    const at::Tensor runs = ints_or_new(a[10], "runs", {max_runs, 4}, place, lengths);
+    const at::Tensor counts = ints_or_new(a[11], "counts", {4}, place, lengths);
+    const int32_t *lp = pointer<int32_t>(lengths), *mp = pointer<int32_t>(more), *fp = pointer<int32_t>(list), *np = pointer<int32_t>(n_free);
+    int32_t *tp = pointer<int32_t>(t.table), *l2 = pointer<int32_t>(lengths2), *n2 = pointer<int32_t>(n_free2);
+    int32_t *op = pointer<int32_t>(offsets), *rp = pointer<int32_t>(runs), *cp = pointer<int32_t>(counts);
+    enqueue([&] {
+        return dgq_kv_plan(lp, mp, t.B, S, rows, tp, t.width, fp, (int32_t)list.numel(), np, l2, n2, op, rp, max_runs, cp, place.stream());
+    });
+    PyObject *r = PyTuple_New(5);
+    if (!r) throw Raised();
+    try {
+        PyTuple_SET_ITEM(r, 0, one(a[7], lengths2));
+        PyTuple_SET_ITEM(r, 1, one(a[8], n_free2));
+        PyTuple_SET_ITEM(r, 2, one(a[9], offsets));
+        PyTuple_SET_ITEM(r, 3, one(a[10], runs));
+        PyTuple_SET_ITEM(r, 4, one(a[11], counts));
+    } catch (...) {
+        Py_DECREF(r);
+        throw;
+    }
+    return r;
+}
+
+// (done, lengths, table, free_blocks, n_free, block_size, lengths_out, n_free_out, stream)
+PyObject *kv_release(Args a) {
+    const KvTable t(a[2]);
+    const Place place(a[8], t.table);
+    const at::Tensor &done = tensor(a[0], at::kByte, "done"), &lengths = ints(a[1], "lengths", {t.B});
+    if (!shape_is(done, {t.B})) raise_value("done has the wrong shape");
+    const at::Tensor &list = tensor(a[3], at::kInt, "free_blocks"), &n_free = ints(a[4], "n_free", {1});
+    if (list.dim() != 1 || list.numel() > INT32_MAX) raise_value("free_blocks must be [capacity]");
+    place.same(done, "done"), place.same(lengths, "lengths"), place.same(list, "free_blocks"), place.same(n_free, "n_free");
+    const int32_t S = integer32(a[5]);
+    const at::Tensor lengths2 = ints_or_new(a[6], "lengths_out", {t.B}, place, lengths);
+    const at::Tensor n_free2 = ints_or_new(a[7], "n_free_out", {1}, place, lengths);
+    const uint8_t *dp = pointer<uint8_t>(done);
+    const int32_t *lp = pointer<int32_t>(lengths), *tp = pointer<int32_t>(t.table), *np = pointer<int32_t>(n_free);
+    int32_t *fp = pointer<int32_t>(list), *l2 = pointer<int32_t>(lengths2), *n2 = pointer<int32_t>(n_free2);
+    enqueue([&] {
+        return dgq_kv_release(dp, lp, tp, t.B, t.width, S, fp, (int32_t)list.numel(), np, l2, n2, place.stream());
+    });
+    return pair(a[6], lengths2, a[7], n_free2);
+}
+
+// (k, v, runs, data, n_blocks, block_size, heads, d, stream)
+PyObject *kv_store(Args a) {
+    const KvCacheIn c(a + 3);
+    const Place place(a[8], c.data);
+    const at::Tensor &k = floats(a[0], "k", 3), &v = floats(a[1], "v", 3), &runs = tensor(a[2], at::kInt, "runs");
+    if (k.scalar_type() != v.scalar_type()) raise_value("k and v differ in type");
+    if (k.sizes() != v.sizes() || k.size(1) != c.heads || k.size(2) != c.d) raise_value("k / v must be [rows, heads, d] of the cache");
+    if (runs.dim() != 2 || runs.size(1) != 4) raise_value("runs must be [n_runs, 4]");
+    place.same(k, "k"), place.same(v, "v"), place.same(runs, "runs");
+    const void *kp = k.data_ptr(), *vp = v.data_ptr();
+    void *cp = c.data.data_ptr();
+    const int32_t *rp = pointer<int32_t>(runs), t = kv_dtype(k.scalar_type());
+    enqueue([&] {
+        return dgq_kv_store(kp, vp, t, k.size(0), step(k, 0), step(k, 1), step(v, 0), step(v, 1), rp, runs.size(0), cp,
+                            c.n_blocks, c.block_size, c.heads, c.d, place.stream());
+    });
+    Py_RETURN_NONE;
+}
+
+// (data, n_blocks, block_size, heads, d, table, lengths, max_rows, dtype, k, v, stream)
+PyObject *kv_load(Args a) {
+    const KvCacheIn c(a);
+    const Place place(a[11], c.data);
+    const KvTable t(a[5]);
+    const at::Tensor &lengths = ints(a[6], "lengths", {t.B});
+    place.same(t.table, "table"), place.same(lengths, "lengths");
+    const int32_t max_rows = integer32(a[7]);
+    if (max_rows < 0) raise_value("max_rows is below 0");
+    at::ScalarType type = at::kFloat;
+    if (given(a[8])) {
+        if (!THPDtype_Check(a[8])) raise(PyExc_TypeError, "dtype must be a torch.dtype");
+        type = reinterpret_cast<THPDtype *>(a[8])->scalar_type;
+    } else if (given(a[9]) && THPVariable_Check(a[9])) {
+        type = THPVariable_Unpack(a[9]).scalar_type();
+    }
+    if (kv_dtype(type) < 0) raise_value("dtype must be float32, float16 or bfloat16");
+    at::Tensor out[2];
+    for (int i = 0; i < 2; ++i) {
+        const char *name = i ? "v" : "k";
+        if (!given(a[9 + i])) {
+            out[i] = empty({t.B, max_rows, c.heads, c.d}, type, c.data);
+            continue;
+        }
+        out[i] = floats(a[9 + i], name, 4);
+        place.same(out[i], name);
+        if (!shape_is(out[i], {t.B, max_rows, c.heads, c.d}) || out[i].scalar_type() != type || !out[i].is_contiguous())
+            raise_value("k / v must be contiguous [B, max_rows, heads, d] of dtype");
+    }
+    const void *cp = c.data.data_ptr();
+    void *kp = out[0].data_ptr(), *vp = out[1].data_ptr();
+    const int32_t *tp = pointer<int32_t>(t.table), *lp = pointer<int32_t>(lengths);
+    enqueue([&] {
+        return dgq_kv_load(cp, c.n_blocks, c.block_size, c.heads, c.d, tp, t.width, lp, t.B, max_rows, kv_dtype(type), kp, vp, place.stream());
+    });
+    return pair(a[9], out[0], a[10], out[1]);
+}
+
+// (q, data, n_blocks, block_size, heads, d, table, lengths, q_offsets, out, workspace, stream)
+PyObject *xattn_kv(Args a) {
+    const KvCacheIn c(a + 1);
+    const Place place(a[11], c.data);
+    const KvTable t(a[6]);
+    const at::Tensor &lengths = ints(a[7], "lengths", {t.B});
+    const bool packed = given(a[8]);
+    const at::Tensor &q = floats(a[0], "q", packed ? 3 : 4);
+    const int64_t N = q.size(packed ? 0 : 1), Hq = q.size(packed ? 1 : 2);
+    if ((!packed && q.size(0) != t.B) || q.size(-1) != c.d || Hq > INT32_MAX || Hq < 1)
+        raise_value("q must be [B, N, heads, d], or [rows, heads, d] with q_offsets");
+    const int32_t *op = packed ? pointer<int32_t>(ints(a[8], "q_offsets", {t.B + (int64_t)1})) : nullptr;
+    if (packed) place.same(THPVariable_Unpack(a[8]), "q_offsets");
+    place.same(q, "q"), place.same(t.table, "table"), place.same(lengths, "lengths");
+    at::Tensor out;
+    if (given(a[9])) {
+        out = floats(a[9], "out", packed ? 3 : 4);
+        place.same(out, "out");
+        if (out.sizes() != q.sizes() || out.scalar_type() != q.scalar_type() || !out.is_contiguous())
+            raise_value("out must be contiguous, of q's shape and type");
+    } else {
+        out = empty(q.sizes(), q.scalar_type(), q);
+    }
+    at::Tensor ws;
+    if (given(a[10])) {
+        if (!THPVariable_Check(a[10])) raise(PyExc_TypeError, "workspace must be a tensor");
+        ws = tensor(a[10], at::kByte, "workspace");
+        place.same(ws, "workspace");
+    } else if (const size_t need = dgq_xattn_kv_workspace_bytes(t.B, N, packed, (int32_t)Hq, c.heads, c.d, t.width, c.block_size)) {
+        ws = empty({(int64_t)need}, at::kByte, q);
+    }
+    void *wp = ws.defined() ? ws.data_ptr() : nullptr, *yp = out.data_ptr();
+    const size_t wb = ws.defined() ? (size_t)ws.numel() : 0;
+    const void *qp = q.data_ptr(), *cp = c.data.data_ptr();
+    const int32_t *tp = pointer<int32_t>(t.table), *lp = pointer<int32_t>(lengths), type = kv_dtype(q.scalar_type());
+    const int64_t sb = packed ? 0 : step(q, 0), sn = step(q, packed ? 0 : 1), sh = step(q, packed ? 1 : 2);
+    enqueue([&] {
+        return dgq_xattn_kv(qp, type, op, sb, sn, sh, t.B, N, (int32_t)Hq, cp, c.n_blocks, c.block_size, c.heads, c.d, tp, t.width, lp,
+                            yp, wp, wb, place.stream());
+    });
+    return one(a[9], out);
+}
+
 template <PyObject *(*F)(Args), int NARGS>
 PyObject *call(PyObject *, Args a, Py_ssize_t n) {
     if (n != NARGS) {
@@ -466,6 +714,11 @@ PyMethodDef kMethods[] = {
     DGQ_METHOD(xattn_logq, 10),
     DGQ_METHOD(xattn_logq_static, 10),
     DGQ_METHOD(selfattn_logq, 10),
+    DGQ_METHOD(kv_plan, 13),
+    DGQ_METHOD(kv_release, 9),
+    DGQ_METHOD(kv_store, 9),
+    DGQ_METHOD(kv_load, 12),
+    DGQ_METHOD(xattn_kv, 12),
     {"set_error_class", set_error_class, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };

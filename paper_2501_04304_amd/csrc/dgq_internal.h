@@ -135,6 +135,28 @@ enum TuneKey { kTuneLinearCfg = 0, kTuneSuperRows, kTuneQuantRows, kTuneXattnWgs
 int tuning_value(int key);
 #endif
 
+// ---- the 8-bit cache of keys and values (layout in include/dgq.h, dgq_kv_store) ------------------
+// Slots are kept in tiles of 32, one row block of the 32 x 32 matrix instructions: 32 e bytes of K, then 32 e of V
+// (e: the head width rounded up to 16).
+struct KvCache {
+    uint8_t *codes;  // [n_blocks, H, S / 32, 64 e]
+    float *scales;   // [n_blocks, H, 2]: K, V
+    int32_t n_blocks, S, H, d;
+};
+constexpr int kKvMaxRequests = 4096;          // what the planner's LDS holds
+constexpr int kKvMaxDim = 256;
+constexpr float kKvLeastScale = 0x1p-96f;     // a block whose scale would be below it holds zeros
+__host__ __device__ inline int kv_padded(int d) { return (d + 15) & ~15; }
+__host__ __device__ inline int64_t kv_slice_bytes(int S, int d) { return (int64_t)S * 2 * kv_padded(d); }
+// slot of place i (0 .. 15) of half h of a V row: the order in which a lane of the matrix cores' half h holds the
+// products of 32 keys (rows 8 j + 4 h + 0 .. 3 of a 32 x 32 result)
+__host__ __device__ inline int kv_slot(int h, int i) { return 4 * h + (i & 3) + 8 * ((i >> 2) & 1) + 16 * (i >> 3); }
+// bytes of (slot, dim) in a tile's two parts
+__host__ __device__ inline int kv_k_byte(int slot, int e) { return ((e >> 4) * 32 + slot) * 16 + (e & 15); }
+__host__ __device__ inline int kv_v_byte(int slot, int e) {
+    return e * 32 + ((slot >> 2) & 1) * 16 + (slot & 3) + ((slot >> 3) & 1) * 4 + (slot >> 4) * 8;
+}
+
 // ---- kernel launchers (each returns a hipError_t from the launch) ----------
 
 // Per-row max and min of x [rows, C].
@@ -212,6 +234,32 @@ hipError_t launch_selfattn(const float *q, const float *k, const float *v, int32
                            int32_t H, int32_t d, int32_t bits, const float *scale_in, float *out,
                            float *scale_out, uint8_t *codes_dump, void *workspace, hipStream_t st);
 size_t selfattn_workspace_bytes(int32_t B, int32_t N, int32_t H, int32_t d);
+
+// The 8-bit cache: block planning, writing, reading back, and the attention that reads it.
+hipError_t launch_kv_plan(const int32_t *lengths, const int32_t *new_rows, int32_t B, int32_t S, int64_t rows,
+                          int32_t *table, int32_t width, const int32_t *free_blocks, int32_t free_capacity,
+                          const int32_t *n_free, int32_t *lengths_out, int32_t *n_free_out, int32_t *row_offsets,
+                          int32_t *runs, int32_t max_runs, int32_t *counts, hipStream_t st);
+hipError_t launch_kv_release(const uint8_t *done, const int32_t *lengths, const int32_t *table, int32_t B, int32_t width,
+                             int32_t S, int32_t *free_blocks, int32_t free_capacity, const int32_t *n_free,
+                             int32_t *lengths_out, int32_t *n_free_out, hipStream_t st);
+hipError_t launch_kv_store(const void *k, const void *v, int32_t dtype, int64_t rows, int64_t k_row, int64_t k_head,
+                           int64_t v_row, int64_t v_head, const int32_t *runs, int32_t n_runs, const KvCache &c,
+                           hipStream_t st);
+hipError_t launch_kv_load(const KvCache &c, const int32_t *table, int32_t width, const int32_t *lengths, int32_t B,
+                          int32_t max_rows, int32_t dtype, void *k, void *v, hipStream_t st);
+
+// q_offsets null: request b has rows [b N, b N + N) of q; else N is the number of all rows.  Strides in elements.
+struct KvQueries {
+    const void *q;
+    const int32_t *offsets;
+    int64_t batch, row, head;
+    int32_t dtype, B, N, Hq;
+    __host__ __device__ int64_t rows() const { return offsets ? N : (int64_t)B * N; }
+};
+size_t xattn_kv_workspace_bytes(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t Hkv, int32_t d, int64_t slots);
+hipError_t launch_xattn_kv(const KvQueries &q, const KvCache &c, const int32_t *table, int32_t width,
+                           const int32_t *lengths, void *out, void *workspace, hipStream_t st);
 
 size_t xattn_workspace_bytes(int32_t B, int32_t N, int32_t H, int32_t d, int32_t nk);
 // the least the attention can work with (the row statistics alone; its maximum then goes
