@@ -24,6 +24,7 @@ typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 typedef float float2v __attribute__((ext_vector_type(2)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float float8v __attribute__((ext_vector_type(8)));
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -38,7 +39,8 @@ struct AttnArgs {
     const int32_t *table, *lengths;
     void *out;
     float *part;     // splits > 1: [splits][rows * Hq][d], then (M, D) [splits][rows * Hq][2]
-    int32_t width, G, splits, tiles;  // tiles: row tiles of all requests together (a bound when packed)
+    int32_t width, G, tiles;  // tiles: row tiles of all requests together (a bound when packed)
+    int32_t splits, chunk;    // a split is `chunk` tiles of 32 slots; as many as the table's width could fill
 };
 
 // 8 bytes (code + 128) -> 8 fp16: 0x6400 | byte is 1024 + byte exactly.
@@ -74,18 +76,30 @@ __device__ void store4(T *p, float a, float b, float c, float d) {
     *reinterpret_cast<vec *>(p) = vec{(T)a, (T)b, (T)c, (T)d};
 }
 
-struct Rows {  // of one request
+struct Rows {  // a row tile of one request; a row is a query and one of the G heads that share a cached head
     int32_t b;
-    int64_t first;  // of all queries' rows
-    int32_t n;      // queries
+    int64_t first;  // first query of the request among all
+    int32_t n;      // its queries; 0: there is no such tile
     int32_t tile;   // row tile within the request
+    // row `m` of the request
+    __device__ bool has(const AttnArgs &a, int64_t m) const { return m < (int64_t)n * a.G; }
+    __device__ const void *query(const AttnArgs &a, int h, int64_t m, int size) const {
+        const int64_t i = m / a.G, head = (int64_t)h * a.G + (m - i * a.G);
+        const int64_t at = a.q.offsets ? (first + i) * a.q.row : b * a.q.batch + i * a.q.row;
+        return static_cast<const char *>(a.q.q) + (at + head * a.q.head) * size;
+    }
+    __device__ int64_t out(const AttnArgs &a, int h, int64_t m) const {
+        const int64_t i = m / a.G;
+        return (first + i) * a.q.Hq + (int64_t)h * a.G + (m - i * a.G);
+    }
 };
 
-// The request that row tile `t` belongs to; n = 0: none.
+// The request that row tile `t` (of R rows) belongs to.
+template <int R>
 __device__ Rows find_rows(const AttnArgs &a, int32_t t) {
     const int lane = threadIdx.x & 63;
     if (!a.q.offsets) {
-        const int32_t per = (int32_t)(((int64_t)a.q.N * a.G + 31) / 32);
+        const int32_t per = (int32_t)(((int64_t)a.q.N * a.G + R - 1) / R);
         const int32_t b = t / per;
         return {b, (int64_t)b * a.q.N, a.q.N, t - b * per};
     }
@@ -97,7 +111,7 @@ __device__ Rows find_rows(const AttnArgs &a, int32_t t) {
             lo = min(max(a.q.offsets[b], 0), a.q.N);
             n = max(min(a.q.offsets[b + 1], a.q.N) - lo, 0);
         }
-        const int64_t mine = ((int64_t)n * a.G + 31) / 32;
+        const int64_t mine = ((int64_t)n * a.G + R - 1) / R;
         int64_t ends = mine;
         for (int o = 1; o < 64; o <<= 1) {
             const int64_t x = __shfl_up(ends, o);
@@ -113,69 +127,129 @@ __device__ Rows find_rows(const AttnArgs &a, int32_t t) {
     return {0, 0, 0, 0};
 }
 
-__device__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ float other_half(float x) { return __shfl_xor(x, 32); }
+__device__ int32_t tiles_of(const AttnArgs &a, int32_t b) {  // of 32 slots
+    return (int32_t)((min((int64_t)max(a.lengths[b], 0), (int64_t)a.width * a.c.S) + 31) / 32);
+}
 
-// One wavefront: 32 rows (a row is a query and one of the G heads that share a cached head) against the tiles of one
-// split of the request's rows.  S^T = K Q^T and O^T = V^T P^T on 32 x 32 x 16 instructions: a lane holds column
-// (lane & 31) of both, so a row's statistics are its lane's (and the other half's), and the products of S^T are the
-// operand of O^T without a move, with V's slots stored in the order in which S^T leaves them.
+__device__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The pieces of one query.  Element 8 s + i of the lane's share is dim dim_of(s) + i; lanes that differ in the bits of
+// `mask` hold the rest of the row.  Returns what a logit (log2 units) is multiplied with.
+template <class T, int N8, class F>
+__device__ float split_query(const T *q, bool live, int d, int mask, F dim_of, half8 (&hi)[N8], half8 *lo) {
+    float8v x[N8];
+    uint32_t top = 0;
+#pragma unroll
+    for (int s = 0; s < N8; ++s) {
+        const int e = dim_of(s);
+        x[s] = live && e < d ? load8(q + e) : float8v(0.f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[s][i]) & 0x7fffffffu);
+    }
+    if (mask & 16) top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+    // 2^up brings the largest to [2^14, 2^15); a row that is not finite gives NaN throughout
+    const int up = min(14 + 127 - (int)(top >> 23), 126);
+    const float lift = top ? __uint_as_float((uint32_t)(127 + up) << 23) : 1.f;
+#pragma unroll
+    for (int s = 0; s < N8; ++s)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float y = x[s][i] * lift;
+            hi[s][i] = (_Float16)y;
+            if constexpr (std::is_same<T, float>::value) lo[s][i] = (_Float16)(y - (float)hi[s][i]);
+        }
+    const float back = top >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : 1.f / lift;
+    return back * (kLog2e / sqrtf((float)d));
+}
+
+// The running sums of a lane's column (one row): logits x of a tile become weights u (in fp16 pieces), and M and D move on.
+// `left` of the tile's 32 slots are rows; slot_of(r) is the slot of x[r].  rescale(f): multiply O by f.
+template <bool kTwo, int R, int kMask, class Slot, class Rescale>
+__device__ void weights(float (&x)[R], float mult, float v_scale, float &v_top, int left, Slot slot_of, float &M, float &D,
+                        Rescale rescale, half8 (&ph)[R / 8], half8 *pl) {
+    v_top = v_scale > v_top ? v_scale : v_top;
+    float s_v = v_scale == 0.f ? v_top : v_scale;
+    if (s_v == 0.f) s_v = 1.f;
+    const float shift = __builtin_amdgcn_logf(s_v);
+    if (left < 32) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (slot_of(r) >= left) x[r] = -FLT_MAX;
+    }
+    float top = x[0];
+#pragma unroll
+    for (int r = 1; r < R; ++r) top = fmaxf(top, x[r]);
+    if (kMask & 16) top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaf(fmaxf(top, __shfl_xor(top, 32)), mult, shift);  // mult is not negative
+    if (__any(top > M + kSlack)) {
+        const float to = fmaxf(M, top), less = exp2_of(M - to);
+        M = to;
+        D *= less;
+        rescale(less);
+    }
+    // One rounding, next to M; M's own is common to all rows.  Where it could reach 1, t is rounded before M is taken off.
+    const float off = shift - M + kLift;
+    if (__any(fabsf(M) > kLargeMax)) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) x[r] = exp2_of(fmaf(x[r], mult, shift) - M + kLift);
+    } else {
+#pragma unroll
+        for (int r = 0; r < R; ++r) x[r] = exp2_of(fmaf(x[r], mult, off));
+    }
+    if (left < 32) {  // whatever stood there, and whatever it became with a scale of 0
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (slot_of(r) >= left) x[r] = 0.f;
+    }
+#pragma unroll
+    for (int r = 0; r < R; r += 2) {
+        const half2v hi = __builtin_convertvector(float2v{x[r], x[r + 1]}, half2v);
+        ph[r >> 3][r & 7] = hi[0], ph[r >> 3][(r & 7) + 1] = hi[1];
+        if constexpr (kTwo) {
+            const half2v lo = __builtin_convertvector(float2v{x[r] - (float)hi[0], x[r + 1] - (float)hi[1]}, half2v);
+            pl[r >> 3][r & 7] = lo[0], pl[r >> 3][(r & 7) + 1] = lo[1];
+        }
+    }
+    // One fp16: the sum of what is multiplied, so that a lone large u rounds without an error in out.  That needs every u
+    // that counts in D among fp16's normals: beside the values of a block of a far larger scale it may not be, while its
+    // weight is all of D.
+    float sum = 0.f;
+    if (kTwo || s_v < v_top * 0x1p-6f) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) sum += x[r];
+    } else {
+#pragma unroll
+        for (int r = 0; r < R; r += 2)
+            sum = __builtin_amdgcn_fdot2(half2v{ph[r >> 3][r & 7], ph[r >> 3][(r & 7) + 1]},
+                                         half2v{(_Float16)1.f, (_Float16)1.f}, sum, false);
+    }
+    D = fmaf(sum, 1.f / s_v, D);
+}
+
+// ---- many rows: a wavefront takes 32 rows through all of the request's slots --------------------------------------------
+// S^T = K Q^T and O^T = V^T P^T on 32 x 32 x 16 instructions: a lane holds column (lane & 31) of both, so a row's statistics
+// are its lane's (and the other half's), and the products of S^T are the operand of O^T without a move, with V's slots
+// stored in the order in which S^T leaves them.
 // T: type of q and out.  NP: 32-dim steps of the head width.
 template <class T, int NP>
 __global__ __launch_bounds__(256) void k_xattn_kv(AttnArgs a) {
     constexpr bool kTwo = std::is_same<T, float>::value;  // two fp16 pieces
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
     const int d = a.c.d, e16 = kv_padded(d), S = a.c.S, H = a.c.H;
-    // waves of a workgroup: neighbouring splits, then row tiles, of one head
-    const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int split = (int)(wave % a.splits);
-    const int64_t task = wave / a.splits;
+    const int64_t task = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     const int h = (int)(task / a.tiles);
     if (h >= H) return;
-    const Rows rows = find_rows(a, (int32_t)(task % a.tiles));
+    const Rows rows = find_rows<32>(a, (int32_t)(task % a.tiles));
     if (rows.n == 0) return;
     const int64_t length = min((int64_t)max(a.lengths[rows.b], 0), (int64_t)a.width * S);
-    const int32_t n_tiles = (int32_t)((length + 31) / 32), per = (n_tiles + a.splits - 1) / a.splits;
-    const int32_t t0 = split * per, t1 = min(t0 + per, n_tiles);
-    if (a.splits > 1 && t0 >= t1) return;  // the join knows which splits hold something
-
-    // ---- the queries ----
-    const int64_t m = (int64_t)rows.tile * 32 + col;  // row of the request
-    const bool live = m < (int64_t)rows.n * a.G;
-    const int64_t n = live ? m / a.G : 0;
-    const int head = h * a.G + (int)(live ? m - n * a.G : 0);
-    const int64_t at = a.q.offsets ? (rows.first + n) * a.q.row : rows.b * a.q.batch + n * a.q.row;
-    const T *q = static_cast<const T *>(a.q.q) + at + head * a.q.head;
+    const int32_t n_tiles = (int32_t)((length + 31) / 32);
+    const int64_t m = (int64_t)rows.tile * 32 + col;
+    const bool live = rows.has(a, m);
     half8 qh[2 * NP], ql[kTwo ? 2 * NP : 1];
-    float q_scale;
-    {
-        float8v x[2 * NP];
-        uint32_t top = 0;
-#pragma unroll
-        for (int s = 0; s < 2 * NP; ++s) {
-            const int e = (s >> 1) * 32 + half * 16 + (s & 1) * 8;
-            x[s] = live && e < d ? load8(q + e) : float8v(0.f);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[s][i]) & 0x7fffffffu);
-        }
-        top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-        // 2^up brings the largest to [2^14, 2^15); a row that is not finite gives NaN throughout
-        const int up = min(14 + 127 - (int)(top >> 23), 126);
-        const float lift = top ? __uint_as_float((uint32_t)(127 + up) << 23) : 1.f;
-        q_scale = top >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : 1.f / lift;
-        q_scale *= kLog2e / sqrtf((float)d);
-#pragma unroll
-        for (int s = 0; s < 2 * NP; ++s)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float y = x[s][i] * lift;
-                const _Float16 hi = (_Float16)y;
-                qh[s][i] = hi;
-                if constexpr (kTwo) ql[s][i] = (_Float16)(y - (float)hi);
-            }
-    }
+    const T *q = live ? static_cast<const T *>(rows.query(a, h, m, sizeof(T))) : nullptr;
+    const float q_scale = split_query(q, live, d, 32, [&](int s) { return (s >> 1) * 32 + half * 16 + (s & 1) * 8; }, qh, ql);
 
-    // ---- the rows ----
     float16v O[NP];
 #pragma unroll
     for (int i = 0; i < NP; ++i)
@@ -183,7 +257,7 @@ __global__ __launch_bounds__(256) void k_xattn_kv(AttnArgs a) {
         for (int r = 0; r < 16; ++r) O[i][r] = 0.f;
     float M = kNoMax, D = 0.f, v_top = 0.f;
     const int32_t *entries = a.table + (int64_t)rows.b * a.width;
-    for (int32_t t = t0; t < t1; ++t) {
+    for (int32_t t = 0; t < n_tiles; ++t) {
         const int32_t block = entries[t * 32 / S];
         if (block < 0 || block >= a.c.n_blocks) continue;
         const int64_t slice = (int64_t)block * H + h;
@@ -198,81 +272,32 @@ __global__ __launch_bounds__(256) void k_xattn_kv(AttnArgs a) {
         for (int s = 0; s < NP; ++s)  // dims that are not there repeat the last one; nothing reads their sums
             vw[s] = *reinterpret_cast<const uint4 *>(tile + 32 * e16 + min(s * 32 + col, e16 - 1) * 32 + half * 16);
 
-        float16v x;
+        float16v acc;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) x[r] = 0.f;
+        for (int r = 0; r < 16; ++r) acc[r] = 0.f;
 #pragma unroll
         for (int s = 0; s < NP; ++s) {
             const half8 k0 = to_half8(kw[s].x, kw[s].y), k1 = to_half8(kw[s].z, kw[s].w);
-            x = __builtin_amdgcn_mfma_f32_32x32x16_f16(k0, qh[2 * s], x, 0, 0, 0);
-            x = __builtin_amdgcn_mfma_f32_32x32x16_f16(k1, qh[2 * s + 1], x, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(k0, qh[2 * s], acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(k1, qh[2 * s + 1], acc, 0, 0, 0);
             if constexpr (kTwo) {
-                x = __builtin_amdgcn_mfma_f32_32x32x16_f16(k0, ql[2 * s], x, 0, 0, 0);
-                x = __builtin_amdgcn_mfma_f32_32x32x16_f16(k1, ql[2 * s + 1], x, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(k0, ql[2 * s], acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(k1, ql[2 * s + 1], acc, 0, 0, 0);
             }
         }
-
-        v_top = scale.y > v_top ? scale.y : v_top;
-        float s_v = scale.y == 0.f ? v_top : scale.y;
-        if (s_v == 0.f) s_v = 1.f;
-        const float mult = q_scale * scale.x, shift = __builtin_amdgcn_logf(s_v);
-        const int left = (int)min(length - (int64_t)t * 32, (int64_t)32);  // rows of this tile
-        if (left < 32) {
+        float x[16];
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (8 * (r >> 2) + 4 * half + (r & 3) >= left) x[r] = -FLT_MAX;
-        }
-        float top = x[0];
-#pragma unroll
-        for (int r = 1; r < 16; ++r) top = fmaxf(top, x[r]);
-        top = fmaf(fmaxf(top, other_half(top)), mult, shift);  // mult is not negative
-        if (__any(top > M + kSlack)) {
-            const float to = fmaxf(M, top), less = exp2_of(M - to);
-            M = to;
-            D *= less;
-#pragma unroll
-            for (int i = 0; i < NP; ++i)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) O[i][r] *= less;
-        }
-        // One rounding, next to M; M's own is common to all rows.  Where it could reach 1, t is rounded before M is taken off.
-        const float off = shift - M + kLift;
-        if (__any(fabsf(M) > kLargeMax)) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) x[r] = exp2_of(fmaf(x[r], mult, shift) - M + kLift);
-        } else {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) x[r] = exp2_of(fmaf(x[r], mult, off));
-        }
-        if (left < 32) {  // whatever stood there, and whatever it became with a scale of 0
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (8 * (r >> 2) + 4 * half + (r & 3) >= left) x[r] = 0.f;
-        }
+        for (int r = 0; r < 16; ++r) x[r] = acc[r];
         half8 ph[2], pl[2];
-        float sum = 0.f;
+        weights<kTwo, 16, 32>(x, q_scale * scale.x, scale.y, v_top, (int)min(length - (int64_t)t * 32, (int64_t)32),
+                              [&](int r) { return 8 * (r >> 2) + 4 * half + (r & 3); }, M, D,
+                              [&](float less) {
 #pragma unroll
-        for (int r = 0; r < 16; r += 2) {
-            const half2v hi = __builtin_convertvector(float2v{x[r], x[r + 1]}, half2v);
-            ph[r >> 3][r & 7] = hi[0], ph[r >> 3][(r & 7) + 1] = hi[1];
-            if constexpr (kTwo) {
-                const half2v lo = __builtin_convertvector(float2v{x[r] - (float)hi[0], x[r + 1] - (float)hi[1]}, half2v);
-                pl[r >> 3][r & 7] = lo[0], pl[r >> 3][(r & 7) + 1] = lo[1];
-            }
-        }
-        // One fp16: the sum of what is multiplied, so that a lone large u rounds without an error in out.  That needs every u
-        // that counts in D among fp16's normals: beside the values of a block of a far larger scale it may not be, while its
-        // weight is all of D.
-        if (kTwo || s_v < v_top * 0x1p-6f) {
+                                  for (int i = 0; i < NP; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) sum += x[r];
-        } else {
-#pragma unroll
-            for (int r = 0; r < 16; r += 2)
-                sum = __builtin_amdgcn_fdot2(half2v{ph[r >> 3][r & 7], ph[r >> 3][(r & 7) + 1]},
-                                             half2v{(_Float16)1.f, (_Float16)1.f}, sum, false);
-        }
-        D = fmaf(sum, 1.f / s_v, D);
+                                      for (int r = 0; r < 16; ++r) O[i][r] *= less;
+                              },
+                              ph, pl);
 #pragma unroll
         for (int s = 0; s < NP; ++s) {
             const half8 v0 = to_half8(vw[s].x, vw[s].y), v1 = to_half8(vw[s].z, vw[s].w);
@@ -284,42 +309,189 @@ __global__ __launch_bounds__(256) void k_xattn_kv(AttnArgs a) {
             }
         }
     }
-    D += other_half(D);
+    D += __shfl_xor(D, 32);
     if (!live) return;
-
-    const int64_t row = (rows.first + n) * a.q.Hq + head;
-    if (a.splits > 1) {
-        const int64_t all = a.q.rows() * a.q.Hq, p = split * all + row;
-        float *to = a.part + p * d;
-#pragma unroll
-        for (int s = 0; s < NP; ++s)
-#pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const int e = s * 32 + 8 * (r >> 2) + 4 * half;
-                if (e < d) *reinterpret_cast<float4 *>(to + e) = float4{O[s][r], O[s][r + 1], O[s][r + 2], O[s][r + 3]};
-            }
-        if (half == 0) reinterpret_cast<float2 *>(a.part + a.splits * all * d)[p] = float2{M, D};
-        return;
-    }
     const float inv = D == 0.f ? 0.f : 1.f / D;
-    T *to = static_cast<T *>(a.out) + row * d;
+    T *to = static_cast<T *>(a.out) + rows.out(a, h, m) * d;
 #pragma unroll
     for (int s = 0; s < NP; ++s)
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
             const int e = s * 32 + 8 * (r >> 2) + 4 * half;
-            if (e < d)
-                store4(to + e, O[s][r] * inv, O[s][r + 1] * inv, O[s][r + 2] * inv, O[s][r + 3] * inv);
+            if (e < d) store4(to + e, O[s][r] * inv, O[s][r + 1] * inv, O[s][r + 2] * inv, O[s][r + 3] * inv);
         }
 }
 
-// The splits of one row (query and head) added up: out = sum 2^(M_i - M) O_i / sum 2^(M_i - M) D_i.
+// ---- few rows: a workgroup takes 16 rows through one split of the request's slots ----------------------------------------
+// Bound by the cache's bytes, or by latency.  The four wavefronts take a quarter of the split's tiles each and add up in
+// LDS; the tiles of one are loaded while the one before is worked on, with block numbers and scales fetched for all of a
+// wavefront's tiles at once.  16 x 16 x 32 instructions: half the statistics and half the sums of a 32-row tile that would
+// be empty for the most part.  Row m of the u-th K operand is slot 16 (m / 8) + 8 u + m % 8, which leaves a lane with the 8
+// slots that stand together in V.
+// NC: 64-dim steps of the head width.
+template <int NC>
+struct FewTile {
+    uint4 k[2][NC];
+    uint2 v[4 * NC];
+};
+
+template <class T, int NC>
+__global__ __launch_bounds__(256, NC < 3 ? 2 : 1) void k_xattn_kv_few(AttnArgs a) {
+    constexpr bool kTwo = std::is_same<T, float>::value;
+    constexpr int kPitch = 68;  // floats of one row's 64 dims in LDS
+    __shared__ float part[4][16][kPitch], stats[2][4][16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = lane >> 4, col = lane & 15;
+    const int d = a.c.d, e16 = kv_padded(d), S = a.c.S, H = a.c.H, shift_S = __ffs(S) - 1;
+    const int split = (int)(blockIdx.x % (uint32_t)a.splits);
+    const int64_t task = blockIdx.x / (uint32_t)a.splits;
+    const int h = (int)(task / a.tiles);
+    const Rows rows = find_rows<16>(a, (int32_t)(task % a.tiles));
+    if (rows.n == 0) return;
+    const int64_t length = min((int64_t)max(a.lengths[rows.b], 0), (int64_t)a.width * S);
+    const int32_t n_tiles = (int32_t)((length + 31) / 32);
+    const int32_t t0 = split * a.chunk, t1 = min(t0 + a.chunk, n_tiles);
+    if (split > 0 && t0 >= t1) return;  // the join knows how many splits there are
+    const int32_t per = (t1 - t0 + 3) / 4, w0 = t0 + wave * per, w1 = min(w0 + per, t1);
+
+    // block numbers and scales of this wavefront's tiles: at most 64 blocks
+    const int32_t block0 = (w0 * 32) >> shift_S;
+    int32_t id = -1;
+    float k_scale = 0.f, v_scale = 0.f;
+    if (w0 < w1 && block0 + lane <= ((w1 * 32 - 1) >> shift_S)) {
+        id = a.table[(int64_t)rows.b * a.width + block0 + lane];
+        if (id >= a.c.n_blocks) id = -1;
+        if (id >= 0) {
+            const float2 scale = reinterpret_cast<const float2 *>(a.c.scales)[(int64_t)id * H + h];
+            k_scale = scale.x, v_scale = scale.y;
+        }
+    }
+
+    const int64_t m = (int64_t)rows.tile * 16 + col;
+    const bool live = rows.has(a, m);
+    half8 qh[2 * NC], ql[kTwo ? 2 * NC : 1];
+    const T *q = live ? static_cast<const T *>(rows.query(a, h, m, sizeof(T))) : nullptr;
+    const float q_scale = split_query(q, live, d, 48, [&](int s) { return (s >> 1) * 64 + group * 16 + (s & 1) * 8; }, qh, ql);
+
+    floatx4 O[4 * NC];
+#pragma unroll
+    for (int i = 0; i < 4 * NC; ++i) O[i] = floatx4(0.f);
+    float M = kNoMax, D = 0.f, v_top = 0.f;
+    const int k_at = (group * 32 + 16 * (col >> 3) + (col & 7)) * 16;
+    const int v_at = 32 * e16 + col * 32 + (group & 1) * 16 + (group >> 1) * 8;
+    const int n_dims = e16 / 16;
+
+    auto load = [&](FewTile<NC> &x, int32_t t) {
+        const int32_t block = max(__builtin_amdgcn_readlane(id, ((t * 32) >> shift_S) - block0), 0);
+        const uint8_t *tile = a.c.codes + ((int64_t)block * H + h) * kv_slice_bytes(S, d) + (int64_t)(t & ((S >> 5) - 1)) * 64 * e16;
+#pragma unroll
+        for (int s = 0; s < NC; ++s)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                if (4 * s + group < n_dims) x.k[u][s] = *reinterpret_cast<const uint4 *>(tile + k_at + s * 2048 + u * 128);
+#pragma unroll
+        for (int i = 0; i < 4 * NC; ++i)
+            if (i < n_dims) x.v[i] = *reinterpret_cast<const uint2 *>(tile + v_at + i * 512);
+    };
+    auto work = [&](const FewTile<NC> &w, int32_t t) {
+        const int at = ((t * 32) >> shift_S) - block0;
+        if (__builtin_amdgcn_readlane(id, at) < 0) return;
+        const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scale), at));
+        const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scale), at));
+        floatx4 acc[2] = {floatx4(0.f), floatx4(0.f)};
+#pragma unroll
+        for (int s = 0; s < NC; ++s)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const half8 k0 = to_half8(w.k[u][s].x, w.k[u][s].y), k1 = to_half8(w.k[u][s].z, w.k[u][s].w);
+                acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, qh[2 * s], acc[u], 0, 0, 0);
+                acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, qh[2 * s + 1], acc[u], 0, 0, 0);
+                if constexpr (kTwo) {
+                    acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, ql[2 * s], acc[u], 0, 0, 0);
+                    acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, ql[2 * s + 1], acc[u], 0, 0, 0);
+                }
+            }
+        float x[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) x[r] = acc[r >> 2][r & 3];
+        half8 ph[1], pl[1];
+        weights<kTwo, 8, 48>(x, q_scale * ks, vs, v_top, (int)min(length - (int64_t)t * 32, (int64_t)32),
+                             [&](int r) { return 16 * (group >> 1) + 8 * (r >> 2) + 4 * (group & 1) + (r & 3); }, M, D,
+                             [&](float less) {
+#pragma unroll
+                                 for (int i = 0; i < 4 * NC; ++i) O[i] *= less;
+                             },
+                             ph, pl);
+#pragma unroll
+        for (int i = 0; i < 4 * NC; ++i)
+            if (i < n_dims) {
+                const half8 v = to_half8(w.v[i].x, w.v[i].y);
+                O[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph[0], O[i], 0, 0, 0);
+                if constexpr (kTwo) O[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl[0], O[i], 0, 0, 0);
+            }
+    };
+    {
+        FewTile<NC> x, y;
+#pragma unroll
+        for (int s = 0; s < NC; ++s)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) x.k[u][s] = y.k[u][s] = uint4{0, 0, 0, 0};  // chunks that are not there: finite
+        if (w0 < w1) load(x, w0);
+        for (int32_t t = w0; t < w1; t += 2) {
+            if (t + 1 < w1) load(y, t + 1);
+            work(x, t);
+            if (t + 1 < w1) {
+                if (t + 2 < w1) load(x, t + 2);
+                work(y, t + 1);
+            }
+        }
+    }
+
+    // ---- the four wavefronts' sums ----
+    D += __shfl_xor(D, 16);
+    D += __shfl_xor(D, 32);
+    if (group == 0) stats[0][wave][col] = M, stats[1][wave][col] = D;
+    __syncthreads();
+    const float all_M = fmaxf(fmaxf(stats[0][0][col], stats[0][1][col]), fmaxf(stats[0][2][col], stats[0][3][col]));
+    const float mine = exp2_of(M - all_M);
+    const int row = threadIdx.x >> 4, quad = threadIdx.x & 15;
+    float row_M = kNoMax, row_D = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) row_M = fmaxf(row_M, stats[0][w][row]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) row_D = fmaf(stats[1][w][row], exp2_of(stats[0][w][row] - row_M), row_D);
+    const int64_t out_m = (int64_t)rows.tile * 16 + row;
+    const bool out_live = rows.has(a, out_m);
+    const int64_t out_row = out_live ? rows.out(a, h, out_m) : 0;
+    const bool alone = n_tiles <= a.chunk;
+    const int64_t all = a.q.rows() * a.q.Hq, p = split * all + out_row;
+    const float inv = alone ? (row_D == 0.f ? 0.f : 1.f / row_D) : 1.f;
+#pragma unroll
+    for (int s = 0; s < NC; ++s) {
+        if (s) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<floatx4 *>(&part[wave][col][i * 16 + group * 4]) = O[4 * s + i] * mine;
+        __syncthreads();
+        const int e = s * 64 + quad * 4;
+        if (out_live && e < d) {
+            floatx4 sum = floatx4(0.f);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) sum += *reinterpret_cast<const floatx4 *>(&part[w][row][quad * 4]);
+            sum *= inv;
+            if (alone) store4(static_cast<T *>(a.out) + out_row * d + e, sum[0], sum[1], sum[2], sum[3]);
+            else *reinterpret_cast<floatx4 *>(a.part + p * d + e) = sum;
+        }
+    }
+    if (!alone && out_live && quad == 0) reinterpret_cast<float2 *>(a.part + a.splits * all * d)[p] = float2{row_M, row_D};
+}
+
+// The splits of one row (query and head) added up: out = sum 2^(M_i - M) O_i / sum 2^(M_i - M) D_i.  A workgroup has a row;
+// threads are a quad of dims and one of 256 / quads runs of splits, whose sums meet in LDS.
 template <class T>
 __global__ __launch_bounds__(256) void k_xattn_kv_join(AttnArgs a) {
-    const int d = a.c.d, lane = threadIdx.x & 63;
-    const int64_t all = a.q.rows() * a.q.Hq, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= all) return;
-    const int64_t n = row / a.q.Hq;
+    __shared__ float sums[256][4], weight[256], top[4], total[4];
+    const int d = a.c.d, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t all = a.q.rows() * a.q.Hq, row = blockIdx.x, n = row / a.q.Hq;
     int32_t b = -1;
     if (!a.q.offsets) {
         b = (int32_t)(n / a.q.N);
@@ -330,61 +502,91 @@ __global__ __launch_bounds__(256) void k_xattn_kv_join(AttnArgs a) {
         if (!found) return;  // a row that no request has is left as it was
         b = __shfl(b, __ffsll((unsigned long long)found) - 1);
     }
-    const int64_t length = min((int64_t)max(a.lengths[b], 0), (int64_t)a.width * a.c.S);
-    const int32_t n_tiles = (int32_t)((length + 31) / 32), per = (n_tiles + a.splits - 1) / a.splits;
-    const int active = per ? (n_tiles + per - 1) / per : 0;
+    const int active = (tiles_of(a, b) + a.chunk - 1) / a.chunk;
+    if (active <= 1) return;  // the only split has written out itself
     const float2 *stats = reinterpret_cast<const float2 *>(a.part + a.splits * all * d) + row;
+    const int quads = d / 4, runs = 256 / quads, quad = tid % quads, run = tid / quads;
     float M = kNoMax;
-    for (int i = 0; i < active; ++i) M = fmaxf(M, stats[i * all].x);
-    float D = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < active; ++i) {
-        const float2 s = stats[i * all];
-        const float w = exp2_of(s.x - M);
-        D = fmaf(w, s.y, D);
-        for (int j = 0; j < 4; ++j)
-            if (lane + 64 * j < d) o[j] = fmaf(w, a.part[(i * all + row) * d + lane + 64 * j], o[j]);
+    for (int i = tid; i < active; i += 256) M = fmaxf(M, stats[i * all].x);
+    for (int o = 32; o; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
+    if (lane == 0) top[wave] = M;
+    __syncthreads();
+    M = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+    float D = 0.f;
+    floatx4 sum = floatx4(0.f);
+    for (int i0 = 0; i0 < active; i0 += 256) {
+        __syncthreads();
+        if (i0 + tid < active) {
+            const float2 s = stats[(i0 + tid) * all];
+            weight[tid] = exp2_of(s.x - M);
+            D = fmaf(weight[tid], s.y, D);
+        }
+        __syncthreads();
+        const int here = min(active - i0, 256);
+        if (run < runs) {
+#pragma unroll 4
+            for (int i = run; i < here; i += runs)
+                sum += *reinterpret_cast<const floatx4 *>(a.part + ((i0 + i) * all + row) * d + quad * 4) * weight[i];
+        }
     }
-    const float inv = D == 0.f ? 0.f : 1.f / D;
-    T *to = static_cast<T *>(a.out) + row * d;
-    for (int j = 0; j < 4; ++j)
-        if (lane + 64 * j < d) to[lane + 64 * j] = (T)(o[j] * inv);
+    for (int o = 32; o; o >>= 1) D += __shfl_xor(D, o);
+    if (lane == 0) total[wave] = D;
+    *reinterpret_cast<floatx4 *>(sums[tid]) = sum;
+    __syncthreads();
+    D = total[0] + total[1] + total[2] + total[3];
+    if (tid < quads) {
+        for (int i = 1; i < runs; ++i) sum += *reinterpret_cast<const floatx4 *>(sums[i * quads + tid]);
+        const float inv = D == 0.f ? 0.f : 1.f / D;
+        store4(static_cast<T *>(a.out) + row * d + tid * 4, sum[0] * inv, sum[1] * inv, sum[2] * inv, sum[3] * inv);
+    }
 }
 
 struct Plan {
-    int32_t tiles, splits;
+    bool few;
+    int32_t tiles, splits, chunk;
 };
 
-// Row tiles, and into how many parts each request's rows are split: only where the tiles alone leave the chip's
-// 256 x 8 wavefronts empty, and no part below four tiles of 32 rows.
+// Which kernel, its row tiles, and into how many parts each request's slots are split.
 Plan plan_of(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t Hkv, int64_t slots) {
     const int64_t G = Hq / Hkv;
-    const int64_t tiles = packed ? rows * G / 32 + B : B * ((rows / B * G + 31) / 32);
-    const int64_t waves = tiles * Hkv;
-    const int64_t most = std::max<int64_t>(1, slots / 128);
-    const int64_t want = 2048 / std::max<int64_t>(1, waves);
-    return {(int32_t)tiles, (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), 256))};
+    auto tiles_of_rows = [&](int64_t R) { return packed ? rows * G / R + B : B * ((rows / B * G + R - 1) / R); };
+    const int64_t wide = tiles_of_rows(32);
+    if (rows * G > 16 * (int64_t)B && wide * Hkv >= 1024) return {false, (int32_t)wide, 1, 0};
+    const int64_t tiles = tiles_of_rows(16), groups = tiles * Hkv, slot_tiles = (slots + 31) / 32;
+    // parts for about 1024 workgroups, none below 16 tiles (four to a wavefront) or above 256 (what one can look up)
+    const int64_t want = std::max<int64_t>(1, 1024 / std::max<int64_t>(1, groups));
+    const int64_t chunk = std::min<int64_t>(256, std::max<int64_t>(16, ((slot_tiles + want - 1) / want + 3) / 4 * 4));
+    return {true, (int32_t)tiles, (int32_t)std::max<int64_t>(1, (slot_tiles + chunk - 1) / chunk), (int32_t)chunk};
 }
 
 template <class T>
-hipError_t launch(const AttnArgs &a, hipStream_t st) {
-    const int64_t waves = (int64_t)a.tiles * a.c.H * a.splits;
-    const dim3 grid((uint32_t)((waves + 3) / 4));
-    auto go = [&](auto np) { k_xattn_kv<T, decltype(np)::value><<<grid, 256, 0, st>>>(a); };
-    switch ((a.c.d + 31) / 32) {
-        case 1: go(std::integral_constant<int, 1>{}); break;
-        case 2: go(std::integral_constant<int, 2>{}); break;
-        case 3: go(std::integral_constant<int, 3>{}); break;
-        case 4: go(std::integral_constant<int, 4>{}); break;
-        case 5: go(std::integral_constant<int, 5>{}); break;
-        case 6: go(std::integral_constant<int, 6>{}); break;
-        case 7: go(std::integral_constant<int, 7>{}); break;
-        default: go(std::integral_constant<int, 8>{}); break;
+hipError_t launch(const AttnArgs &a, bool few, hipStream_t st) {
+    if (!few) {
+        const dim3 grid((uint32_t)(((int64_t)a.tiles * a.c.H + 3) / 4));
+        auto go = [&](auto np) { k_xattn_kv<T, decltype(np)::value><<<grid, 256, 0, st>>>(a); };
+        switch ((a.c.d + 31) / 32) {
+            case 1: go(std::integral_constant<int, 1>{}); break;
+            case 2: go(std::integral_constant<int, 2>{}); break;
+            case 3: go(std::integral_constant<int, 3>{}); break;
+            case 4: go(std::integral_constant<int, 4>{}); break;
+            case 5: go(std::integral_constant<int, 5>{}); break;
+            case 6: go(std::integral_constant<int, 6>{}); break;
+            case 7: go(std::integral_constant<int, 7>{}); break;
+            default: go(std::integral_constant<int, 8>{}); break;
+        }
+        return hipGetLastError();
+    }
+    const dim3 grid((uint32_t)((int64_t)a.tiles * a.c.H * a.splits));
+    switch ((a.c.d + 63) / 64) {
+        case 1: k_xattn_kv_few<T, 1><<<grid, 256, 0, st>>>(a); break;
+        case 2: k_xattn_kv_few<T, 2><<<grid, 256, 0, st>>>(a); break;
+        case 3: k_xattn_kv_few<T, 3><<<grid, 256, 0, st>>>(a); break;
+        default: k_xattn_kv_few<T, 4><<<grid, 256, 0, st>>>(a); break;
     }
     if (a.splits > 1) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        const int64_t all = a.q.rows() * a.q.Hq;
-        k_xattn_kv_join<T><<<(uint32_t)((all + 3) / 4), 256, 0, st>>>(a);
+        k_xattn_kv_join<T><<<(uint32_t)(a.q.rows() * a.q.Hq), 256, 0, st>>>(a);
     }
     return hipGetLastError();
 }
@@ -399,8 +601,9 @@ size_t xattn_kv_workspace_bytes(int32_t B, int64_t rows, bool packed, int32_t Hq
 hipError_t launch_xattn_kv(const KvQueries &q, const KvCache &c, const int32_t *table, int32_t width,
                            const int32_t *lengths, void *out, void *workspace, hipStream_t st) {
     const Plan p = plan_of(q.B, q.rows(), q.offsets != nullptr, q.Hq, c.H, (int64_t)width * c.S);
-    const AttnArgs a{q, c, table, lengths, out, static_cast<float *>(workspace), width, q.Hq / c.H, p.splits, p.tiles};
-    return q.dtype == DGQ_F32 ? launch<float>(a, st) : q.dtype == DGQ_F16 ? launch<_Float16>(a, st) : launch<__bf16>(a, st);
+    const AttnArgs a{q, c, table, lengths, out, static_cast<float *>(workspace), width, q.Hq / c.H, p.tiles, p.splits, p.chunk};
+    return q.dtype == DGQ_F32 ? launch<float>(a, p.few, st)
+           : q.dtype == DGQ_F16 ? launch<_Float16>(a, p.few, st) : launch<__bf16>(a, p.few, st);
 }
 
 }  // namespace dgq
