@@ -227,99 +227,172 @@ __device__ void weights(float (&x)[R], float mult, float v_scale, float &v_top, 
     D = fmaf(sum, 1.f / s_v, D);
 }
 
-// ---- many rows: a wavefront takes 32 rows through all of the request's slots --------------------------------------------
+// ---- many rows: a workgroup takes 128 QT rows through all of the request's slots ------------------------------------------
 // S^T = K Q^T and O^T = V^T P^T on 32 x 32 x 16 instructions: a lane holds column (lane & 31) of both, so a row's statistics
 // are its lane's (and the other half's), and the products of S^T are the operand of O^T without a move, with V's slots
 // stored in the order in which S^T leaves them.
-// T: type of q and out.  NP: 32-dim steps of the head width.
-template <class T, int NP>
-__global__ __launch_bounds__(256) void k_xattn_kv(AttnArgs a) {
+// Two tiles of 32 slots are a stage: each wavefront loads K or V of one of them (a stage ahead, in registers), makes fp16 of
+// it once for all four, and puts it into LDS in units of 16 bytes, one operand of one lane, so that every read and write of
+// 64 lanes is 1 KiB without a bank met twice.  Two stages of LDS, one barrier a stage.
+// T: type of q and out.  NP: 32-dim steps of the head width.  QT: blocks of 32 rows to a wavefront.
+template <class T, int NP, int QT>
+__global__ __launch_bounds__(256, NP <= 4 ? 2 : 1) void k_xattn_kv(AttnArgs a) {
     constexpr bool kTwo = std::is_same<T, float>::value;  // two fp16 pieces
-    const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
-    const int d = a.c.d, e16 = kv_padded(d), S = a.c.S, H = a.c.H;
-    const int64_t task = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int h = (int)(task / a.tiles);
-    if (h >= H) return;
-    const Rows rows = find_rows<32>(a, (int32_t)(task % a.tiles));
+    constexpr int kPart = NP * 128;                       // units of K or V of a tile
+    extern __shared__ uint4 lds[];                        // [2 stages][2 tiles][K, V][kPart]
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
+    const int d = a.c.d, e16 = kv_padded(d), S = a.c.S, H = a.c.H, shift_S = __ffs(S) - 1;
+    const int h = (int)(blockIdx.x / (uint32_t)a.tiles);
+    const Rows rows = find_rows<128 * QT>(a, (int32_t)(blockIdx.x % (uint32_t)a.tiles));
     if (rows.n == 0) return;
     const int64_t length = min((int64_t)max(a.lengths[rows.b], 0), (int64_t)a.width * S);
-    const int32_t n_tiles = (int32_t)((length + 31) / 32);
-    const int64_t m = (int64_t)rows.tile * 32 + col;
-    const bool live = rows.has(a, m);
-    half8 qh[2 * NP], ql[kTwo ? 2 * NP : 1];
-    const T *q = live ? static_cast<const T *>(rows.query(a, h, m, sizeof(T))) : nullptr;
-    const float q_scale = split_query(q, live, d, 32, [&](int s) { return (s >> 1) * 32 + half * 16 + (s & 1) * 8; }, qh, ql);
+    const int32_t n_tiles = (int32_t)((length + 31) / 32), n_stages = (n_tiles + 1) / 2;
 
-    float16v O[NP];
-#pragma unroll
-    for (int i = 0; i < NP; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) O[i][r] = 0.f;
-    float M = kNoMax, D = 0.f, v_top = 0.f;
-    const int32_t *entries = a.table + (int64_t)rows.b * a.width;
-    for (int32_t t = 0; t < n_tiles; ++t) {
-        const int32_t block = entries[t * 32 / S];
-        if (block < 0 || block >= a.c.n_blocks) continue;
-        const int64_t slice = (int64_t)block * H + h;
-        const uint8_t *tile = a.c.codes + slice * kv_slice_bytes(S, d) + (int64_t)(t * 32 % S / 32) * 64 * e16;
-        const float2 scale = reinterpret_cast<const float2 *>(a.c.scales)[slice];
-
-        uint4 kw[NP], vw[NP];
-#pragma unroll
-        for (int s = 0; s < NP; ++s)  // a last half that is not there reads V's first bytes, against zeros of q
-            kw[s] = *reinterpret_cast<const uint4 *>(tile + ((2 * s + half) * 32 + col) * 16);
-#pragma unroll
-        for (int s = 0; s < NP; ++s)  // dims that are not there repeat the last one; nothing reads their sums
-            vw[s] = *reinterpret_cast<const uint4 *>(tile + 32 * e16 + min(s * 32 + col, e16 - 1) * 32 + half * 16);
-
-        float16v acc;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[r] = 0.f;
-#pragma unroll
-        for (int s = 0; s < NP; ++s) {
-            const half8 k0 = to_half8(kw[s].x, kw[s].y), k1 = to_half8(kw[s].z, kw[s].w);
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(k0, qh[2 * s], acc, 0, 0, 0);
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(k1, qh[2 * s + 1], acc, 0, 0, 0);
-            if constexpr (kTwo) {
-                acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(k0, ql[2 * s], acc, 0, 0, 0);
-                acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(k1, ql[2 * s + 1], acc, 0, 0, 0);
+    // block numbers and scales of 64 blocks, one a lane
+    int32_t block0 = 0, id = -1;
+    float k_scale = 0.f, v_scale = 0.f;
+    auto look_up = [&](int32_t first) {
+        block0 = first;
+        id = -1;
+        if (((int64_t)(first + lane) << shift_S) < length) {
+            id = a.table[(int64_t)rows.b * a.width + first + lane];
+            if (id >= a.c.n_blocks) id = -1;
+            if (id >= 0) {
+                const float2 scale = reinterpret_cast<const float2 *>(a.c.scales)[(int64_t)id * H + h];
+                k_scale = scale.x, v_scale = scale.y;
             }
         }
-        float x[16];
+    };
+    look_up(0);
+
+    uint4 ahead[NP];
+    const int my_tile = wave >> 1, my_part = wave & 1;
+    auto load = [&](int32_t st) {  // this wavefront's share of a stage
+        const int32_t t = 2 * st + my_tile;
+        if (t >= n_tiles) return;
+        const int32_t block = __builtin_amdgcn_readlane(id, ((t * 32) >> shift_S) - block0);
+        if (block < 0) return;
+        const uint8_t *tile = a.c.codes + ((int64_t)block * H + h) * kv_slice_bytes(S, d) + (int64_t)(t & ((S >> 5) - 1)) * 64 * e16;
+        // the last half step of K may not be there (then the bytes of V behind it meet zeros of q), nor the last dims of V
+        // (they repeat the last one; nothing reads their sums)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) x[r] = acc[r];
-        half8 ph[2], pl[2];
-        weights<kTwo, 16, 32>(x, q_scale * scale.x, scale.y, v_top, (int)min(length - (int64_t)t * 32, (int64_t)32),
-                              [&](int r) { return 8 * (r >> 2) + 4 * half + (r & 3); }, M, D,
-                              [&](float less) {
-#pragma unroll
-                                  for (int i = 0; i < NP; ++i)
-#pragma unroll
-                                      for (int r = 0; r < 16; ++r) O[i][r] *= less;
-                              },
-                              ph, pl);
+        for (int s = 0; s < NP; ++s)
+            ahead[s] = *reinterpret_cast<const uint4 *>(
+                tile + (my_part ? 32 * e16 + min(s * 32 + col, e16 - 1) * 32 + half * 16 : ((2 * s + half) * 32 + col) * 16));
+    };
+    auto keep = [&](int32_t st) {
+        uint4 *to = lds + (((st & 1) * 2 + my_tile) * 2 + my_part) * kPart;
 #pragma unroll
         for (int s = 0; s < NP; ++s) {
-            const half8 v0 = to_half8(vw[s].x, vw[s].y), v1 = to_half8(vw[s].z, vw[s].w);
-            O[s] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v0, ph[0], O[s], 0, 0, 0);
-            O[s] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v1, ph[1], O[s], 0, 0, 0);
-            if constexpr (kTwo) {
-                O[s] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v0, pl[0], O[s], 0, 0, 0);
-                O[s] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v1, pl[1], O[s], 0, 0, 0);
-            }
+            const half8 lo = to_half8(ahead[s].x, ahead[s].y), hi = to_half8(ahead[s].z, ahead[s].w);
+            // K: [chunk of 16 dims][its halves][slot]; V: [32 dims][halves of the tile][half][dim]
+            const int at = my_part ? (s * 4 + half) * 32 + col : (2 * s + half) * 64 + col;
+            to[at] = __builtin_bit_cast(uint4, lo);
+            to[at + (my_part ? 64 : 32)] = __builtin_bit_cast(uint4, hi);
         }
+    };
+    load(0);
+
+    half8 qh[QT][2 * NP], ql[QT][kTwo ? 2 * NP : 1];
+    float q_scale[QT];
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+        const int64_t m = (int64_t)rows.tile * (128 * QT) + (wave * QT + i) * 32 + col;
+        const bool live = rows.has(a, m);
+        const T *q = live ? static_cast<const T *>(rows.query(a, h, m, sizeof(T))) : nullptr;
+        q_scale[i] = split_query(q, live, d, 32, [&](int s) { return (s >> 1) * 32 + half * 16 + (s & 1) * 8; }, qh[i], ql[i]);
     }
-    D += __shfl_xor(D, 32);
-    if (!live) return;
-    const float inv = D == 0.f ? 0.f : 1.f / D;
-    T *to = static_cast<T *>(a.out) + rows.out(a, h, m) * d;
+    float16v O[QT][NP];
+    float M[QT], D[QT], v_top = 0.f;
 #pragma unroll
-    for (int s = 0; s < NP; ++s)
+    for (int i = 0; i < QT; ++i) {
+        M[i] = kNoMax, D[i] = 0.f;
 #pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-            const int e = s * 32 + 8 * (r >> 2) + 4 * half;
-            if (e < d) store4(to + e, O[s][r] * inv, O[s][r + 1] * inv, O[s][r + 2] * inv, O[s][r + 3] * inv);
+        for (int s = 0; s < NP; ++s)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) O[i][s][r] = 0.f;
+    }
+    keep(0);
+    __syncthreads();
+    for (int32_t st = 0; st < n_stages; ++st) {
+        const bool more = st + 1 < n_stages;
+        int32_t ids[2];
+        float ks[2], vs[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int at = min(((2 * st + i) * 32 >> shift_S) - block0, 63);
+            ids[i] = 2 * st + i < n_tiles ? __builtin_amdgcn_readlane(id, at) : -1;
+            ks[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scale), at));
+            vs[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scale), at));
         }
+        if (more) {
+            // 64 blocks hold whole stages (64 slots), so a stage never needs two look-ups
+            if ((((st + 1) * 64) >> shift_S) - block0 >= 64) look_up(((st + 1) * 64) >> shift_S);
+            load(st + 1);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (ids[i] < 0) continue;
+            const uint4 *K = lds + ((st & 1) * 2 + i) * 2 * kPart, *V = K + kPart;
+            float16v acc[QT];
+#pragma unroll
+            for (int j = 0; j < QT; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[j][r] = 0.f;
+#pragma unroll
+            for (int s = 0; s < 2 * NP; ++s) {
+                const half8 k = __builtin_bit_cast(half8, K[((s >> 1) * 2 + half) * 64 + (s & 1) * 32 + col]);
+#pragma unroll
+                for (int j = 0; j < QT; ++j) {
+                    acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, qh[j][s], acc[j], 0, 0, 0);
+                    if constexpr (kTwo) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, ql[j][s], acc[j], 0, 0, 0);
+                }
+            }
+            half8 ph[QT][2], pl[QT][2];
+#pragma unroll
+            for (int j = 0; j < QT; ++j) {
+                float x[16];
+#pragma unroll
+                for (int r = 0; r < 16; ++r) x[r] = acc[j][r];
+                weights<kTwo, 16, 32>(x, q_scale[j] * ks[i], vs[i], v_top, (int)min(length - (int64_t)(2 * st + i) * 32, (int64_t)32),
+                                      [&](int r) { return 8 * (r >> 2) + 4 * half + (r & 3); }, M[j], D[j],
+                                      [&](float less) {
+#pragma unroll
+                                          for (int s = 0; s < NP; ++s)
+#pragma unroll
+                                              for (int r = 0; r < 16; ++r) O[j][s][r] *= less;
+                                      },
+                                      ph[j], pl[j]);
+            }
+#pragma unroll
+            for (int s = 0; s < NP; ++s)
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    const half8 v = __builtin_bit_cast(half8, V[(s * 4 + g * 2 + half) * 32 + col]);
+#pragma unroll
+                    for (int j = 0; j < QT; ++j) {
+                        O[j][s] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, ph[j][g], O[j][s], 0, 0, 0);
+                        if constexpr (kTwo) O[j][s] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pl[j][g], O[j][s], 0, 0, 0);
+                    }
+                }
+        }
+        if (more) keep(st + 1);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int j = 0; j < QT; ++j) {
+        const float sum = D[j] + __shfl_xor(D[j], 32), inv = sum == 0.f ? 0.f : 1.f / sum;
+        const int64_t m = (int64_t)rows.tile * (128 * QT) + (wave * QT + j) * 32 + col;
+        if (!rows.has(a, m)) continue;
+        T *to = static_cast<T *>(a.out) + rows.out(a, h, m) * d;
+#pragma unroll
+        for (int s = 0; s < NP; ++s)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const int e = s * 32 + 8 * (r >> 2) + 4 * half;
+                if (e < d) store4(to + e, O[j][s][r] * inv, O[j][s][r + 1] * inv, O[j][s][r + 2] * inv, O[j][s][r + 3] * inv);
+            }
+    }
 }
 
 // ---- few rows: a workgroup takes 16 rows through one split of the request's slots ----------------------------------------
@@ -541,6 +614,8 @@ __global__ __launch_bounds__(256) void k_xattn_kv_join(AttnArgs a) {
     }
 }
 
+constexpr int kRowBlocks = 1;
+
 struct Plan {
     bool few;
     int32_t tiles, splits, chunk;
@@ -550,8 +625,8 @@ struct Plan {
 Plan plan_of(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t Hkv, int64_t slots) {
     const int64_t G = Hq / Hkv;
     auto tiles_of_rows = [&](int64_t R) { return packed ? rows * G / R + B : B * ((rows / B * G + R - 1) / R); };
-    const int64_t wide = tiles_of_rows(32);
-    if (rows * G > 16 * (int64_t)B && wide * Hkv >= 1024) return {false, (int32_t)wide, 1, 0};
+    const int64_t wide = tiles_of_rows(128 * kRowBlocks);
+    if (rows * G > 16 * (int64_t)B && wide * Hkv >= 256) return {false, (int32_t)wide, 1, 0};
     const int64_t tiles = tiles_of_rows(16), groups = tiles * Hkv, slot_tiles = (slots + 31) / 32;
     // parts for about 1024 workgroups, none below 16 tiles (four to a wavefront) or above 256 (what one can look up)
     const int64_t want = std::max<int64_t>(1, 1024 / std::max<int64_t>(1, groups));
@@ -562,8 +637,13 @@ Plan plan_of(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t Hkv, int6
 template <class T>
 hipError_t launch(const AttnArgs &a, bool few, hipStream_t st) {
     if (!few) {
-        const dim3 grid((uint32_t)(((int64_t)a.tiles * a.c.H + 3) / 4));
-        auto go = [&](auto np) { k_xattn_kv<T, decltype(np)::value><<<grid, 256, 0, st>>>(a); };
+        const dim3 grid((uint32_t)((int64_t)a.tiles * a.c.H));
+        hipError_t e = hipSuccess;
+        auto go = [&](auto np) {
+            constexpr int NP = decltype(np)::value, bytes = NP * 16384;
+            e = DGQ_ENSURE_LDS((k_xattn_kv<T, NP, kRowBlocks>), bytes);
+            if (e == hipSuccess) k_xattn_kv<T, NP, kRowBlocks><<<grid, 256, bytes, st>>>(a);
+        };
         switch ((a.c.d + 31) / 32) {
             case 1: go(std::integral_constant<int, 1>{}); break;
             case 2: go(std::integral_constant<int, 2>{}); break;
@@ -574,7 +654,7 @@ hipError_t launch(const AttnArgs &a, bool few, hipStream_t st) {
             case 7: go(std::integral_constant<int, 7>{}); break;
             default: go(std::integral_constant<int, 8>{}); break;
         }
-        return hipGetLastError();
+        return e == hipSuccess ? hipGetLastError() : e;
     }
     const dim3 grid((uint32_t)((int64_t)a.tiles * a.c.H * a.splits));
     switch ((a.c.d + 63) / 64) {

@@ -365,6 +365,37 @@ def test_attention(dgq, shape, dtype):
     assert torch.equal(out, other)
 
 
+MANY = [  # at least 256 workgroups of 128 rows, from one slot to several look-ups of 64 blocks; every step of the head width
+    (32, 32, 1, 8, 270, [1, 0, 33]),
+    (32, 8, 1, 40, 2100, [77, 154]),
+    (64, 10, 1, 64, 400, [1, 2, 31, 32, 65, 231, 0]),
+    (128, 4, 7, 96, 333, [127, 300, 129, 64]),
+    (32, 2, 4, 128, 4200, [70]),
+    (64, 8, 1, 160, 2050, [77, 95]),
+    (32, 33, 1, 192, 513, [40, 5]),
+    (32, 16, 2, 224, 1025, [50]),
+    (64, 64, 1, 256, 257, [65, 130]),
+    (32, 1, 1, 16, 33000, [4200]),
+]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", MANY, ids=lambda s: "S%d_H%d_G%d_d%d_N%d" % s[:5])
+def test_attention_of_many_rows(dgq, shape, dtype):
+    import torch
+    S, H, G, d, N, lengths = shape
+    rng = np.random.default_rng(d + N)
+    c, table, held = _filled(dgq, rng, lengths, S, H, d)
+    q, qn = _floats(rng, (len(lengths), N, H * G, d), dtype)
+    out = dgq.dgq_xattn_kv(q, c, _i32(table), _i32(lengths))
+    again = dgq.dgq_xattn_kv(q, c, _i32(table), _i32(lengths), out=torch.full_like(q, float("nan")))
+    torch.cuda.synchronize()
+    assert torch.equal(out, again)
+    got = out.float().cpu().numpy()
+    rows = np.unique(np.r_[0:40, rng.integers(0, N, 200), N - 140:N])  # whole tiles at both ends, and some between
+    _check_attention(held, table, lengths, qn[:, rows], got[:, rows], dtype, d)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_packed_queries(dgq, dtype):
     """Requests with different numbers of queries, none among them; rows of no request keep what was there."""
@@ -389,14 +420,18 @@ def test_packed_queries(dgq, dtype):
     _check_attention(held, table[4:5], lengths[4:5], [qn[starts[4]:starts[5]]], one.float().cpu().numpy(), dtype, d)
 
 
-def test_many_packed_requests(dgq):
-    """More requests than a wavefront looks through at once, most of them with a query or none."""
+@pytest.mark.parametrize("H", [1, 4])
+def test_many_packed_requests(dgq, H):
+    """More requests than a wavefront looks through at once, most of them with a query or none; with four heads enough of
+    them for the kernel of many rows."""
     import torch
     rng = np.random.default_rng(9)
-    S, H, d, B = 32, 1, 16, 200
+    S, d, B = 32, 16, 200
     lengths = [int(x) for x in rng.integers(0, 40, B)]
     n = [int(x) for x in rng.choice([0, 1, 1, 2, 40], B)]
     n[60:130] = [0] * 70
+    if H > 1:
+        n[3], n[140], n[199] = 2000, 400, 1500
     c, table, held = _filled(dgq, rng, lengths, S, H, d)
     starts = np.concatenate([[0], np.cumsum(n)])
     q, qn = _floats(rng, (starts[-1], H, d), "fp32")
@@ -432,7 +467,7 @@ def test_few_queries_over_long_rows(dgq, dtype, B, N, H, G, d, lengths):
     _check_attention(held, table, lengths, qn, out.float().cpu().numpy(), dtype, d)
 
 
-@pytest.mark.parametrize("N", [1, 70])
+@pytest.mark.parametrize("N", [1, 70, 5500])
 def test_lengths_and_blocks_that_are_not_there(dgq, N):
     """Lengths past the table and below zero, blocks outside the cache: those rows are not there."""
     import torch
@@ -450,7 +485,7 @@ def test_lengths_and_blocks_that_are_not_there(dgq, N):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("N,n", [(40, 300), (1, 2000)])
+@pytest.mark.parametrize("N,n", [(40, 300), (1, 2000), (16500, 300)])
 def test_blocks_of_very_different_scales(dgq, dtype, N, n):
     """Values that grow and shrink by 2^40 from block to block, among them blocks of zeros, with all weight on any of them."""
     import torch
@@ -471,7 +506,7 @@ def test_blocks_of_very_different_scales(dgq, dtype, N, n):
     k, v = (held.exact(w, table, 0, n) for w in (0, 1))
     want, big = ref.attention(qn[0].astype(np.float64), k, v)
     # the bound in units of what a row adds most to this output
-    for i in range(N):
+    for i in range(0, N, max(1, N // 60)):
         for h in range(H):
             x = k[:, h] @ qn[0, i, h] / np.sqrt(d)
             p = np.exp(x - x.max())
@@ -483,7 +518,7 @@ def test_blocks_of_very_different_scales(dgq, dtype, N, n):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("N,n", [(40, 100), (2, 900)])
+@pytest.mark.parametrize("N,n", [(40, 100), (2, 900), (16500, 100)])
 def test_sharp_and_extreme_queries(dgq, dtype, N, n):
     """Logits in the hundreds, queries near the types' ends, zeros; a query that is not finite spoils itself alone."""
     import torch
@@ -507,7 +542,7 @@ def test_sharp_and_extreme_queries(dgq, dtype, N, n):
     qn = q.float().cpu().numpy()
     bad = {(4, 0), (5, 1), (6, 0)} if N > 4 else set()
     k, v = (held.exact(w, table, 0, n) for w in (0, 1))
-    for i in range(N):
+    for i in [*range(min(N, 40)), *range(40, N, 500)]:
         for h in range(H):
             if (i, h) in bad:
                 assert np.isnan(out[0, i, h]).all()
@@ -521,7 +556,8 @@ def test_sharp_and_extreme_queries(dgq, dtype, N, n):
             assert (np.abs(out[0, i, h] - want[0, 0]) <= lim).all(), (i, h)
 
 
-def test_rows_of_a_block_that_is_not_finite(dgq):
+@pytest.mark.parametrize("N", [4, 5500])
+def test_rows_of_a_block_that_is_not_finite(dgq, N):
     """NaN in one request's block stays with that request and head."""
     import torch
     rng = np.random.default_rng(14)
@@ -530,18 +566,19 @@ def test_rows_of_a_block_that_is_not_finite(dgq):
         v[70, 1, 3] = float("nan")
         return k, v
     c, table, held = _filled(dgq, rng, [40, 40, 40], 32, 2, 16, gain=gain)
-    q, qn = _floats(rng, (3, 4, 2, 16), "fp32")
+    q, qn = _floats(rng, (3, N, 2, 16), "fp32")
     out = dgq.dgq_xattn_kv(q, c, _i32(table), _i32([40] * 3)).cpu().numpy()
     assert np.isnan(out[1, :, 1]).all() and np.isfinite(out[[0, 2]]).all() and np.isfinite(out[1, :, 0]).all()
 
 
-def test_what_stands_behind_a_request_does_not_matter(dgq):
+@pytest.mark.parametrize("N", [9, 33000])
+def test_what_stands_behind_a_request_does_not_matter(dgq, N):
     """Slots behind the length hold what a former owner of the block left: large values."""
     import torch
     rng = np.random.default_rng(15)
     S, H, d = 64, 1, 32
     c, table, held = _filled(dgq, rng, [128], S, H, d, gain=lambda k, v: (k * 100, v * 100))
-    q, qn = _floats(rng, (1, 9, H, d), "fp32", spread=False)
+    q, qn = _floats(rng, (1, N, H, d), "fp32", spread=False)
     for n in (1, 31, 33, 64, 65, 100):
         out = dgq.dgq_xattn_kv(q * 0.01, c, _i32(table), _i32([n])).cpu().numpy()
         k, v = (held.exact(w, table, 0, n) for w in (0, 1))
@@ -589,7 +626,7 @@ def test_offsets_past_32_bits(dgq):
             rows = slice(i * S, min(n, i * S + S))
             lim = np.abs(y[rows]).max((0, 2)) / 127 * 0.5001
             assert (np.abs(x[rows] - y[rows]).max((0, 2)) <= lim).all()
-    for N in (1, 40):
+    for N in (1, 40, 4200):
         q, qn = _floats(rng, (1, N, H, d), "fp32")
         out = dgq.dgq_xattn_kv(q, c, table, _i32([n])).cpu().numpy()
         k64, v64 = k2[0].cpu().numpy().astype(np.float64), v2[0].cpu().numpy().astype(np.float64)
