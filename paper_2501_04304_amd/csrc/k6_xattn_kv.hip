@@ -6,7 +6,7 @@
 //   t_j = l_j log2(e) + log2(s_v),  M = running max of t,  u_j = 2^(t_j - M),
 //   O = sum u_j c'_j,  D = sum u_j / s_v,  out = O / D,
 // and u_j is at most 1 in units of what its row adds, whatever the blocks' scales are.  (A block of zero values takes the
-// largest scale seen so far in its place: its O is 0 with any, its share of D is right with any.)
+// scale in its place that leaves M alone: its O is 0 with any, its share of D is right with any.)
 //
 // Codes are exact in fp16.  Queries are multiplied by a power of two that brings the row's largest element to
 // [2^14, 2^15): an fp16 or bf16 query is then exact in one fp16 (bf16 elements below 2^-28 of the row's largest lose
@@ -28,10 +28,12 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float float8v __attribute__((ext_vector_type(8)));
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kWideRows = 128;       // rows of a workgroup of the kernel for many
 constexpr float kNoMax = -1e30f;   // M before the first row: finite, so that M - M stays 0
 constexpr float kLift = 6.f;       // u carries 2^6, away from fp16's subnormals
 constexpr float kSlack = 8.f;      // M is raised only when a row exceeds it by 2^8: u stays below 2^15
 constexpr float kLargeMax = 0x1p18f;
+constexpr float kLeastShift = 96.f;  // -log2(kKvLeastScale)
 
 struct AttnArgs {
     KvQueries q;
@@ -163,87 +165,114 @@ __device__ float split_query(const T *q, bool live, int d, int mask, F dim_of, h
     return back * (kLog2e / sqrtf((float)d));
 }
 
-// The running sums of a lane's column (one row): logits x of a tile become weights u (in fp16 pieces), and M and D move on.
-// `left` of the tile's 32 slots are rows; slot_of(r) is the slot of x[r].  rescale(f): multiply O by f.
-template <bool kTwo, int R, int kMask, class Slot, class Rescale>
-__device__ void weights(float (&x)[R], float mult, float v_scale, float &v_top, int left, Slot slot_of, float &M, float &D,
-                        Rescale rescale, half8 (&ph)[R / 8], half8 *pl) {
+// Over the lanes that hold one column: the other half's, and with kMask 48 the four of a 16-lane column.
+template <int kMask>
+__device__ float column_max(float x) {
+    auto fold = [](float x, auto swap) {
+        const auto r = swap(__float_as_uint(x));
+        return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    };
+    if (kMask & 16) x = fold(x, [](uint32_t u) { return __builtin_amdgcn_permlane16_swap(u, u, false, false); });
+    return fold(x, [](uint32_t u) { return __builtin_amdgcn_permlane32_swap(u, u, false, false); });
+}
+
+// Two weights u = 2^(x mult + off) in fp16 pieces, and their sum: of one piece, the sum of what is multiplied, so that a lone
+// large u rounds without an error in out.
+template <bool kTwo, class X, class P>
+__device__ void weigh_two(const X &x, int r, float mult, float off, float &sum, P &ph, P &pl) {
+    const float2v u{exp2_of(fmaf(x[r], mult, off)), exp2_of(fmaf(x[r + 1], mult, off))};
+    const half2v hi = __builtin_convertvector(u, half2v);
+    ph[r >> 3][r & 7] = hi[0], ph[r >> 3][(r & 7) + 1] = hi[1];
+    if constexpr (kTwo) {
+        const half2v lo = __builtin_convertvector(float2v{u[0] - (float)hi[0], u[1] - (float)hi[1]}, half2v);
+        pl[r >> 3][r & 7] = lo[0], pl[r >> 3][(r & 7) + 1] = lo[1];
+        sum += u[0] + u[1];
+    } else {
+        sum = __builtin_amdgcn_fdot2(hi, half2v{(_Float16)1.f, (_Float16)1.f}, sum, false);
+    }
+}
+
+// The running sums of a lane's column (one row).
+struct Column {
+    float M = kNoMax, D = 0.f;
+};
+
+// A tile's logits x become weights, and M and D move on.  `left` of its 32 slots are rows; slot_of(r) is the slot of x[r].
+// v_top: the largest value scale so far.  rescale(f): multiply O by f.
+// Nearly every tile is whole, with a scale like the others', and does not raise M: what others need is behind branches that
+// leave the straight line's registers alone (O in a second copy of the line would cost 80 more).
+template <bool kTwo, int R, int kMask, class X, class Slot, class Rescale, class P>
+__device__ void weights(X &x, float mult, float v_scale, float &v_top, int left, Slot slot_of, Column &c, Rescale rescale, P &ph, P &pl) {
     v_top = v_scale > v_top ? v_scale : v_top;
-    float s_v = v_scale == 0.f ? v_top : v_scale;
-    if (s_v == 0.f) s_v = 1.f;
-    const float shift = __builtin_amdgcn_logf(s_v);
     if (left < 32) {
+        if (mult == 0.f) mult = FLT_MIN;  // so that it takes -inf to -inf; 0 to the others all the same
 #pragma unroll
         for (int r = 0; r < R; ++r)
-            if (slot_of(r) >= left) x[r] = -FLT_MAX;
+            if (slot_of(r) >= left) x[r] = -INFINITY;
     }
     float top = x[0];
 #pragma unroll
-    for (int r = 1; r < R; ++r) top = fmaxf(top, x[r]);
-    if (kMask & 16) top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaf(fmaxf(top, __shfl_xor(top, 32)), mult, shift);  // mult is not negative
-    if (__any(top > M + kSlack)) {
-        const float to = fmaxf(M, top), less = exp2_of(M - to);
-        M = to;
-        D *= less;
+    for (int r = 1; r + 1 < R; r += 2) top = fmaxf(fmaxf(top, x[r]), x[r + 1]);
+    top = column_max<kMask>(fmaxf(top, x[R - 1])) * mult;  // mult is not negative
+    float shift = __builtin_amdgcn_logf(v_scale), inv = __builtin_amdgcn_rcpf(v_scale);
+    if (v_scale == 0.f) {
+        // Zero values: any scale gives the same sums.  One that leaves M where it is, for what follows must not be measured
+        // against rows that add nothing; the least there is where M is not set yet.
+        shift = fmaxf(c.M - top, -kLeastShift);
+        inv = exp2_of(-shift);
+    }
+    top += shift;
+    if (__any(top > c.M + kSlack)) {
+        const float to = fmaxf(c.M, top), less = exp2_of(c.M - to);
+        c.M = to;
+        c.D *= less;
         rescale(less);
     }
-    // One rounding, next to M; M's own is common to all rows.  Where it could reach 1, t is rounded before M is taken off.
-    const float off = shift - M + kLift;
-    if (__any(fabsf(M) > kLargeMax)) {
+    float off = shift - c.M + kLift;  // one rounding, next to M; M's own is common to all rows
+    if (__any(fabsf(c.M) > kLargeMax)) {  // where it could reach 1: t is rounded before M is taken off
 #pragma unroll
-        for (int r = 0; r < R; ++r) x[r] = exp2_of(fmaf(x[r], mult, shift) - M + kLift);
-    } else {
-#pragma unroll
-        for (int r = 0; r < R; ++r) x[r] = exp2_of(fmaf(x[r], mult, off));
+        for (int r = 0; r < R; ++r) x[r] = fmaf(x[r], mult, shift) - c.M;
+        mult = 1.f, off = kLift;
     }
-    if (left < 32) {  // whatever stood there, and whatever it became with a scale of 0
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-            if (slot_of(r) >= left) x[r] = 0.f;
-    }
-#pragma unroll
-    for (int r = 0; r < R; r += 2) {
-        const half2v hi = __builtin_convertvector(float2v{x[r], x[r + 1]}, half2v);
-        ph[r >> 3][r & 7] = hi[0], ph[r >> 3][(r & 7) + 1] = hi[1];
-        if constexpr (kTwo) {
-            const half2v lo = __builtin_convertvector(float2v{x[r] - (float)hi[0], x[r + 1] - (float)hi[1]}, half2v);
-            pl[r >> 3][r & 7] = lo[0], pl[r >> 3][(r & 7) + 1] = lo[1];
-        }
-    }
-    // One fp16: the sum of what is multiplied, so that a lone large u rounds without an error in out.  That needs every u
-    // that counts in D among fp16's normals: beside the values of a block of a far larger scale it may not be, while its
-    // weight is all of D.
     float sum = 0.f;
-    if (kTwo || s_v < v_top * 0x1p-6f) {
 #pragma unroll
-        for (int r = 0; r < R; ++r) sum += x[r];
-    } else {
+    for (int r = 0; r < R; r += 2) weigh_two<kTwo>(x, r, mult, off, sum, ph, pl);
+    // Summing what is multiplied needs every u that counts in D among fp16's normals: beside the values of a block of a far
+    // larger scale it may not be, while its weight is all of D.
+    if (!kTwo && !(v_scale >= v_top * 0x1p-6f && v_scale > 0.f)) {
+        sum = 0.f;
 #pragma unroll
-        for (int r = 0; r < R; r += 2)
-            sum = __builtin_amdgcn_fdot2(half2v{ph[r >> 3][r & 7], ph[r >> 3][(r & 7) + 1]},
-                                         half2v{(_Float16)1.f, (_Float16)1.f}, sum, false);
+        for (int r = 0; r < R; ++r) sum += exp2_of(fmaf(x[r], mult, off));
     }
-    D = fmaf(sum, 1.f / s_v, D);
+    c.D = fmaf(sum, inv, c.D);
 }
 
-// ---- many rows: a workgroup takes 128 QT rows through all of the request's slots ------------------------------------------
+// ---- many rows: a workgroup takes 128 rows through all of the request's slots ---------------------------------------------
 // S^T = K Q^T and O^T = V^T P^T on 32 x 32 x 16 instructions: a lane holds column (lane & 31) of both, so a row's statistics
 // are its lane's (and the other half's), and the products of S^T are the operand of O^T without a move, with V's slots
 // stored in the order in which S^T leaves them.
-// Two tiles of 32 slots are a stage: each wavefront loads K or V of one of them (a stage ahead, in registers), makes fp16 of
-// it once for all four, and puts it into LDS in units of 16 bytes, one operand of one lane, so that every read and write of
-// 64 lanes is 1 KiB without a bank met twice.  Two stages of LDS, one barrier a stage.
-// T: type of q and out.  NP: 32-dim steps of the head width.  QT: blocks of 32 rows to a wavefront.
-template <class T, int NP, int QT>
-__global__ __launch_bounds__(256, NP <= 4 ? 2 : 1) void k_xattn_kv(AttnArgs a) {
+// Two tiles of 32 slots are a stage: each wavefront loads K or V of one of them (two stages ahead, in registers), makes fp16
+// of it once for all four, and puts it into LDS in units of 16 bytes, one operand of one lane, so that every read and write of
+// 64 lanes is 1 KiB without a bank met twice.
+// The exponentials of a tile stand among the products of the next tile's logits: a matrix instruction of 32 cycles leaves
+// room for some eight others, and with all of one kind behind all of the other the two take turns (2 x 4096 x 24 x 128 over
+// 4000 rows: matrix pipes busy 32 % of 509 us).  Operands are read from LDS a tile ahead: K before the tile's largest logit
+// is sought, V where K's registers fall free.
+// LDS: two stages of K, three of V.  One barrier a stage, behind the first tile; in front of it the next stage is written.
+// K's place there was last read in front of the barrier before.  V's second tile of a stage is read behind that barrier, so
+// its place is written again only two barriers later.
+// T: type of q and out.  NP: 32-dim steps of the head width.
+// wavefronts to a SIMD that the registers leave
+constexpr int wide_waves(bool two, int NP) { return NP <= 1 ? 4 : NP <= 2 ? 3 : NP <= 4 ? 2 : 1; }
+template <class T, int NP>
+__global__ __launch_bounds__(256, wide_waves(std::is_same<T, float>::value, NP)) void k_xattn_kv(AttnArgs a) {
     constexpr bool kTwo = std::is_same<T, float>::value;  // two fp16 pieces
     constexpr int kPart = NP * 128;                       // units of K or V of a tile
-    extern __shared__ uint4 lds[];                        // [2 stages][2 tiles][K, V][kPart]
+    extern __shared__ uint4 lds[];                        // [2 stages of K, 3 of V][2 tiles][kPart]
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
     const int d = a.c.d, e16 = kv_padded(d), S = a.c.S, H = a.c.H, shift_S = __ffs(S) - 1;
     const int h = (int)(blockIdx.x / (uint32_t)a.tiles);
-    const Rows rows = find_rows<128 * QT>(a, (int32_t)(blockIdx.x % (uint32_t)a.tiles));
+    const Rows rows = find_rows<kWideRows>(a, (int32_t)(blockIdx.x % (uint32_t)a.tiles));
     if (rows.n == 0) return;
     const int64_t length = min((int64_t)max(a.lengths[rows.b], 0), (int64_t)a.width * S);
     const int32_t n_tiles = (int32_t)((length + 31) / 32), n_stages = (n_tiles + 1) / 2;
@@ -267,7 +296,9 @@ __global__ __launch_bounds__(256, NP <= 4 ? 2 : 1) void k_xattn_kv(AttnArgs a) {
 
     uint4 ahead[NP];
     const int my_tile = wave >> 1, my_part = wave & 1;
-    auto load = [&](int32_t st) {  // this wavefront's share of a stage
+    // This wavefront's share of a stage.  64 blocks hold whole stages (64 slots): a stage needs one look-up.
+    auto load = [&](int32_t st) {
+        if ((int32_t)(((int64_t)st * 64) >> shift_S) - block0 >= 64) look_up((int32_t)(((int64_t)st * 64) >> shift_S));
         const int32_t t = 2 * st + my_tile;
         if (t >= n_tiles) return;
         const int32_t block = __builtin_amdgcn_readlane(id, ((t * 32) >> shift_S) - block0);
@@ -281,7 +312,7 @@ __global__ __launch_bounds__(256, NP <= 4 ? 2 : 1) void k_xattn_kv(AttnArgs a) {
                 tile + (my_part ? 32 * e16 + min(s * 32 + col, e16 - 1) * 32 + half * 16 : ((2 * s + half) * 32 + col) * 16));
     };
     auto keep = [&](int32_t st) {
-        uint4 *to = lds + (((st & 1) * 2 + my_tile) * 2 + my_part) * kPart;
+        uint4 *to = lds + ((my_part * 2 + (st & 1)) * 2 + my_tile) * kPart;
 #pragma unroll
         for (int s = 0; s < NP; ++s) {
             const half8 lo = to_half8(ahead[s].x, ahead[s].y), hi = to_half8(ahead[s].z, ahead[s].w);
@@ -291,108 +322,90 @@ __global__ __launch_bounds__(256, NP <= 4 ? 2 : 1) void k_xattn_kv(AttnArgs a) {
             to[at + (my_part ? 64 : 32)] = __builtin_bit_cast(uint4, hi);
         }
     };
-    load(0);
+    // what a stage's tiles are multiplied with, and whether they are there; before the look-up moves on
+    struct Stage {
+        float ks[2], vs[2];
+        bool there[2];
+    };
+    auto terms_of = [&](int32_t st) {
+        Stage x;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int at = min(((2 * st + i) * 32 >> shift_S) - block0, 63);
+            x.there[i] = 2 * st + i < n_tiles && __builtin_amdgcn_readlane(id, at) >= 0;
+            x.ks[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scale), at));
+            x.vs[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scale), at));
+        }
+        return x;
+    };
 
-    half8 qh[QT][2 * NP], ql[QT][kTwo ? 2 * NP : 1];
-    float q_scale[QT];
+    load(0);
+    half8 qh[2 * NP], ql[kTwo ? 2 * NP : 1];
+    const int64_t m = (int64_t)rows.tile * kWideRows + wave * 32 + col;
+    const bool live = rows.has(a, m);
+    const T *q = live ? static_cast<const T *>(rows.query(a, h, m, sizeof(T))) : nullptr;
+    const float q_scale = split_query(q, live, d, 32, [&](int s) { return (s >> 1) * 32 + half * 16 + (s & 1) * 8; }, qh, ql);
+    float16v O[NP];
+    Column sums;
+    float v_top = 0.f;
 #pragma unroll
-    for (int i = 0; i < QT; ++i) {
-        const int64_t m = (int64_t)rows.tile * (128 * QT) + (wave * QT + i) * 32 + col;
-        const bool live = rows.has(a, m);
-        const T *q = live ? static_cast<const T *>(rows.query(a, h, m, sizeof(T))) : nullptr;
-        q_scale[i] = split_query(q, live, d, 32, [&](int s) { return (s >> 1) * 32 + half * 16 + (s & 1) * 8; }, qh[i], ql[i]);
-    }
-    float16v O[QT][NP];
-    float M[QT], D[QT], v_top = 0.f;
+    for (int s = 0; s < NP; ++s)
 #pragma unroll
-    for (int i = 0; i < QT; ++i) {
-        M[i] = kNoMax, D[i] = 0.f;
-#pragma unroll
-        for (int s = 0; s < NP; ++s)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) O[i][s][r] = 0.f;
-    }
+        for (int r = 0; r < 16; ++r) O[s][r] = 0.f;
+
+    Stage now = terms_of(0);
     keep(0);
     __syncthreads();
     for (int32_t st = 0; st < n_stages; ++st) {
         const bool more = st + 1 < n_stages;
-        int32_t ids[2];
-        float ks[2], vs[2];
+        if (more) load(st + 1);
+        const Stage then = terms_of(st + 1);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const int at = min(((2 * st + i) * 32 >> shift_S) - block0, 63);
-            ids[i] = 2 * st + i < n_tiles ? __builtin_amdgcn_readlane(id, at) : -1;
-            ks[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scale), at));
-            vs[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scale), at));
-        }
-        if (more) {
-            // 64 blocks hold whole stages (64 slots), so a stage never needs two look-ups
-            if ((((st + 1) * 64) >> shift_S) - block0 >= 64) look_up(((st + 1) * 64) >> shift_S);
-            load(st + 1);
-        }
+            if (!now.there[i]) continue;
+            const uint4 *K = lds + ((st & 1) * 2 + i) * kPart, *V = lds + ((2 + (st & 1)) * 2 + i) * kPart;
+            float16v x;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            if (ids[i] < 0) continue;
-            const uint4 *K = lds + ((st & 1) * 2 + i) * 2 * kPart, *V = K + kPart;
-            float16v acc[QT];
-#pragma unroll
-            for (int j = 0; j < QT; ++j)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) acc[j][r] = 0.f;
+            for (int r = 0; r < 16; ++r) x[r] = 0.f;
 #pragma unroll
             for (int s = 0; s < 2 * NP; ++s) {
                 const half8 k = __builtin_bit_cast(half8, K[((s >> 1) * 2 + half) * 64 + (s & 1) * 32 + col]);
-#pragma unroll
-                for (int j = 0; j < QT; ++j) {
-                    acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, qh[j][s], acc[j], 0, 0, 0);
-                    if constexpr (kTwo) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, ql[j][s], acc[j], 0, 0, 0);
-                }
+                x = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, qh[s], x, 0, 0, 0);
+                if constexpr (kTwo) x = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, ql[s], x, 0, 0, 0);
             }
-            half8 ph[QT][2], pl[QT][2];
+            half8 ph[2], pl[2];
+            weights<kTwo, 16, 32>(
+                x, q_scale * now.ks[i], now.vs[i], v_top, (int)min(length - (int64_t)(2 * st + i) * 32, (int64_t)32),
+                [&](int r) { return 8 * (r >> 2) + 4 * half + (r & 3); }, sums,
+                [&](float less) {
 #pragma unroll
-            for (int j = 0; j < QT; ++j) {
-                float x[16];
+                    for (int s = 0; s < NP; ++s)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) x[r] = acc[j][r];
-                weights<kTwo, 16, 32>(x, q_scale[j] * ks[i], vs[i], v_top, (int)min(length - (int64_t)(2 * st + i) * 32, (int64_t)32),
-                                      [&](int r) { return 8 * (r >> 2) + 4 * half + (r & 3); }, M[j], D[j],
-                                      [&](float less) {
+                        for (int r = 0; r < 16; ++r) O[s][r] *= less;
+                },
+                ph, pl);
 #pragma unroll
-                                          for (int s = 0; s < NP; ++s)
-#pragma unroll
-                                              for (int r = 0; r < 16; ++r) O[j][s][r] *= less;
-                                      },
-                                      ph[j], pl[j]);
+            for (int s = 0; s < 2 * NP; ++s) {
+                const half8 v = __builtin_bit_cast(half8, V[((s >> 1) * 4 + (s & 1) * 2 + half) * 32 + col]);
+                O[s >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, ph[s & 1], O[s >> 1], 0, 0, 0);
+                if constexpr (kTwo) O[s >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pl[s & 1], O[s >> 1], 0, 0, 0);
             }
-#pragma unroll
-            for (int s = 0; s < NP; ++s)
-#pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    const half8 v = __builtin_bit_cast(half8, V[(s * 4 + g * 2 + half) * 32 + col]);
-#pragma unroll
-                    for (int j = 0; j < QT; ++j) {
-                        O[j][s] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, ph[j][g], O[j][s], 0, 0, 0);
-                        if constexpr (kTwo) O[j][s] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pl[j][g], O[j][s], 0, 0, 0);
-                    }
-                }
         }
         if (more) keep(st + 1);
         __syncthreads();
+        now = then;
     }
+
+    const float D = sums.D + __shfl_xor(sums.D, 32), inv = D == 0.f ? 0.f : 1.f / D;
+    if (!live) return;
+    T *to = static_cast<T *>(a.out) + rows.out(a, h, m) * d;
 #pragma unroll
-    for (int j = 0; j < QT; ++j) {
-        const float sum = D[j] + __shfl_xor(D[j], 32), inv = sum == 0.f ? 0.f : 1.f / sum;
-        const int64_t m = (int64_t)rows.tile * (128 * QT) + (wave * QT + j) * 32 + col;
-        if (!rows.has(a, m)) continue;
-        T *to = static_cast<T *>(a.out) + rows.out(a, h, m) * d;
+    for (int s = 0; s < NP; ++s)
 #pragma unroll
-        for (int s = 0; s < NP; ++s)
-#pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const int e = s * 32 + 8 * (r >> 2) + 4 * half;
-                if (e < d) store4(to + e, O[j][s][r] * inv, O[j][s][r + 1] * inv, O[j][s][r + 2] * inv, O[j][s][r + 3] * inv);
-            }
-    }
+        for (int r = 0; r < 16; r += 4) {
+            const int e = s * 32 + 8 * (r >> 2) + 4 * half;
+            if (e < d) store4(to + e, O[s][r] * inv, O[s][r + 1] * inv, O[s][r + 2] * inv, O[s][r + 3] * inv);
+        }
 }
 
 // ---- few rows: a workgroup takes 16 rows through one split of the request's slots ----------------------------------------
@@ -448,7 +461,8 @@ __global__ __launch_bounds__(256, NC < 3 ? 2 : 1) void k_xattn_kv_few(AttnArgs a
     floatx4 O[4 * NC];
 #pragma unroll
     for (int i = 0; i < 4 * NC; ++i) O[i] = floatx4(0.f);
-    float M = kNoMax, D = 0.f, v_top = 0.f;
+    Column sums;
+    float v_top = 0.f;
     const int k_at = (group * 32 + 16 * (col >> 3) + (col & 7)) * 16;
     const int v_at = 32 * e16 + col * 32 + (group & 1) * 16 + (group >> 1) * 8;
     const int n_dims = e16 / 16;
@@ -487,13 +501,14 @@ __global__ __launch_bounds__(256, NC < 3 ? 2 : 1) void k_xattn_kv_few(AttnArgs a
 #pragma unroll
         for (int r = 0; r < 8; ++r) x[r] = acc[r >> 2][r & 3];
         half8 ph[1], pl[1];
-        weights<kTwo, 8, 48>(x, q_scale * ks, vs, v_top, (int)min(length - (int64_t)t * 32, (int64_t)32),
-                             [&](int r) { return 16 * (group >> 1) + 8 * (r >> 2) + 4 * (group & 1) + (r & 3); }, M, D,
-                             [&](float less) {
+        weights<kTwo, 8, 48>(
+            x, q_scale * ks, vs, v_top, (int)min(length - (int64_t)t * 32, (int64_t)32),
+            [&](int r) { return 16 * (group >> 1) + 8 * (r >> 2) + 4 * (group & 1) + (r & 3); }, sums,
+            [&](float less) {
 #pragma unroll
-                                 for (int i = 0; i < 4 * NC; ++i) O[i] *= less;
-                             },
-                             ph, pl);
+                for (int i = 0; i < 4 * NC; ++i) O[i] *= less;
+            },
+            ph, pl);
 #pragma unroll
         for (int i = 0; i < 4 * NC; ++i)
             if (i < n_dims) {
@@ -520,6 +535,7 @@ __global__ __launch_bounds__(256, NC < 3 ? 2 : 1) void k_xattn_kv_few(AttnArgs a
     }
 
     // ---- the four wavefronts' sums ----
+    float M = sums.M, D = sums.D;
     D += __shfl_xor(D, 16);
     D += __shfl_xor(D, 32);
     if (group == 0) stats[0][wave][col] = M, stats[1][wave][col] = D;
@@ -614,8 +630,6 @@ __global__ __launch_bounds__(256) void k_xattn_kv_join(AttnArgs a) {
     }
 }
 
-constexpr int kRowBlocks = 1;
-
 struct Plan {
     bool few;
     int32_t tiles, splits, chunk;
@@ -625,7 +639,7 @@ struct Plan {
 Plan plan_of(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t Hkv, int64_t slots) {
     const int64_t G = Hq / Hkv;
     auto tiles_of_rows = [&](int64_t R) { return packed ? rows * G / R + B : B * ((rows / B * G + R - 1) / R); };
-    const int64_t wide = tiles_of_rows(128 * kRowBlocks);
+    const int64_t wide = tiles_of_rows(kWideRows);
     if (rows * G > 16 * (int64_t)B && wide * Hkv >= 256) return {false, (int32_t)wide, 1, 0};
     const int64_t tiles = tiles_of_rows(16), groups = tiles * Hkv, slot_tiles = (slots + 31) / 32;
     // parts for about 1024 workgroups, none below 16 tiles (four to a wavefront) or above 256 (what one can look up)
@@ -641,8 +655,8 @@ hipError_t launch(const AttnArgs &a, bool few, hipStream_t st) {
         hipError_t e = hipSuccess;
         auto go = [&](auto np) {
             constexpr int NP = decltype(np)::value, bytes = NP * 16384;
-            e = DGQ_ENSURE_LDS((k_xattn_kv<T, NP, kRowBlocks>), bytes);
-            if (e == hipSuccess) k_xattn_kv<T, NP, kRowBlocks><<<grid, 256, bytes, st>>>(a);
+            e = DGQ_ENSURE_LDS((k_xattn_kv<T, NP>), bytes);
+            if (e == hipSuccess) k_xattn_kv<T, NP><<<grid, 256, bytes, st>>>(a);
         };
         switch ((a.c.d + 31) / 32) {
             case 1: go(std::integral_constant<int, 1>{}); break;
