@@ -42,6 +42,7 @@ struct AttnArgs {
     void *out;
     float *part;     // splits > 1: [splits][rows * Hq][d], then (M, D) [splits][rows * Hq][2]
     int32_t width, G, tiles;  // tiles: row tiles of all requests together (a bound when packed)
+    int32_t rows;             // rows of a row tile, for the kernel of short requests
     int32_t splits, chunk;    // a split is `chunk` tiles of 32 slots; as many as the table's width could fill
 };
 
@@ -57,13 +58,13 @@ __device__ half8 to_half8(uint32_t lo, uint32_t hi) {
     return r;
 }
 
-// 8 elements of a query, 4 of an output: 16-byte aligned, 4-element aligned
-__device__ float8v load8(const float *p) {
+// 8 loaded elements; 4 of an output, 4-element aligned
+__device__ float8v as_floats(const float *p) {
     const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
     return float8v{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 }
-__device__ float8v load8(const _Float16 *p) { return __builtin_convertvector(*reinterpret_cast<const half8 *>(p), float8v); }
-__device__ float8v load8(const __bf16 *p) {
+__device__ float8v as_floats(const _Float16 *p) { return __builtin_convertvector(*reinterpret_cast<const half8 *>(p), float8v); }
+__device__ float8v as_floats(const __bf16 *p) {
     const uint4 w = *reinterpret_cast<const uint4 *>(p);
     float8v r;
     r[0] = __uint_as_float(w.x << 16), r[1] = __uint_as_float(w.x & 0xffff0000u);
@@ -83,22 +84,26 @@ struct Rows {  // a row tile of one request; a row is a query and one of the G h
     int64_t first;  // first query of the request among all
     int32_t n;      // its queries; 0: there is no such tile
     int32_t tile;   // row tile within the request
-    // row `m` of the request
+    // row `m` of the request: fewer than 2^31 (query, head) rows in a call
     __device__ bool has(const AttnArgs &a, int64_t m) const { return m < (int64_t)n * a.G; }
+    __device__ static uint2 parts(const AttnArgs &a, int64_t m) {  // (query, head of the group)
+        if (a.G == 1) return uint2{(uint32_t)m, 0};
+        const uint32_t i = (uint32_t)m / (uint32_t)a.G;
+        return uint2{i, (uint32_t)m - i * (uint32_t)a.G};
+    }
     __device__ const void *query(const AttnArgs &a, int h, int64_t m, int size) const {
-        const int64_t i = m / a.G, head = (int64_t)h * a.G + (m - i * a.G);
-        const int64_t at = a.q.offsets ? (first + i) * a.q.row : b * a.q.batch + i * a.q.row;
-        return static_cast<const char *>(a.q.q) + (at + head * a.q.head) * size;
+        const uint2 p = parts(a, m);
+        const int64_t at = a.q.offsets ? (first + p.x) * a.q.row : b * a.q.batch + p.x * a.q.row;
+        return static_cast<const char *>(a.q.q) + (at + (int64_t)(h * a.G + (int)p.y) * a.q.head) * size;
     }
     __device__ int64_t out(const AttnArgs &a, int h, int64_t m) const {
-        const int64_t i = m / a.G;
-        return (first + i) * a.q.Hq + (int64_t)h * a.G + (m - i * a.G);
+        const uint2 p = parts(a, m);
+        return (first + p.x) * a.q.Hq + (h * a.G + (int)p.y);
     }
 };
 
 // The request that row tile `t` (of R rows) belongs to.
-template <int R>
-__device__ Rows find_rows(const AttnArgs &a, int32_t t) {
+__device__ Rows find_rows(const AttnArgs &a, int32_t t, int32_t R) {
     const int lane = threadIdx.x & 63;
     if (!a.q.offsets) {
         const int32_t per = (int32_t)(((int64_t)a.q.N * a.G + R - 1) / R);
@@ -129,24 +134,43 @@ __device__ Rows find_rows(const AttnArgs &a, int32_t t) {
     return {0, 0, 0, 0};
 }
 
-__device__ int32_t tiles_of(const AttnArgs &a, int32_t b) {  // of 32 slots
-    return (int32_t)((min((int64_t)max(a.lengths[b], 0), (int64_t)a.width * a.c.S) + 31) / 32);
+// Rows of a request: a multiple of 32 below 2^31 holds them.
+__device__ int32_t length_of(const AttnArgs &a, int32_t b) {
+    return __builtin_amdgcn_readfirstlane(min(max(a.lengths[b], 0), a.width * a.c.S));
 }
 
 __device__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// The pieces of one query.  Element 8 s + i of the lane's share is dim dim_of(s) + i; lanes that differ in the bits of
-// `mask` hold the rest of the row.  Returns what a logit (log2 units) is multiplied with.
+// What fp16 leaves of x f, in fp16: one mixed-precision instruction (of x - hi the compiler makes three).
+__device__ _Float16 rest_of(float x, float f, _Float16 hi) { return (_Float16)fmaf(x, f, -(float)hi); }
+
+// One lane's share of a query: element 8 s + i is dim dim_of(s) + i.  Raw: as loaded.
+template <class T, int N8>
+struct Raw {
+    uint4 w[N8 * (sizeof(T) == 4 ? 2 : 1)];
+};
 template <class T, int N8, class F>
-__device__ float split_query(const T *q, bool live, int d, int mask, F dim_of, half8 (&hi)[N8], half8 *lo) {
-    float8v x[N8];
-    uint32_t top = 0;
+__device__ void load_query(Raw<T, N8> &raw, const T *q, bool live, int d, F dim_of) {
+    constexpr int n = sizeof(T) == 4 ? 2 : 1;
 #pragma unroll
     for (int s = 0; s < N8; ++s) {
         const int e = dim_of(s);
-        x[s] = live && e < d ? load8(q + e) : float8v(0.f);
+        const bool in = live && e < d;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[s][i]) & 0x7fffffffu);
+        for (int i = 0; i < n; ++i) raw.w[s * n + i] = in ? reinterpret_cast<const uint4 *>(q + e)[i] : uint4{0, 0, 0, 0};
+    }
+}
+// The fp16 pieces.  Lanes that differ in the bits of `mask` (32, or 48) hold the rest of the row.  Returns what a product is
+// multiplied with to be a logit in log2 units.
+template <class T, int N8>
+__device__ float split_query(const Raw<T, N8> &raw, int d, int mask, half8 (&hi)[N8], half8 *lo) {
+    constexpr int n = sizeof(T) == 4 ? 2 : 1;
+    uint32_t top = 0;
+#pragma unroll
+    for (int s = 0; s < N8; ++s) {
+        const float8v x = as_floats(reinterpret_cast<const T *>(&raw.w[s * n]));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
     }
     if (mask & 16) top = max(top, (uint32_t)__shfl_xor((int)top, 16));
     top = max(top, (uint32_t)__shfl_xor((int)top, 32));
@@ -154,15 +178,99 @@ __device__ float split_query(const T *q, bool live, int d, int mask, F dim_of, h
     const int up = min(14 + 127 - (int)(top >> 23), 126);
     const float lift = top ? __uint_as_float((uint32_t)(127 + up) << 23) : 1.f;
 #pragma unroll
-    for (int s = 0; s < N8; ++s)
+    for (int s = 0; s < N8; ++s) {
+        const float8v x = as_floats(reinterpret_cast<const T *>(&raw.w[s * n]));
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float y = x[s][i] * lift;
+            const float y = x[i] * lift;
             hi[s][i] = (_Float16)y;
-            if constexpr (std::is_same<T, float>::value) lo[s][i] = (_Float16)(y - (float)hi[s][i]);
+            if constexpr (std::is_same<T, float>::value) lo[s][i] = rest_of(x[i], lift, hi[s][i]);
         }
+    }
     const float back = top >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : 1.f / lift;
     return back * (kLog2e / sqrtf((float)d));
+}
+
+// ---- 32 rows between memory and the lanes of the matrix cores ------------------------------------------------------------
+// A lane of an operand has a whole half row: loads and stores in that order touch 32 rows in 16-byte pieces (100 us for 16 x
+// 4096 x 10 x 64 fp32 rows in and out with one slot to attend to; a copy takes 63).  So rows cross memory 128 bytes to 8 lanes
+// and change places in 4 KiB of LDS of the wavefront's own, without a barrier: LDS serves a wavefront in order.  A 16-byte
+// unit u of row r is at unit u ^ (r & 7): no bank twice either way.
+constexpr int kSwapBytes = 4096;
+template <class T>
+constexpr int kUnit = 16 / (int)sizeof(T);  // elements
+template <class T, int NP>
+constexpr int kChunks = sizeof(T) == 4 ? NP : (NP + 1) / 2;  // of 128 bytes of a row
+
+__device__ void wave_order() {  // LDS accesses of the wavefront's lanes stay on their side
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// A lane's place: unit lane % 8 of rows lane / 8 + 8 i.  row: their elements in memory, null where there are none.
+template <class T, int NP>
+struct Swap {
+    uint4 w[kChunks<T, NP> * 4];
+    __device__ void load(const T *const (&row)[4], int d) {
+        const int unit = threadIdx.x & 7;
+#pragma unroll
+        for (int c = 0; c < kChunks<T, NP>; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int e = (c * 8 + unit) * kUnit<T>;
+                w[c * 4 + i] = row[i] && e < d ? *reinterpret_cast<const uint4 *>(row[i] + e) : uint4{0, 0, 0, 0};
+            }
+    }
+    // to the order of a B operand: element 8 s + i of a lane is dim 32 (s / 2) + 16 half + 8 (s % 2) + i of row `col`
+    __device__ void spread(uint4 *lds, Raw<T, 2 * NP> &raw) const {
+        const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+        constexpr int per = 8 / kUnit<T>;  // units of 8 elements
+#pragma unroll
+        for (int c = 0; c < kChunks<T, NP>; ++c) {
+            wave_order();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = (lane >> 3) + 8 * i;
+                lds[r * 8 + ((lane & 7) ^ (r & 7))] = w[c * 4 + i];
+            }
+            wave_order();
+#pragma unroll
+            for (int s = 0; s < 2 * NP; ++s) {
+                constexpr int dims = 8 * kUnit<T>;  // of a chunk
+                if ((s >> 1) * 32 / dims != c) continue;
+                const int u = ((s >> 1) * 32 % dims + half * 16 + (s & 1) * 8) / kUnit<T>;
+#pragma unroll
+                for (int i = 0; i < per; ++i) raw.w[s * per + i] = lds[col * 8 + ((u + i) ^ (col & 7))];
+            }
+        }
+    }
+};
+// O^T as the products leave it, times `inv` of the lane's column, to rows in memory.
+template <class T, int NP>
+__device__ void store_rows(uint4 *lds, const float16v (&O)[NP], float inv, T *const (&row)[4], int d) {
+    typedef T vec __attribute__((ext_vector_type(4)));
+    const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+    constexpr int dims = 8 * kUnit<T>;
+#pragma unroll
+    for (int c = 0; c < kChunks<T, NP>; ++c) {
+        wave_order();
+#pragma unroll
+        for (int s = 0; s < NP; ++s) {
+            if (s * 32 / dims != c) continue;
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const int e = s * 32 % dims + 8 * (r >> 2) + 4 * half, u = e / kUnit<T>;
+                vec *to = reinterpret_cast<vec *>(lds + col * 8 + (u ^ (col & 7))) + (e % kUnit<T>) / 4;
+                *to = vec{(T)(O[s][r] * inv), (T)(O[s][r + 1] * inv), (T)(O[s][r + 2] * inv), (T)(O[s][r + 3] * inv)};
+            }
+        }
+        wave_order();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = (lane >> 3) + 8 * i, e = (c * 8 + (lane & 7)) * kUnit<T>;
+            if (row[i] && e < d) *reinterpret_cast<uint4 *>(row[i] + e) = lds[r * 8 + ((lane & 7) ^ (r & 7))];
+        }
+    }
 }
 
 // Over the lanes that hold one column: the other half's, and with kMask 48 the four of a 16-lane column.
@@ -184,8 +292,9 @@ __device__ void weigh_two(const X &x, int r, float mult, float off, float &sum, 
     const half2v hi = __builtin_convertvector(u, half2v);
     ph[r >> 3][r & 7] = hi[0], ph[r >> 3][(r & 7) + 1] = hi[1];
     if constexpr (kTwo) {
-        const half2v lo = __builtin_convertvector(float2v{u[0] - (float)hi[0], u[1] - (float)hi[1]}, half2v);
-        pl[r >> 3][r & 7] = lo[0], pl[r >> 3][(r & 7) + 1] = lo[1];
+        float one = 1.f;
+        asm("" : "+s"(one));  // a factor that the compiler cannot take out
+        pl[r >> 3][r & 7] = rest_of(u[0], one, hi[0]), pl[r >> 3][(r & 7) + 1] = rest_of(u[1], one, hi[1]);
         sum += u[0] + u[1];
     } else {
         sum = __builtin_amdgcn_fdot2(hi, half2v{(_Float16)1.f, (_Float16)1.f}, sum, false);
@@ -198,13 +307,15 @@ struct Column {
 };
 
 // A tile's logits x become weights, and M and D move on.  `left` of its 32 slots are rows; slot_of(r) is the slot of x[r].
-// v_top: the largest value scale so far.  rescale(f): multiply O by f.
+// v_scale, v_top: bits of the tile's value scale and of the largest so far (not negative: their order is the numbers').
+// rescale(f): multiply O by f.
 // Nearly every tile is whole, with a scale like the others', and does not raise M: what others need is behind branches that
 // leave the straight line's registers alone (O in a second copy of the line would cost 80 more).
 template <bool kTwo, int R, int kMask, class X, class Slot, class Rescale, class P>
-__device__ void weights(X &x, float mult, float v_scale, float &v_top, int left, Slot slot_of, Column &c, Rescale rescale, P &ph, P &pl) {
-    v_top = v_scale > v_top ? v_scale : v_top;
+__device__ void weights(X &x, float mult, uint32_t v_scale, uint32_t &v_top, int left, Slot slot_of, Column &c, Rescale rescale, P &ph, P &pl) {
+    v_top = max(v_top, v_scale);
     if (left < 32) {
+        asm volatile("");  // a branch: as selects it would cost every tile 30 instructions
         if (mult == 0.f) mult = FLT_MIN;  // so that it takes -inf to -inf; 0 to the others all the same
 #pragma unroll
         for (int r = 0; r < R; ++r)
@@ -214,8 +325,9 @@ __device__ void weights(X &x, float mult, float v_scale, float &v_top, int left,
 #pragma unroll
     for (int r = 1; r + 1 < R; r += 2) top = fmaxf(fmaxf(top, x[r]), x[r + 1]);
     top = column_max<kMask>(fmaxf(top, x[R - 1])) * mult;  // mult is not negative
-    float shift = __builtin_amdgcn_logf(v_scale), inv = __builtin_amdgcn_rcpf(v_scale);
-    if (v_scale == 0.f) {
+    float shift = __builtin_amdgcn_logf(__uint_as_float(v_scale)), inv = __builtin_amdgcn_rcpf(__uint_as_float(v_scale));
+    if (v_scale == 0) {
+        asm volatile("");
         // Zero values: any scale gives the same sums.  One that leaves M where it is, for what follows must not be measured
         // against rows that add nothing; the least there is where M is not set yet.
         shift = fmaxf(c.M - top, -kLeastShift);
@@ -239,7 +351,7 @@ __device__ void weights(X &x, float mult, float v_scale, float &v_top, int left,
     for (int r = 0; r < R; r += 2) weigh_two<kTwo>(x, r, mult, off, sum, ph, pl);
     // Summing what is multiplied needs every u that counts in D among fp16's normals: beside the values of a block of a far
     // larger scale it may not be, while its weight is all of D.
-    if (!kTwo && !(v_scale >= v_top * 0x1p-6f && v_scale > 0.f)) {
+    if (!kTwo && v_scale + (6u << 23) < v_top) {
         sum = 0.f;
 #pragma unroll
         for (int r = 0; r < R; ++r) sum += exp2_of(fmaf(x[r], mult, off));
@@ -263,19 +375,30 @@ __device__ void weights(X &x, float mult, float v_scale, float &v_top, int left,
 // its place is written again only two barriers later.
 // T: type of q and out.  NP: 32-dim steps of the head width.
 // wavefronts to a SIMD that the registers leave
-constexpr int wide_waves(bool two, int NP) { return NP <= 1 ? 4 : NP <= 2 ? 3 : NP <= 4 ? 2 : 1; }
+constexpr int wide_waves(int NP) { return NP <= 1 ? 4 : NP <= 2 ? 3 : NP <= 4 ? 2 : 1; }
 template <class T, int NP>
-__global__ __launch_bounds__(256, wide_waves(std::is_same<T, float>::value, NP)) void k_xattn_kv(AttnArgs a) {
+__global__ __launch_bounds__(256, wide_waves(NP)) void k_xattn_kv(AttnArgs a) {
     constexpr bool kTwo = std::is_same<T, float>::value;  // two fp16 pieces
     constexpr int kPart = NP * 128;                       // units of K or V of a tile
     extern __shared__ uint4 lds[];                        // [2 stages of K, 3 of V][2 tiles][kPart]
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
     const int d = a.c.d, e16 = kv_padded(d), S = a.c.S, H = a.c.H, shift_S = __ffs(S) - 1;
     const int h = (int)(blockIdx.x / (uint32_t)a.tiles);
-    const Rows rows = find_rows<kWideRows>(a, (int32_t)(blockIdx.x % (uint32_t)a.tiles));
+    const Rows rows = find_rows(a, (int32_t)(blockIdx.x % (uint32_t)a.tiles), kWideRows);
     if (rows.n == 0) return;
-    const int64_t length = min((int64_t)max(a.lengths[rows.b], 0), (int64_t)a.width * S);
-    const int32_t n_tiles = (int32_t)((length + 31) / 32), n_stages = (n_tiles + 1) / 2;
+    const int32_t length = length_of(a, rows.b);
+    const int32_t n_tiles = (length + 31) / 32, n_stages = (n_tiles + 1) / 2;
+
+    const int64_t m0 = (int64_t)rows.tile * kWideRows + wave * 32 + (lane >> 3);  // and 8, 16, 24 further: this lane's rows
+    uint4 *swap_at = lds + wave * (kSwapBytes / 16);  // in the stages' place, before and after
+    Swap<T, NP> fetched;
+    {
+        const T *row[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            row[i] = rows.has(a, m0 + 8 * i) ? static_cast<const T *>(rows.query(a, h, m0 + 8 * i, sizeof(T))) : nullptr;
+        fetched.load(row, d);
+    }
 
     // block numbers and scales of 64 blocks, one a lane
     int32_t block0 = 0, id = -1;
@@ -324,7 +447,8 @@ __global__ __launch_bounds__(256, wide_waves(std::is_same<T, float>::value, NP))
     };
     // what a stage's tiles are multiplied with, and whether they are there; before the look-up moves on
     struct Stage {
-        float ks[2], vs[2];
+        float ks[2];
+        uint32_t vs[2];
         bool there[2];
     };
     auto terms_of = [&](int32_t st) {
@@ -334,20 +458,20 @@ __global__ __launch_bounds__(256, wide_waves(std::is_same<T, float>::value, NP))
             const int at = min(((2 * st + i) * 32 >> shift_S) - block0, 63);
             x.there[i] = 2 * st + i < n_tiles && __builtin_amdgcn_readlane(id, at) >= 0;
             x.ks[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scale), at));
-            x.vs[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scale), at));
+            x.vs[i] = __builtin_amdgcn_readlane(__float_as_uint(v_scale), at);
         }
         return x;
     };
 
     load(0);
     half8 qh[2 * NP], ql[kTwo ? 2 * NP : 1];
-    const int64_t m = (int64_t)rows.tile * kWideRows + wave * 32 + col;
-    const bool live = rows.has(a, m);
-    const T *q = live ? static_cast<const T *>(rows.query(a, h, m, sizeof(T))) : nullptr;
-    const float q_scale = split_query(q, live, d, 32, [&](int s) { return (s >> 1) * 32 + half * 16 + (s & 1) * 8; }, qh, ql);
+    Raw<T, 2 * NP> raw;
+    fetched.spread(swap_at, raw);
+    const float q_scale = split_query(raw, d, 32, qh, ql);
+    __syncthreads();
     float16v O[NP];
     Column sums;
-    float v_top = 0.f;
+    uint32_t v_top = 0;
 #pragma unroll
     for (int s = 0; s < NP; ++s)
 #pragma unroll
@@ -375,7 +499,7 @@ __global__ __launch_bounds__(256, wide_waves(std::is_same<T, float>::value, NP))
             }
             half8 ph[2], pl[2];
             weights<kTwo, 16, 32>(
-                x, q_scale * now.ks[i], now.vs[i], v_top, (int)min(length - (int64_t)(2 * st + i) * 32, (int64_t)32),
+                x, q_scale * now.ks[i], now.vs[i], v_top, length - (2 * st + i) * 32,
                 [&](int r) { return 8 * (r >> 2) + 4 * half + (r & 3); }, sums,
                 [&](float less) {
 #pragma unroll
@@ -397,15 +521,124 @@ __global__ __launch_bounds__(256, wide_waves(std::is_same<T, float>::value, NP))
     }
 
     const float D = sums.D + __shfl_xor(sums.D, 32), inv = D == 0.f ? 0.f : 1.f / D;
-    if (!live) return;
-    T *to = static_cast<T *>(a.out) + rows.out(a, h, m) * d;
+    T *row[4];
 #pragma unroll
-    for (int s = 0; s < NP; ++s)
+    for (int i = 0; i < 4; ++i) row[i] = rows.has(a, m0 + 8 * i) ? static_cast<T *>(a.out) + rows.out(a, h, m0 + 8 * i) * d : nullptr;
+    store_rows<T, NP>(swap_at, O, inv, row, d);
+}
+
+constexpr int short_waves(bool two, int NP) { return NP <= 1 ? 4 : NP <= 2 ? 3 : NP <= (two ? 3 : 4) ? 2 : 1; }
+
+// ---- many rows, short requests: all of a request's tiles fit LDS ----------------------------------------------------------
+// A workgroup makes fp16 of the request's K and V once and takes a.rows rows through them, 32 to a wavefront at a time, with
+// no barrier after the first; the next 32 queries are loaded while these are worked on.  Bound by the queries' and the
+// output's bytes.
+template <class T, int NP>
+__global__ __launch_bounds__(256, short_waves(sizeof(T) == 4, NP)) void k_xattn_kv_short(AttnArgs a) {
+    constexpr bool kTwo = std::is_same<T, float>::value;
+    constexpr int kPart = NP * 128;  // units of K or V of a tile
+    extern __shared__ uint4 lds[];   // a swap place for each wavefront, then [tiles][K, V][kPart] as in k_xattn_kv
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
+    const int d = a.c.d, e16 = kv_padded(d), S = a.c.S, H = a.c.H, shift_S = __ffs(S) - 1;
+    const int h = (int)(blockIdx.x / (uint32_t)a.tiles);
+    const Rows rows = find_rows(a, (int32_t)(blockIdx.x % (uint32_t)a.tiles), a.rows);
+    if (rows.n == 0) return;
+    const int64_t all_rows = (int64_t)rows.n * a.G, m0 = (int64_t)rows.tile * a.rows;
+    const int32_t here = (int32_t)min((int64_t)a.rows, all_rows - m0);
+    uint4 *swap_at = lds + wave * (kSwapBytes / 16), *tiles = lds + 4 * (kSwapBytes / 16);
+    Swap<T, NP> next;
+    auto fetch = [&](int32_t at) {
+        const T *row[4];
 #pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-            const int e = s * 32 + 8 * (r >> 2) + 4 * half;
-            if (e < d) store4(to + e, O[s][r] * inv, O[s][r + 1] * inv, O[s][r + 2] * inv, O[s][r + 3] * inv);
+        for (int i = 0; i < 4; ++i) {
+            const int32_t m = at + (lane >> 3) + 8 * i;
+            row[i] = m < here ? static_cast<const T *>(rows.query(a, h, m0 + m, sizeof(T))) : nullptr;
         }
+        next.load(row, d);
+    };
+    fetch(wave * 32);
+
+    // at most 64 blocks: a lane looks one up, whether the request reaches it or not
+    int32_t id = lane < a.width ? a.table[(int64_t)rows.b * a.width + lane] : -1;
+    const int32_t length = length_of(a, rows.b);
+    const int32_t n_tiles = (length + 31) / 32;
+    if (id >= a.c.n_blocks) id = -1;
+    float2 scale{0.f, 0.f};
+    if (id >= 0) scale = reinterpret_cast<const float2 *>(a.c.scales)[(int64_t)id * H + h];
+    for (int p = wave; p < 2 * n_tiles; p += 4) {
+        const int t = p >> 1, part = p & 1;
+        const int32_t block = __builtin_amdgcn_readlane(id, (t * 32) >> shift_S);
+        if (block < 0) continue;
+        const uint8_t *tile = a.c.codes + ((int64_t)block * H + h) * kv_slice_bytes(S, d) + (int64_t)(t & ((S >> 5) - 1)) * 64 * e16;
+        uint4 w[NP];
+#pragma unroll
+        for (int s = 0; s < NP; ++s)
+            w[s] = *reinterpret_cast<const uint4 *>(
+                tile + (part ? 32 * e16 + min(s * 32 + col, e16 - 1) * 32 + half * 16 : ((2 * s + half) * 32 + col) * 16));
+#pragma unroll
+        for (int s = 0; s < NP; ++s) {
+            const int at = part ? (s * 4 + half) * 32 + col : (2 * s + half) * 64 + col;
+            tiles[p * kPart + at] = __builtin_bit_cast(uint4, to_half8(w[s].x, w[s].y));
+            tiles[p * kPart + at + (part ? 64 : 32)] = __builtin_bit_cast(uint4, to_half8(w[s].z, w[s].w));
+        }
+    }
+    __syncthreads();
+
+    for (int32_t at = wave * 32; at < here; at += 128) {
+        half8 qh[2 * NP], ql[kTwo ? 2 * NP : 1];
+        Raw<T, 2 * NP> raw;
+        next.spread(swap_at, raw);
+        const float q_scale = split_query(raw, d, 32, qh, ql);
+        if (at + 128 < here) fetch(at + 128);
+        float16v O[NP];
+#pragma unroll
+        for (int s = 0; s < NP; ++s)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) O[s][r] = 0.f;
+        Column sums;
+        uint32_t v_top = 0;
+        for (int32_t t = 0; t < n_tiles; ++t) {
+            const int block = (t * 32) >> shift_S;
+            if (__builtin_amdgcn_readlane(id, block) < 0) continue;
+            const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scale.x), block));
+            const uint32_t vs = __builtin_amdgcn_readlane(__float_as_uint(scale.y), block);
+            const uint4 *K = tiles + t * 2 * kPart, *V = K + kPart;
+            float16v x;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) x[r] = 0.f;
+#pragma unroll
+            for (int s = 0; s < 2 * NP; ++s) {
+                const half8 k = __builtin_bit_cast(half8, K[((s >> 1) * 2 + half) * 64 + (s & 1) * 32 + col]);
+                x = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, qh[s], x, 0, 0, 0);
+                if constexpr (kTwo) x = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, ql[s], x, 0, 0, 0);
+            }
+            half8 ph[2], pl[2];
+            weights<kTwo, 16, 32>(
+                x, q_scale * ks, vs, v_top, length - t * 32,
+                [&](int r) { return 8 * (r >> 2) + 4 * half + (r & 3); }, sums,
+                [&](float less) {
+#pragma unroll
+                    for (int s = 0; s < NP; ++s)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) O[s][r] *= less;
+                },
+                ph, pl);
+#pragma unroll
+            for (int s = 0; s < 2 * NP; ++s) {
+                const half8 v = __builtin_bit_cast(half8, V[((s >> 1) * 4 + (s & 1) * 2 + half) * 32 + col]);
+                O[s >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, ph[s & 1], O[s >> 1], 0, 0, 0);
+                if constexpr (kTwo) O[s >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pl[s & 1], O[s >> 1], 0, 0, 0);
+            }
+        }
+        const float D = sums.D + __shfl_xor(sums.D, 32), inv = D == 0.f ? 0.f : 1.f / D;
+        T *row[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int32_t m = at + (lane >> 3) + 8 * i;
+            row[i] = m < here ? static_cast<T *>(a.out) + rows.out(a, h, m0 + m) * d : nullptr;
+        }
+        store_rows<T, NP>(swap_at, O, inv, row, d);
+    }
 }
 
 // ---- few rows: a workgroup takes 16 rows through one split of the request's slots ----------------------------------------
@@ -426,15 +659,15 @@ __global__ __launch_bounds__(256, NC < 3 ? 2 : 1) void k_xattn_kv_few(AttnArgs a
     constexpr bool kTwo = std::is_same<T, float>::value;
     constexpr int kPitch = 68;  // floats of one row's 64 dims in LDS
     __shared__ float part[4][16][kPitch], stats[2][4][16];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = lane >> 4, col = lane & 15;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = lane >> 4, col = lane & 15;
     const int d = a.c.d, e16 = kv_padded(d), S = a.c.S, H = a.c.H, shift_S = __ffs(S) - 1;
     const int split = (int)(blockIdx.x % (uint32_t)a.splits);
     const int64_t task = blockIdx.x / (uint32_t)a.splits;
     const int h = (int)(task / a.tiles);
-    const Rows rows = find_rows<16>(a, (int32_t)(task % a.tiles));
+    const Rows rows = find_rows(a, (int32_t)(task % a.tiles), 16);
     if (rows.n == 0) return;
-    const int64_t length = min((int64_t)max(a.lengths[rows.b], 0), (int64_t)a.width * S);
-    const int32_t n_tiles = (int32_t)((length + 31) / 32);
+    const int32_t length = length_of(a, rows.b);
+    const int32_t n_tiles = (length + 31) / 32;
     const int32_t t0 = split * a.chunk, t1 = min(t0 + a.chunk, n_tiles);
     if (split > 0 && t0 >= t1) return;  // the join knows how many splits there are
     const int32_t per = (t1 - t0 + 3) / 4, w0 = t0 + wave * per, w1 = min(w0 + per, t1);
@@ -454,15 +687,17 @@ __global__ __launch_bounds__(256, NC < 3 ? 2 : 1) void k_xattn_kv_few(AttnArgs a
 
     const int64_t m = (int64_t)rows.tile * 16 + col;
     const bool live = rows.has(a, m);
+    Raw<T, 2 * NC> raw;
+    load_query(raw, live ? static_cast<const T *>(rows.query(a, h, m, sizeof(T))) : nullptr, live, d,
+               [&](int s) { return (s >> 1) * 64 + group * 16 + (s & 1) * 8; });
     half8 qh[2 * NC], ql[kTwo ? 2 * NC : 1];
-    const T *q = live ? static_cast<const T *>(rows.query(a, h, m, sizeof(T))) : nullptr;
-    const float q_scale = split_query(q, live, d, 48, [&](int s) { return (s >> 1) * 64 + group * 16 + (s & 1) * 8; }, qh, ql);
+    const float q_scale = split_query(raw, d, 48, qh, ql);
 
     floatx4 O[4 * NC];
 #pragma unroll
     for (int i = 0; i < 4 * NC; ++i) O[i] = floatx4(0.f);
     Column sums;
-    float v_top = 0.f;
+    uint32_t v_top = 0;
     const int k_at = (group * 32 + 16 * (col >> 3) + (col & 7)) * 16;
     const int v_at = 32 * e16 + col * 32 + (group & 1) * 16 + (group >> 1) * 8;
     const int n_dims = e16 / 16;
@@ -483,7 +718,7 @@ __global__ __launch_bounds__(256, NC < 3 ? 2 : 1) void k_xattn_kv_few(AttnArgs a
         const int at = ((t * 32) >> shift_S) - block0;
         if (__builtin_amdgcn_readlane(id, at) < 0) return;
         const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scale), at));
-        const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scale), at));
+        const uint32_t vs = __builtin_amdgcn_readlane(__float_as_uint(v_scale), at);
         floatx4 acc[2] = {floatx4(0.f), floatx4(0.f)};
 #pragma unroll
         for (int s = 0; s < NC; ++s)
@@ -502,7 +737,7 @@ __global__ __launch_bounds__(256, NC < 3 ? 2 : 1) void k_xattn_kv_few(AttnArgs a
         for (int r = 0; r < 8; ++r) x[r] = acc[r >> 2][r & 3];
         half8 ph[1], pl[1];
         weights<kTwo, 8, 48>(
-            x, q_scale * ks, vs, v_top, (int)min(length - (int64_t)t * 32, (int64_t)32),
+            x, q_scale * ks, vs, v_top, length - t * 32,
             [&](int r) { return 16 * (group >> 1) + 8 * (r >> 2) + 4 * (group & 1) + (r & 3); }, sums,
             [&](float less) {
 #pragma unroll
@@ -591,7 +826,7 @@ __global__ __launch_bounds__(256) void k_xattn_kv_join(AttnArgs a) {
         if (!found) return;  // a row that no request has is left as it was
         b = __shfl(b, __ffsll((unsigned long long)found) - 1);
     }
-    const int active = (tiles_of(a, b) + a.chunk - 1) / a.chunk;
+    const int active = ((length_of(a, b) + 31) / 32 + a.chunk - 1) / a.chunk;
     if (active <= 1) return;  // the only split has written out itself
     const float2 *stats = reinterpret_cast<const float2 *>(a.part + a.splits * all * d) + row;
     const int quads = d / 4, runs = 256 / quads, quad = tid % quads, run = tid / quads;
@@ -630,33 +865,48 @@ __global__ __launch_bounds__(256) void k_xattn_kv_join(AttnArgs a) {
     }
 }
 
+enum Kernel { kFew, kShort, kLong };
 struct Plan {
-    bool few;
-    int32_t tiles, splits, chunk;
+    Kernel kernel;
+    int32_t tiles, rows, splits, chunk;
 };
+constexpr int kShortBytes = 32 * 1024;  // of tiles: three workgroups to a CU, with the swap places
+constexpr int tile_bytes(int d) { return (d + 31) / 32 * 4096; }  // fp16 of a tile's K and V
 
 // Which kernel, its row tiles, and into how many parts each request's slots are split.
-Plan plan_of(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t Hkv, int64_t slots) {
+Plan plan_of(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t Hkv, int32_t d, int64_t slots) {
     const int64_t G = Hq / Hkv;
     auto tiles_of_rows = [&](int64_t R) { return packed ? rows * G / R + B : B * ((rows / B * G + R - 1) / R); };
-    const int64_t wide = tiles_of_rows(kWideRows);
-    if (rows * G > 16 * (int64_t)B && wide * Hkv >= 256) return {false, (int32_t)wide, 1, 0};
-    const int64_t tiles = tiles_of_rows(16), groups = tiles * Hkv, slot_tiles = (slots + 31) / 32;
+    const int64_t wide = tiles_of_rows(kWideRows), slot_tiles = (slots + 31) / 32;
+    if (rows * G > 16 * (int64_t)B && wide * Hkv >= 256) {
+        if (slot_tiles * tile_bytes(d) > kShortBytes) return {kLong, (int32_t)wide, kWideRows, 1, 0};
+        // 128 rows at a time, as often as leaves some 1536 workgroups (six to a CU: lengths differ)
+        const int64_t times = std::max<int64_t>(1, std::min<int64_t>(16, wide * Hkv / 1536));
+        return {kShort, (int32_t)tiles_of_rows(128 * times), (int32_t)(128 * times), 1, 0};
+    }
+    const int64_t tiles = tiles_of_rows(16), groups = tiles * Hkv;
     // parts for about 1024 workgroups, none below 16 tiles (four to a wavefront) or above 256 (what one can look up)
     const int64_t want = std::max<int64_t>(1, 1024 / std::max<int64_t>(1, groups));
     const int64_t chunk = std::min<int64_t>(256, std::max<int64_t>(16, ((slot_tiles + want - 1) / want + 3) / 4 * 4));
-    return {true, (int32_t)tiles, (int32_t)std::max<int64_t>(1, (slot_tiles + chunk - 1) / chunk), (int32_t)chunk};
+    return {kFew, (int32_t)tiles, 16, (int32_t)std::max<int64_t>(1, (slot_tiles + chunk - 1) / chunk), (int32_t)chunk};
 }
 
 template <class T>
-hipError_t launch(const AttnArgs &a, bool few, hipStream_t st) {
-    if (!few) {
+hipError_t launch(const AttnArgs &a, Kernel kernel, hipStream_t st) {
+    if (kernel != kFew) {
         const dim3 grid((uint32_t)((int64_t)a.tiles * a.c.H));
         hipError_t e = hipSuccess;
         auto go = [&](auto np) {
-            constexpr int NP = decltype(np)::value, bytes = NP * 16384;
-            e = DGQ_ENSURE_LDS((k_xattn_kv<T, NP>), bytes);
-            if (e == hipSuccess) k_xattn_kv<T, NP><<<grid, 256, bytes, st>>>(a);
+            constexpr int NP = decltype(np)::value;
+            if (kernel == kShort) {
+                const int bytes = (int)(((int64_t)a.width * a.c.S + 31) / 32) * tile_bytes(a.c.d) + 4 * kSwapBytes;
+                e = DGQ_ENSURE_LDS((k_xattn_kv_short<T, NP>), kShortBytes + 4 * kSwapBytes);
+                if (e == hipSuccess) k_xattn_kv_short<T, NP><<<grid, 256, bytes, st>>>(a);
+            } else {
+                constexpr int bytes = NP * 16384;
+                e = DGQ_ENSURE_LDS((k_xattn_kv<T, NP>), bytes);
+                if (e == hipSuccess) k_xattn_kv<T, NP><<<grid, 256, bytes, st>>>(a);
+            }
         };
         switch ((a.c.d + 31) / 32) {
             case 1: go(std::integral_constant<int, 1>{}); break;
@@ -688,16 +938,16 @@ hipError_t launch(const AttnArgs &a, bool few, hipStream_t st) {
 }  // namespace
 
 size_t xattn_kv_workspace_bytes(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t Hkv, int32_t d, int64_t slots) {
-    const Plan p = plan_of(B, rows, packed, Hq, Hkv, slots);
+    const Plan p = plan_of(B, rows, packed, Hq, Hkv, d, slots);
     return p.splits > 1 ? (size_t)p.splits * rows * Hq * (d + 2) * sizeof(float) : 0;
 }
 
 hipError_t launch_xattn_kv(const KvQueries &q, const KvCache &c, const int32_t *table, int32_t width,
                            const int32_t *lengths, void *out, void *workspace, hipStream_t st) {
-    const Plan p = plan_of(q.B, q.rows(), q.offsets != nullptr, q.Hq, c.H, (int64_t)width * c.S);
-    const AttnArgs a{q, c, table, lengths, out, static_cast<float *>(workspace), width, q.Hq / c.H, p.tiles, p.splits, p.chunk};
-    return q.dtype == DGQ_F32 ? launch<float>(a, p.few, st)
-           : q.dtype == DGQ_F16 ? launch<_Float16>(a, p.few, st) : launch<__bf16>(a, p.few, st);
+    const Plan p = plan_of(q.B, q.rows(), q.offsets != nullptr, q.Hq, c.H, c.d, (int64_t)width * c.S);
+    const AttnArgs a{q, c, table, lengths, out, static_cast<float *>(workspace), width, q.Hq / c.H, p.tiles, p.rows, p.splits, p.chunk};
+    return q.dtype == DGQ_F32 ? launch<float>(a, p.kernel, st)
+           : q.dtype == DGQ_F16 ? launch<_Float16>(a, p.kernel, st) : launch<__bf16>(a, p.kernel, st);
 }
 
 }  // namespace dgq
