@@ -173,103 +173,210 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_release(
     }
 }
 
-// ---- writing ---------------------------------------------------------------------------------------------------------
+// ---- between rows and a tile's bytes ----------------------------------------------------------------------------------
+// An item is 4 rows (slots 4 q .. 4 q + 3) by one 16-byte load of dims: V keeps 4 such slots of a dim in one word, K keeps the
+// dims of a slot together, so an item's codes are whole words of either, and rows cross memory in whole lines.  The words
+// meet in an image of the tile in LDS, which crosses memory in whole lines too.  16-byte units of the image change places so
+// that the items of a wavefront, whose words lie 128 or 512 bytes apart, meet few banks twice.
+template <class T>
+constexpr int kVec = 16 / (int)sizeof(T);
+
+__host__ __device__ inline int k_unit(int unit) { return unit ^ ((unit >> 5) & 7); }  // [chunk][32 slots]
+__host__ __device__ inline int v_unit(int unit) { return unit ^ ((unit >> 3) & 7); }  // [dim][2]
+// words of the image: dims e .. e + 3 of a slot; slots 4 q .. 4 q + 3 of a dim (q < 8)
+__device__ int k_word(int slot, int e) { return k_unit((e >> 4) * 32 + slot) * 4 + ((e >> 2) & 3); }
+__device__ int v_word(int q, int e) { return v_unit(e * 2 + (q & 1)) * 4 + (q >> 1); }
 
 template <class T>
-__device__ float as_float(T x) { return (float)x; }
-
-__device__ uint32_t byte_of(float x, float inv) {
-    const float r = rintf(x * inv);
-    // NaN fails both comparisons and becomes 0
-    return r >= 127.f ? 255u : r <= -127.f ? 1u : (uint32_t)((r == r ? (int)r : 0) + 128);
+__device__ void to_floats(const uint4 &w, float (&f)[kVec<T>]) {
+    if constexpr (sizeof(T) == 4) {
+        f[0] = __uint_as_float(w.x), f[1] = __uint_as_float(w.y), f[2] = __uint_as_float(w.z), f[3] = __uint_as_float(w.w);
+    } else {
+        const T *x = reinterpret_cast<const T *>(&w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = (float)x[i];
+    }
 }
 
-// One workgroup per (run, head, K or V).  Two passes over the run's rows: the first finds max |x|, the second, which
-// finds them in the L2, makes the codes.  Rows that the block held before keep their values, coded against the new scale.
-template <class T>
+// code + 128 of a finite x
+__device__ float code_of(float x, float inv) { return fminf(fmaxf(rintf(x * inv), -127.f), 127.f) + 128.f; }
+__device__ float value_of(uint32_t word, int byte, float scale) { return ((float)((word >> (8 * byte)) & 255) - 128.f) * scale; }
+
+// ---- writing ---------------------------------------------------------------------------------------------------------
+// One workgroup per (run, head, K or V).  The run's rows are read once, into registers: max |x|, then the codes.  Bound by
+// the bytes; I: items of a thread.
+template <class T, int I>
 __global__ __launch_bounds__(256) void k_kv_store(
     const T *__restrict__ k, const T *__restrict__ v, int64_t rows, int64_t k_row, int64_t k_head, int64_t v_row,
     int64_t v_head, const int4 *__restrict__ runs, KvCache c) {
+    extern __shared__ uint32_t image[];  // [S / 32][e16 8 words]
+    __shared__ uint32_t tops[4];
+    constexpr int V = kVec<T>;
     const int4 run = runs[blockIdx.x];
-    const int32_t block = run.x, slot0 = run.z, n = run.w, h = blockIdx.y, S = c.S, d = c.d;
+    const int32_t block = run.x, slot0 = run.z, n = run.w, h = blockIdx.y, S = c.S, d = c.d, tid = threadIdx.x;
     const bool is_v = blockIdx.z;
     if (n < 1 || block < 0 || block >= c.n_blocks || slot0 < 0 || (int64_t)slot0 + n > S || run.y < 0 || (int64_t)run.y + n > rows)
         return;
     const int64_t stride = is_v ? v_row : k_row;
-    const T *x = (is_v ? v + h * v_head : k + h * k_head) + run.y * stride;
-
-    uint32_t top = 0;  // |x| as bits: their order is the numbers', and NaN is above infinity
-    for (int i = threadIdx.x; i < n * d; i += 256) {
-        const int r = i / d, e = i - r * d;
-        top = max(top, __float_as_uint(as_float(x[r * stride + e])) & 0x7fffffffu);
-    }
-    for (int o = 32; o; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
-    __shared__ uint32_t tops[4];
-    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
-    __syncthreads();
-    top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
-
+    const T *x = (is_v ? v + h * v_head : k + h * k_head) + (run.y - (int64_t)slot0) * stride;  // of slot 0, were it there
+    const int groups = d / V, quad0 = slot0 / 4, items = ((slot0 + n - 1) / 4 - quad0 + 1) * groups;
     float *scale = c.scales + ((int64_t)block * c.H + h) * 2 + is_v;
     const float s_old = slot0 > 0 ? *scale : 0.f;
+
+    uint4 w[I][4];
+    uint32_t top = 0;  // |x| as bits: their order is the numbers', and NaN is above infinity
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+        const int item = tid + 256 * i, quad = quad0 + item / groups, e = (item % groups) * V;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int slot = quad * 4 + r;
+            w[i][r] = uint4{0, 0, 0, 0};
+            if (item < items && slot >= slot0 && slot < slot0 + n) w[i][r] = *reinterpret_cast<const uint4 *>(x + slot * stride + e);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float f[V];
+            to_floats<T>(w[i][r], f);
+#pragma unroll
+            for (int o = 0; o < V; ++o) top = max(top, __float_as_uint(f[o]) & 0x7fffffffu);
+        }
+    for (int o = 32; o; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+    if ((tid & 63) == 0) tops[tid >> 6] = top;
+    __syncthreads();  // (every thread has read the old scale)
+    top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
     float s = __uint_as_float(top) * (1.f / 127.f);
     if (s < kKvLeastScale) s = 0.f;
     s = __uint_as_float(max(__float_as_uint(s), __float_as_uint(s_old)));  // as bits: NaN stays
     const float inv = s > 0.f ? 1.f / s : 0.f;
-    __syncthreads();
-    if (threadIdx.x == 0) *scale = s;
+    if (tid == 0) *scale = s;
 
-    const int e16 = kv_padded(d);
-    uint8_t *codes = c.codes + ((int64_t)block * c.H + h) * kv_slice_bytes(S, d);
-    // a thread makes 16 bytes: of K, 16 dims of one slot; of V, 16 slots of one dim
-    for (int u = threadIdx.x; u < S * e16 / 16; u += 256) {
-        const int tile = u / (2 * e16), w = u - tile * 2 * e16;
-        uint8_t *to = codes + (int64_t)tile * 64 * e16 + (is_v ? 32 * e16 : 0) + w * 16;
-        uint4 word = *reinterpret_cast<const uint4 *>(to);
-        uint32_t *word32 = reinterpret_cast<uint32_t *>(&word);
-        for (int i = 0; i < 16; ++i) {
-            const int slot = tile * 32 + (is_v ? kv_slot(w & 1, i) : w & 31);
-            const int e = is_v ? w >> 1 : (w >> 5) * 16 + i;
-            uint32_t byte = 128;
-            if (e < d && slot < slot0 + n) {
-                const uint32_t was = (word32[i >> 2] >> (8 * (i & 3))) & 255;
-                byte = slot >= slot0 ? byte_of(as_float(x[(slot - slot0) * stride + e]), inv)
-                                     : byte_of((float)((int)was - 128) * s_old, inv);
+    const int e16 = kv_padded(d), units = e16 * 2, n_tiles = S / 32;  // units of 16 bytes of a tile's K or V
+    uint4 *codes = reinterpret_cast<uint4 *>(c.codes + ((int64_t)block * c.H + h) * kv_slice_bytes(S, d)) + (is_v ? units : 0);
+    // What the items leave open: rows in front (coded against the new scale), rows behind, dims from d on.
+    if (slot0 > 0 || n < S || d < e16) {
+        for (int u = tid; u < n_tiles * units; u += 256) {
+            const int tile = u / units, at = u - tile * units;
+            uint4 word{0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};
+            if (slot0 > tile * 32 && inv > 0.f) {
+                word = codes[tile * 2 * units + at];
+                uint32_t *b = reinterpret_cast<uint32_t *>(&word);
+                for (int i = 0; i < 16; ++i) {
+                    const int slot = tile * 32 + (is_v ? kv_slot(at & 1, i) : at & 31), e = is_v ? at >> 1 : (at >> 5) * 16 + i;
+                    const uint32_t byte = slot < slot0 && e < d ? (uint32_t)code_of(value_of(b[i >> 2], i & 3, s_old), inv) : 128u;
+                    b[i >> 2] = (b[i >> 2] & ~(255u << (8 * (i & 3)))) | byte << (8 * (i & 3));
+                }
             }
-            word32[i >> 2] = (word32[i >> 2] & ~(255u << (8 * (i & 3)))) | byte << (8 * (i & 3));
+            reinterpret_cast<uint4 *>(image)[tile * units + (is_v ? v_unit(at) : k_unit(at))] = word;
         }
-        *reinterpret_cast<uint4 *>(to) = word;
+        __syncthreads();
+    }
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+        const int item = tid + 256 * i, quad = quad0 + item / groups, e = (item % groups) * V;
+        if (item >= items) break;
+        uint32_t *to = image + (quad >> 3) * units * 4;
+        float f[4][V];
+        uint32_t mask = 0;  // of the four slots, as bytes
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            to_floats<T>(w[i][r], f[r]);
+            if (quad * 4 + r >= slot0 && quad * 4 + r < slot0 + n) mask |= 255u << (8 * r);
+#pragma unroll
+            for (int o = 0; o < V; ++o) f[r][o] = inv > 0.f ? code_of(f[r][o], inv) : 128.f;
+        }
+        if (is_v) {
+#pragma unroll
+            for (int o = 0; o < V; ++o) {
+                uint32_t word = 0;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) word |= (uint32_t)f[r][o] << (8 * r);
+                uint32_t *p = to + v_word(quad & 7, e + o);
+                *p = mask == 0xffffffffu ? word : (*p & ~mask) | (word & mask);  // no other thread has these bytes
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if (!(mask >> (8 * r) & 1)) continue;
+#pragma unroll
+                for (int o = 0; o < V; o += 4)
+                    to[k_word((quad & 7) * 4 + r, e + o)] = (uint32_t)f[r][o] | (uint32_t)f[r][o + 1] << 8 | (uint32_t)f[r][o + 2] << 16 |
+                                                            (uint32_t)f[r][o + 3] << 24;
+            }
+        }
+    }
+    __syncthreads();
+    for (int u = tid; u < n_tiles * units; u += 256) {
+        const int tile = u / units, at = u - tile * units;
+        codes[tile * 2 * units + at] = reinterpret_cast<const uint4 *>(image)[tile * units + (is_v ? v_unit(at) : k_unit(at))];
     }
 }
 
 // ---- reading back ------------------------------------------------------------------------------------------------------
-
+// One workgroup per (32 rows of a request, head), K and V.  Bound by the bytes written.
 template <class T>
 __global__ __launch_bounds__(256) void k_kv_load(KvCache c, const int32_t *__restrict__ table, int32_t width,
                                                  const int32_t *__restrict__ lengths, int32_t max_rows,
                                                  T *__restrict__ k, T *__restrict__ v) {
-    const int tile = blockIdx.x, h = blockIdx.y, b = blockIdx.z, S = c.S, d = c.d, e16 = kv_padded(d);
-    const int64_t length = min((int64_t)max(lengths[b], 0), (int64_t)width * S);
-    const int row0 = tile * 32;
+    extern __shared__ uint32_t image[];  // [K, V][e16 8 words]
+    constexpr int V = kVec<T>;
+    const int row0 = blockIdx.x * 32, h = blockIdx.y, b = blockIdx.z, S = c.S, d = c.d, units = kv_padded(d) * 2, tid = threadIdx.x;
+    const int length = min(max(lengths[b], 0), width * S);
     int32_t block = -1;
     if (row0 < length) block = table[(int64_t)b * width + row0 / S];
-    const bool there = block >= 0 && block < c.n_blocks;
+    const bool there = block >= 0 && block < c.n_blocks;  // of the whole workgroup
     float2 scale{0.f, 0.f};
-    const uint8_t *codes = c.codes;
     if (there) {
         scale = reinterpret_cast<const float2 *>(c.scales)[(int64_t)block * c.H + h];
-        codes += ((int64_t)block * c.H + h) * kv_slice_bytes(S, d) + (int64_t)(row0 % S / 32) * 64 * e16;
-    }
-    for (int i = threadIdx.x; i < 32 * d; i += 256) {
-        const int slot = i / d, e = i - slot * d, row = row0 + slot;
-        if (row >= max_rows) break;
-        const int64_t to = (((int64_t)b * max_rows + row) * c.H + h) * d + e;
-        float kx = 0.f, vx = 0.f;
-        if (there && row < length) {
-            kx = (float)((int)codes[kv_k_byte(slot, e)] - 128) * scale.x;
-            vx = (float)((int)codes[32 * e16 + kv_v_byte(slot, e)] - 128) * scale.y;
+        const uint4 *codes = reinterpret_cast<const uint4 *>(c.codes + ((int64_t)block * c.H + h) * kv_slice_bytes(S, d)) +
+                             (row0 % S / 32) * 2 * units;
+        for (int u = tid; u < 2 * units; u += 256) {
+            const int at = u < units ? k_unit(u) : units + v_unit(u - units);
+            reinterpret_cast<uint4 *>(image)[at] = codes[u];
         }
-        k[to] = (T)kx;
-        v[to] = (T)vx;
+        __syncthreads();
+    }
+    const int groups = d / V, most = min(length, max_rows);
+    for (int item = tid; item < 16 * groups; item += 256) {
+        const bool is_v = item >= 8 * groups;
+        const int at = is_v ? item - 8 * groups : item, quad = at / groups, e = (at - quad * groups) * V;
+        float f[4][V];
+        if (!there) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int o = 0; o < V; ++o) f[r][o] = 0.f;
+        } else if (is_v) {
+#pragma unroll
+            for (int o = 0; o < V; ++o) {
+                const uint32_t word = image[units * 4 + v_word(quad, e + o)];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) f[r][o] = value_of(word, r, scale.y);
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int o = 0; o < V; o += 4) {
+                    const uint32_t word = image[k_word(quad * 4 + r, e + o)];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) f[r][o + j] = value_of(word, j, scale.x);
+                }
+        }
+        T *to = (is_v ? v : k) + (((int64_t)b * max_rows + row0 + quad * 4) * c.H + h) * d + e;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int row = row0 + quad * 4 + r;
+            if (row >= max_rows) break;
+            typedef T vec __attribute__((ext_vector_type(V)));
+            vec x;
+#pragma unroll
+            for (int o = 0; o < V; ++o) x[o] = (T)(row < most ? f[r][o] : 0.f);
+            *reinterpret_cast<vec *>(to + (int64_t)r * c.H * d) = x;
+        }
     }
 }
 
@@ -300,10 +407,16 @@ hipError_t launch_kv_store(const void *k, const void *v, int32_t dtype, int64_t 
                            int64_t v_row, int64_t v_head, const int32_t *runs, int32_t n_runs, const KvCache &c,
                            hipStream_t st) {
     const dim3 grid(n_runs, c.H, 2);
+    const int bytes = c.S * kv_padded(c.d);  // at most 32 KiB
     auto go = [&](auto x) {
         using T = decltype(x);
-        k_kv_store<T><<<grid, 256, 0, st>>>(static_cast<const T *>(k), static_cast<const T *>(v), rows, k_row, k_head, v_row,
-                                            v_head, reinterpret_cast<const int4 *>(runs), c);
+        const T *kt = static_cast<const T *>(k), *vt = static_cast<const T *>(v);
+        const int4 *r = reinterpret_cast<const int4 *>(runs);
+        const int items = (c.S / 4 * (c.d / kVec<T>) + 255) / 256;  // at most 8 (fp32), 4
+        if (items <= 1) k_kv_store<T, 1><<<grid, 256, bytes, st>>>(kt, vt, rows, k_row, k_head, v_row, v_head, r, c);
+        else if (items <= 2) k_kv_store<T, 2><<<grid, 256, bytes, st>>>(kt, vt, rows, k_row, k_head, v_row, v_head, r, c);
+        else if (items <= 4) k_kv_store<T, 4><<<grid, 256, bytes, st>>>(kt, vt, rows, k_row, k_head, v_row, v_head, r, c);
+        else if constexpr (sizeof(T) == 4) k_kv_store<T, 8><<<grid, 256, bytes, st>>>(kt, vt, rows, k_row, k_head, v_row, v_head, r, c);
     };
     dtype == DGQ_F32 ? go(float{}) : dtype == DGQ_F16 ? go(_Float16{}) : go(__bf16{});
     return hipGetLastError();
@@ -314,7 +427,7 @@ hipError_t launch_kv_load(const KvCache &c, const int32_t *table, int32_t width,
     const dim3 grid((max_rows + 31) / 32, c.H, B);
     auto go = [&](auto x) {
         using T = decltype(x);
-        k_kv_load<T><<<grid, 256, 0, st>>>(c, table, width, lengths, max_rows, static_cast<T *>(k), static_cast<T *>(v));
+        k_kv_load<T><<<grid, 256, 64 * kv_padded(c.d), st>>>(c, table, width, lengths, max_rows, static_cast<T *>(k), static_cast<T *>(v));
     };
     dtype == DGQ_F32 ? go(float{}) : dtype == DGQ_F16 ? go(_Float16{}) : go(__bf16{});
     return hipGetLastError();
