@@ -571,7 +571,7 @@ typedef enum dgq_dtype { DGQ_F32 = 0, DGQ_F16 = 1, DGQ_BF16 = 2 } dgq_dtype;
  *   runs         int32 [max_runs, 4], 16-byte aligned, max_runs >= rows / block_size + 2 B: one entry for every block that
  *                gets rows, (block, first row in the packed tensors, first slot, rows), requests in order; (-1, 0, 0, 0)
  *                behind them.  It is the rows' slot map with one entry a block, since a block's rows share a scale
- *   counts       int32 [4]: runs, blocks taken, requests not served, row_offsets[B]
+ *   counts       int32 [4], 16-byte aligned: runs, blocks taken, requests not served, row_offsets[B]
  * 1 <= B <= DGQ_KV_MAX_REQUESTS, width * block_size < 2^31.  Enqueues on `stream`; neither synchronises nor allocates.
  */
 int dgq_kv_plan(const int32_t *lengths, const int32_t *new_rows, int32_t B, int32_t block_size, int64_t rows,

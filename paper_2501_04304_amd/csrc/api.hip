@@ -1312,7 +1312,7 @@ int dgq_kv_plan(const int32_t *lengths, const int32_t *new_rows, int32_t B, int3
         return fail(DGQ_EINVAL, "dgq_kv_plan: the new state needs buffers of its own");
     if (max_runs < rows / block_size + 2 * (int64_t)B)
         return fail(DGQ_ESHAPE, "dgq_kv_plan: max_runs below rows / block_size + 2 B");
-    if (!aligned16(runs)) return fail(DGQ_EALIGN, "dgq_kv_plan: runs not 16-byte aligned");
+    if (!aligned16(runs) || !aligned16(counts)) return fail(DGQ_EALIGN, "dgq_kv_plan: runs or counts not 16-byte aligned");
     DGQ_HIP(launch_kv_plan(lengths, new_rows, B, block_size, rows, table, width, free_blocks, free_capacity, n_free, lengths_out,
                            n_free_out, row_offsets, runs, (int32_t)max_runs, counts, static_cast<hipStream_t>(stream)));
     return DGQ_OK;

@@ -143,7 +143,7 @@ struct KvCache {
     float *scales;   // [n_blocks, H, 2]: K, V
     int32_t n_blocks, S, H, d;
 };
-constexpr int kKvMaxRequests = 4096;          // what the planner's LDS holds
+constexpr int kKvMaxRequests = DGQ_KV_MAX_REQUESTS;  // 16 to a thread of the planner
 constexpr int kKvMaxDim = 256;
 constexpr float kKvLeastScale = 0x1p-96f;     // a block whose scale would be below it holds zeros
 __host__ __device__ inline int kv_padded(int d) { return (d + 15) & ~15; }

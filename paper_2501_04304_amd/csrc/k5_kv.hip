@@ -5,34 +5,48 @@
 // (block, head) has one scale for K and one for V:
 //   s = max |x| * (1/127) over the block's rows,  code = clamp(rne(x * (1/s)), -127, 127),  stored byte = code + 128.
 // The layout (dgq_internal.h, kv_*) is the attention's: a lane's 16-byte load is an operand of the matrix cores.
+#include <algorithm>
+#include <type_traits>
+
 #include "dgq_internal.h"
 
 namespace dgq {
 namespace {
 
-constexpr int kPlanThreads = 1024;
+constexpr int kPlanArrays = 4;  // 32-bit words a request in LDS
 
-// Inclusive sums over the workgroup of two 64-bit values per thread; `total` of both for everyone.
-struct Pair {
-    int64_t a, b;
-};
-__device__ Pair scan_pair(Pair v, Pair &total, Pair *lds /* [kPlanThreads / 64] */) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int o = 1; o < 64; o <<= 1) {
-        const int64_t a = __shfl_up(v.a, o), b = __shfl_up(v.b, o);
-        if (lane >= o) v.a += a, v.b += b;
-    }
+// x of the lane that the DPP control names, 0 where there is none.
+template <int CTRL, int ROWS = 15>
+__device__ int64_t dpp(int64_t x) {
+    const int lo = __builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 15, false);
+    const int hi = __builtin_amdgcn_update_dpp(0, (int)(x >> 32), CTRL, ROWS, 15, false);
+    return (int64_t)((uint64_t)(uint32_t)hi << 32 | (uint32_t)lo);
+}
+// Inclusive sums over a wavefront: within rows of 16 lanes, then row 0 to 1 and 2 to 3, then the first half to the second.
+__device__ int64_t wave_sums(int64_t x) {
+    x += dpp<0x111>(x);
+    x += dpp<0x112>(x);
+    x += dpp<0x114>(x);
+    x += dpp<0x118>(x);
+    x += dpp<0x142, 0xa>(x);
+    x += dpp<0x143, 0xc>(x);
+    return x;
+}
+// Inclusive sums over the workgroup, and the total.  lds: an entry a wavefront, of this call's own.
+template <int WAVES>
+__device__ int64_t group_sums(int64_t x, int64_t &total, int64_t *lds) {
+    const int wave = threadIdx.x >> 6;
+    x = wave_sums(x);
+    if ((threadIdx.x & 63) == 63) lds[wave] = x;
     __syncthreads();
-    if (lane == 63) lds[wave] = v;
-    __syncthreads();
-    Pair before{0, 0};
-    total = {0, 0};
-    for (int w = 0; w < kPlanThreads / 64; ++w) {
-        const Pair p = lds[w];
-        if (w < wave) before.a += p.a, before.b += p.b;
-        total.a += p.a, total.b += p.b;
+    total = 0;
+    int64_t before = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        if (w < wave) before += lds[w];
+        total += lds[w];
     }
-    return {v.a + before.a, v.b + before.b};
+    return x + before;
 }
 
 // First index in [0, n) whose entry is above x (n if none); `ends` ascending.
@@ -45,131 +59,138 @@ __device__ int first_above(const int32_t *ends, int n, int32_t x) {
     return lo;
 }
 
-__device__ int64_t blocks_of(int64_t rows, int32_t S) { return (rows + S - 1) / S; }
+__device__ int32_t clamp31(int64_t x) { return (int32_t)min(x, (int64_t)INT32_MAX); }
 
-// What one request asks for.
-struct Ask {
-    int64_t old, add, total, take;
-    bool ok;
-    __device__ Ask(int32_t length, int32_t more, int32_t S, int64_t width)
-        : old(length), add(more), total(old + add), take(0), ok(old >= 0 && add >= 0 && total <= width * S) {
-        if (ok) take = blocks_of(total, S) - blocks_of(old, S);
-    }
-};
-
-// Every workgroup scans all requests (at most kKvMaxRequests: a few per thread) and writes its share of the runs, so
-// nothing has to be passed between workgroups: the sums over some thousand requests take less than a second launch.
-// Bound by latency: two scans and a search per run.  The prefixes that a run needs stay in LDS, 12 bytes a request.
-__global__ __launch_bounds__(kPlanThreads) void k_kv_plan(
-    const int32_t *__restrict__ lengths, const int32_t *__restrict__ new_rows, int32_t B, int32_t S, int64_t rows,
+// Every workgroup sums over all requests (PER to a thread, in registers) and writes its share of the runs, so nothing has to be
+// passed between workgroups: the sums over some thousand requests take less than a second launch.  Bound by latency: one
+// read of the requests, two sums, a search and a read of the free list for every run.
+template <int THREADS, int PER>
+__global__ __launch_bounds__(THREADS) void k_kv_plan(
+    const int32_t *__restrict__ lengths, const int32_t *__restrict__ new_rows, int32_t B, int32_t shift_S, int64_t rows,
     int32_t *table, int32_t width, const int32_t *__restrict__ free_blocks, int32_t free_capacity,
     const int32_t *__restrict__ n_free_in, int32_t *__restrict__ lengths_out, int32_t *__restrict__ n_free_out,
     int32_t *__restrict__ row_offsets, int4 *__restrict__ runs, int32_t max_runs, int32_t *__restrict__ counts) {
-    __shared__ int32_t run_ends[kKvMaxRequests], row0[kKvMaxRequests], take0[kKvMaxRequests];
-    __shared__ Pair sums[kPlanThreads / 64];
+    extern __shared__ int32_t request[];  // [kPlanArrays][B]
+    __shared__ int64_t sums[4][THREADS / 64];
+    int32_t *run_ends = request, *row0 = request + B, *take0 = request + 2 * B, *held = request + 3 * B;
+    const int32_t S = 1 << shift_S, b0 = threadIdx.x * PER;
+    int32_t old[PER], add[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        old[i] = b0 + i < B ? lengths[b0 + i] : 0;
+        add[i] = b0 + i < B ? new_rows[b0 + i] : 0;
+    }
     const int32_t n_free = min(max(*n_free_in, 0), free_capacity);
-    const int per = (B + kPlanThreads - 1) / kPlanThreads;
-    const int b0 = min((int)threadIdx.x * per, B), b1 = min(b0 + per, B);
 
-    // rows of the packed tensors and blocks asked for, in the order of the requests
-    Pair mine{0, 0}, total;
-    for (int b = b0; b < b1; ++b) {
-        mine.a += max(new_rows[b], 0);
+    // Rows of the packed tensors, and blocks asked for, in the order of the requests.  (A request whose rows end behind
+    // `rows` counts here too: those before it, which is all that may be served, are not touched by that.)
+    auto fits = [&](int i) { return old[i] >= 0 && add[i] >= 0 && (int64_t)old[i] + add[i] <= (int64_t)width << shift_S; };
+    auto need = [&](int i) { return (((int64_t)old[i] + add[i] + S - 1) >> shift_S) - (((int64_t)old[i] + S - 1) >> shift_S); };
+    int64_t my_rows = 0, my_blocks = 0, all_rows, total;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        my_rows += max(add[i], 0);
+        if (fits(i)) my_blocks += need(i);
     }
-    Pair rows_before = scan_pair(mine, total, sums);
-    const int64_t all_rows = total.a;
-    int64_t at = rows_before.a - mine.a;
-    Pair asked{0, 0};
-    for (int b = b0; b < b1; ++b) {
-        const Ask ask(lengths[b], new_rows[b], S, width);
-        row0[b] = (int32_t)min(at, (int64_t)INT32_MAX);
-        at += max(new_rows[b], 0);
-        if (ask.ok && at <= rows) asked.a += ask.take;
-    }
-    Pair ends = scan_pair(asked, total, sums);
-    int64_t blocks = ends.a - asked.a;
+    int64_t row = group_sums<THREADS / 64>(my_rows, all_rows, sums[0]) - my_rows, block = group_sums<THREADS / 64>(my_blocks, total, sums[1]) - my_blocks;
 
     // a request is served if the free blocks reach for it and for all before it
-    at = rows_before.a - mine.a;
-    Pair given{0, 0};  // runs, blocks
-    int64_t refused = 0;
-    for (int b = b0; b < b1; ++b) {
-        const Ask ask(lengths[b], new_rows[b], S, width);
-        at += max(new_rows[b], 0);
-        const bool ok = ask.ok && at <= rows;
-        take0[b] = (int32_t)min(blocks, (int64_t)INT32_MAX);
-        if (ok) blocks += ask.take;
-        const bool served = ok && (ask.add == 0 || blocks <= n_free);
-        if (served && ask.add > 0) given.a += blocks_of(ask.total, S) - ask.old / S, given.b += ask.take;
-        run_ends[b] = (int32_t)given.a;
-        refused += !served;
-        if (blockIdx.x == 0) {
-            lengths_out[b] = served ? (int32_t)ask.total : lengths[b];
-            row_offsets[b] = row0[b];
+    int32_t served = 0;  // bits
+    int64_t my_runs = 0, others = 0;  // others: blocks taken, and requests not served in the upper half
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int64_t first = block, end = row + max(add[i], 0);
+        const bool ok = fits(i);
+        if (ok) block += need(i);
+        const bool yes = ok && end <= rows && (add[i] == 0 || block <= n_free);
+        if (b0 + i < B) {
+            row0[b0 + i] = clamp31(row);
+            take0[b0 + i] = clamp31(first);
+            held[b0 + i] = old[i];
+            if (yes) served |= 1 << i;
+            if (yes && add[i] > 0) my_runs += (((int64_t)old[i] + add[i] + S - 1) >> shift_S) - (old[i] >> shift_S), others += need(i);
+            if (!yes) others += (int64_t)1 << 32;
+            if (blockIdx.x == 0) {
+                lengths_out[b0 + i] = yes ? old[i] + add[i] : old[i];
+                row_offsets[b0 + i] = clamp31(row);
+            }
         }
+        row = end;
     }
-    ends = scan_pair(given, total, sums);
-    const int32_t before = (int32_t)(ends.a - given.a);
-    for (int b = b0; b < b1; ++b) run_ends[b] += before;
-    const int32_t n_runs = (int32_t)min(total.a, (int64_t)max_runs);
-    const int64_t taken = total.b;
-    scan_pair({refused, 0}, total, sums);  // its barriers also publish run_ends
+    int64_t all_runs, all_others;
+    int64_t run = group_sums<THREADS / 64>(my_runs, all_runs, sums[2]) - my_runs;
+    group_sums<THREADS / 64>(others, all_others, sums[3]);
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+        if (b0 + i < B) {
+            if (served >> i & 1 && add[i] > 0) run += (((int64_t)old[i] + add[i] + S - 1) >> shift_S) - (old[i] >> shift_S);
+            run_ends[b0 + i] = (int32_t)run;
+        }
+    __syncthreads();
+    const int32_t n_runs = (int32_t)min(all_runs, (int64_t)max_runs), taken = (int32_t)all_others;
     if (blockIdx.x == 0 && threadIdx.x == 0) {
-        row_offsets[B] = (int32_t)min(all_rows, (int64_t)INT32_MAX);
-        *n_free_out = n_free - (int32_t)taken;
-        counts[0] = n_runs;
-        counts[1] = (int32_t)taken;
-        counts[2] = (int32_t)total.a;
-        counts[3] = (int32_t)min(all_rows, (int64_t)INT32_MAX);
+        row_offsets[B] = clamp31(all_rows);
+        *n_free_out = n_free - taken;
+        *reinterpret_cast<int4 *>(counts) = int4{n_runs, taken, (int32_t)(all_others >> 32), clamp31(all_rows)};
     }
-    for (int64_t i = (int64_t)blockIdx.x * kPlanThreads + threadIdx.x; i < max_runs; i += (int64_t)gridDim.x * kPlanThreads) {
-        int4 run{-1, 0, 0, 0};
+    for (int64_t i = (int64_t)blockIdx.x * THREADS + threadIdx.x; i < max_runs; i += (int64_t)gridDim.x * THREADS) {
+        int4 out{-1, 0, 0, 0};
         if (i < n_runs) {
             const int r = first_above(run_ends, B, (int32_t)i);
-            const int64_t old = lengths[r], total_r = old + new_rows[r], have = blocks_of(old, S);
-            const int64_t col = old / S + (i - (r ? run_ends[r - 1] : 0));
+            const int32_t length = held[r], more = (r + 1 < B ? row0[r + 1] : (int32_t)all_rows) - row0[r];
+            const int32_t have = (int32_t)(((int64_t)length + S - 1) >> shift_S);
+            const int32_t col = (length >> shift_S) + (int32_t)(i - (r ? run_ends[r - 1] : 0));
             int32_t *entry = table + (int64_t)r * width + col;
             if (col >= have) {
-                run.x = free_blocks[n_free - 1 - (int32_t)(take0[r] + (col - have))];
-                *entry = run.x;
+                out.x = free_blocks[n_free - 1 - (take0[r] + (col - have))];
+                *entry = out.x;
             } else {
-                run.x = *entry;
+                out.x = *entry;
             }
-            const int64_t first = max(old, col * S);  // row of the request that starts the run
-            run.y = (int32_t)(row0[r] + (first - old));
-            run.z = (int32_t)(first - col * S);
-            run.w = (int32_t)(min(col * S + S, total_r) - first);
+            const int64_t start = (int64_t)col << shift_S, first = max((int64_t)length, start);  // row of the request that starts the run
+            out.y = (int32_t)(row0[r] + (first - length));
+            out.z = (int32_t)(first - start);
+            out.w = (int32_t)(min(start + S, (int64_t)length + more) - first);
         }
-        runs[i] = run;
+        runs[i] = out;
     }
 }
 
 // The blocks of finished requests go to the end of the free list, in the order of the requests.
-__global__ __launch_bounds__(kPlanThreads) void k_kv_release(
+template <int THREADS, int PER>
+__global__ __launch_bounds__(THREADS) void k_kv_release(
     const uint8_t *__restrict__ done, const int32_t *__restrict__ lengths, const int32_t *__restrict__ table, int32_t B,
-    int32_t width, int32_t S, int32_t *__restrict__ free_blocks, int32_t free_capacity,
+    int32_t width, int32_t shift_S, int32_t *__restrict__ free_blocks, int32_t free_capacity,
     const int32_t *__restrict__ n_free_in, int32_t *__restrict__ lengths_out, int32_t *__restrict__ n_free_out) {
-    __shared__ int32_t ends_lds[kKvMaxRequests];
-    __shared__ Pair sums[kPlanThreads / 64];
+    extern __shared__ int32_t ends[];  // [B]
+    __shared__ int64_t sums[THREADS / 64];
+    const int32_t b0 = threadIdx.x * PER;
+    int32_t held[PER];
+    int64_t mine = 0, total;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        held[i] = 0;
+        if (b0 + i >= B) continue;
+        const int32_t length = lengths[b0 + i];
+        const bool out = done[b0 + i];
+        if (out) held[i] = (int32_t)min(((int64_t)max(length, 0) + (1 << shift_S) - 1) >> shift_S, (int64_t)width);
+        if (blockIdx.x == 0) lengths_out[b0 + i] = out ? 0 : length;
+        mine += held[i];
+    }
     const int32_t n_free = min(max(*n_free_in, 0), free_capacity);
-    const int per = (B + kPlanThreads - 1) / kPlanThreads;
-    const int b0 = min((int)threadIdx.x * per, B), b1 = min(b0 + per, B);
-    auto held = [&](int b) { return done[b] ? min(blocks_of(max(lengths[b], 0), S), (int64_t)width) : (int64_t)0; };
     const int64_t room = free_capacity - n_free;  // a list that would overflow drops what does not fit
-    Pair mine{0, 0}, total;
-    for (int b = b0; b < b1; ++b) mine.a += held(b);
-    int64_t at = scan_pair(mine, total, sums).a - mine.a;
-    for (int b = b0; b < b1; ++b) {
-        at += held(b);
-        ends_lds[b] = (int32_t)min(at, room);
-        if (blockIdx.x == 0) lengths_out[b] = done[b] ? 0 : lengths[b];
+    int64_t at = group_sums<THREADS / 64>(mine, total, sums) - mine;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        at += held[i];
+        if (b0 + i < B) ends[b0 + i] = (int32_t)min(at, room);
     }
     __syncthreads();
-    const int32_t n = (int32_t)min(total.a, room);
+    const int32_t n = (int32_t)min(total, room);
     if (blockIdx.x == 0 && threadIdx.x == 0) *n_free_out = n_free + n;
-    for (int64_t i = (int64_t)blockIdx.x * kPlanThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kPlanThreads) {
-        const int r = first_above(ends_lds, B, (int32_t)i);
-        free_blocks[n_free + i] = table[(int64_t)r * width + (i - (r ? ends_lds[r - 1] : 0))];
+    for (int64_t i = (int64_t)blockIdx.x * THREADS + threadIdx.x; i < n; i += (int64_t)gridDim.x * THREADS) {
+        const int r = first_above(ends, B, (int32_t)i);
+        free_blocks[n_free + i] = table[(int64_t)r * width + (i - (r ? ends[r - 1] : 0))];
     }
 }
 
@@ -382,24 +403,45 @@ __global__ __launch_bounds__(256) void k_kv_load(KvCache c, const int32_t *__res
 
 }  // namespace
 
+// Threads of a workgroup and requests to a thread: few of either where they cover B (16 requests: 3.0 us with 256 threads, 6.9
+// with 1024), and no more than 4 to a thread, whose reads lie apart (2048 requests: 11.5 us with 16 to each of 256).
+template <int T, int P>
+struct PlanSize {
+    static constexpr int threads = T, per = P;
+};
+template <class F>
+static void by_requests(int32_t B, F go) {
+    static_assert(kKvMaxRequests == 4 * 1024, "the last choice holds the most requests");
+    if (B <= 256) go(PlanSize<256, 1>{});
+    else if (B <= 1024) go(PlanSize<1024, 1>{});
+    else go(PlanSize<1024, 4>{});
+}
+
 hipError_t launch_kv_plan(const int32_t *lengths, const int32_t *new_rows, int32_t B, int32_t S, int64_t rows,
                           int32_t *table, int32_t width, const int32_t *free_blocks, int32_t free_capacity,
                           const int32_t *n_free, int32_t *lengths_out, int32_t *n_free_out, int32_t *row_offsets,
                           int32_t *runs, int32_t max_runs, int32_t *counts, hipStream_t st) {
-    const int grid = std::min(256, (max_runs + kPlanThreads - 1) / kPlanThreads);
-    k_kv_plan<<<grid, kPlanThreads, 0, st>>>(lengths, new_rows, B, S, rows, table, width, free_blocks, free_capacity, n_free,
-                                             lengths_out, n_free_out, row_offsets, reinterpret_cast<int4 *>(runs), max_runs,
-                                             counts);
-    return hipGetLastError();
+    hipError_t e = hipSuccess;
+    by_requests(B, [&](auto size) {
+        constexpr int T = decltype(size)::threads, P = decltype(size)::per;
+        e = DGQ_ENSURE_LDS((k_kv_plan<T, P>), kPlanArrays * 4 * T * P);
+        if (e == hipSuccess)
+            k_kv_plan<T, P><<<std::min<int64_t>(256, ((int64_t)max_runs + T - 1) / T), T, kPlanArrays * 4 * B, st>>>(
+                lengths, new_rows, B, __builtin_ctz(S), rows, table, width, free_blocks, free_capacity, n_free, lengths_out,
+                n_free_out, row_offsets, reinterpret_cast<int4 *>(runs), max_runs, counts);
+    });
+    return e == hipSuccess ? hipGetLastError() : e;
 }
 
 hipError_t launch_kv_release(const uint8_t *done, const int32_t *lengths, const int32_t *table, int32_t B, int32_t width,
                              int32_t S, int32_t *free_blocks, int32_t free_capacity, const int32_t *n_free,
                              int32_t *lengths_out, int32_t *n_free_out, hipStream_t st) {
     const int64_t most = std::min((int64_t)B * width, (int64_t)free_capacity);
-    const int grid = (int)std::min<int64_t>(64, (most + kPlanThreads - 1) / kPlanThreads);
-    k_kv_release<<<std::max(grid, 1), kPlanThreads, 0, st>>>(done, lengths, table, B, width, S, free_blocks, free_capacity,
-                                                             n_free, lengths_out, n_free_out);
+    by_requests(B, [&](auto size) {
+        constexpr int T = decltype(size)::threads, P = decltype(size)::per;
+        k_kv_release<T, P><<<std::max<int64_t>(1, std::min<int64_t>(64, (most + T - 1) / T)), T, 4 * B, st>>>(
+            done, lengths, table, B, width, __builtin_ctz(S), free_blocks, free_capacity, n_free, lengths_out, n_free_out);
+    });
     return hipGetLastError();
 }
 

@@ -67,7 +67,7 @@ def test_refusals(lib):
         plan(-1, **{name: None})
     plan(-4, S=16), plan(-4, S=0), plan(-1, B=0), plan(-1, W=0), plan(-4, B=4097, most=9000), plan(-4, W=1 << 27)
     plan(-1, rows=-1), plan(-1, cap=0), plan(-4, rows=1 << 31, most=1 << 30), plan(-1, l2=p), plan(-1, n2=p), plan(-3, most=3)
-    plan(-2, runs=q)
+    plan(-2, runs=q), plan(-2, counts=q)
 
     def release(code, **kw):
         a = dict(done=p, lengths=p, table=p, B=2, W=4, S=32, free=p, cap=8, n=p, l2=o, n2=o)
