@@ -666,33 +666,26 @@ __global__ __launch_bounds__(256, NC < 3 ? 2 : 1) void k_xattn_kv_few(AttnArgs a
     const int h = (int)(task / a.tiles);
     const Rows rows = find_rows(a, (int32_t)(task % a.tiles), 16);
     if (rows.n == 0) return;
-    const int32_t length = length_of(a, rows.b);
-    const int32_t n_tiles = (length + 31) / 32;
-    const int32_t t0 = split * a.chunk, t1 = min(t0 + a.chunk, n_tiles);
-    if (split > 0 && t0 >= t1) return;  // the join knows how many splits there are
-    const int32_t per = (t1 - t0 + 3) / 4, w0 = t0 + wave * per, w1 = min(w0 + per, t1);
-
-    // block numbers and scales of this wavefront's tiles: at most 64 blocks
-    const int32_t block0 = (w0 * 32) >> shift_S;
-    int32_t id = -1;
-    float k_scale = 0.f, v_scale = 0.f;
-    if (w0 < w1 && block0 + lane <= ((w1 * 32 - 1) >> shift_S)) {
-        id = a.table[(int64_t)rows.b * a.width + block0 + lane];
-        if (id >= a.c.n_blocks) id = -1;
-        if (id >= 0) {
-            const float2 scale = reinterpret_cast<const float2 *>(a.c.scales)[(int64_t)id * H + h];
-            k_scale = scale.x, v_scale = scale.y;
-        }
-    }
-
+    // A wavefront's tiles, and its block numbers (at most 64), do not wait for the length.
+    const int32_t per = a.chunk / 4, t0 = split * a.chunk, w0 = t0 + wave * per, block0 = (int32_t)(((int64_t)w0 * 32) >> shift_S);
+    int32_t id = block0 + lane < a.width ? a.table[(int64_t)rows.b * a.width + block0 + lane] : -1;
     const int64_t m = (int64_t)rows.tile * 16 + col;
     const bool live = rows.has(a, m);
     Raw<T, 2 * NC> raw;
     load_query(raw, live ? static_cast<const T *>(rows.query(a, h, m, sizeof(T))) : nullptr, live, d,
                [&](int s) { return (s >> 1) * 64 + group * 16 + (s & 1) * 8; });
-    half8 qh[2 * NC], ql[kTwo ? 2 * NC : 1];
-    const float q_scale = split_query(raw, d, 48, qh, ql);
+    const int32_t length = length_of(a, rows.b), n_tiles = (length + 31) / 32;
+    if (split > 0 && t0 >= n_tiles) return;  // the join knows how many splits there are
+    const int32_t w1 = min(min(w0 + per, t0 + a.chunk), n_tiles);
+    if (id >= a.c.n_blocks) id = -1;
+    float k_scale = 0.f, v_scale = 0.f;
+    if (id >= 0 && w0 < w1) {
+        const float2 scale = reinterpret_cast<const float2 *>(a.c.scales)[(int64_t)id * H + h];
+        k_scale = scale.x, v_scale = scale.y;
+    }
 
+    half8 qh[2 * NC], ql[kTwo ? 2 * NC : 1];
+    float q_scale;
     floatx4 O[4 * NC];
 #pragma unroll
     for (int i = 0; i < 4 * NC; ++i) O[i] = floatx4(0.f);
@@ -759,6 +752,7 @@ __global__ __launch_bounds__(256, NC < 3 ? 2 : 1) void k_xattn_kv_few(AttnArgs a
 #pragma unroll
             for (int u = 0; u < 2; ++u) x.k[u][s] = y.k[u][s] = uint4{0, 0, 0, 0};  // chunks that are not there: finite
         if (w0 < w1) load(x, w0);
+        q_scale = split_query(raw, d, 48, qh, ql);
         for (int32_t t = w0; t < w1; t += 2) {
             if (t + 1 < w1) load(y, t + 1);
             work(x, t);
@@ -870,6 +864,7 @@ struct Plan {
     Kernel kernel;
     int32_t tiles, rows, splits, chunk;
 };
+constexpr int kFewGroups = 768, kFewChunk = 16;
 constexpr int kShortBytes = 32 * 1024;  // of tiles: three workgroups to a CU, with the swap places
 constexpr int tile_bytes(int d) { return (d + 31) / 32 * 4096; }  // fp16 of a tile's K and V
 
@@ -885,9 +880,12 @@ Plan plan_of(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t Hkv, int3
         return {kShort, (int32_t)tiles_of_rows(128 * times), (int32_t)(128 * times), 1, 0};
     }
     const int64_t tiles = tiles_of_rows(16), groups = tiles * Hkv;
-    // parts for about 1024 workgroups, none below 16 tiles (four to a wavefront) or above 256 (what one can look up)
-    const int64_t want = std::max<int64_t>(1, 1024 / std::max<int64_t>(1, groups));
-    const int64_t chunk = std::min<int64_t>(256, std::max<int64_t>(16, ((slot_tiles + want - 1) / want + 3) / 4 * 4));
+    // Parts for kFewGroups workgroups, what the chip holds at once (three to a CU): more of them wait for a place while the last
+    // ones run (32 queries over 1 .. 8192 rows: 80 us with 2048, 59 with 768, 73 with 512).  None below kFewChunk tiles or above
+    // 256 (what one can look up).
+    const int64_t want = std::max<int64_t>(1, kFewGroups / std::max<int64_t>(1, groups));
+    const int64_t least = std::min<int64_t>(kFewChunk, slot_tiles), part = std::max(least, (slot_tiles + want - 1) / want);
+    const int64_t chunk = std::min<int64_t>(256, (part + 3) / 4 * 4);
     return {kFew, (int32_t)tiles, 16, (int32_t)std::max<int64_t>(1, (slot_tiles + chunk - 1) / chunk), (int32_t)chunk};
 }
 
