@@ -1399,6 +1399,8 @@ int dgq_xattn_kv(const void *q, int32_t dtype, const int32_t *q_offsets, int64_t
         return fail(DGQ_EALIGN, "dgq_xattn_kv: strides must be multiples of 16 bytes, not negative");
     if (!aligned16(q) || !aligned16(out)) return fail(DGQ_EALIGN, "dgq_xattn_kv: tensor not 16-byte aligned");
     const KvQueries in{q, q_offsets, q_batch_stride, q_row_stride, q_head_stride, dtype, B, (int32_t)N, Hq};
+    if (!xattn_kv_fits(B, in.rows(), q_offsets != nullptr, Hq, H, d, (int64_t)width * block_size))
+        return fail(DGQ_EUNSUPPORTED, "dgq_xattn_kv: too many requests for a table so wide");
     const size_t need = xattn_kv_workspace_bytes(B, in.rows(), q_offsets != nullptr, Hq, H, d, (int64_t)width * block_size);
     if (need && (!workspace || workspace_bytes < need || !aligned16(workspace)))
         return fail(DGQ_EWORKSPACE, "dgq_xattn_kv: workspace missing, too small or misaligned");

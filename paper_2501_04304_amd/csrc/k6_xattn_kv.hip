@@ -386,9 +386,18 @@ __global__ __launch_bounds__(256, wide_waves(NP)) void k_xattn_kv(AttnArgs a) {
     const int h = (int)(blockIdx.x / (uint32_t)a.tiles);
     const Rows rows = find_rows(a, (int32_t)(blockIdx.x % (uint32_t)a.tiles), kWideRows);
     if (rows.n == 0) return;
-    const int32_t length = length_of(a, rows.b);
-    const int32_t n_tiles = (length + 31) / 32, n_stages = (n_tiles + 1) / 2;
-
+    // block numbers and scales of 64 blocks, one a lane, whether the request reaches them or not: they do not wait for its length
+    int32_t block0 = 0, id = -1;
+    float k_scale = 0.f, v_scale = 0.f;
+    auto look_up = [&](int32_t first) {
+        block0 = first;
+        id = first + lane < a.width ? a.table[(int64_t)rows.b * a.width + first + lane] : -1;
+        if (id >= a.c.n_blocks) id = -1;
+        if (id >= 0) {
+            const float2 scale = reinterpret_cast<const float2 *>(a.c.scales)[(int64_t)id * H + h];
+            k_scale = scale.x, v_scale = scale.y;
+        }
+    };
     const int64_t m0 = (int64_t)rows.tile * kWideRows + wave * 32 + (lane >> 3);  // and 8, 16, 24 further: this lane's rows
     uint4 *swap_at = lds + wave * (kSwapBytes / 16);  // in the stages' place, before and after
     Swap<T, NP> fetched;
@@ -399,23 +408,8 @@ __global__ __launch_bounds__(256, wide_waves(NP)) void k_xattn_kv(AttnArgs a) {
             row[i] = rows.has(a, m0 + 8 * i) ? static_cast<const T *>(rows.query(a, h, m0 + 8 * i, sizeof(T))) : nullptr;
         fetched.load(row, d);
     }
-
-    // block numbers and scales of 64 blocks, one a lane
-    int32_t block0 = 0, id = -1;
-    float k_scale = 0.f, v_scale = 0.f;
-    auto look_up = [&](int32_t first) {
-        block0 = first;
-        id = -1;
-        if (((int64_t)(first + lane) << shift_S) < length) {
-            id = a.table[(int64_t)rows.b * a.width + first + lane];
-            if (id >= a.c.n_blocks) id = -1;
-            if (id >= 0) {
-                const float2 scale = reinterpret_cast<const float2 *>(a.c.scales)[(int64_t)id * H + h];
-                k_scale = scale.x, v_scale = scale.y;
-            }
-        }
-    };
     look_up(0);
+    const int32_t length = length_of(a, rows.b), n_tiles = (length + 31) / 32, n_stages = (n_tiles + 1) / 2;
 
     uint4 ahead[NP];
     const int my_tile = wave >> 1, my_part = wave & 1;
@@ -484,19 +478,36 @@ __global__ __launch_bounds__(256, wide_waves(NP)) void k_xattn_kv(AttnArgs a) {
         const bool more = st + 1 < n_stages;
         if (more) load(st + 1);
         const Stage then = terms_of(st + 1);
+        // Operands ahead of their products where the registers are there: the first of a stage are waited for, no others.
+        half8 kf[2 * NP], vf[2 * NP];
+        auto read_v = [&](int i) {
+            const uint4 *V = lds + ((2 + (st & 1)) * 2 + i) * kPart;
+#pragma unroll
+            for (int s = 0; s < 2 * NP; ++s) vf[s] = __builtin_bit_cast(half8, V[((s >> 1) * 4 + (s & 1) * 2 + half) * 32 + col]);
+        };
+        auto read_k = [&](int i) {
+            const uint4 *K = lds + ((st & 1) * 2 + i) * kPart;
+#pragma unroll
+            for (int s = 0; s < 2 * NP; ++s) kf[s] = __builtin_bit_cast(half8, K[((s >> 1) * 2 + half) * 64 + (s & 1) * 32 + col]);
+        };
+        read_k(0);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            if (!now.there[i]) continue;
-            const uint4 *K = lds + ((st & 1) * 2 + i) * kPart, *V = lds + ((2 + (st & 1)) * 2 + i) * kPart;
+            if (kTwo && i == 1) read_k(1);
             float16v x;
 #pragma unroll
             for (int r = 0; r < 16; ++r) x[r] = 0.f;
 #pragma unroll
             for (int s = 0; s < 2 * NP; ++s) {
-                const half8 k = __builtin_bit_cast(half8, K[((s >> 1) * 2 + half) * 64 + (s & 1) * 32 + col]);
-                x = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, qh[s], x, 0, 0, 0);
-                if constexpr (kTwo) x = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, ql[s], x, 0, 0, 0);
+                x = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[s], qh[s], x, 0, 0, 0);
+                if constexpr (kTwo) x = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[s], ql[s], x, 0, 0, 0);
             }
+            if constexpr (!kTwo) {
+                read_v(i);
+                if (i == 0) read_k(1);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (!now.there[i]) continue;
             half8 ph[2], pl[2];
             weights<kTwo, 16, 32>(
                 x, q_scale * now.ks[i], now.vs[i], v_top, length - (2 * st + i) * 32,
@@ -508,11 +519,11 @@ __global__ __launch_bounds__(256, wide_waves(NP)) void k_xattn_kv(AttnArgs a) {
                         for (int r = 0; r < 16; ++r) O[s][r] *= less;
                 },
                 ph, pl);
+            if constexpr (kTwo) read_v(i);
 #pragma unroll
             for (int s = 0; s < 2 * NP; ++s) {
-                const half8 v = __builtin_bit_cast(half8, V[((s >> 1) * 4 + (s & 1) * 2 + half) * 32 + col]);
-                O[s >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, ph[s & 1], O[s >> 1], 0, 0, 0);
-                if constexpr (kTwo) O[s >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pl[s & 1], O[s >> 1], 0, 0, 0);
+                O[s >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[s], ph[s & 1], O[s >> 1], 0, 0, 0);
+                if constexpr (kTwo) O[s >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[s], pl[s & 1], O[s >> 1], 0, 0, 0);
             }
         }
         if (more) keep(st + 1);
@@ -565,21 +576,30 @@ __global__ __launch_bounds__(256, short_waves(sizeof(T) == 4, NP)) void k_xattn_
     if (id >= a.c.n_blocks) id = -1;
     float2 scale{0.f, 0.f};
     if (id >= 0) scale = reinterpret_cast<const float2 *>(a.c.scales)[(int64_t)id * H + h];
-    for (int p = wave; p < 2 * n_tiles; p += 4) {
-        const int t = p >> 1, part = p & 1;
-        const int32_t block = __builtin_amdgcn_readlane(id, (t * 32) >> shift_S);
-        if (block < 0) continue;
-        const uint8_t *tile = a.c.codes + ((int64_t)block * H + h) * kv_slice_bytes(S, d) + (int64_t)(t & ((S >> 5) - 1)) * 64 * e16;
-        uint4 w[NP];
+    constexpr int kBatch = NP <= 2 ? 4 : 2;  // parts whose loads are under way together
+    for (int p0 = wave; p0 < 2 * n_tiles; p0 += 4 * kBatch) {
+        uint4 w[kBatch][NP];
 #pragma unroll
-        for (int s = 0; s < NP; ++s)
-            w[s] = *reinterpret_cast<const uint4 *>(
-                tile + (part ? 32 * e16 + min(s * 32 + col, e16 - 1) * 32 + half * 16 : ((2 * s + half) * 32 + col) * 16));
+        for (int j = 0; j < kBatch; ++j) {
+            const int p = p0 + 4 * j, t = p >> 1, part = p & 1;
+            if (p >= 2 * n_tiles) break;
+            const int32_t block = max(__builtin_amdgcn_readlane(id, (t * 32) >> shift_S), 0);  // what is not there is not used
+            const uint8_t *tile = a.c.codes + ((int64_t)block * H + h) * kv_slice_bytes(S, d) + (int64_t)(t & ((S >> 5) - 1)) * 64 * e16;
 #pragma unroll
-        for (int s = 0; s < NP; ++s) {
-            const int at = part ? (s * 4 + half) * 32 + col : (2 * s + half) * 64 + col;
-            tiles[p * kPart + at] = __builtin_bit_cast(uint4, to_half8(w[s].x, w[s].y));
-            tiles[p * kPart + at + (part ? 64 : 32)] = __builtin_bit_cast(uint4, to_half8(w[s].z, w[s].w));
+            for (int s = 0; s < NP; ++s)
+                w[j][s] = *reinterpret_cast<const uint4 *>(
+                    tile + (part ? 32 * e16 + min(s * 32 + col, e16 - 1) * 32 + half * 16 : ((2 * s + half) * 32 + col) * 16));
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            const int p = p0 + 4 * j, part = p & 1;
+            if (p >= 2 * n_tiles) break;
+#pragma unroll
+            for (int s = 0; s < NP; ++s) {
+                const int at = part ? (s * 4 + half) * 32 + col : (2 * s + half) * 64 + col;
+                tiles[p * kPart + at] = __builtin_bit_cast(uint4, to_half8(w[j][s].x, w[j][s].y));
+                tiles[p * kPart + at + (part ? 64 : 32)] = __builtin_bit_cast(uint4, to_half8(w[j][s].z, w[j][s].w));
+            }
         }
     }
     __syncthreads();
@@ -862,10 +882,14 @@ __global__ __launch_bounds__(256) void k_xattn_kv_join(AttnArgs a) {
 enum Kernel { kFew, kShort, kLong };
 struct Plan {
     Kernel kernel;
-    int32_t tiles, rows, splits, chunk;
+    int64_t tiles;
+    int32_t rows, splits, chunk;
+    int64_t groups(int32_t Hkv) const { return tiles * Hkv * splits; }  // workgroups
 };
 constexpr int kFewGroups = 768, kFewChunk = 16;
-constexpr int kShortBytes = 32 * 1024;  // of tiles: three workgroups to a CU, with the swap places
+// LDS for the tiles of a short request: what lets three workgroups to a CU in, with their swap places (64 KiB, two: 231 rows of 64
+// dims at batch 16 take 170 us, 158 in stages).
+constexpr int kShortBytes = 32 * 1024;
 constexpr int tile_bytes(int d) { return (d + 31) / 32 * 4096; }  // fp16 of a tile's K and V
 
 // Which kernel, its row tiles, and into how many parts each request's slots are split.
@@ -874,10 +898,10 @@ Plan plan_of(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t Hkv, int3
     auto tiles_of_rows = [&](int64_t R) { return packed ? rows * G / R + B : B * ((rows / B * G + R - 1) / R); };
     const int64_t wide = tiles_of_rows(kWideRows), slot_tiles = (slots + 31) / 32;
     if (rows * G > 16 * (int64_t)B && wide * Hkv >= 256) {
-        if (slot_tiles * tile_bytes(d) > kShortBytes) return {kLong, (int32_t)wide, kWideRows, 1, 0};
+        if (slot_tiles * tile_bytes(d) > kShortBytes) return {kLong, wide, kWideRows, 1, 0};
         // 128 rows at a time, as often as leaves some 1536 workgroups (six to a CU: lengths differ)
         const int64_t times = std::max<int64_t>(1, std::min<int64_t>(16, wide * Hkv / 1536));
-        return {kShort, (int32_t)tiles_of_rows(128 * times), (int32_t)(128 * times), 1, 0};
+        return {kShort, tiles_of_rows(128 * times), (int32_t)(128 * times), 1, 0};
     }
     const int64_t tiles = tiles_of_rows(16), groups = tiles * Hkv;
     // Parts for kFewGroups workgroups, what the chip holds at once (three to a CU): more of them wait for a place while the last
@@ -886,7 +910,7 @@ Plan plan_of(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t Hkv, int3
     const int64_t want = std::max<int64_t>(1, kFewGroups / std::max<int64_t>(1, groups));
     const int64_t least = std::min<int64_t>(kFewChunk, slot_tiles), part = std::max(least, (slot_tiles + want - 1) / want);
     const int64_t chunk = std::min<int64_t>(256, (part + 3) / 4 * 4);
-    return {kFew, (int32_t)tiles, 16, (int32_t)std::max<int64_t>(1, (slot_tiles + chunk - 1) / chunk), (int32_t)chunk};
+    return {kFew, tiles, 16, (int32_t)std::max<int64_t>(1, (slot_tiles + chunk - 1) / chunk), (int32_t)chunk};
 }
 
 template <class T>
@@ -940,10 +964,19 @@ size_t xattn_kv_workspace_bytes(int32_t B, int64_t rows, bool packed, int32_t Hq
     return p.splits > 1 ? (size_t)p.splits * rows * Hq * (d + 2) * sizeof(float) : 0;
 }
 
+bool xattn_kv_fits(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t Hkv, int32_t d, int64_t slots) {
+    return plan_of(B, rows, packed, Hq, Hkv, d, slots).groups(Hkv) <= INT32_MAX;
+}
+
+int xattn_kv_kernel(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t Hkv, int32_t d, int64_t slots) {
+    const Plan p = plan_of(B, rows, packed, Hq, Hkv, d, slots);
+    return p.kernel == kFew ? p.splits > 1 : p.kernel == kShort ? 2 : 3;
+}
+
 hipError_t launch_xattn_kv(const KvQueries &q, const KvCache &c, const int32_t *table, int32_t width,
                            const int32_t *lengths, void *out, void *workspace, hipStream_t st) {
     const Plan p = plan_of(q.B, q.rows(), q.offsets != nullptr, q.Hq, c.H, c.d, (int64_t)width * c.S);
-    const AttnArgs a{q, c, table, lengths, out, static_cast<float *>(workspace), width, q.Hq / c.H, p.tiles, p.rows, p.splits, p.chunk};
+    const AttnArgs a{q, c, table, lengths, out, static_cast<float *>(workspace), width, q.Hq / c.H, (int32_t)p.tiles, p.rows, p.splits, p.chunk};
     return q.dtype == DGQ_F32 ? launch<float>(a, p.kernel, st)
            : q.dtype == DGQ_F16 ? launch<_Float16>(a, p.kernel, st) : launch<__bf16>(a, p.kernel, st);
 }

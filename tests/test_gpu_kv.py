@@ -365,7 +365,8 @@ def test_attention(dgq, shape, dtype):
     assert torch.equal(out, other)
 
 
-MANY = [  # at least 256 workgroups of 128 rows, from one slot to several look-ups of 64 blocks; every step of the head width
+MANY = [  # at least 256 workgroups of 128 rows, from one slot to several look-ups of 64 blocks; every step of the head width; both
+          # kernels for many rows
     (32, 32, 1, 8, 270, [1, 0, 33]),
     (32, 8, 1, 40, 2100, [77, 154]),
     (64, 10, 1, 64, 400, [1, 2, 31, 32, 65, 231, 0]),
@@ -376,7 +377,20 @@ MANY = [  # at least 256 workgroups of 128 rows, from one slot to several look-u
     (32, 16, 2, 224, 1025, [50]),
     (64, 64, 1, 256, 257, [65, 130]),
     (32, 1, 1, 16, 33000, [4200]),
+    (32, 2, 1, 32, 16500, [31]),
+    (64, 8, 1, 64, 4096, [77]),
+    (64, 3, 1, 96, 11100, [60]),       # one block a request, of which the table has no other
+    (32, 6, 2, 120, 2800, [32, 0]),
+    (32, 40, 1, 152, 901, [30]),
+    (32, 32, 1, 192, 1030, [1]),
+    (32, 16, 1, 216, 2060, [25]),
+    (32, 9, 4, 256, 1000, [17]),
 ]
+
+
+def width_of(S, lengths):
+    """A column more than the lengths need, or the one that is enough for all."""
+    return 1 if max(lengths) <= S else -(-max(lengths) // S) + 1
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -385,7 +399,7 @@ def test_attention_of_many_rows(dgq, shape, dtype):
     import torch
     S, H, G, d, N, lengths = shape
     rng = np.random.default_rng(d + N)
-    c, table, held = _filled(dgq, rng, lengths, S, H, d)
+    c, table, held = _filled(dgq, rng, lengths, S, H, d, W=width_of(S, lengths))
     q, qn = _floats(rng, (len(lengths), N, H * G, d), dtype)
     out = dgq.dgq_xattn_kv(q, c, _i32(table), _i32(lengths))
     again = dgq.dgq_xattn_kv(q, c, _i32(table), _i32(lengths), out=torch.full_like(q, float("nan")))
