@@ -192,8 +192,8 @@ __device__ float split_query(const Raw<T, N8> &raw, int d, int mask, half8 (&hi)
 }
 
 // ---- 32 rows between memory and the lanes of the matrix cores ------------------------------------------------------------
-// A lane of an operand has a whole half row: loads and stores in that order touch 32 rows in 16-byte pieces (100 us for 16 x
-// 4096 x 10 x 64 fp32 rows in and out with one slot to attend to; a copy takes 63).  So rows cross memory 128 bytes to 8 lanes
+// A lane of an operand has a whole half row: loads and stores in that order touch 32 rows in 16-byte pieces (103 us for 16 x
+// 4096 x 10 x 64 fp32 rows in and out with one slot to attend to, 84 this way; a copy takes 63).  So rows cross memory 128 bytes to 8 lanes
 // and change places in 4 KiB of LDS of the wavefront's own, without a barrier: LDS serves a wavefront in order.  A 16-byte
 // unit u of row r is at unit u ^ (r & 7): no bank twice either way.
 constexpr int kSwapBytes = 4096;
@@ -363,16 +363,14 @@ __device__ void weights(X &x, float mult, uint32_t v_scale, uint32_t &v_top, int
 // S^T = K Q^T and O^T = V^T P^T on 32 x 32 x 16 instructions: a lane holds column (lane & 31) of both, so a row's statistics
 // are its lane's (and the other half's), and the products of S^T are the operand of O^T without a move, with V's slots
 // stored in the order in which S^T leaves them.
-// Two tiles of 32 slots are a stage: each wavefront loads K or V of one of them (two stages ahead, in registers), makes fp16
-// of it once for all four, and puts it into LDS in units of 16 bytes, one operand of one lane, so that every read and write of
-// 64 lanes is 1 KiB without a bank met twice.
-// The exponentials of a tile stand among the products of the next tile's logits: a matrix instruction of 32 cycles leaves
-// room for some eight others, and with all of one kind behind all of the other the two take turns (2 x 4096 x 24 x 128 over
-// 4000 rows: matrix pipes busy 32 % of 509 us).  Operands are read from LDS a tile ahead: K before the tile's largest logit
-// is sought, V where K's registers fall free.
-// LDS: two stages of K, three of V.  One barrier a stage, behind the first tile; in front of it the next stage is written.
-// K's place there was last read in front of the barrier before.  V's second tile of a stage is read behind that barrier, so
-// its place is written again only two barriers later.
+// Two tiles of 32 slots are a stage: each wavefront loads K or V of one of them (a stage ahead, in registers), makes fp16 of it
+// once for all four, and puts it into LDS in units of 16 bytes, one operand of one lane, so that every read and write of 64
+// lanes is 1 KiB without a bank met twice (2 x 4096 x 24 x 128 over 4000 rows: 1057 us with every wavefront converting for
+// itself).  Two stages of LDS and one barrier a stage: a stage's place was last read in front of the barrier before.
+// Bound by vector instructions: of 64-dim bf16 heads over 1024 rows, 114 a tile of 32 x 32 beside 8 products, vector pipes busy
+// 60 % and matrix pipes 27 % of the time, 16 of the 114 exponentials of two issue slots each.  Exponentials placed by hand among
+// the next tile's products gained 3 % on 128 dims and cost the narrow heads a wavefront of occupancy, 10 to 25 % (121 us
+// for 110 at 16 x 4096 x 10 x 64 fp32); so did both tiles' logits up front.
 // T: type of q and out.  NP: 32-dim steps of the head width.
 // wavefronts to a SIMD that the registers leave
 constexpr int wide_waves(int NP) { return NP <= 1 ? 4 : NP <= 2 ? 3 : NP <= 4 ? 2 : 1; }
@@ -380,7 +378,7 @@ template <class T, int NP>
 __global__ __launch_bounds__(256, wide_waves(NP)) void k_xattn_kv(AttnArgs a) {
     constexpr bool kTwo = std::is_same<T, float>::value;  // two fp16 pieces
     constexpr int kPart = NP * 128;                       // units of K or V of a tile
-    extern __shared__ uint4 lds[];                        // [2 stages of K, 3 of V][2 tiles][kPart]
+    extern __shared__ uint4 lds[];                        // [K, V][2 stages][2 tiles][kPart]; before and after, swap places
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
     const int d = a.c.d, e16 = kv_padded(d), S = a.c.S, H = a.c.H, shift_S = __ffs(S) - 1;
     const int h = (int)(blockIdx.x / (uint32_t)a.tiles);
@@ -543,7 +541,8 @@ constexpr int short_waves(bool two, int NP) { return NP <= 1 ? 4 : NP <= 2 ? 3 :
 // ---- many rows, short requests: all of a request's tiles fit LDS ----------------------------------------------------------
 // A workgroup makes fp16 of the request's K and V once and takes a.rows rows through them, 32 to a wavefront at a time, with
 // no barrier after the first; the next 32 queries are loaded while these are worked on.  Bound by the queries' and the
-// output's bytes.
+// output's bytes and by what the exponentials add to their time: 16 x 4096 x 10 x 64 over 77 rows takes 96 us in fp32 and 58 in
+// bf16, 84 and 48 over one row (100 and 69 in stages; a copy of the bytes 63 and 31).
 template <class T, int NP>
 __global__ __launch_bounds__(256, short_waves(sizeof(T) == 4, NP)) void k_xattn_kv_short(AttnArgs a) {
     constexpr bool kTwo = std::is_same<T, float>::value;
@@ -666,7 +665,8 @@ __global__ __launch_bounds__(256, short_waves(sizeof(T) == 4, NP)) void k_xattn_
 // LDS; the tiles of one are loaded while the one before is worked on, with block numbers and scales fetched for all of a
 // wavefront's tiles at once.  16 x 16 x 32 instructions: half the statistics and half the sums of a 32-row tile that would
 // be empty for the most part.  Row m of the u-th K operand is slot 16 (m / 8) + 8 u + m % 8, which leaves a lane with the 8
-// slots that stand together in V.
+// slots that stand together in V.  32 bf16 queries of 4 heads each over 1 .. 8192 rows of 8 heads of 128: 53 us and 5 for the
+// join, 269 MB, where a stream of reads takes 39; one fp32 query over 32768 rows of 8 heads of 64: 10 and 4.
 // NC: 64-dim steps of the head width.
 template <int NC>
 struct FewTile {
