@@ -1349,7 +1349,7 @@ int dgq_kv_store(const void *k, const void *v, int32_t dtype, int64_t rows, int6
     if (rows < 0 || n_runs < 0) return fail(DGQ_EINVAL, "dgq_kv_store: sizes below 0");
     if (rows == 0 || n_runs == 0) return DGQ_OK;
     if (!k || !v || !runs) return fail(DGQ_EINVAL, "dgq_kv_store: null pointer");
-    if (rows > INT32_MAX || n_runs > INT32_MAX) return fail(DGQ_EUNSUPPORTED, "dgq_kv_store: rows or n_runs above 2^31 - 1");
+    if (rows > INT32_MAX || n_runs > kMaxGroups) return fail(DGQ_EUNSUPPORTED, "dgq_kv_store: rows above 2^31 - 1 or n_runs above 2^24 - 1");
     if (!kv_stride_ok(k_row_stride, dtype) || !kv_stride_ok(k_head_stride, dtype) || !kv_stride_ok(v_row_stride, dtype) ||
         !kv_stride_ok(v_head_stride, dtype))
         return fail(DGQ_EALIGN, "dgq_kv_store: strides must be multiples of 16 bytes, not negative");
@@ -1368,7 +1368,7 @@ int dgq_kv_load(const void *cache, int32_t n_blocks, int32_t block_size, int32_t
     if (!kv_dtype_ok(dtype) || max_rows < 0) return fail(DGQ_EINVAL, "dgq_kv_load: bad dtype, or max_rows below 0");
     if (max_rows == 0) return DGQ_OK;
     if (!table || !lengths || !k || !v) return fail(DGQ_EINVAL, "dgq_kv_load: null pointer");
-    if (B > 65535) return fail(DGQ_EUNSUPPORTED, "dgq_kv_load: B above 65535");
+    if (B > 65535 || max_rows > 32 * kMaxGroups) return fail(DGQ_EUNSUPPORTED, "dgq_kv_load: B above 65535 or max_rows above 2^29 - 32");
     if (!aligned16(k) || !aligned16(v)) return fail(DGQ_EALIGN, "dgq_kv_load: tensor not 16-byte aligned");
     DGQ_HIP(launch_kv_load(c, table, width, lengths, B, max_rows, dtype, k, v, static_cast<hipStream_t>(stream)));
     return DGQ_OK;
@@ -1392,7 +1392,6 @@ int dgq_xattn_kv(const void *q, int32_t dtype, const int32_t *q_offsets, int64_t
     if (Hq % H) return fail(DGQ_EUNSUPPORTED, "dgq_xattn_kv: query heads must be a multiple of the cached ones");
     if (N == 0) return DGQ_OK;
     if (!q || !table || !lengths || !out) return fail(DGQ_EINVAL, "dgq_xattn_kv: null pointer");
-    // the grid: at most one workgroup for every 8 rows of (query, head), and one a request and head more
     if (N > INT32_MAX || (q_offsets ? N : N * B) > INT32_MAX / Hq || B > INT32_MAX / Hq)
         return fail(DGQ_EUNSUPPORTED, "dgq_xattn_kv: more than 2^31 rows of queries and heads");
     if (!kv_stride_ok(q_batch_stride, dtype) || !kv_stride_ok(q_row_stride, dtype) || !kv_stride_ok(q_head_stride, dtype))
@@ -1400,7 +1399,7 @@ int dgq_xattn_kv(const void *q, int32_t dtype, const int32_t *q_offsets, int64_t
     if (!aligned16(q) || !aligned16(out)) return fail(DGQ_EALIGN, "dgq_xattn_kv: tensor not 16-byte aligned");
     const KvQueries in{q, q_offsets, q_batch_stride, q_row_stride, q_head_stride, dtype, B, (int32_t)N, Hq};
     if (!xattn_kv_fits(B, in.rows(), q_offsets != nullptr, Hq, H, d, (int64_t)width * block_size))
-        return fail(DGQ_EUNSUPPORTED, "dgq_xattn_kv: too many requests for a table so wide");
+        return fail(DGQ_EUNSUPPORTED, "dgq_xattn_kv: more requests, heads and table columns than one launch takes");
     const size_t need = xattn_kv_workspace_bytes(B, in.rows(), q_offsets != nullptr, Hq, H, d, (int64_t)width * block_size);
     if (need && (!workspace || workspace_bytes < need || !aligned16(workspace)))
         return fail(DGQ_EWORKSPACE, "dgq_xattn_kv: workspace missing, too small or misaligned");

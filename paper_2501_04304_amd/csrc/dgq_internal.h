@@ -145,17 +145,13 @@ struct KvCache {
 };
 constexpr int kKvMaxRequests = DGQ_KV_MAX_REQUESTS;  // 16 to a thread of the planner
 constexpr int kKvMaxDim = 256;
+constexpr int64_t kMaxGroups = (1 << 24) - 1;  // workgroups of 256 threads along x: a launch has fewer than 2^32 threads there
 constexpr float kKvLeastScale = 0x1p-96f;     // a block whose scale would be below it holds zeros
 __host__ __device__ inline int kv_padded(int d) { return (d + 15) & ~15; }
 __host__ __device__ inline int64_t kv_slice_bytes(int S, int d) { return (int64_t)S * 2 * kv_padded(d); }
 // slot of place i (0 .. 15) of half h of a V row: the order in which a lane of the matrix cores' half h holds the
 // products of 32 keys (rows 8 j + 4 h + 0 .. 3 of a 32 x 32 result)
 __host__ __device__ inline int kv_slot(int h, int i) { return 4 * h + (i & 3) + 8 * ((i >> 2) & 1) + 16 * (i >> 3); }
-// bytes of (slot, dim) in a tile's two parts
-__host__ __device__ inline int kv_k_byte(int slot, int e) { return ((e >> 4) * 32 + slot) * 16 + (e & 15); }
-__host__ __device__ inline int kv_v_byte(int slot, int e) {
-    return e * 32 + ((slot >> 2) & 1) * 16 + (slot & 3) + ((slot >> 3) & 1) * 4 + (slot >> 4) * 8;
-}
 
 // ---- kernel launchers (each returns a hipError_t from the launch) ----------
 

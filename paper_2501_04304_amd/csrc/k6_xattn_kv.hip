@@ -965,7 +965,8 @@ size_t xattn_kv_workspace_bytes(int32_t B, int64_t rows, bool packed, int32_t Hq
 }
 
 bool xattn_kv_fits(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t Hkv, int32_t d, int64_t slots) {
-    return plan_of(B, rows, packed, Hq, Hkv, d, slots).groups(Hkv) <= INT32_MAX;
+    const Plan p = plan_of(B, rows, packed, Hq, Hkv, d, slots);
+    return p.groups(Hkv) <= kMaxGroups && (p.splits == 1 || rows * Hq <= kMaxGroups);
 }
 
 int xattn_kv_kernel(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t Hkv, int32_t d, int64_t slots) {

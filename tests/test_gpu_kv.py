@@ -343,6 +343,7 @@ SHAPES = [  # S, H, G, d, N, lengths
     (128, 1, 2, 200, 17, [140]),
     (32, 1, 1, 256, 65, [77, 32]),
     (32, 1, 1, 224, 3, [200]),
+    (32, 8, 1, 16, 1, [9000, 8193, 8192, 40] + [0, 1] * 48),  # the longest part of a split, 64 blocks to a wavefront
 ]
 
 

@@ -87,7 +87,7 @@ def test_refusals(lib):
         store(-2, **{name: q})
     for name in ("kr", "kh", "vr", "vh"):
         store(-2, **{name: 18}), store(-2, **{name: -16}), store(-2, **{name: 20, "dtype": 1})
-    store(-1, dtype=3), store(-1, rows=-1), store(-1, n=-1), store(-4, rows=1 << 31), store(-4, n=1 << 31)
+    store(-1, dtype=3), store(-1, rows=-1), store(-1, n=-1), store(-4, rows=1 << 31), store(-4, n=1 << 24)
     store(-1, blocks=0), store(-1, H=0), store(-4, S=256), store(-4, d=12), store(-4, d=264), store(-4, H=65536)
     store(0, rows=0), store(0, n=0)  # nothing to write
 
@@ -98,6 +98,7 @@ def test_refusals(lib):
     for name in ("cache", "table", "lengths", "k", "v"):
         load(-1, **{name: None})
     load(-2, cache=q), load(-2, k=q), load(-2, v=q), load(-1, dtype=-1), load(-1, rows=-1), load(-1, B=0), load(-4, B=65536)
+    load(-4, rows=1 << 29)
     load(-4, d=20), load(-1, W=0), load(0, rows=0)
 
     def attend(code, **kw):
@@ -113,6 +114,7 @@ def test_refusals(lib):
         attend(-2, **{name: 2}), attend(-2, **{name: -4}), attend(-2, **{name: 4, "dtype": 2})
     attend(-1, dtype=4), attend(-1, N=-1), attend(-1, Hq=0), attend(-4, Hq=3, H=2), attend(-4, d=4), attend(-4, S=8), attend(-1, B=0)
     attend(-4, N=1 << 31), attend(-4, N=1 << 30, Hq=4), attend(-4, W=1 << 26), attend(0, N=0)
+    attend(-4, N=1, B=1 << 20, H=32, Hq=32), attend(-4, N=1, B=1 << 20, W=1 << 14, H=2, ws=p, nbytes=1 << 60)
     need = lib.dgq_xattn_kv_workspace_bytes(1, 1, 0, 2, 1, 16, 64, 32)
     assert need > 0
     attend(-6, N=1, W=64, ws=None), attend(-6, N=1, W=64, ws=p, nbytes=need - 1), attend(-6, N=1, W=64, ws=q, nbytes=need)
