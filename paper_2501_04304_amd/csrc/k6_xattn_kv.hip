@@ -372,11 +372,13 @@ __device__ void weights(X &x, float mult, uint32_t v_scale, uint32_t &v_top, int
 // the next tile's products gained 3 % on 128 dims and cost the narrow heads a wavefront of occupancy, 10 to 25 % (121 us
 // for 110 at 16 x 4096 x 10 x 64 fp32); so did both tiles' logits up front.
 // T: type of q and out.  NP: 32-dim steps of the head width.
-// wavefronts to a SIMD that the registers leave
-constexpr int wide_waves(int NP) { return NP <= 1 ? 4 : NP <= 2 ? 3 : NP <= 4 ? 2 : 1; }
+// wavefronts to a SIMD that the registers leave (and LDS: two workgroups of 160 dims fill it; 8 x 512 x 40 x 160 over 2048 rows:
+// 482 us in fp32 and 305 in bf16, 629 and 489 with one)
+constexpr int wide_waves(int NP) { return NP <= 1 ? 4 : NP <= 2 ? 3 : NP <= 5 ? 2 : 1; }
 template <class T, int NP>
 __global__ __launch_bounds__(256, wide_waves(NP)) void k_xattn_kv(AttnArgs a) {
     constexpr bool kTwo = std::is_same<T, float>::value;  // two fp16 pieces
+    constexpr bool kAhead = !kTwo && NP <= 6 && NP != 5;   // 5: a second wavefront instead; 7 and 8: no registers left
     constexpr int kPart = NP * 128;                       // units of K or V of a tile
     extern __shared__ uint4 lds[];                        // [K, V][2 stages][2 tiles][kPart]; before and after, swap places
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, col = lane & 31;
@@ -491,7 +493,7 @@ __global__ __launch_bounds__(256, wide_waves(NP)) void k_xattn_kv(AttnArgs a) {
         read_k(0);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            if (kTwo && i == 1) read_k(1);
+            if (!kAhead && i == 1) read_k(1);
             float16v x;
 #pragma unroll
             for (int r = 0; r < 16; ++r) x[r] = 0.f;
@@ -500,7 +502,7 @@ __global__ __launch_bounds__(256, wide_waves(NP)) void k_xattn_kv(AttnArgs a) {
                 x = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[s], qh[s], x, 0, 0, 0);
                 if constexpr (kTwo) x = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[s], ql[s], x, 0, 0, 0);
             }
-            if constexpr (!kTwo) {
+            if constexpr (kAhead) {
                 read_v(i);
                 if (i == 0) read_k(1);
                 __builtin_amdgcn_sched_barrier(0);
@@ -517,7 +519,7 @@ __global__ __launch_bounds__(256, wide_waves(NP)) void k_xattn_kv(AttnArgs a) {
                         for (int r = 0; r < 16; ++r) O[s][r] *= less;
                 },
                 ph, pl);
-            if constexpr (kTwo) read_v(i);
+            if constexpr (!kAhead) read_v(i);
 #pragma unroll
             for (int s = 0; s < 2 * NP; ++s) {
                 O[s >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[s], ph[s & 1], O[s >> 1], 0, 0, 0);
@@ -667,7 +669,9 @@ __global__ __launch_bounds__(256, short_waves(sizeof(T) == 4, NP)) void k_xattn_
 // be empty for the most part.  Row m of the u-th K operand is slot 16 (m / 8) + 8 u + m % 8, which leaves a lane with the 8
 // slots that stand together in V.  32 bf16 queries of 4 heads each over 1 .. 8192 rows of 8 heads of 128: 53 us and 5 for the
 // join, 269 MB, where a stream of reads takes 39; one fp32 query over 32768 rows of 8 heads of 64: 10 and 4.
-// NC: 64-dim steps of the head width.
+// NC: 64-dim steps of the head width.  Up to 128 dims a wavefront holds two tiles in registers; above, one, whose K is loaded
+// again behind its products with q and V behind those with P: two workgroups to a CU then instead of one (2 x 1024 x 8 x 160
+// over 2048 rows: 76 us in fp32 and 68 in bf16, 146 and 136 with two tiles; narrow heads lose 5 to 15 % by it).
 template <int NC>
 struct FewTile {
     uint4 k[2][NC];
@@ -675,8 +679,9 @@ struct FewTile {
 };
 
 template <class T, int NC>
-__global__ __launch_bounds__(256, NC < 3 ? 2 : 1) void k_xattn_kv_few(AttnArgs a) {
+__global__ __launch_bounds__(256, 2) void k_xattn_kv_few(AttnArgs a) {
     constexpr bool kTwo = std::is_same<T, float>::value;
+    constexpr bool kRefill = NC >= 3;  // one tile in registers
     constexpr int kPitch = 68;  // floats of one row's 64 dims in LDS
     __shared__ float part[4][16][kPitch], stats[2][4][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = lane >> 4, col = lane & 15;
@@ -715,21 +720,32 @@ __global__ __launch_bounds__(256, NC < 3 ? 2 : 1) void k_xattn_kv_few(AttnArgs a
     const int v_at = 32 * e16 + col * 32 + (group & 1) * 16 + (group >> 1) * 8;
     const int n_dims = e16 / 16;
 
-    auto load = [&](FewTile<NC> &x, int32_t t) {
+    auto tile_of = [&](int32_t t) {
         const int32_t block = max(__builtin_amdgcn_readlane(id, ((t * 32) >> shift_S) - block0), 0);
-        const uint8_t *tile = a.c.codes + ((int64_t)block * H + h) * kv_slice_bytes(S, d) + (int64_t)(t & ((S >> 5) - 1)) * 64 * e16;
+        return a.c.codes + ((int64_t)block * H + h) * kv_slice_bytes(S, d) + (int64_t)(t & ((S >> 5) - 1)) * 64 * e16;
+    };
+    auto load_k = [&](FewTile<NC> &x, const uint8_t *tile) {
 #pragma unroll
         for (int s = 0; s < NC; ++s)
 #pragma unroll
             for (int u = 0; u < 2; ++u)
                 if (4 * s + group < n_dims) x.k[u][s] = *reinterpret_cast<const uint4 *>(tile + k_at + s * 2048 + u * 128);
+    };
+    auto load_v = [&](FewTile<NC> &x, const uint8_t *tile) {
 #pragma unroll
         for (int i = 0; i < 4 * NC; ++i)
             if (i < n_dims) x.v[i] = *reinterpret_cast<const uint2 *>(tile + v_at + i * 512);
     };
-    auto work = [&](const FewTile<NC> &w, int32_t t) {
+    auto load = [&](FewTile<NC> &x, int32_t t) {
+        const uint8_t *tile = tile_of(t);
+        load_k(x, tile);
+        load_v(x, tile);
+    };
+    auto work = [&](FewTile<NC> &w, int32_t t) {
         const int at = ((t * 32) >> shift_S) - block0;
-        if (__builtin_amdgcn_readlane(id, at) < 0) return;
+        const bool there = __builtin_amdgcn_readlane(id, at) >= 0;
+        if (!kRefill && !there) return;
+        const uint8_t *next = tile_of(kRefill ? min(t + 1, w1 - 1) : t);
         const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scale), at));
         const uint32_t vs = __builtin_amdgcn_readlane(__float_as_uint(v_scale), at);
         floatx4 acc[2] = {floatx4(0.f), floatx4(0.f)};
@@ -745,6 +761,8 @@ __global__ __launch_bounds__(256, NC < 3 ? 2 : 1) void k_xattn_kv_few(AttnArgs a
                     acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, ql[2 * s + 1], acc[u], 0, 0, 0);
                 }
             }
+        if (kRefill) load_k(w, next);
+        if (kRefill && !there) return load_v(w, next);
         float x[8];
 #pragma unroll
         for (int r = 0; r < 8; ++r) x[r] = acc[r >> 2][r & 3];
@@ -764,14 +782,20 @@ __global__ __launch_bounds__(256, NC < 3 ? 2 : 1) void k_xattn_kv_few(AttnArgs a
                 O[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph[0], O[i], 0, 0, 0);
                 if constexpr (kTwo) O[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl[0], O[i], 0, 0, 0);
             }
+        if (kRefill) load_v(w, next);
     };
-    {
-        FewTile<NC> x, y;
+    FewTile<NC> x;
+#pragma unroll
+    for (int s = 0; s < NC; ++s)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) x.k[u][s] = uint4{0, 0, 0, 0};  // chunks that are not there: finite
+    if (w0 < w1) load(x, w0);
+    if constexpr (!kRefill) {
+        FewTile<NC> y;
 #pragma unroll
         for (int s = 0; s < NC; ++s)
 #pragma unroll
-            for (int u = 0; u < 2; ++u) x.k[u][s] = y.k[u][s] = uint4{0, 0, 0, 0};  // chunks that are not there: finite
-        if (w0 < w1) load(x, w0);
+            for (int u = 0; u < 2; ++u) y.k[u][s] = uint4{0, 0, 0, 0};
         q_scale = split_query(raw, d, 48, qh, ql);
         for (int32_t t = w0; t < w1; t += 2) {
             if (t + 1 < w1) load(y, t + 1);
@@ -781,6 +805,9 @@ __global__ __launch_bounds__(256, NC < 3 ? 2 : 1) void k_xattn_kv_few(AttnArgs a
                 work(y, t + 1);
             }
         }
+    } else {
+        q_scale = split_query(raw, d, 48, qh, ql);
+        for (int32_t t = w0; t < w1; ++t) work(x, t);
     }
 
     // ---- the four wavefronts' sums ----
@@ -897,7 +924,12 @@ Plan plan_of(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t Hkv, int3
     const int64_t G = Hq / Hkv;
     auto tiles_of_rows = [&](int64_t R) { return packed ? rows * G / R + B : B * ((rows / B * G + R - 1) / R); };
     const int64_t wide = tiles_of_rows(kWideRows), slot_tiles = (slots + 31) / 32;
-    if (rows * G > 16 * (int64_t)B && wide * Hkv >= 256) {
+    // 128 rows at a time leave part of the chip idle below 256 workgroups; 16 at a time convert and multiply for half-empty tiles
+    // above.  Where they meet: at 128 over few slots (2 x 1024 x 8 x 128 bf16 over 77 rows: 9 us, 11 by 16; half the rows: 9 and 7),
+    // at 192 over more (4 x 900 x 6 x 160 over 512 rows: 29 and 39; 2 x 1024 x 8: 28 and 27), at 256 with narrow heads, whose long
+    // rows keep the statistics busy (4 x 900 x 6 x 64 over 2048 rows: 53 and 41; 8 x 256 x 16: 52 and 54).
+    const int64_t enough = slot_tiles <= 8 ? 128 : d <= 64 ? 256 : 192;
+    if (rows * G > 16 * (int64_t)B && wide * Hkv >= enough) {
         if (slot_tiles * tile_bytes(d) > kShortBytes) return {kLong, wide, kWideRows, 1, 0};
         // 128 rows at a time, as often as leaves some 1536 workgroups (six to a CU: lengths differ)
         const int64_t times = std::max<int64_t>(1, std::min<int64_t>(16, wide * Hkv / 1536));

@@ -500,6 +500,28 @@ def test_lengths_and_blocks_that_are_not_there(dgq, N):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [40, 128, 160, 256])
+@pytest.mark.parametrize("N,lengths", [(33, [600, 417]), (2, [1900, 1000]), (1100, [70, 90])])
+def test_blocks_that_are_not_there_at_every_width(dgq, dtype, d, N, lengths):
+    """Every third block is missing, in the middle of what a wavefront walks through and at its end."""
+    import torch
+    rng = np.random.default_rng(d + N)
+    S, H = 32, 8
+    c, table, held = _filled(dgq, rng, lengths, S, H, d)
+    bad = table.copy()
+    bad[:, 2::3] = -1
+    q, qn = _floats(rng, (2, N, H, d), dtype)
+    out = dgq.dgq_xattn_kv(q, c, _i32(bad), _i32(lengths)).float().cpu().numpy()
+    rows = np.unique(np.r_[0:33, N - 40:N].clip(0, N - 1))
+    for b, n in enumerate(lengths):
+        there = np.arange(n) // S % 3 != 2
+        k, v = (held.exact(w, table, b, n)[there] for w in (0, 1))
+        want, big = ref.attention(qn[b][rows].astype(np.float64), k, v)
+        err = np.abs(out[b][rows].astype(np.float64) - want)
+        assert (err <= ref.tolerance(dtype, d, int(there.sum()), big, v, want)).all(), (b, float(err.max()))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("N,n", [(40, 300), (1, 2000), (16500, 300)])
 def test_blocks_of_very_different_scales(dgq, dtype, N, n):
     """Values that grow and shrink by 2^40 from block to block, among them blocks of zeros, with all weight on any of them."""
