@@ -59,8 +59,8 @@ int dgq_probe_linear_kernel(int64_t rows, int32_t out_channels, int32_t n_chunks
 
 /*
  * The kernel that dgq_xattn_kv takes for these arguments (as of dgq_xattn_kv_workspace_bytes; host only, for tests that mean to
- * reach one of them): 0 few rows, 1 few rows with the slots split, 2 many rows with whole requests in LDS, 3 many rows in stages.
- * DGQ_EINVAL for what is not a call.
+ * reach one of them): 0 few rows, 1 few rows with the slots split (fp32 queries may
+ * take fewer splits, or none), 2 many rows with whole requests in LDS, 3 many rows in stages.  DGQ_EINVAL for what is not a call.
  */
 int dgq_probe_xattn_kv_kernel(int32_t B, int64_t N, int32_t packed, int32_t Hq, int32_t H, int32_t d, int32_t width,
                               int32_t block_size);

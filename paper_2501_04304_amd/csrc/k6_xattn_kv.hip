@@ -850,23 +850,71 @@ __global__ __launch_bounds__(256, 2) void k_xattn_kv_few(AttnArgs a) {
     if (!alone && out_live && quad == 0) reinterpret_cast<float2 *>(a.part + a.splits * all * d)[p] = float2{row_M, row_D};
 }
 
-// The splits of one row (query and head) added up: out = sum 2^(M_i - M) O_i / sum 2^(M_i - M) D_i.  A workgroup has a row;
-// threads are a quad of dims and one of 256 / quads runs of splits, whose sums meet in LDS.
+// The request of row `n`, a query among all, or -1.
+__device__ int32_t request_of(const AttnArgs &a, int64_t n) {
+    if (!a.q.offsets) return (int32_t)(n / a.q.N);
+    int32_t b = -1;
+    for (int i = threadIdx.x & 63; i < a.q.B && b < 0; i += 64)
+        if (a.q.offsets[i] <= n && n < a.q.offsets[i + 1]) b = i;
+    const uint64_t found = __ballot(b >= 0);
+    return found ? __shfl(b, __ffsll((unsigned long long)found) - 1) : -1;
+}
+
+// The splits of one row (query and head) added up: out = sum 2^(M_i - M) O_i / sum 2^(M_i - M) D_i, for at most kJoinFew: a
+// wavefront has a row, a lane a quad of dims and one of 64 / quads runs of splits, and nothing waits for another wavefront
+// (2 x 256 x 8 x 64 fp32 over 2048 rows, 3 splits: the call takes 18 us, 24 with a workgroup to a row; 1 x 1 x 8 x 256 over 8000
+// rows, 16 splits: 21 and 20, so it is for at most 2048 / d of them).
+constexpr int kJoinFew = 16;
+template <class T>
+__global__ __launch_bounds__(256) void k_xattn_kv_join_few(AttnArgs a) {
+    const int d = a.c.d, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t all = a.q.rows() * a.q.Hq, row = (int64_t)blockIdx.x * 4 + wave;
+    if (row >= all) return;
+    const int32_t b = request_of(a, row / a.q.Hq);
+    if (b < 0) return;  // a row that no request has is left as it was
+    const int active = ((length_of(a, b) + 31) / 32 + a.chunk - 1) / a.chunk;
+    if (active <= 1) return;  // the only split has written out itself
+    float2 mine{kNoMax, 0.f};
+    if (lane < active) mine = reinterpret_cast<const float2 *>(a.part + a.splits * all * d)[lane * all + row];
+    float M = mine.x;
+    for (int o = 8; o; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 16));
+    M = __shfl(M, 0);
+    const float weight = lane < active ? exp2_of(mine.x - M) : 0.f;
+    float D = weight * mine.y;
+    for (int o = 8; o; o >>= 1) D += __shfl_xor(D, o, 16);
+    D = __shfl(D, 0);
+    const int quads = d / 4, runs = min(64 / quads, active), run = lane / quads, quad = lane - run * quads;
+    floatx4 sum = floatx4(0.f);
+    for (int i0 = run; i0 - run < active; i0 += 4 * runs) {
+        floatx4 part[4];  // four loads under way
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int i = i0 + j * runs;
+            part[j] = floatx4(0.f);
+            if (run < runs && i < active) part[j] = *reinterpret_cast<const floatx4 *>(a.part + (i * all + row) * d + quad * 4);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum += part[j] * __shfl(weight, (i0 + j * runs) & 63);
+    }
+    floatx4 total = sum;
+    for (int r = 1; r < runs; ++r)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) total[j] += __shfl(sum[j], (lane + r * quads) & 63);
+    if (lane < quads) {
+        const float inv = D == 0.f ? 0.f : 1.f / D;
+        store4(static_cast<T *>(a.out) + row * d + quad * 4, total[0] * inv, total[1] * inv, total[2] * inv, total[3] * inv);
+    }
+}
+
+// The same for more splits: a workgroup has a row; threads are a quad of dims and one of 256 / quads runs of splits, whose sums
+// meet in LDS.
 template <class T>
 __global__ __launch_bounds__(256) void k_xattn_kv_join(AttnArgs a) {
     __shared__ float sums[256][4], weight[256], top[4], total[4];
     const int d = a.c.d, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t all = a.q.rows() * a.q.Hq, row = blockIdx.x, n = row / a.q.Hq;
-    int32_t b = -1;
-    if (!a.q.offsets) {
-        b = (int32_t)(n / a.q.N);
-    } else {
-        for (int i = lane; i < a.q.B && b < 0; i += 64)
-            if (a.q.offsets[i] <= n && n < a.q.offsets[i + 1]) b = i;
-        const uint64_t found = __ballot(b >= 0);
-        if (!found) return;  // a row that no request has is left as it was
-        b = __shfl(b, __ffsll((unsigned long long)found) - 1);
-    }
+    const int32_t b = request_of(a, n);
+    if (b < 0) return;  // a row that no request has is left as it was
     const int active = ((length_of(a, b) + 31) / 32 + a.chunk - 1) / a.chunk;
     if (active <= 1) return;  // the only split has written out itself
     const float2 *stats = reinterpret_cast<const float2 *>(a.part + a.splits * all * d) + row;
@@ -913,14 +961,15 @@ struct Plan {
     int32_t rows, splits, chunk;
     int64_t groups(int32_t Hkv) const { return tiles * Hkv * splits; }  // workgroups
 };
-constexpr int kFewGroups = 768, kFewChunk = 16;
+constexpr int kFewChunk = 16;
 // LDS for the tiles of a short request: what lets three workgroups to a CU in, with their swap places (64 KiB, two: 231 rows of 64
 // dims at batch 16 take 170 us, 158 in stages).
 constexpr int kShortBytes = 32 * 1024;
 constexpr int tile_bytes(int d) { return (d + 31) / 32 * 4096; }  // fp16 of a tile's K and V
 
 // Which kernel, its row tiles, and into how many parts each request's slots are split.
-Plan plan_of(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t Hkv, int32_t d, int64_t slots) {
+// fp32: queries are; false where it isn't known, which takes as many splits or more.
+Plan plan_of(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t Hkv, int32_t d, int64_t slots, bool fp32) {
     const int64_t G = Hq / Hkv;
     auto tiles_of_rows = [&](int64_t R) { return packed ? rows * G / R + B : B * ((rows / B * G + R - 1) / R); };
     const int64_t wide = tiles_of_rows(kWideRows), slot_tiles = (slots + 31) / 32;
@@ -936,10 +985,11 @@ Plan plan_of(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t Hkv, int3
         return {kShort, tiles_of_rows(128 * times), (int32_t)(128 * times), 1, 0};
     }
     const int64_t tiles = tiles_of_rows(16), groups = tiles * Hkv;
-    // Parts for kFewGroups workgroups, what the chip holds at once (three to a CU): more of them wait for a place while the last
-    // ones run (32 queries over 1 .. 8192 rows: 80 us with 2048, 59 with 768, 73 with 512).  None below kFewChunk tiles or above
-    // 256 (what one can look up).
-    const int64_t want = std::max<int64_t>(1, kFewGroups / std::max<int64_t>(1, groups));
+    // Parts for what the chip holds at once, three workgroups to a CU or two: more of them wait for a place while the last ones run
+    // (32 bf16 queries of 128 dims over 1 .. 8192 rows: 84 us with 1024, 57 with 768, 71 with 512; in fp32, over 2048 .. 4096 rows,
+    // 52, 58 and 46; of 160 dims 71, 78 and 67).  None below kFewChunk tiles or above 256 (what one can look up).
+    const int64_t held = d <= 64 || (d <= 128 && !fp32) ? 768 : 512;
+    const int64_t want = std::max<int64_t>(1, held / std::max<int64_t>(1, groups));
     const int64_t least = std::min<int64_t>(kFewChunk, slot_tiles), part = std::max(least, (slot_tiles + want - 1) / want);
     const int64_t chunk = std::min<int64_t>(256, (part + 3) / 4 * 4);
     return {kFew, tiles, 16, (int32_t)std::max<int64_t>(1, (slot_tiles + chunk - 1) / chunk), (int32_t)chunk};
@@ -984,7 +1034,9 @@ hipError_t launch(const AttnArgs &a, Kernel kernel, hipStream_t st) {
     if (a.splits > 1) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        k_xattn_kv_join<T><<<(uint32_t)(a.q.rows() * a.q.Hq), 256, 0, st>>>(a);
+        const int64_t all = a.q.rows() * a.q.Hq;
+        if (a.splits <= kJoinFew && a.splits * a.c.d <= 2048) k_xattn_kv_join_few<T><<<(uint32_t)((all + 3) / 4), 256, 0, st>>>(a);
+        else k_xattn_kv_join<T><<<(uint32_t)all, 256, 0, st>>>(a);
     }
     return hipGetLastError();
 }
@@ -992,23 +1044,23 @@ hipError_t launch(const AttnArgs &a, Kernel kernel, hipStream_t st) {
 }  // namespace
 
 size_t xattn_kv_workspace_bytes(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t Hkv, int32_t d, int64_t slots) {
-    const Plan p = plan_of(B, rows, packed, Hq, Hkv, d, slots);
+    const Plan p = plan_of(B, rows, packed, Hq, Hkv, d, slots, false);
     return p.splits > 1 ? (size_t)p.splits * rows * Hq * (d + 2) * sizeof(float) : 0;
 }
 
 bool xattn_kv_fits(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t Hkv, int32_t d, int64_t slots) {
-    const Plan p = plan_of(B, rows, packed, Hq, Hkv, d, slots);
+    const Plan p = plan_of(B, rows, packed, Hq, Hkv, d, slots, false);
     return p.groups(Hkv) <= kMaxGroups && (p.splits == 1 || rows * Hq <= kMaxGroups);
 }
 
 int xattn_kv_kernel(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t Hkv, int32_t d, int64_t slots) {
-    const Plan p = plan_of(B, rows, packed, Hq, Hkv, d, slots);
+    const Plan p = plan_of(B, rows, packed, Hq, Hkv, d, slots, false);
     return p.kernel == kFew ? p.splits > 1 : p.kernel == kShort ? 2 : 3;
 }
 
 hipError_t launch_xattn_kv(const KvQueries &q, const KvCache &c, const int32_t *table, int32_t width,
                            const int32_t *lengths, void *out, void *workspace, hipStream_t st) {
-    const Plan p = plan_of(q.B, q.rows(), q.offsets != nullptr, q.Hq, c.H, c.d, (int64_t)width * c.S);
+    const Plan p = plan_of(q.B, q.rows(), q.offsets != nullptr, q.Hq, c.H, c.d, (int64_t)width * c.S, q.dtype == DGQ_F32);
     const AttnArgs a{q, c, table, lengths, out, static_cast<float *>(workspace), width, q.Hq / c.H, (int32_t)p.tiles, p.rows, p.splits, p.chunk};
     return q.dtype == DGQ_F32 ? launch<float>(a, p.kernel, st)
            : q.dtype == DGQ_F16 ? launch<_Float16>(a, p.kernel, st) : launch<__bf16>(a, p.kernel, st);

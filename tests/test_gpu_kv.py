@@ -482,6 +482,27 @@ def test_few_queries_over_long_rows(dgq, dtype, B, N, H, G, d, lengths):
     _check_attention(held, table, lengths, qn, out.float().cpu().numpy(), dtype, d)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d,lengths", [(64, [20000, 530]), (8, [140000]), (256, [6000, 5000]), (128, [7000, 100, 2100]),
+                                       (256, [4000, 1]), (40, [8100, 512, 513])])
+def test_packed_rows_of_many_splits(dgq, dtype, d, lengths):
+    """Two to hundreds of splits, by every join; requests of one split beside them; rows of no request stay as they were."""
+    import torch
+    rng = np.random.default_rng(d)
+    B, H, G = len(lengths), 1, 3
+    c, table, held = _filled(dgq, rng, lengths, 64, H, d)
+    starts = [1 + 2 * b for b in range(B + 1)]
+    n = starts[-1] + 1
+    q, qn = _floats(rng, (n, H * G, d), dtype)
+    assert dgq.dgq_xattn_kv_workspace_bytes(B, n, True, H * G, H, d, table.shape[1], 64) > 0
+    out = torch.full_like(q, 7.0)
+    dgq.dgq_xattn_kv(q, c, _i32(table), _i32(lengths), q_offsets=_i32(starts), out=out)
+    out = out.float().cpu().numpy()
+    assert (out[0] == 7).all() and (out[-1] == 7).all()
+    at = [slice(*s) for s in zip(starts, starts[1:])]
+    _check_attention(held, table, lengths, [qn[s] for s in at], [out[s] for s in at], dtype, d)
+
+
 @pytest.mark.parametrize("N", [1, 70, 5500])
 def test_lengths_and_blocks_that_are_not_there(dgq, N):
     """Lengths past the table and below zero, blocks outside the cache: those rows are not there."""
