@@ -644,6 +644,7 @@ int dgq_kv_load(const void *cache, int32_t n_blocks, int32_t block_size, int32_t
  *             the rows are split over the chip and a second kernel joins the parts, which it holds
  * fp32 queries count with 22 bits, fp16 and bf16 ones with all of theirs; probabilities are rounded to fp16 for 16-bit
  * types and to 22 bits for fp32; sums are fp32.  A query with NaN or infinity gives NaN in its own row and head only.
+ * Logits may have any size, as long as d max|q| max|k|, of a query and the rows that it meets, is below 2^127.
  * The same call gives the same bits; the order of a row's sums, and with it its last bits, goes by the sizes of the call.
  * Hq a multiple of H, d a multiple of 8 up to 256 (DGQ_EUNSUPPORTED otherwise).  Enqueues on `stream`; neither
  * synchronises nor allocates.

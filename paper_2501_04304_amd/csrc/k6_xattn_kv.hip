@@ -29,7 +29,7 @@ typedef float float8v __attribute__((ext_vector_type(8)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kWideRows = 128;       // rows of a workgroup of the kernel for many
-constexpr float kNoMax = -1e30f;   // M before the first row: finite, so that M - M stays 0
+constexpr float kNoMax = -FLT_MAX;  // M before the first row: below every logit, and finite, so that M - M stays 0
 constexpr float kLift = 6.f;       // u carries 2^6, away from fp16's subnormals
 constexpr float kSlack = 8.f;      // M is raised only when a row exceeds it by 2^8: u stays below 2^15
 constexpr float kLargeMax = 0x1p18f;
