@@ -324,16 +324,18 @@ __device__ void weights(X &x, float mult, uint32_t v_scale, uint32_t &v_top, int
     float top = x[0];
 #pragma unroll
     for (int r = 1; r + 1 < R; r += 2) top = fmaxf(fmaxf(top, x[r]), x[r + 1]);
-    top = column_max<kMask>(fmaxf(top, x[R - 1])) * mult;  // mult is not negative
+    top = column_max<kMask>(fmaxf(top, x[R - 1]));
     float shift = __builtin_amdgcn_logf(__uint_as_float(v_scale)), inv = __builtin_amdgcn_rcpf(__uint_as_float(v_scale));
     if (v_scale == 0) {
         asm volatile("");
         // Zero values: any scale gives the same sums.  One that leaves M where it is, for what follows must not be measured
         // against rows that add nothing; the least there is where M is not set yet.
-        shift = fmaxf(c.M - top, -kLeastShift);
+        shift = fmaxf(c.M - top * mult, -kLeastShift);
         inv = exp2_of(-shift);
     }
-    top += shift;
+    // mult is not negative, so this is the largest of the rows' own t, to the bit: a product and a sum rounded apart may be the
+    // next number, which is 2^64 times the weight away where t is a billion
+    top = fmaf(top, mult, shift);
     if (__any(top > c.M + kSlack)) {
         const float to = fmaxf(c.M, top), less = exp2_of(c.M - to);
         c.M = to;

@@ -2,7 +2,7 @@
 import numpy as np
 import pytest
 
-from test_gpu_kv import _filled, _floats, _i32, _type, dgq  # noqa: F401  (dgq is a fixture)
+from test_gpu_kv import TYPES, _filled, _floats, _i32, _type, dgq  # noqa: F401  (dgq is a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -39,3 +39,42 @@ def test_logits_far_below_zero(dgq, form, dtype):  # noqa: F811
     for b, r in enumerate(best):
         want = held.values(1, table[b, r // S], r % S)
         assert (np.abs(out[b] - want) <= ENDS[dtype] * np.abs(want)).all(), (b, out[b, 0, 0, :4], want[0, :4])
+
+
+def _of_a_billion(dgq, form, dtype):  # noqa: F811
+    S, H, d, N, rows, W = FORMS[form]
+    rng = np.random.default_rng(rows + N + 1)
+    lengths = [60, rows // 2, rows]
+
+    def gain(k, v):
+        return k * 3e4, v
+    c, table, held = _filled(dgq, rng, lengths, S, H, d, W=W, gain=gain)
+    q, _ = _floats(rng, (3, N, H, d), "fp32")
+    q = (q * 1e4).clamp(-65504, 65504).to(_type(dtype))
+    out = dgq.dgq_xattn_kv(q, c, _i32(table), _i32(lengths)).float().cpu().numpy()
+    qn = q.double().cpu().numpy()
+    seen = 0
+    for b, n in enumerate(lengths):
+        k, v = (held.exact(w, table, b, n) for w in (0, 1))
+        for h in range(H):
+            some = np.arange(N) if N < 600 else rng.choice(N, 600, replace=False)
+            x = qn[b, some, h] @ k[:, h].T / np.sqrt(d)
+            big = (np.abs(qn[b, some, h]) @ np.abs(k[:, h]).T).max(1) / np.sqrt(d)
+            order = np.argsort(x, 1)
+            first, second = order[:, -1], order[:, -2]
+            rows_ = np.arange(len(some))
+            # clear of the logits' roundings, (2^-22 + (d + 8) 2^-24) of sum |q k| each: the largest takes all
+            clear = x[rows_, first] - x[rows_, second] > 4 * (2.0 ** -22 + (d + 8) * 2.0 ** -24) * big + 1000
+            want = v[first[clear], h]
+            err = np.abs(out[b, some[clear], h] - want)
+            assert (err <= ENDS[dtype] * np.abs(want)).all(), (b, h, float(np.nanmax(err)), int((~(err <= ENDS[dtype] * np.abs(want))).any(1).sum()))
+            seen += int(clear.sum())
+    assert seen >= 0.8 * min(N, 600) * 3 * H
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("form", FORMS)
+def test_logits_of_a_billion(dgq, form, dtype):  # noqa: F811
+    """Logits whose neighbours in fp32 lie 16 to 1024 apart: the running maximum has to be the very number that the largest
+    row's logit is, next to which the row's weight is 1."""
+    _of_a_billion(dgq, form, dtype)
