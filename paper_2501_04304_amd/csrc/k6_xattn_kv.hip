@@ -140,6 +140,9 @@ __device__ int32_t length_of(const AttnArgs &a, int32_t b) {
 }
 
 __device__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+// The root of 2^x.  M moves by more than fp32's range where scales lie far apart, and D, which holds 1 / scale, moves the
+// other way: D times the root, twice, stays in range.
+__device__ float half_of(float x) { return exp2_of(0.5f * x); }
 
 // What fp16 leaves of x f, in fp16: one mixed-precision instruction (of x - hi the compiler makes three).
 __device__ _Float16 rest_of(float x, float f, _Float16 hi) { return (_Float16)fmaf(x, f, -(float)hi); }
@@ -321,42 +324,45 @@ __device__ void weights(X &x, float mult, uint32_t v_scale, uint32_t &v_top, int
         for (int r = 0; r < R; ++r)
             if (slot_of(r) >= left) x[r] = -INFINITY;
     }
-    float top = x[0];
+    float most = x[0];
 #pragma unroll
-    for (int r = 1; r + 1 < R; r += 2) top = fmaxf(fmaxf(top, x[r]), x[r + 1]);
-    top = column_max<kMask>(fmaxf(top, x[R - 1]));
+    for (int r = 1; r + 1 < R; r += 2) most = fmaxf(fmaxf(most, x[r]), x[r + 1]);
+    most = column_max<kMask>(fmaxf(most, x[R - 1]));
     float shift = __builtin_amdgcn_logf(__uint_as_float(v_scale)), inv = __builtin_amdgcn_rcpf(__uint_as_float(v_scale));
     if (v_scale == 0) {
         asm volatile("");
         // Zero values: any scale gives the same sums.  One that leaves M where it is, for what follows must not be measured
         // against rows that add nothing; the least there is where M is not set yet.
-        shift = fmaxf(c.M - top * mult, -kLeastShift);
+        shift = fmaxf(c.M - most * mult, -kLeastShift);
         inv = exp2_of(-shift);
     }
     // mult is not negative, so this is the largest of the rows' own t, to the bit: a product and a sum rounded apart may be the
     // next number, which is 2^64 times the weight away where t is a billion
-    top = fmaf(top, mult, shift);
+    const float top = fmaf(most, mult, shift);
     if (__any(top > c.M + kSlack)) {
-        const float to = fmaxf(c.M, top), less = exp2_of(c.M - to);
+        const float to = fmaxf(c.M, top), half = half_of(c.M - to);
         c.M = to;
-        c.D *= less;
-        rescale(less);
+        c.D = c.D * half * half;
+        rescale(half * half);
     }
     float off = shift - c.M + kLift;  // one rounding, next to M; M's own is common to all rows
     if (__any(fabsf(c.M) > kLargeMax)) {  // where it could reach 1: t is rounded before M is taken off
 #pragma unroll
         for (int r = 0; r < R; ++r) x[r] = fmaf(x[r], mult, shift) - c.M;
-        mult = 1.f, off = kLift;
+        mult = 1.f, off = kLift, most = top - c.M;
     }
     float sum = 0.f;
 #pragma unroll
     for (int r = 0; r < R; r += 2) weigh_two<kTwo>(x, r, mult, off, sum, ph, pl);
-    // Summing what is multiplied needs every u that counts in D among fp16's normals: beside the values of a block of a far
-    // larger scale it may not be, while its weight is all of D.
-    if (!kTwo && v_scale + (6u << 23) < v_top) {
+    // What a row adds to D, u / s_v, may count where u itself does not: beside the values of a block of a far larger scale u is
+    // below fp16's normals, or below fp32's, while its weight may be all of D.  Then D takes powers of their own, measured against
+    // the tile's largest.
+    if (v_scale + ((kTwo ? 64u : 6u) << 23) < v_top) {
+        const float over = fmaf(most, mult, off), half = half_of(over - shift);
         sum = 0.f;
 #pragma unroll
-        for (int r = 0; r < R; ++r) sum += exp2_of(fmaf(x[r], mult, off));
+        for (int r = 0; r < R; ++r) sum += exp2_of(fmaf(x[r], mult, off) - over);
+        sum *= half, inv = half;
     }
     c.D = fmaf(sum, inv, c.D);
 }
@@ -819,13 +825,16 @@ __global__ __launch_bounds__(256, 2) void k_xattn_kv_few(AttnArgs a) {
     if (group == 0) stats[0][wave][col] = M, stats[1][wave][col] = D;
     __syncthreads();
     const float all_M = fmaxf(fmaxf(stats[0][0][col], stats[0][1][col]), fmaxf(stats[0][2][col], stats[0][3][col]));
-    const float mine = exp2_of(M - all_M);
+    const float mine = exp2_of(M - all_M);  // of O
     const int row = threadIdx.x >> 4, quad = threadIdx.x & 15;
     float row_M = kNoMax, row_D = 0.f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) row_M = fmaxf(row_M, stats[0][w][row]);
 #pragma unroll
-    for (int w = 0; w < 4; ++w) row_D = fmaf(stats[1][w][row], exp2_of(stats[0][w][row] - row_M), row_D);
+    for (int w = 0; w < 4; ++w) {
+        const float half = half_of(stats[0][w][row] - row_M);
+        row_D = fmaf(stats[1][w][row] * half, half, row_D);
+    }
     const int64_t out_m = (int64_t)rows.tile * 16 + row;
     const bool out_live = rows.has(a, out_m);
     const int64_t out_row = out_live ? rows.out(a, h, out_m) : 0;
@@ -881,8 +890,8 @@ __global__ __launch_bounds__(256) void k_xattn_kv_join_few(AttnArgs a) {
     float M = mine.x;
     for (int o = 8; o; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 16));
     M = __shfl(M, 0);
-    const float weight = lane < active ? exp2_of(mine.x - M) : 0.f;
-    float D = weight * mine.y;
+    const float half = lane < active ? half_of(mine.x - M) : 0.f, weight = half * half;
+    float D = mine.y * half * half;
     for (int o = 8; o; o >>= 1) D += __shfl_xor(D, o, 16);
     D = __shfl(D, 0);
     const int quads = d / 4, runs = min(64 / quads, active), run = lane / quads, quad = lane - run * quads;
@@ -933,8 +942,9 @@ __global__ __launch_bounds__(256) void k_xattn_kv_join(AttnArgs a) {
         __syncthreads();
         if (i0 + tid < active) {
             const float2 s = stats[(i0 + tid) * all];
-            weight[tid] = exp2_of(s.x - M);
-            D = fmaf(weight[tid], s.y, D);
+            const float half = half_of(s.x - M);
+            weight[tid] = half * half;
+            D = fmaf(s.y * half, half, D);
         }
         __syncthreads();
         const int here = min(active - i0, 256);

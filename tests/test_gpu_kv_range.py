@@ -78,3 +78,35 @@ def test_logits_of_a_billion(dgq, form, dtype):  # noqa: F811
     """Logits whose neighbours in fp32 lie 16 to 1024 apart: the running maximum has to be the very number that the largest
     row's logit is, next to which the row's weight is 1."""
     _of_a_billion(dgq, form, dtype)
+
+
+@pytest.mark.parametrize("small,large", [(-90, 45), (-95, 9), (-95, 118)])
+@pytest.mark.parametrize("last", [False, True], ids=["large_first", "small_first"])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("form", FORMS)
+def test_equal_logits_over_scales_far_apart(dgq, form, dtype, last, small, large):  # noqa: F811
+    """Rows of equal weight in blocks of values near 2^small, near 2^large and of zeros: the mean of all, however many times
+    one scale is the other.  (A tile, a wavefront's share and a split each meet both.)"""
+    if dtype == "fp16" and large > 9:
+        pytest.skip("fp16 does not hold the mean")
+    S, H, d, N, rows, W = FORMS[form]
+    rng = np.random.default_rng(rows + N + 2)
+    lengths = [S + 20, rows // 2, rows]
+
+    def gain(k, v):
+        at = np.concatenate([np.arange(n) // S for n in lengths])
+        one = np.concatenate([(np.arange(n) // S < -(-n // S) // 2) == last for n in lengths])  # halves, at either end
+        f = np.where(one, 2.0 ** small, 2.0 ** large) * np.where(at % 5 == 3, 0, 1)
+        import torch
+        v = v.abs().clamp(0.5, 4) * torch.from_numpy(f.astype(np.float32)).cuda()[:, None, None]
+        k.zero_()
+        return k, v
+    c, table, held = _filled(dgq, rng, lengths, S, H, d, W=W, gain=gain)
+    q, _ = _floats(rng, (3, N, H, d), dtype)
+    out = dgq.dgq_xattn_kv(q, c, _i32(table), _i32(lengths)).float().cpu().numpy()
+    for b, n in enumerate(lengths):
+        want = held.exact(1, table, b, n).mean(0)  # all values positive: nothing cancels
+        # a weight in fp16 pieces (2^-22, 2^-11), 2^x and 1/x of the hardware (2^-22 each, twice), n sums in fp32
+        rel = (2.0 ** -22 if dtype == "fp32" else 2.0 ** -11) + 4 * 2.0 ** -22 + 2 * (n + 40) * 2.0 ** -24
+        lim = (rel + {"fp32": 2.0 ** -24, "fp16": 2.0 ** -11, "bf16": 2.0 ** -8}[dtype] * 1.01) * want
+        assert (np.abs(out[b] - want) <= lim).all(), (b, float((out[b] / want).min()), float((out[b] / want).max()))
