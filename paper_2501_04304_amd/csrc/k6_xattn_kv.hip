@@ -6,7 +6,7 @@
 //   t_j = l_j log2(e) + log2(s_v),  M = running max of t,  u_j = 2^(t_j - M),
 //   O = sum u_j c'_j,  D = sum u_j / s_v,  out = O / D,
 // and u_j is at most 1 in units of what its row adds, whatever the blocks' scales are.  (A block of zero values takes the
-// scale in its place that leaves M alone: its O is 0 with any, its share of D is right with any.)
+// least scale that a block may have: its O is 0 with any, its share of D is right with any.)
 //
 // Codes are exact in fp16.  Queries are multiplied by a power of two that brings the row's largest element to
 // [2^14, 2^15): an fp16 or bf16 query is then exact in one fp16 (bf16 elements below 2^-28 of the row's largest lose
@@ -33,7 +33,7 @@ constexpr float kNoMax = -FLT_MAX;  // M before the first row: below every logit
 constexpr float kLift = 6.f;       // u carries 2^6, away from fp16's subnormals
 constexpr float kSlack = 8.f;      // M is raised only when a row exceeds it by 2^8: u stays below 2^15
 constexpr float kLargeMax = 0x1p18f;
-constexpr float kLeastShift = 96.f;  // -log2(kKvLeastScale)
+constexpr uint32_t kLeastScaleBits = __builtin_bit_cast(uint32_t, kKvLeastScale);
 
 struct AttnArgs {
     KvQueries q;
@@ -316,6 +316,9 @@ struct Column {
 // leave the straight line's registers alone (O in a second copy of the line would cost 80 more).
 template <bool kTwo, int R, int kMask, class X, class Slot, class Rescale, class P>
 __device__ void weights(X &x, float mult, uint32_t v_scale, uint32_t &v_top, int left, Slot slot_of, Column &c, Rescale rescale, P &ph, P &pl) {
+    // A block of zero values has a scale of 0 and takes the least there is: its codes are zeros, so its O is 0 and its share of D
+    // right with any, and M is raised by rows that add nothing only where it is far below them.
+    v_scale = max(v_scale, kLeastScaleBits);
     v_top = max(v_top, v_scale);
     if (left < 32) {
         asm volatile("");  // a branch: as selects it would cost every tile 30 instructions
@@ -329,13 +332,6 @@ __device__ void weights(X &x, float mult, uint32_t v_scale, uint32_t &v_top, int
     for (int r = 1; r + 1 < R; r += 2) most = fmaxf(fmaxf(most, x[r]), x[r + 1]);
     most = column_max<kMask>(fmaxf(most, x[R - 1]));
     float shift = __builtin_amdgcn_logf(__uint_as_float(v_scale)), inv = __builtin_amdgcn_rcpf(__uint_as_float(v_scale));
-    if (v_scale == 0) {
-        asm volatile("");
-        // Zero values: any scale gives the same sums.  One that leaves M where it is, for what follows must not be measured
-        // against rows that add nothing; the least there is where M is not set yet.
-        shift = fmaxf(c.M - most * mult, -kLeastShift);
-        inv = exp2_of(-shift);
-    }
     // mult is not negative, so this is the largest of the rows' own t, to the bit: a product and a sum rounded apart may be the
     // next number, which is 2^64 times the weight away where t is a billion
     const float top = fmaf(most, mult, shift);

@@ -41,12 +41,15 @@ def test_logits_far_below_zero(dgq, form, dtype):  # noqa: F811
         assert (np.abs(out[b] - want) <= ENDS[dtype] * np.abs(want)).all(), (b, out[b, 0, 0, :4], want[0, :4])
 
 
-def _of_a_billion(dgq, form, dtype):  # noqa: F811
+def _of_a_billion(dgq, form, dtype, zeros):  # noqa: F811
     S, H, d, N, rows, W = FORMS[form]
     rng = np.random.default_rng(rows + N + 1)
     lengths = [60, rows // 2, rows]
 
     def gain(k, v):
+        if zeros:  # every third block of every request
+            at = np.concatenate([np.arange(n) // S % 3 == 1 for n in lengths])
+            v[at] = 0
         return k * 3e4, v
     c, table, held = _filled(dgq, rng, lengths, S, H, d, W=W, gain=gain)
     q, _ = _floats(rng, (3, N, H, d), "fp32")
@@ -77,7 +80,14 @@ def _of_a_billion(dgq, form, dtype):  # noqa: F811
 def test_logits_of_a_billion(dgq, form, dtype):  # noqa: F811
     """Logits whose neighbours in fp32 lie 16 to 1024 apart: the running maximum has to be the very number that the largest
     row's logit is, next to which the row's weight is 1."""
-    _of_a_billion(dgq, form, dtype)
+    _of_a_billion(dgq, form, dtype, zeros=False)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("form", FORMS)
+def test_zero_values_beside_logits_of_a_billion(dgq, form, dtype):  # noqa: F811
+    """The same where every third block's values are zeros: its rows take weight, or leave it, like any others."""
+    _of_a_billion(dgq, form, dtype, zeros=True)
 
 
 @pytest.mark.parametrize("small,large", [(-90, 45), (-95, 9), (-95, 118)])
