@@ -64,6 +64,9 @@ int dgq_probe_linear_kernel(int64_t rows, int32_t out_channels, int32_t n_chunks
  */
 int dgq_probe_xattn_kv_kernel(int32_t B, int64_t N, int32_t packed, int32_t Hq, int32_t H, int32_t d, int32_t width,
                               int32_t block_size);
+/* The rows (queries times heads of a group) that a workgroup of it takes; whole requests in LDS: 128 in each of 1 to 16 passes. */
+int dgq_probe_xattn_kv_rows(int32_t B, int64_t N, int32_t packed, int32_t Hq, int32_t H, int32_t d, int32_t width,
+                            int32_t block_size);
 
 #ifdef __cplusplus
 }

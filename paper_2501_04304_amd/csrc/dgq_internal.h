@@ -256,6 +256,7 @@ struct KvQueries {
 size_t xattn_kv_workspace_bytes(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t Hkv, int32_t d, int64_t slots);
 bool xattn_kv_fits(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t Hkv, int32_t d, int64_t slots);  // a grid
 int xattn_kv_kernel(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t Hkv, int32_t d, int64_t slots);  // dgq_probe.h
+int32_t xattn_kv_rows(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t Hkv, int32_t d, int64_t slots);  // dgq_probe.h
 hipError_t launch_xattn_kv(const KvQueries &q, const KvCache &c, const int32_t *table, int32_t width,
                            const int32_t *lengths, void *out, void *workspace, hipStream_t st);
 

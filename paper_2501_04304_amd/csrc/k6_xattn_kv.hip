@@ -1066,6 +1066,10 @@ int xattn_kv_kernel(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t Hk
     return p.kernel == kFew ? p.splits > 1 : p.kernel == kShort ? 2 : 3;
 }
 
+int32_t xattn_kv_rows(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t Hkv, int32_t d, int64_t slots) {
+    return plan_of(B, rows, packed, Hq, Hkv, d, slots, false).rows;
+}
+
 hipError_t launch_xattn_kv(const KvQueries &q, const KvCache &c, const int32_t *table, int32_t width,
                            const int32_t *lengths, void *out, void *workspace, hipStream_t st) {
     const Plan p = plan_of(q.B, q.rows(), q.offsets != nullptr, q.Hq, c.H, c.d, (int64_t)width * c.S, q.dtype == DGQ_F32);

@@ -144,13 +144,22 @@ int dgq_probe_linear_kernel(int64_t rows, int32_t out_channels, int32_t n_chunks
     return block >= 0 ? block : 10 + ring_shape(s);
 }
 
+static bool xattn_kv_call(int32_t B, int64_t N, int32_t Hq, int32_t H, int32_t d, int32_t width, int32_t block_size) {
+    if (B >= 1 && N >= 1 && H >= 1 && Hq >= 1 && Hq % H == 0 && d >= 1 && width >= 1 && block_size >= 1) return true;
+    set_error("dgq_probe_xattn_kv: not a call");
+    return false;
+}
+
 int dgq_probe_xattn_kv_kernel(int32_t B, int64_t N, int32_t packed, int32_t Hq, int32_t H, int32_t d, int32_t width,
                               int32_t block_size) {
-    if (B < 1 || N < 1 || H < 1 || Hq < 1 || Hq % H || d < 1 || width < 1 || block_size < 1) {
-        set_error("dgq_probe_xattn_kv_kernel: not a call");
-        return DGQ_EINVAL;
-    }
+    if (!xattn_kv_call(B, N, Hq, H, d, width, block_size)) return DGQ_EINVAL;
     return xattn_kv_kernel(B, packed ? N : (int64_t)B * N, packed != 0, Hq, H, d, (int64_t)width * block_size);
+}
+
+int dgq_probe_xattn_kv_rows(int32_t B, int64_t N, int32_t packed, int32_t Hq, int32_t H, int32_t d, int32_t width,
+                            int32_t block_size) {
+    if (!xattn_kv_call(B, N, Hq, H, d, width, block_size)) return DGQ_EINVAL;
+    return xattn_kv_rows(B, packed ? N : (int64_t)B * N, packed != 0, Hq, H, d, (int64_t)width * block_size);
 }
 
 }  // extern "C"

@@ -1,5 +1,7 @@
-"""The shapes of the tests at the ends of the range reach the kernels that they are named for (on the CPU: the library's own
-choice)."""
+"""The shapes of the tests reach the kernels, joins and passes that they are named for (on the CPU: the library's own choice)."""
+import ctypes
+
+import test_gpu_kv_passes
 import test_gpu_kv_range as gpu
 from test_kv_kernel_choice import FEW, SHORT, SPLIT, STAGES, kernel  # noqa: F401  (kernel is a fixture)
 
@@ -19,3 +21,21 @@ def test_forms(kernel):  # noqa: F811
             assert splits > 16
         else:
             assert splits == 0
+
+
+def test_passes():
+    rows = dgq.lib().dgq_probe_xattn_kv_rows
+    rows.argtypes = [ctypes.c_int32, ctypes.c_int64] + [ctypes.c_int32] * 6
+    for passes, (S, H, G, d, N, lengths, W) in test_gpu_kv_passes.EVEN.items():
+        assert max(lengths) <= W * S and N * G % 32 and N * G % 128 and N * G > 128 * passes
+        assert rows(len(lengths), N, 0, H * G, H, d, W, S) == 128 * passes
+    S, H, G, d, n, lengths, W = test_gpu_kv_passes.PACKED
+    assert rows(len(n), sum(n) + 8, 1, H * G, H, d, W, S) == 256
+    assert rows(0, 1, 0, 1, 1, 8, 1, 32) == -1
+
+
+def test_passes_take_the_kernel_of_short_requests(kernel):  # noqa: F811
+    for S, H, G, d, N, lengths, W in test_gpu_kv_passes.EVEN.values():
+        assert kernel(len(lengths), N, 0, H * G, H, d, W, S) == SHORT
+    S, H, G, d, n, lengths, W = test_gpu_kv_passes.PACKED
+    assert kernel(len(n), sum(n) + 8, 1, H * G, H, d, W, S) == SHORT
