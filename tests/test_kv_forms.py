@@ -3,6 +3,7 @@ import ctypes
 
 import test_gpu_kv_passes
 import test_gpu_kv_range as gpu
+import test_gpu_kv_splits
 from test_kv_kernel_choice import FEW, SHORT, SPLIT, STAGES, kernel  # noqa: F401  (kernel is a fixture)
 
 import paper_2501_04304_amd as dgq
@@ -39,3 +40,15 @@ def test_passes_take_the_kernel_of_short_requests(kernel):  # noqa: F811
         assert kernel(len(lengths), N, 0, H * G, H, d, W, S) == SHORT
     S, H, G, d, n, lengths, W = test_gpu_kv_passes.PACKED
     assert kernel(len(n), sum(n) + 8, 1, H * G, H, d, W, S) == SHORT
+
+
+def test_splits():
+    """of two queries and of four, with a head or three of them to the cached one"""
+    joins = set()
+    for d, rows, splits in test_gpu_kv_splits.SHAPES:
+        width = -(-rows // 64) + 1
+        for N, Hq in ((4, 3), (2, 1)):
+            for packed in (False, True):
+                assert dgq.dgq_xattn_kv_workspace_bytes(1, N, packed, Hq, 1, d, width, 64) == splits * N * Hq * (d + 2) * 4, d
+        joins.add("one pass" if 16 < splits <= 256 else "two" if splits > 256 else "a wavefront" if splits * d <= 2048 else "one pass")
+    assert joins == {"one pass", "two", "a wavefront"}
