@@ -118,3 +118,52 @@ def test_equal_logits_over_scales_far_apart(dgq, form, last, dtype, small, large
         rel = (2.0 ** -22 if dtype == "fp32" else 2.0 ** -11) + 4 * 2.0 ** -22 + 2 * (n + 40) * 2.0 ** -24
         lim = (rel + {"fp32": 2.0 ** -24, "fp16": 2.0 ** -11, "bf16": 2.0 ** -8}[dtype] * 1.01) * want
         assert (np.abs(out[b] - want) <= lim).all(), (b, float((out[b] / want).min()), float((out[b] / want).max()))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("form", FORMS)
+def test_softmax_over_scales_far_apart(dgq, form, dtype):  # noqa: F811
+    """Values that grow and shrink from block to block, by 2^40 or what the type holds, among them blocks of zeros; the weight
+    lies on a few rows of any of them.  Each element is held to its own sum of p |v|, so that a wrong denominator shows."""
+    import torch
+    S, H, d, N, rows, W = FORMS[form]
+    rng = np.random.default_rng(rows + N + 3)
+    lengths = [S + 9, rows // 2, rows]
+
+    def gain(k, v):
+        f = []
+        for n in lengths:
+            e = 2.0 ** rng.integers(-40, 9 if dtype == "fp16" else 41, -(-n // S))
+            e[3::4] = 0
+            f.append(np.repeat(e, S)[:n])
+        return k * 3, v * torch.from_numpy(np.concatenate(f).astype(np.float32)).cuda()[:, None, None]
+    c, table, held = _filled(dgq, rng, lengths, S, H, d, W=W, gain=gain)
+    q, _ = _floats(rng, (3, N, H, d), dtype)
+    q = q * 4
+    qn = q.float().cpu().numpy()
+    out = dgq.dgq_xattn_kv(q, c, _i32(table), _i32(lengths)).float().cpu().numpy()
+    told = seen = 0
+    for b, n in enumerate(lengths):
+        k, v = (held.exact(w, table, b, n) for w in (0, 1))
+        s = np.stack([held.scales[table[b, r // S], :, 1] for r in range(n)]).astype(np.float64)
+        some = np.arange(N) if N < 200 else rng.choice(N, 200, replace=False)
+        for h in range(H):
+            x = qn[b, some, h].astype(np.float64) @ k[:, h].T / np.sqrt(d)
+            big = float((np.abs(qn[b, some, h]) @ np.abs(k[:, h]).T).max() / np.sqrt(d))
+            p = np.exp(x - x.max(1, keepdims=True))
+            p /= p.sum(1, keepdims=True)
+            want = p @ v[:, h]
+            # A logit: kv_reference.tolerance's.  A weight: 2^-22 or 2^-11, 2^x, log2 and 1/x 2^-22 each; one that is below fp16's normals
+            # is off by 2^-25 2^-6 of the largest (in units of what a row adds), and where the line below is the sum of such
+            # weights, of scales at most 2^6 apart, by 2^6 times as much.  The sums: 2 (n + 40) 2^-24.
+            logit = (2.0 ** -22 + (d + 4) * 2.0 ** -24) * big + 2 * 64 * 2.0 ** -24
+            rel = 2 * logit * 1.01 + 6 * 2.0 ** -22 + 2 * (n + 40) * 2.0 ** -24
+            rel += 2.0 ** -22 if dtype == "fp32" else 2.0 ** -11 + n * 2.0 ** -25
+            lim = rel * (p @ np.abs(v[:, h])) + n * 2.0 ** -31 * 127 * (p * s[:, h]).max(1)[:, None]
+            lim += {"fp32": 2.0 ** -24, "fp16": 2.0 ** -11, "bf16": 2.0 ** -8}[dtype] * 1.01 * np.abs(want)
+            if dtype == "fp16":
+                lim += 2.0 ** -25  # its subnormal numbers
+            assert (np.abs(out[b, some, h] - want) <= lim).all(), (b, h, float((np.abs(out[b, some, h] - want) / lim).max()))
+            told += int((lim.max(1) < 0.5 * np.abs(want).max(1)).sum())
+            seen += len(some)
+    assert told >= (0.6 if dtype == "fp16" else 0.9) * seen  # rows where zeros, or twice the output, would not pass
