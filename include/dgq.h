@@ -548,6 +548,11 @@ int dgq_xattn_logq_intv(const float *q, const float *k, const uint8_t *v_codes,
  * Everything a step needs stays on the device: lengths, tables and the list of free blocks are int32 tensors that
  * kernels read and write, so a step can be captured in a graph with lengths that change between replays.
  *
+ * Requests share blocks by naming them in their rows of the table.  Full blocks may be shared by any of them.  A block that is
+ * filled in part may be shared only as long as none of the requests that name it gets new rows: these would go into that block, whose rows
+ * are then coded again for all, and two requests that grow would get the same slots (a race between the writes of one call).  So a
+ * request that is to grow starts from a prompt's full blocks, with its other rows written anew.
+ *
  * What a kernel finds in these tensors is checked there, without an error: lengths below 0 count as 0 and above
  * width * block_size as that, and a block index outside [0, n_blocks) is a block that is not there.
  */
@@ -561,7 +566,8 @@ typedef enum dgq_dtype { DGQ_F32 = 0, DGQ_F16 = 1, DGQ_BF16 = 2 } dgq_dtype;
  * at rows row_offsets[b] .. of the packed tensors that dgq_kv_store takes (requests in order, row_offsets the exclusive
  * sums of new_rows; below 0 counts as 0).  A request is served if its lengths and new_rows are not negative, the table's
  * row has room for all its rows, its rows lie within `rows`, and the free blocks reach for it and all before it; else it
- * stays as it is.  With new_rows[b] = 0 it is served if the former hold.
+ * stays as it is.  With new_rows[b] = 0 it is served if the former hold.  The last block of a request that grows, if it is filled in
+ * part, must be its own (above); nothing here looks for others that name it.
  *   rows         rows of the packed tensors (host; what counts[3] may not pass)
  *   table        int32 [B, width]: entries of blocks that a request gets are written, no others
  *   free_blocks  int32 [free_capacity], the first n_free[0] of them free; blocks are taken from the end, requests in
@@ -605,7 +611,8 @@ size_t dgq_kv_cache_bytes(int32_t n_blocks, int32_t block_size, int32_t H, int32
  * Rows of K and V into the cache: every run puts its rows into slots slot .. slot + n - 1 of its block, K and V and every
  * head with a scale of their own:
  *   s = max |x| * (1/127) over the run's rows (0 if that is below 2^-96: such rows become zeros); a run that starts at a slot
- *   above 0 continues the block: s = max(s, the block's scale), and the rows in front keep their values, code * old scale
+ *   above 0 continues the block: s = max(s, the block's scale), and where that is larger the rows in front, code * old scale,
+ *   are rounded again against s (each time by s / 2 at most); where it is not they keep their codes
  *   code = clamp(rne(x * (1/s)), -127, 127)       (separate fp32 operations)
  * Slots behind the run hold code 0 afterwards.  NaN or infinity in x makes the scale, and with it every value of the
  * block and head, not finite.

@@ -490,14 +490,17 @@ def dgq_kv_cache_bytes(n_blocks: int, block_size: int, heads: int, d: int) -> in
 def dgq_kv_plan(lengths, new_rows, table, free_blocks, n_free, block_size: int, rows: int, lengths_out=None,
                 n_free_out=None, row_offsets=None, runs=None, counts=None, stream=None) -> KVPlan:
     """Blocks and runs for new_rows[b] more rows of every request (int32 device tensors; rows: of the packed K and V that
-    dgq_kv_store takes).  Fills new entries of `table` [B, width] and returns a KVPlan; what is passed is written into."""
+    dgq_kv_store takes).  Fills new entries of `table` [B, width] and returns a KVPlan; what is passed is written into, and what
+    is not passed are parts of one allocation: whoever keeps `lengths` and `n_free` for long passes buffers for them, or clones
+    them.  A partly filled last block of a request that grows must not be named by another one."""
     return KVPlan(*(_hot or _load_hot()).kv_plan(lengths, new_rows, table, free_blocks, n_free, block_size, rows,
                                                  lengths_out, n_free_out, row_offsets, runs, counts, stream))
 
 
 def dgq_kv_release(done, lengths, table, free_blocks, n_free, block_size: int, lengths_out=None, n_free_out=None,
                    stream=None):
-    """Blocks of the requests with done[b] != 0 (uint8 [B]) back to the end of free_blocks.  Returns (lengths, n_free)."""
+    """Blocks of the requests with done[b] != 0 (uint8 [B]) back to the end of free_blocks.  Returns (lengths, n_free), parts of
+    one allocation where they are not passed.  A block goes back as often as a finished request names it."""
     return (_hot or _load_hot()).kv_release(done, lengths, table, free_blocks, n_free, block_size, lengths_out,
                                             n_free_out, stream)
 
