@@ -640,7 +640,7 @@ int dgq_kv_load(const void *cache, int32_t n_blocks, int32_t block_size, int32_t
  * Cross-attention to the cache: every query of request b against that request's rows,
  *   L[i, j] = (q[i, h, :] . k[j, h / G, :]) / sqrt(d),  out[i, h, :] = sum_j softmax_j(L)[i, j] v[j, h / G, :],
  * over j < lengths[b], with Hq = G H query heads to H cached ones.  A request without rows gives zeros.  Probabilities
- * stay in fp32 precision (no codes): this is the attention of layers whose text is longer than dgq_xattn_logq takes, of
+ * are not quantized to codes (their roundings are below): this is the attention of layers whose text is longer than dgq_xattn_logq takes, of
  * several lengths in one batch, or kept in 8 bits.
  *   q, out    [B, N, Hq, d] of `dtype` (q_offsets NULL: N queries for every request), or [N, Hq, d] with q_offsets int32
  *             [B + 1] ascending: request b has rows q_offsets[b] .. q_offsets[b + 1] - 1; rows of no request keep what
@@ -649,8 +649,9 @@ int dgq_kv_load(const void *cache, int32_t n_blocks, int32_t block_size, int32_t
  *   lengths   int32 [B], table int32 [B, width]
  *   workspace dgq_xattn_kv_workspace_bytes(...) bytes, 16-byte aligned (0 bytes: NULL): where few queries meet many rows
  *             the rows are split over the chip and a second kernel joins the parts, which it holds
- * fp32 queries count with 22 bits, fp16 and bf16 ones with all of theirs; probabilities are rounded to fp16 for 16-bit
- * types and to 22 bits for fp32; sums are fp32.  A query with NaN or infinity gives NaN in its own row and head only.
+ * fp32 queries count with 22 bits, fp16 and bf16 ones with all of theirs (elements 2^28 below their row's largest: to 2^-39
+ * of that); probabilities are rounded to fp16's 11 bits for 16-bit types and to 22 for fp32 (those 2^20 below a row's largest, in
+ * units of what a row adds to out: to 2^-31 of that); sums are fp32.  A query with NaN or infinity gives NaN in its own row and head only.
  * Logits may have any size, as long as d max|q| max|k|, of a query and the rows that it meets, is below 2^127.
  * The same call gives the same bits; the order of a row's sums, and with it its last bits, goes by the sizes of the call.
  * Hq a multiple of H, d a multiple of 8 up to 256 (DGQ_EUNSUPPORTED otherwise).  Enqueues on `stream`; neither

@@ -143,7 +143,7 @@ struct KvCache {
     float *scales;   // [n_blocks, H, 2]: K, V
     int32_t n_blocks, S, H, d;
 };
-constexpr int kKvMaxRequests = DGQ_KV_MAX_REQUESTS;  // 16 to a thread of the planner
+constexpr int kKvMaxRequests = DGQ_KV_MAX_REQUESTS;  // 4 to a thread of the planner
 constexpr int kKvMaxDim = 256;
 constexpr int64_t kMaxGroups = (1 << 24) - 1;  // workgroups of 256 threads along x: a launch has fewer than 2^32 threads there
 constexpr float kKvLeastScale = 0x1p-96f;     // a block whose scale would be below it holds zeros

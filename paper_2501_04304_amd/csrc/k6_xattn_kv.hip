@@ -9,7 +9,7 @@
 // least scale that a block may have: its O is 0 with any, its share of D is right with any.)
 //
 // Codes are exact in fp16.  Queries are multiplied by a power of two that brings the row's largest element to
-// [2^14, 2^15): an fp16 or bf16 query is then exact in one fp16 (bf16 elements below 2^-28 of the row's largest lose
+// [2^14, 2^15): an fp16 or bf16 query is then exact in one fp16 (elements below 2^-28 of the row's largest lose
 // bits), an fp32 query is two (22 bits).  u is rounded to one fp16 for 16-bit outputs (2^-11; D sums the
 // rounded ones, so a row that takes most of the weight adds no error), to two for fp32 ones.  Sums are fp32.
 #include <cfloat>
@@ -371,13 +371,14 @@ __device__ void weights(X &x, float mult, uint32_t v_scale, uint32_t &v_top, int
 // once for all four, and puts it into LDS in units of 16 bytes, one operand of one lane, so that every read and write of 64
 // lanes is 1 KiB without a bank met twice (2 x 4096 x 24 x 128 over 4000 rows: 1057 us with every wavefront converting for
 // itself).  Two stages of LDS and one barrier a stage: a stage's place was last read in front of the barrier before.
-// Bound by vector instructions: of 64-dim bf16 heads over 1024 rows, 114 a tile of 32 x 32 beside 8 products, vector pipes busy
-// 60 % and matrix pipes 27 % of the time, 16 of the 114 exponentials of two issue slots each.  Exponentials placed by hand among
+// Bound by both pipes in turn, with narrow heads mostly by vector instructions: of 64-dim bf16 heads over 1024 rows 117 for a tile of
+// 32 x 32 beside 8 products, 16 of them exponentials of two issue slots each, vector pipes busy 66 % and matrix pipes 29 % of the time;
+// of 128-dim heads 44 % and 35 %.  Exponentials placed by hand among
 // the next tile's products gained 3 % on 128 dims and cost the narrow heads a wavefront of occupancy, 10 to 25 % (121 us
 // for 110 at 16 x 4096 x 10 x 64 fp32); so did both tiles' logits up front.
 // T: type of q and out.  NP: 32-dim steps of the head width.
 // wavefronts to a SIMD that the registers leave (and LDS: two workgroups of 160 dims fill it; 8 x 512 x 40 x 160 over 2048 rows:
-// 482 us in fp32 and 305 in bf16, 629 and 489 with one)
+// 489 us in fp32 and 299 in bf16, 629 and 489 with one)
 constexpr int wide_waves(int NP) { return NP <= 1 ? 4 : NP <= 2 ? 3 : NP <= 5 ? 2 : 1; }
 template <class T, int NP>
 __global__ __launch_bounds__(256, wide_waves(NP)) void k_xattn_kv(AttnArgs a) {
@@ -547,8 +548,8 @@ constexpr int short_waves(bool two, int NP) { return NP <= 1 ? 4 : NP <= 2 ? 3 :
 // ---- many rows, short requests: all of a request's tiles fit LDS ----------------------------------------------------------
 // A workgroup makes fp16 of the request's K and V once and takes a.rows rows through them, 32 to a wavefront at a time, with
 // no barrier after the first; the next 32 queries are loaded while these are worked on.  Bound by the queries' and the
-// output's bytes and by what the exponentials add to their time: 16 x 4096 x 10 x 64 over 77 rows takes 96 us in fp32 and 58 in
-// bf16, 84 and 48 over one row (100 and 69 in stages; a copy of the bytes 63 and 31).
+// output's bytes and by what the exponentials add to their time: 16 x 4096 x 10 x 64 over 77 rows takes 91 us in fp32 and 59 in
+// bf16, 81 and 48 over one row (100 and 69 in stages; a copy of the bytes 63 and 31).
 template <class T, int NP>
 __global__ __launch_bounds__(256, short_waves(sizeof(T) == 4, NP)) void k_xattn_kv_short(AttnArgs a) {
     constexpr bool kTwo = std::is_same<T, float>::value;
