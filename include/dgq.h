@@ -548,10 +548,10 @@ int dgq_xattn_logq_intv(const float *q, const float *k, const uint8_t *v_codes,
  * Everything a step needs stays on the device: lengths, tables and the list of free blocks are int32 tensors that
  * kernels read and write, so a step can be captured in a graph with lengths that change between replays.
  *
- * Requests share blocks by naming them in their rows of the table.  Full blocks may be shared by any of them.  A block that is
- * filled in part may be shared only as long as none of the requests that name it gets new rows: these would go into that block, whose rows
- * are then coded again for all, and two requests that grow would get the same slots (a race between the writes of one call).  So a
- * request that is to grow starts from a prompt's full blocks, with its other rows written anew.
+ * Requests share blocks by naming them in their rows of the table.  Full blocks may be shared by any of them.  A block that
+ * is filled in part may be shared only as long as none of the requests that name it gets new rows: these would go into that
+ * block, whose rows are then coded again for all, and two requests that grow would get the same slots (a race between the
+ * writes of one call).  So a request that is to grow starts from a prompt's full blocks, with its other rows written anew.
  *
  * What a kernel finds in these tensors is checked there, without an error: lengths below 0 count as 0 and above
  * width * block_size as that, and a block index outside [0, n_blocks) is a block that is not there.
@@ -566,8 +566,8 @@ typedef enum dgq_dtype { DGQ_F32 = 0, DGQ_F16 = 1, DGQ_BF16 = 2 } dgq_dtype;
  * at rows row_offsets[b] .. of the packed tensors that dgq_kv_store takes (requests in order, row_offsets the exclusive
  * sums of new_rows; below 0 counts as 0).  A request is served if its lengths and new_rows are not negative, the table's
  * row has room for all its rows, its rows lie within `rows`, and the free blocks reach for it and all before it; else it
- * stays as it is.  With new_rows[b] = 0 it is served if the former hold.  The last block of a request that grows, if it is filled in
- * part, must be its own (above); nothing here looks for others that name it.
+ * stays as it is.  With new_rows[b] = 0 it is served if the former hold.  The last block of a request that grows, if it is
+ * filled in part, must be its own (above); nothing here looks for others that name it.
  *   rows         rows of the packed tensors (host; what counts[3] may not pass)
  *   table        int32 [B, width]: entries of blocks that a request gets are written, no others
  *   free_blocks  int32 [free_capacity], the first n_free[0] of them free; blocks are taken from the end, requests in
@@ -619,7 +619,7 @@ size_t dgq_kv_cache_bytes(int32_t n_blocks, int32_t block_size, int32_t H, int32
  *   k, v     [rows, H, d] of `dtype`, dims contiguous; row and head strides in elements, multiples of 16 bytes (so both may
  *            be views of one projection's output), bases 16-byte aligned
  *   runs     int32 [n_runs, 4] as dgq_kv_plan writes them, 16-byte aligned; entries with n < 1 or that point outside
- *            the cache or the tensors are passed over.  No two runs of a call may name the same block
+ *            the cache or the tensors are passed over.  No two runs of a call may name the same block; n_runs below 2^24
  *   cache    dgq_kv_cache_bytes(...) bytes, 16-byte aligned
  * Enqueues on `stream`; neither synchronises nor allocates.
  */
@@ -630,7 +630,8 @@ int dgq_kv_store(const void *k, const void *v, int32_t dtype, int64_t rows, int6
 /*
  * The values that the cache holds: k, v [B, max_rows, H, d] of `dtype`, contiguous, 16-byte aligned; rows from a
  * request's length on (and of blocks that are not there) are zeros.  What dgq_xattn_logq takes as k and v for a batch
- * of one prompt length, and what moves a prompt elsewhere.  Enqueues on `stream`; neither synchronises nor allocates.
+ * of one prompt length, and what moves a prompt elsewhere.  B at most 65535, max_rows at most 2^29 - 32.  Enqueues on
+ * `stream`; neither synchronises nor allocates.
  */
 int dgq_kv_load(const void *cache, int32_t n_blocks, int32_t block_size, int32_t H, int32_t d, const int32_t *table,
                 int32_t width, const int32_t *lengths, int32_t B, int32_t max_rows, int32_t dtype, void *k, void *v,
@@ -640,8 +641,8 @@ int dgq_kv_load(const void *cache, int32_t n_blocks, int32_t block_size, int32_t
  * Cross-attention to the cache: every query of request b against that request's rows,
  *   L[i, j] = (q[i, h, :] . k[j, h / G, :]) / sqrt(d),  out[i, h, :] = sum_j softmax_j(L)[i, j] v[j, h / G, :],
  * over j < lengths[b], with Hq = G H query heads to H cached ones.  A request without rows gives zeros.  Probabilities
- * are not quantized to codes (their roundings are below): this is the attention of layers whose text is longer than dgq_xattn_logq takes, of
- * several lengths in one batch, or kept in 8 bits.
+ * are not quantized to codes (their roundings are below): this is the attention of layers whose text is longer than
+ * dgq_xattn_logq takes, of several lengths in one batch, or kept in 8 bits.
  *   q, out    [B, N, Hq, d] of `dtype` (q_offsets NULL: N queries for every request), or [N, Hq, d] with q_offsets int32
  *             [B + 1] ascending: request b has rows q_offsets[b] .. q_offsets[b + 1] - 1; rows of no request keep what
  *             out held.  dims contiguous; q's batch, row and head strides in elements, multiples of 16 bytes; out is
@@ -649,9 +650,10 @@ int dgq_kv_load(const void *cache, int32_t n_blocks, int32_t block_size, int32_t
  *   lengths   int32 [B], table int32 [B, width]
  *   workspace dgq_xattn_kv_workspace_bytes(...) bytes, 16-byte aligned (0 bytes: NULL): where few queries meet many rows
  *             the rows are split over the chip and a second kernel joins the parts, which it holds
- * fp32 queries count with 22 bits, fp16 and bf16 ones with all of theirs (elements 2^28 below their row's largest: to 2^-39
- * of that); probabilities are rounded to fp16's 11 bits for 16-bit types and to 22 for fp32 (those 2^20 below a row's largest, in
- * units of what a row adds to out: to 2^-31 of that); sums are fp32.  A query with NaN or infinity gives NaN in its own row and head only.
+ * fp32 queries count with 22 bits, fp16 and bf16 ones with all of theirs (elements 2^28 below their row's largest: to
+ * 2^-39 of that); probabilities are rounded to fp16's 11 bits for 16-bit types and to 22 for fp32 (those 2^20 below a
+ * row's largest, in units of what a row adds to out: to 2^-31 of that); sums are fp32.  A query with NaN or infinity
+ * gives NaN in its own row and head only.
  * Logits may have any size, as long as d max|q| max|k|, of a query and the rows that it meets, is below 2^127.
  * The same call gives the same bits; the order of a row's sums, and with it its last bits, goes by the sizes of the call.
  * Hq a multiple of H, d a multiple of 8 up to 256 (DGQ_EUNSUPPORTED otherwise).  Enqueues on `stream`; neither

@@ -523,6 +523,6 @@ def dgq_xattn_kv_workspace_bytes(B, N, packed, Hq, heads, d, width, block_size) 
 def dgq_xattn_kv(q, cache: KVCache, table, lengths, q_offsets=None, out=None, workspace=None, stream=None):
     """Cross-attention of q [B, N, Hq, d], or packed q [rows, Hq, d] with q_offsets int32 [B + 1], to the first lengths[b]
     rows of each request's blocks.  q: fp32, fp16 or bf16, dims contiguous; Hq a multiple of the cache's heads.  Returns
-    out, contiguous, of q's shape and type."""
+    out, contiguous, of q's shape and type; packed rows of no request keep what it held (anything, if it is not passed)."""
     return (_hot or _load_hot()).xattn_kv(q, cache.data, cache.n_blocks, cache.block_size, cache.heads, cache.d, table,
                                           lengths, q_offsets, out, workspace, stream)
