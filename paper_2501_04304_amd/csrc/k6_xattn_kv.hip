@@ -354,6 +354,7 @@ __device__ void weights(X &x, float mult, uint32_t v_scale, uint32_t &v_top, int
     // below fp16's normals, or below fp32's, while its weight may be all of D.  Then D takes powers of their own, measured against
     // the tile's largest.
     if (v_scale + ((kTwo ? 64u : 6u) << 23) < v_top) {
+        asm volatile("" : "+v"(off));  // else the straight line keeps its exponents for this branch: 1 to 8 registers
         const float over = fmaf(most, mult, off), half = half_of(over - shift);
         sum = 0.f;
 #pragma unroll
@@ -548,8 +549,8 @@ constexpr int short_waves(bool two, int NP) { return NP <= 1 ? 4 : NP <= 2 ? 3 :
 // ---- many rows, short requests: all of a request's tiles fit LDS ----------------------------------------------------------
 // A workgroup makes fp16 of the request's K and V once and takes a.rows rows through them, 32 to a wavefront at a time, with
 // no barrier after the first; the next 32 queries are loaded while these are worked on.  Bound by the queries' and the
-// output's bytes and by what the exponentials add to their time: 16 x 4096 x 10 x 64 over 77 rows takes 91 us in fp32 and 59 in
-// bf16, 81 and 48 over one row (100 and 69 in stages; a copy of the bytes 63 and 31).
+// output's bytes and by what the exponentials add to their time: 16 x 4096 x 10 x 64 over 77 rows takes 89 us in fp32 and 59 in
+// bf16, 79 and 47 over one row (100 and 69 in stages; a copy of the bytes 63 and 31).
 template <class T, int NP>
 __global__ __launch_bounds__(256, short_waves(sizeof(T) == 4, NP)) void k_xattn_kv_short(AttnArgs a) {
     constexpr bool kTwo = std::is_same<T, float>::value;
