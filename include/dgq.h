@@ -33,14 +33,19 @@
  *                          text keys and values of many requests kept in blocks of
  *                          8-bit codes over the denoising steps, and the
  *                          cross-attention to prompts of any lengths that reads them
+ *   dgq_groupnorm          group norm of a map's rows with SiLU, the embedding added
+ *                          before it or scaling and shifting after it
+ *   dgq_w4_pack, dgq_w4_unpack, dgq_w4_matvec
+ *                          weights in 4 bits with a scale and a zero per group of
+ *                          inputs, and products of few rows with them
  *
  * Conventions
  *   - Every tensor pointer is a DEVICE pointer unless the comment says "host".
  *     Tensors are row-major with the innermost dimension contiguous and a base
- *     address aligned to 16 bytes (else DGQ_EALIGN).
+ *     address aligned to 16 bytes (else DGQ_EALIGN) unless the call says otherwise.
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).
  *     The hot calls (quantize_act, linear and its variants, conv3x3_codes,
- *     quantize_value, the attentions, the kv calls) only enqueue work: they neither
+ *     quantize_value, the attentions, the kv calls, groupnorm, the w4 calls) only enqueue work: they neither
  *     synchronise nor allocate.  The caller owns every tensor and
  *     keeps it alive until the stream has passed the call.
  *   - Return value: DGQ_OK or a negative dgq_status.  Nothing is enqueued when
@@ -665,6 +670,79 @@ int dgq_xattn_kv(const void *q, int32_t dtype, const int32_t *q_offsets, int64_t
                  int64_t q_head_stride, int32_t B, int64_t N, int32_t Hq, const void *cache, int32_t n_blocks,
                  int32_t block_size, int32_t H, int32_t d, const int32_t *table, int32_t width,
                  const int32_t *lengths, void *out, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * ---- around the convolutions: group norm, and products of few rows with weights in 4 bits ----
+ *
+ * A residual block normalises its map by groups of channels before each convolution, applies SiLU and takes in the time
+ * embedding, a row for each image, through a product with weights that are read once a step.
+ */
+typedef enum dgq_act { DGQ_ACT_NONE = 0, DGQ_ACT_SILU = 1 } dgq_act;  /* SiLU: t / (1 + exp(-t)) */
+
+/*
+ * Group norm of rows of channels, C / G channels to a group, over the rows of each image:
+ *   x'[n, c] = x[n, c] + add[b, c],   m, v = mean and variance (over n, not n - 1) of x' over an image's rows and a group
+ *   t = (x' - m) / sqrt(v + eps) * weight[c] + bias[c],   t = t * (1 + scale[b, c]) + shift[b, c],   y = act(t)
+ *   x, out    [B, N, C] (offsets NULL: N rows for every image), or [N, C] with offsets int32 [B + 1] ascending: image b has rows
+ *             offsets[b] .. offsets[b + 1] - 1, none of them allowed; rows of no image keep what out held.  x: channels
+ *             contiguous, batch and row strides in elements, not negative; out: contiguous.  Aligned to an element;
+ *             16 bytes, as all widths here are that are a multiple of 8, are read fastest.  out may be x (contiguous, same type)
+ *   dtype, out_dtype   dgq_dtype of x and out; out has x's type or fp32
+ *   weight, bias       fp32 [C], or NULL for 1 and 0
+ *   add, scale, shift  fp32 [B, C], channels contiguous, rows `stride` elements apart, or NULL for none
+ *   workspace dgq_groupnorm_workspace_bytes(...) bytes, 16-byte aligned: sums and tables, written before they are read
+ * Sums are in 64 bits and in an order of the call's sizes, x' - m is taken before it is rounded: the same call gives the same bits,
+ * and a map whose mean is thousands of times its deviation loses nothing to that.  NaN or infinity stays in its image and
+ * group, all of whose values become NaN.  A group of one value, or of equal ones, gives its bias (eps above 0).
+ * C a multiple of G, at most 2^20; B at most 65535.  Enqueues on `stream`; neither synchronises nor allocates.
+ */
+size_t dgq_groupnorm_workspace_bytes(int32_t B, int64_t N, int32_t packed, int32_t C, int32_t G, int32_t dtype);
+int dgq_groupnorm(const void *x, int32_t dtype, int64_t x_batch_stride, int64_t x_row_stride, const int32_t *offsets,
+                  int32_t B, int64_t N, int32_t C, int32_t G, const float *weight, const float *bias, float eps,
+                  const float *add, int64_t add_stride, const float *scale, int64_t scale_stride, const float *shift,
+                  int64_t shift_stride, int32_t act, void *out, int32_t out_dtype, void *workspace,
+                  size_t workspace_bytes, void *stream);
+
+/*
+ * Bytes of [O, C] weights in 4 bits with a scale and a zero for every `group` inputs (32, 64 or 128) of an output; 0 for sizes
+ * that are not supported (O and C from 1, O up to 2^24, C up to 2^20).  With R = ceil(O / 16), T = ceil(C / 128):
+ *   codes  u8 [R, T, 1024]: 32-bit word (4 (16 q + r) + j) of a unit holds output r of its 16 and inputs 32 j + 8 q + i of its
+ *          128, i of 0 .. 7, in nibble i / 2 (even i) or 4 + i / 2 (odd i)
+ *   words  u32 [R, T, 16, 128 / group] behind them: the pattern of the group's fp32 scale s, whose 4 lowest bits are its zero
+ * A value is s (code - zero).  Outputs and inputs that are not there are values 0.  Unlike dgq_pack_weight's, which belong to
+ * int8 activations and have one scale an output, these are for rows that are not quantized.
+ */
+size_t dgq_w4_bytes(int32_t O, int32_t C, int32_t group);
+
+/*
+ * Weights into that form.  For every output and group, in separate fp32 operations:
+ *   lo = min(0, min w), hi = max(0, max w),  s = (hi - lo) * (1/15) with the 4 lowest bits of its pattern cleared, 0 if below 2^-96
+ *   zero = clamp(rne(-lo * (1/s)), 0, 15),   code = clamp(rne(w * (1/s)) + zero, 0, 15)
+ * (s = 0: all codes 0).  A group with NaN, infinity or hi - lo above fp32 gets the scale NaN.
+ *   w     [O, C] of `dtype`, inputs contiguous, rows w_row_stride elements apart, aligned to an element
+ *   data  dgq_w4_bytes(...) bytes, 16-byte aligned, all of them written
+ * Enqueues on `stream`; neither synchronises nor allocates.
+ */
+int dgq_w4_pack(const void *w, int32_t dtype, int64_t w_row_stride, int32_t O, int32_t C, int32_t group, void *data,
+                void *stream);
+
+/* The values: w [O, C] of `dtype`, contiguous, each rounded once.  Enqueues on `stream`; neither synchronises nor allocates. */
+int dgq_w4_unpack(const void *data, int32_t O, int32_t C, int32_t group, int32_t dtype, void *w, void *stream);
+
+/*
+ * Products with such weights: y[m, o] = act(sum_k x[m, k] s (code[o, k] - zero) + bias[o]).  For few rows, whose time is the
+ * weights' bytes; any number is taken (64 rows at a time, which read the weights anew).
+ *   x     [M, C] of `dtype`, inputs contiguous, rows x_row_stride elements apart, aligned to an element
+ *   bias  fp32 [O], or NULL
+ *   y     [M, O] of out_dtype (dtype or fp32), contiguous
+ * fp32 rows count with 23 bits, fp16 and bf16 ones with all of theirs (bf16 and fp32: elements 2^29 below the largest of their
+ * 128 inputs: to 2^-39 of that); codes less zeros are exact, sums are fp32 and rounded once to y.  NaN or infinity in a row of x
+ * makes that row not finite, no other.
+ * The same call gives the same bits; the order of the sums goes by the sizes.  Enqueues on `stream`; neither synchronises nor
+ * allocates.
+ */
+int dgq_w4_matvec(const void *x, int32_t dtype, int64_t x_row_stride, int32_t M, const void *data, int32_t O, int32_t C,
+                  int32_t group, const float *bias, int32_t act, void *y, int32_t out_dtype, void *stream);
 
 #ifdef __cplusplus
 }

@@ -40,6 +40,7 @@ class GroupsInfo(C.Structure):
 
 DIM_AUTO, DIM_CHANNEL, DIM_PIXEL = -1, 0, 1
 GROUPING_GRID, GROUPING_CHANNEL, GROUPING_PIXEL = 0, 1, 2
+ACT_NONE, ACT_SILU = 0, 1
 
 
 def lib():
@@ -104,6 +105,16 @@ def lib():
         L.dgq_xattn_kv_workspace_bytes.restype = sz
         L.dgq_xattn_kv.argtypes = [vp, i32, vp, i64, i64, i64, i32, i64, i32, vp, i32, i32, i32, i32, vp, i32, vp, vp, vp, sz,
                                    vp]
+        f32 = C.c_float
+        L.dgq_groupnorm_workspace_bytes.argtypes = [i32, i64, i32, i32, i32, i32]
+        L.dgq_groupnorm_workspace_bytes.restype = sz
+        L.dgq_groupnorm.argtypes = [vp, i32, i64, i64, vp, i32, i64, i32, i32, vp, vp, f32, vp, i64, vp, i64, vp, i64, i32, vp,
+                                    i32, vp, sz, vp]
+        L.dgq_w4_bytes.argtypes = [i32, i32, i32]
+        L.dgq_w4_bytes.restype = sz
+        L.dgq_w4_pack.argtypes = [vp, i32, i64, i32, i32, i32, vp, vp]
+        L.dgq_w4_unpack.argtypes = [vp, i32, i32, i32, i32, vp, vp]
+        L.dgq_w4_matvec.argtypes = [vp, i32, i64, i32, vp, i32, i32, i32, vp, i32, vp, i32, vp]
         L.dgq_last_error.restype = C.c_char_p
         L.dgq_version.restype = C.c_int
         _lib = L
@@ -526,3 +537,64 @@ def dgq_xattn_kv(q, cache: KVCache, table, lengths, q_offsets=None, out=None, wo
     out, contiguous, of q's shape and type; packed rows of no request keep what it held (anything, if it is not passed)."""
     return (_hot or _load_hot()).xattn_kv(q, cache.data, cache.n_blocks, cache.block_size, cache.heads, cache.d, table,
                                           lengths, q_offsets, out, workspace, stream)
+
+
+def _dtype_code(dtype):
+    import torch
+    return {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}.get(dtype, -1)
+
+
+def dgq_groupnorm_workspace_bytes(B, N, packed, C, G, dtype) -> int:
+    """N: rows of an image, or of all images (packed); dtype: x's torch type."""
+    return int(lib().dgq_groupnorm_workspace_bytes(B, N, int(bool(packed)), C, G, _dtype_code(dtype)))
+
+
+def dgq_groupnorm(x, num_groups: int, weight=None, bias=None, eps: float = 1e-5, act: int = ACT_NONE, add=None, scale=None,
+                  shift=None, offsets=None, dtype=None, out=None, workspace=None, stream=None):
+    """Group norm of x [B, N, C], or of packed x [rows, C] with offsets int32 [B + 1], over each image's rows and the C /
+    num_groups channels of a group: act((norm(x + add) * weight + bias) * (1 + scale) + shift).  x: fp32,
+    fp16 or bf16, channels contiguous; weight, bias fp32 [C]; add, scale, shift fp32 [B, C], columns of a wider tensor if they
+    are.  Returns out, contiguous, of x's shape and of `dtype` (x's type, or float32); it may be x.  Packed rows of no image
+    keep what it held."""
+    return (_hot or _load_hot()).groupnorm(x, num_groups, weight, bias, eps, act, add, scale, shift, offsets, dtype, out,
+                                           workspace, stream)
+
+
+@dataclass
+class W4Weight:
+    """A layer's weights in 4 bits with a scale and a zero for every `group` inputs of an output, in the uint8 device tensor
+    `data` of dgq_w4_bytes() bytes (layout in include/dgq.h)."""
+    data: object
+    out_channels: int
+    in_channels: int
+    group: int
+
+    @classmethod
+    def empty(cls, out_channels: int, in_channels: int, group: int, device="cuda"):
+        import torch
+        nbytes = dgq_w4_bytes(out_channels, in_channels, group)
+        if nbytes == 0:
+            raise ValueError("no such weights: group is 32, 64 or 128, out_channels up to 2^24, in_channels up to 2^20")
+        return cls(torch.empty(nbytes, dtype=torch.uint8, device=device), out_channels, in_channels, group)
+
+
+def dgq_w4_bytes(out_channels: int, in_channels: int, group: int) -> int:
+    return int(lib().dgq_w4_bytes(out_channels, in_channels, group))
+
+
+def dgq_w4_pack(weight: W4Weight, w, stream=None) -> W4Weight:
+    """w [out_channels, in_channels] (fp32, fp16 or bf16, inputs contiguous) into weight.data.  Returns weight."""
+    (_hot or _load_hot()).w4_pack(w, weight.data, weight.out_channels, weight.in_channels, weight.group, stream)
+    return weight
+
+
+def dgq_w4_unpack(weight: W4Weight, dtype=None, out=None, stream=None):
+    """The values that the weights stand for, [out_channels, in_channels] of `dtype` (fp32 by default)."""
+    return (_hot or _load_hot()).w4_unpack(weight.data, weight.out_channels, weight.in_channels, weight.group, dtype, out, stream)
+
+
+def dgq_w4_matvec(x, weight: W4Weight, bias=None, act: int = ACT_NONE, dtype=None, out=None, stream=None):
+    """act(x W^T + bias) for the few rows of x [rows, in_channels] (fp32, fp16 or bf16, inputs contiguous): [rows,
+    out_channels] of `dtype` (x's type, or float32).  bias: fp32 [out_channels]."""
+    return (_hot or _load_hot()).w4_matvec(x, weight.data, weight.out_channels, weight.in_channels, weight.group, bias, act, dtype,
+                                           out, stream)

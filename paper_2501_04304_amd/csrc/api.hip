@@ -1408,3 +1408,122 @@ int dgq_xattn_kv(const void *q, int32_t dtype, const int32_t *q_offsets, int64_t
 }
 
 }  // extern "C"
+
+// ---- group norm, and weights in 4 bits ------------------------------------------------------------
+namespace {
+
+bool act_ok(int32_t a) { return a == DGQ_ACT_NONE || a == DGQ_ACT_SILU; }
+// an output's type: the input's, or fp32
+bool out_dtype_ok(int32_t out, int32_t in) { return out == in || out == DGQ_F32; }
+bool aligned_to(const void *p, int32_t dtype) { return (reinterpret_cast<uintptr_t>(p) & (dtype == DGQ_F32 ? 3u : 1u)) == 0; }
+
+constexpr int32_t kMaxChannels = 1 << 20, kMaxOutputs = 1 << 24;
+
+// Sizes of a group norm's call; an error names it.
+int norm_sizes(const char *who, int32_t B, int64_t N, bool packed, int32_t C, int32_t G, int32_t dtype) {
+    const std::string name(who);
+    if (!kv_dtype_ok(dtype)) return fail(DGQ_EINVAL, name + ": bad dtype");
+    if (B < 1 || N < 0 || C < 1 || G < 1) return fail(DGQ_EINVAL, name + ": empty tensor");
+    if (C % G) return fail(DGQ_EUNSUPPORTED, name + ": C must be a multiple of G");
+    if (B > 65535 || C > kMaxChannels) return fail(DGQ_EUNSUPPORTED, name + ": B above 65535 or C above 2^20");
+    if (N > INT32_MAX || (!packed && N * B > INT32_MAX)) return fail(DGQ_EUNSUPPORTED, name + ": more than 2^31 - 1 rows");
+    return DGQ_OK;
+}
+
+bool w4_sizes_ok(int32_t O, int32_t C, int32_t group) {
+    return O >= 1 && O <= kMaxOutputs && C >= 1 && C <= kMaxChannels && (group == 32 || group == 64 || group == 128);
+}
+int w4_of(const char *who, const void *data, int32_t O, int32_t C, int32_t group, W4 *out) {
+    const std::string name(who);
+    if (!data) return fail(DGQ_EINVAL, name + ": null pointer");
+    if (O < 1 || C < 1) return fail(DGQ_EINVAL, name + ": empty weights");
+    if (!w4_sizes_ok(O, C, group)) return fail(DGQ_EUNSUPPORTED, name + ": needs groups of 32, 64 or 128, O up to 2^24, C up to 2^20");
+    if (!aligned16(data)) return fail(DGQ_EALIGN, name + ": data not 16-byte aligned");
+    *out = {static_cast<uint8_t *>(const_cast<void *>(data)), O, C, group, (O + 15) / 16, (C + 127) / 128};
+    return DGQ_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t dgq_groupnorm_workspace_bytes(int32_t B, int64_t N, int32_t packed, int32_t C, int32_t G, int32_t dtype) {
+    if (N < 1 || norm_sizes("dgq_groupnorm_workspace_bytes", B, N, packed != 0, C, G, dtype)) return 0;
+    NormCall n{};
+    static const int32_t some = 0;
+    n.dtype = dtype, n.offsets = packed ? &some : nullptr, n.B = B, n.N = N, n.C = C, n.G = G;
+    return groupnorm_workspace_bytes(n);
+}
+
+int dgq_groupnorm(const void *x, int32_t dtype, int64_t x_batch_stride, int64_t x_row_stride, const int32_t *offsets,
+                  int32_t B, int64_t N, int32_t C, int32_t G, const float *weight, const float *bias, float eps,
+                  const float *add, int64_t add_stride, const float *scale, int64_t scale_stride, const float *shift,
+                  int64_t shift_stride, int32_t act, void *out, int32_t out_dtype, void *workspace,
+                  size_t workspace_bytes, void *stream) {
+    if (const int rc = norm_sizes("dgq_groupnorm", B, N, offsets != nullptr, C, G, dtype)) return rc;
+    if (!out_dtype_ok(out_dtype, dtype)) return fail(DGQ_EINVAL, "dgq_groupnorm: out_dtype must be x's or fp32");
+    if (!act_ok(act)) return fail(DGQ_EINVAL, "dgq_groupnorm: bad act");
+    if (!(eps >= 0.f && eps <= std::numeric_limits<float>::max())) return fail(DGQ_EINVAL, "dgq_groupnorm: eps must be a number from 0 on");
+    if (N == 0) return DGQ_OK;
+    if (!x || !out) return fail(DGQ_EINVAL, "dgq_groupnorm: null pointer");
+    if (x_batch_stride < 0 || x_row_stride < 0 || add_stride < 0 || scale_stride < 0 || shift_stride < 0)
+        return fail(DGQ_EINVAL, "dgq_groupnorm: strides below 0");
+    if (!aligned_to(x, dtype) || !aligned_to(out, out_dtype)) return fail(DGQ_EALIGN, "dgq_groupnorm: tensor not aligned to its elements");
+    for (const void *p : {(const void *)offsets, (const void *)weight, (const void *)bias, (const void *)add, (const void *)scale, (const void *)shift})
+        if (!aligned_to(p, DGQ_F32)) return fail(DGQ_EALIGN, "dgq_groupnorm: tensor not aligned to its elements");
+    const NormCall n{x, dtype, x_batch_stride, x_row_stride, offsets, B, N, C, G, weight, bias, eps,
+                     {add, scale, shift, add_stride, scale_stride, shift_stride}, act, out, out_dtype};
+    const size_t need = groupnorm_workspace_bytes(n);
+    if (need && (!workspace || workspace_bytes < need || !aligned16(workspace)))
+        return fail(DGQ_EWORKSPACE, "dgq_groupnorm: workspace missing, too small or misaligned");
+    DGQ_HIP(launch_groupnorm(n, workspace, static_cast<hipStream_t>(stream)));
+    return DGQ_OK;
+}
+
+size_t dgq_w4_bytes(int32_t O, int32_t C, int32_t group) {
+    if (!w4_sizes_ok(O, C, group)) return 0;
+    return (size_t)((O + 15) / 16) * ((C + 127) / 128) * (1024 + 64 * (128 / group));
+}
+
+int dgq_w4_pack(const void *w, int32_t dtype, int64_t w_row_stride, int32_t O, int32_t C, int32_t group, void *data,
+                void *stream) {
+    W4 m;
+    if (const int rc = w4_of("dgq_w4_pack", data, O, C, group, &m)) return rc;
+    if (!kv_dtype_ok(dtype)) return fail(DGQ_EINVAL, "dgq_w4_pack: bad dtype");
+    if (!w) return fail(DGQ_EINVAL, "dgq_w4_pack: null pointer");
+    if (w_row_stride < 0) return fail(DGQ_EINVAL, "dgq_w4_pack: stride below 0");
+    if (m.units() > 4 * kMaxGroups) return fail(DGQ_EUNSUPPORTED, "dgq_w4_pack: more than 2^26 units of 16 x 128 weights");
+    if (!aligned_to(w, dtype)) return fail(DGQ_EALIGN, "dgq_w4_pack: tensor not aligned to its elements");
+    DGQ_HIP(launch_w4_pack(w, dtype, w_row_stride, m, static_cast<hipStream_t>(stream)));
+    return DGQ_OK;
+}
+
+int dgq_w4_unpack(const void *data, int32_t O, int32_t C, int32_t group, int32_t dtype, void *w, void *stream) {
+    W4 m;
+    if (const int rc = w4_of("dgq_w4_unpack", data, O, C, group, &m)) return rc;
+    if (!kv_dtype_ok(dtype)) return fail(DGQ_EINVAL, "dgq_w4_unpack: bad dtype");
+    if (!w) return fail(DGQ_EINVAL, "dgq_w4_unpack: null pointer");
+    if (m.units() > 4 * kMaxGroups) return fail(DGQ_EUNSUPPORTED, "dgq_w4_unpack: more than 2^26 units of 16 x 128 weights");
+    if (!aligned_to(w, dtype)) return fail(DGQ_EALIGN, "dgq_w4_unpack: tensor not aligned to its elements");
+    DGQ_HIP(launch_w4_unpack(m, dtype, w, static_cast<hipStream_t>(stream)));
+    return DGQ_OK;
+}
+
+int dgq_w4_matvec(const void *x, int32_t dtype, int64_t x_row_stride, int32_t M, const void *data, int32_t O, int32_t C,
+                  int32_t group, const float *bias, int32_t act, void *y, int32_t out_dtype, void *stream) {
+    W4 m;
+    if (const int rc = w4_of("dgq_w4_matvec", data, O, C, group, &m)) return rc;
+    if (!kv_dtype_ok(dtype)) return fail(DGQ_EINVAL, "dgq_w4_matvec: bad dtype");
+    if (!out_dtype_ok(out_dtype, dtype)) return fail(DGQ_EINVAL, "dgq_w4_matvec: out_dtype must be x's or fp32");
+    if (!act_ok(act)) return fail(DGQ_EINVAL, "dgq_w4_matvec: bad act");
+    if (M < 0 || x_row_stride < 0) return fail(DGQ_EINVAL, "dgq_w4_matvec: rows or stride below 0");
+    if (M == 0) return DGQ_OK;
+    if (!x || !y) return fail(DGQ_EINVAL, "dgq_w4_matvec: null pointer");
+    if (M > kMaxChannels) return fail(DGQ_EUNSUPPORTED, "dgq_w4_matvec: more than 2^20 rows");
+    if (!aligned_to(x, dtype) || !aligned_to(y, out_dtype) || !aligned_to(bias, DGQ_F32))
+        return fail(DGQ_EALIGN, "dgq_w4_matvec: tensor not aligned to its elements");
+    DGQ_HIP(launch_w4_matvec({x, dtype, x_row_stride, M, bias, act, y, out_dtype}, m, static_cast<hipStream_t>(stream)));
+    return DGQ_OK;
+}
+
+}  // extern "C"

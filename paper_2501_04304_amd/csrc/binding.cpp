@@ -721,6 +721,158 @@ PyObject *xattn_kv(Args a) {
     return one(a[9], out);
 }
 
+// ---- group norm, and weights in 4 bits ----
+
+// The type named by a dtype argument, `otherwise` where none is given.
+at::ScalarType dtype_of(PyObject *o, at::ScalarType otherwise) {
+    if (!given(o)) return otherwise;
+    if (!THPDtype_Check(o)) raise(PyExc_TypeError, "dtype must be a torch.dtype");
+    const at::ScalarType t = reinterpret_cast<THPDtype *>(o)->scalar_type;
+    if (kv_dtype(t) < 0) raise_value("dtype must be float32, float16 or bfloat16");
+    return t;
+}
+
+// A contiguous output of `type`: the caller's, whose type stands for a dtype that is not given, or a new one.
+at::Tensor output(PyObject *o, PyObject *dtype, at::ScalarType in, at::IntArrayRef sizes, const at::Tensor &like, const Place &place,
+                  const char *name) {
+    const bool mine = given(o);
+    at::ScalarType type = in;
+    if (mine && THPVariable_Check(o)) type = THPVariable_Unpack(o).scalar_type();
+    type = dtype_of(dtype, type);
+    if (!mine) return empty(sizes, type, like);
+    const at::Tensor t = floats(o, name, (int64_t)sizes.size());
+    place.same(t, name);
+    if (t.sizes() != sizes || t.scalar_type() != type || !t.is_contiguous()) {
+        PyErr_Format(PyExc_ValueError, "%s has the wrong shape or type, or is not contiguous", name);
+        throw Raised();
+    }
+    return t;
+}
+
+// fp32 [n], or null
+const float *vector_of(PyObject *o, const char *name, int64_t n, const Place &place) {
+    if (!given(o)) return nullptr;
+    const at::Tensor &t = tensor(o, at::kFloat, name);
+    if (!shape_is(t, {n})) {
+        PyErr_Format(PyExc_ValueError, "%s has the wrong shape", name);
+        throw Raised();
+    }
+    place.same(t, name);
+    return pointer<float>(t);
+}
+
+// fp32 [B, C] with rows of any stride, or null
+struct Rows {
+    const float *data = nullptr;
+    int64_t stride = 0;
+    Rows(PyObject *o, const char *name, int64_t B, int64_t C, const Place &place) {
+        if (!given(o)) return;
+        const at::Tensor &t = floats(o, name, 2);
+        if (t.scalar_type() != at::kFloat) {
+            PyErr_Format(PyExc_TypeError, "%s must be of dtype torch.float32", name);
+            throw Raised();
+        }
+        if (!shape_is(t, {B, C})) {
+            PyErr_Format(PyExc_ValueError, "%s must be [images, channels]", name);
+            throw Raised();
+        }
+        place.same(t, name);
+        data = pointer<float>(t), stride = step(t, 0);
+    }
+};
+
+// (x, num_groups, weight, bias, eps, act, add, scale, shift, offsets, dtype, out, workspace, stream)
+PyObject *groupnorm(Args a) {
+    const bool packed = given(a[9]);
+    const at::Tensor &x = floats(a[0], "x", packed ? 2 : 3);
+    const Place place(a[13], x);
+    const int32_t *op = nullptr;
+    int64_t B = x.size(0);
+    if (packed) {
+        const at::Tensor &offsets = tensor(a[9], at::kInt, "offsets");
+        if (offsets.dim() != 1 || offsets.numel() < 1) raise_value("offsets must be [images + 1]");
+        place.same(offsets, "offsets");
+        op = pointer<int32_t>(offsets), B = offsets.numel() - 1;
+    }
+    const int64_t N = x.size(packed ? 0 : 1), channels = x.size(-1);
+    if (B > INT32_MAX || channels > INT32_MAX) raise_value("x is too large");
+    const int32_t C = (int32_t)channels, G = integer32(a[1]), act = integer32(a[5]), type = kv_dtype(x.scalar_type());
+    const double eps = PyFloat_AsDouble(a[4]);
+    if (eps == -1 && PyErr_Occurred()) throw Raised();
+    const float *wp = vector_of(a[2], "weight", C, place), *bp = vector_of(a[3], "bias", C, place);
+    const Rows add(a[6], "add", B, C, place), scale(a[7], "scale", B, C, place), shift(a[8], "shift", B, C, place);
+    const at::Tensor out = output(a[11], a[10], x.scalar_type(), x.sizes(), x, place, "out");
+    at::Tensor ws;
+    if (given(a[12])) {
+        ws = tensor(a[12], at::kByte, "workspace");
+        place.same(ws, "workspace");
+    } else if (const size_t need = dgq_groupnorm_workspace_bytes((int32_t)B, N, packed, C, G, type)) {
+        ws = empty({(int64_t)need}, at::kByte, x);
+    }
+    void *sp = ws.defined() ? ws.data_ptr() : nullptr, *yp = out.data_ptr();
+    const size_t sb = ws.defined() ? (size_t)ws.numel() : 0;
+    const void *xp = x.data_ptr();
+    enqueue([&] {
+        return dgq_groupnorm(xp, type, packed ? 0 : step(x, 0), step(x, packed ? 0 : 1), op, (int32_t)B, N, C, G, wp, bp, (float)eps,
+                             add.data, add.stride, scale.data, scale.stride, shift.data, shift.stride, act, yp,
+                             kv_dtype(out.scalar_type()), sp, sb, place.stream());
+    });
+    return one(a[11], out);
+}
+
+// (data, out_channels, in_channels, group) from a[0]
+struct W4In {
+    const at::Tensor &data;
+    int32_t O, C, group;
+    explicit W4In(Args a) : data(tensor(a[0], at::kByte, "weight.data")), O(integer32(a[1])), C(integer32(a[2])), group(integer32(a[3])) {
+        holds(data, (int64_t)dgq_w4_bytes(O, C, group), "weight.data");
+    }
+};
+
+// (w, data, out_channels, in_channels, group, stream)
+PyObject *w4_pack(Args a) {
+    const W4In m(a + 1);
+    const Place place(a[5], m.data);
+    const at::Tensor &w = floats(a[0], "w", 2);
+    if (!shape_is(w, {m.O, m.C})) raise_value("w must be [out_channels, in_channels] of the weight");
+    place.same(w, "w");
+    const void *wp = w.data_ptr();
+    void *dp = m.data.data_ptr();
+    enqueue([&] { return dgq_w4_pack(wp, kv_dtype(w.scalar_type()), step(w, 0), m.O, m.C, m.group, dp, place.stream()); });
+    Py_RETURN_NONE;
+}
+
+// (data, out_channels, in_channels, group, dtype, out, stream)
+PyObject *w4_unpack(Args a) {
+    const W4In m(a);
+    const Place place(a[6], m.data);
+    const at::Tensor out = output(a[5], a[4], at::kFloat, {m.O, m.C}, m.data, place, "out");
+    const void *dp = m.data.data_ptr();
+    void *wp = out.data_ptr();
+    enqueue([&] { return dgq_w4_unpack(dp, m.O, m.C, m.group, kv_dtype(out.scalar_type()), wp, place.stream()); });
+    return one(a[5], out);
+}
+
+// (x, data, out_channels, in_channels, group, bias, act, dtype, out, stream)
+PyObject *w4_matvec(Args a) {
+    const W4In m(a + 1);
+    const Place place(a[9], m.data);
+    const at::Tensor &x = floats(a[0], "x", 2);
+    if (x.size(1) != m.C) raise_value("x must be [rows, in_channels] of the weight");
+    if (x.size(0) > INT32_MAX) raise_value("x is too large");
+    place.same(x, "x");
+    const int32_t M = (int32_t)x.size(0), act = integer32(a[6]);
+    const float *bp = vector_of(a[5], "bias", m.O, place);
+    const at::Tensor out = output(a[8], a[7], x.scalar_type(), {M, m.O}, x, place, "out");
+    const void *xp = x.data_ptr(), *dp = m.data.data_ptr();
+    void *yp = out.data_ptr();
+    enqueue([&] {
+        return dgq_w4_matvec(xp, kv_dtype(x.scalar_type()), step(x, 0), M, dp, m.O, m.C, m.group, bp, act, yp,
+                             kv_dtype(out.scalar_type()), place.stream());
+    });
+    return one(a[8], out);
+}
+
 template <PyObject *(*F)(Args), int NARGS>
 PyObject *call(PyObject *, Args a, Py_ssize_t n) {
     if (n != NARGS) {
@@ -759,6 +911,10 @@ PyMethodDef kMethods[] = {
     DGQ_METHOD(kv_store, 9),
     DGQ_METHOD(kv_load, 12),
     DGQ_METHOD(xattn_kv, 12),
+    DGQ_METHOD(groupnorm, 14),
+    DGQ_METHOD(w4_pack, 6),
+    DGQ_METHOD(w4_unpack, 7),
+    DGQ_METHOD(w4_matvec, 10),
     {"set_error_class", set_error_class, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };

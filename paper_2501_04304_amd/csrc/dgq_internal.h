@@ -260,6 +260,51 @@ int32_t xattn_kv_rows(int32_t B, int64_t rows, bool packed, int32_t Hq, int32_t 
 hipError_t launch_xattn_kv(const KvQueries &q, const KvCache &c, const int32_t *table, int32_t width,
                            const int32_t *lengths, void *out, void *workspace, hipStream_t st);
 
+// Group norm (k7_groupnorm.hip).  Strides in elements.
+struct NormTerms {  // fp32 [B, C] with rows of their own stride, or null
+    const float *add, *scale, *shift;
+    int64_t add_row, scale_row, shift_row;
+};
+struct NormCall {
+    const void *x;
+    int32_t dtype;
+    int64_t x_batch, x_row;
+    const int32_t *offsets;  // null: image b has rows [b N, b N + N); else N is the number of all rows
+    int32_t B;
+    int64_t N;
+    int32_t C, G;
+    const float *weight, *bias;
+    float eps;
+    NormTerms terms;
+    int32_t act;
+    void *out;
+    int32_t out_dtype;
+    int64_t rows() const { return offsets ? N : B * N; }
+};
+size_t groupnorm_workspace_bytes(const NormCall &n);
+hipError_t launch_groupnorm(const NormCall &n, void *workspace, hipStream_t st);
+
+// ---- weights in 4 bits (layout in include/dgq.h, dgq_w4_bytes; k8_w4.hip) ----------------------------
+struct W4 {
+    uint8_t *codes;  // [R, T, 1024]; behind them the groups' words [R, T, 16, 128 / group]
+    int32_t O, C, group, R, T;
+    __host__ __device__ int64_t units() const { return (int64_t)R * T; }
+    __device__ uint32_t *words() const { return reinterpret_cast<uint32_t *>(codes + units() * 1024); }
+};
+struct W4Product {
+    const void *x;
+    int32_t dtype;
+    int64_t x_row;  // elements
+    int32_t M;
+    const float *bias;
+    int32_t act;
+    void *y;
+    int32_t out_dtype;
+};
+hipError_t launch_w4_pack(const void *w, int32_t dtype, int64_t w_row, const W4 &m, hipStream_t st);
+hipError_t launch_w4_unpack(const W4 &m, int32_t dtype, void *w, hipStream_t st);
+hipError_t launch_w4_matvec(const W4Product &p, const W4 &m, hipStream_t st);
+
 size_t xattn_workspace_bytes(int32_t B, int32_t N, int32_t H, int32_t d, int32_t nk);
 // the least the attention can work with (the row statistics alone; its maximum then goes
 // through atomics on scale[] and one more launch that clears it)

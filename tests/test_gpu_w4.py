@@ -1,0 +1,335 @@
+"""dgq_w4_pack, dgq_w4_unpack and dgq_w4_matvec against their definitions (w4_reference)."""
+import numpy as np
+import pytest
+
+import w4_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+TYPES = ["fp32", "fp16", "bf16"]
+GROUPS = [32, 64, 128]
+
+
+@pytest.fixture(scope="module")
+def dgq():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    import paper_2501_04304_amd as m
+    m.lib()
+    return m
+
+
+def _type(name):
+    import torch
+    return {"fp32": torch.float32, "fp16": torch.float16, "bf16": torch.bfloat16}[name]
+
+
+def _up(a, dtype="fp32"):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a)).to(_type(dtype)).cuda()
+
+
+def _layer(rng, O, C, dtype="fp32"):
+    w = rng.standard_normal((O, C)) * (0.5 + rng.random((O, 1))) * (0.5 + rng.random((1, C))) / np.sqrt(C)
+    t = _up(w.astype(np.float32), dtype)
+    return t, t.float().cpu().numpy()
+
+
+def _packed(dgq, codes, words, group, O, C):
+    import torch
+    w = dgq.W4Weight.empty(O, C, group)
+    data = ref.lay_out(codes, words, group)
+    assert data.nbytes == w.data.numel() == dgq.dgq_w4_bytes(O, C, group)
+    w.data.copy_(torch.from_numpy(data))
+    return w
+
+
+SIZES = [(1, 1), (16, 128), (15, 127), (17, 129), (1, 1000), (1003, 1), (40, 256), (320, 96), (129, 515)]
+
+
+def _bytes_equal(dgq, w, wn, group):
+    O, C = wn.shape
+    codes, words = ref.quantize(wn, group)
+    assert np.array_equal(w.data.cpu().numpy(), ref.lay_out(codes, words, group))
+    return codes, words
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("group", GROUPS)
+@pytest.mark.parametrize("O,C", SIZES)
+def test_pack_and_unpack(dgq, O, C, group, dtype):
+    import torch
+    rng = np.random.default_rng(O * 7 + C)
+    t, wn = _layer(rng, O, C, dtype)
+    wn[0, 0] = 0.0
+    if O > 3 and C > 40:
+        wn[1] = 0                      # a row of zeros
+        wn[2] = np.abs(wn[2])          # of one sign
+        wn[3] = -np.abs(wn[3])
+        wn[O - 1, :32] = wn[O - 1, 0]  # equal weights
+    t = _up(wn, dtype)
+    w = dgq.W4Weight.empty(O, C, group)
+    w.data.fill_(0xEE)
+    assert dgq.dgq_w4_pack(w, t) is w
+    codes, words = _bytes_equal(dgq, w, wn, group)
+    v = ref.values(codes, words, group, O, C)
+    got = dgq.dgq_w4_unpack(w)
+    assert got.dtype == torch.float32 and np.array_equal(got.cpu().numpy(), v)  # 20 bits times 4: nothing is rounded
+    for to in TYPES:
+        got = dgq.dgq_w4_unpack(w, dtype=_type(to))
+        assert torch.equal(got.cpu(), torch.from_numpy(v.astype(np.float32)).to(_type(to)))
+
+
+@pytest.mark.parametrize("group", GROUPS)
+def test_pack_of_strided_weights(dgq, group):
+    """Columns of a wider layer from an odd place on, and rows that are read several times."""
+    import torch
+    rng = np.random.default_rng(3)
+    for dtype in TYPES:
+        wide, n = _layer(rng, 50, 333, dtype)
+        w = dgq.W4Weight.empty(50, 200, group)
+        dgq.dgq_w4_pack(w, wide[:, 7:207])
+        _bytes_equal(dgq, w, n[:, 7:207], group)
+        dgq.dgq_w4_pack(w, torch.as_strided(wide, (50, 200), (0, 1)))
+        _bytes_equal(dgq, w, np.stack([n.reshape(-1)[:200]] * 50), group)
+
+
+@pytest.mark.parametrize("group", GROUPS)
+def test_pack_at_the_ends_of_the_range(dgq, group):
+    """Scales below 2^-96, at it, at fp32's largest spread; NaN and infinity in one group leave the others alone."""
+    rng = np.random.default_rng(4)
+    w = rng.standard_normal((16, 512)).astype(np.float32)
+    w[0] *= np.float32(2.0 ** -100)
+    w[1] *= np.float32(2.0 ** -130)
+    w[2, :300] *= np.float32(2.0 ** -93)
+    w[3] *= np.float32(2.0 ** 124)
+    w[4, ::2], w[4, 1::2] = np.float32(3.4e38), np.float32(-3.4e38)  # the spread is past fp32
+    w[5, 130] = np.nan
+    w[6, 511] = np.inf
+    w[7, 0] = -np.inf
+    w[8, :64] = np.nan
+    w[9] = np.float32(2.0 ** -149)
+    t = _up(w)
+    m = dgq.W4Weight.empty(16, 512, group)
+    dgq.dgq_w4_pack(m, t)
+    codes, words = _bytes_equal(dgq, m, w, group)
+    assert (words == ref.NAN_WORD).sum() == 512 // group * 1 + 3 + (2 if group == 32 else 1)
+    with np.errstate(invalid="ignore"):
+        want = ref.values(codes, words, group, 16, 512)
+    assert np.array_equal(dgq.dgq_w4_unpack(m).cpu().numpy(), want, equal_nan=True)
+
+
+# ---- products ----
+
+ROWS = [1, 2, 5, 16, 17, 32, 33, 64, 100]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("group", GROUPS)
+@pytest.mark.parametrize("O,C", SIZES + [(64, 1280), (1030, 300), (33, 4000)])
+def test_products_of_small_integers(dgq, O, C, group, dtype):
+    """Integers and scales of powers of two: every sum is a number of fp32, so every bit has to be right, and so is each place."""
+    rng = np.random.default_rng(O + 3 * C)
+    R, T = -(-O // 16), -(-C // 128)
+    codes = rng.integers(0, 16, (16 * R, 128 * T))
+    words = np.float32(2.0) ** rng.integers(-1, 2, (16 * R, 128 * T // group))
+    words = words.astype(np.float32).view(np.uint32) | rng.integers(0, 16, words.shape).astype(np.uint32)
+    w = _packed(dgq, codes, words, group, O, C)
+    bias = rng.integers(-9, 9, O).astype(np.float32)
+    for M in ROWS:
+        x = rng.integers(-4, 5, (M, C)).astype(np.float32)
+        want = x.astype(np.float64) @ ref.values(codes, words, group, O, C).T
+        assert np.abs(want).max() < 2 ** 20
+        got = dgq.dgq_w4_matvec(_up(x, dtype), w, dtype=_type("fp32"))
+        assert got.shape == (M, O) and np.array_equal(got.cpu().numpy(), want), M
+        got = dgq.dgq_w4_matvec(_up(x, dtype), w, _up(bias), dtype=_type("fp32"))
+        assert np.array_equal(got.cpu().numpy(), want + bias), M
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("group", GROUPS)
+@pytest.mark.parametrize("M,C,O", [(1, 320, 1280), (2, 2051, 103), (16, 1280, 64), (40, 700, 48), (3, 5000, 20), (70, 130, 33)])
+def test_products(dgq, M, C, O, group, dtype):
+    rng = np.random.default_rng(M + C)
+    _, wn = _layer(rng, O, C)
+    codes, words = ref.quantize(wn, group)
+    w = _packed(dgq, codes, words, group, O, C)
+    x = rng.standard_normal((M, C)) * np.where(rng.random(C) < 0.02, 8, 1) + 0.5
+    t = _up(x.astype(np.float32), dtype)
+    x = t.float().cpu().numpy()
+    bias = 0.1 * rng.standard_normal(O).astype(np.float32)
+    for act in (False, True):
+        for to in {dtype, "fp32"}:
+            got = dgq.dgq_w4_matvec(t, w, _up(bias), act=int(act), dtype=_type(to)).float().cpu().numpy().astype(np.float64)
+            want, tol = ref.matvec(x, codes, words, group, O, bias, act, to, pieces=2 if dtype == "fp32" else 1)
+            assert (np.abs(got - want) <= tol).all(), (act, to, np.abs(got - want).max(), tol.min())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_single_inputs_at_any_size(dgq, dtype):
+    """One input a row, one weight of one an output: the product is x itself, whatever its size (fp32: to 23 bits)."""
+    rng = np.random.default_rng(6)
+    O, C, group = 32, 32, 32
+    codes = np.full((32, 128), 3)
+    codes[np.arange(32), np.arange(32)] = 4
+    words = np.full((32, 4), np.float32(1).view(np.uint32) | np.uint32(3))
+    w = _packed(dgq, codes, words, group, O, C)
+    ends = (-14, 15) if dtype == "fp16" else (-120, 127)
+    x = np.zeros((40, C), np.float32)
+    x[np.arange(40), rng.integers(0, 32, 40)] = ((1 + rng.random(40)) * 2.0 ** rng.integers(*ends, 40)).astype(np.float32)
+    t = _up(x, dtype)
+    x = t.float().cpu().numpy()
+    got = dgq.dgq_w4_matvec(t, w, dtype=_type("fp32")).cpu().numpy()
+    assert (np.abs(got - x) <= np.abs(x) * (2.0 ** -23 if dtype == "fp32" else 0)).all()
+
+
+def test_rows_of_far_exponents(dgq):
+    """Elements 2^20 and 2^60 apart in one unit and in different ones."""
+    rng = np.random.default_rng(16)
+    M, O, C, group = 20, 48, 600, 32
+    codes, words = ref.quantize(_layer(rng, O, C)[1], group)
+    w = _packed(dgq, codes, words, group, O, C)
+    for spread in (20, 60, 110):
+        x = (rng.standard_normal((M, C)) * 2.0 ** rng.integers(-spread, 5, (M, C))).astype(np.float32)
+        x[1, :256] = 0
+        x[2] = 0
+        got = dgq.dgq_w4_matvec(_up(x), w).cpu().numpy()
+        want, tol = ref.matvec(x, codes, words, group, O, pieces=2)
+        assert (np.abs(got - want) <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_with_what_is_not_finite(dgq, dtype):
+    rng = np.random.default_rng(7)
+    O, C, group = 40, 300, 64
+    codes, words = ref.quantize(_layer(rng, O, C)[1], group)
+    words[5, 2] = ref.NAN_WORD
+    w = _packed(dgq, codes, words, group, O, C)
+    x = rng.standard_normal((20, C)).astype(np.float32)
+    want = dgq.dgq_w4_matvec(_up(x, dtype), w).float().cpu().numpy()
+    assert np.isnan(want[:, 5]).all() and not np.isnan(np.delete(want, 5, 1)).any()
+    x[3, 299], x[17, 0] = np.nan, np.inf
+    got = dgq.dgq_w4_matvec(_up(x, dtype), w).float().cpu().numpy()
+    assert not np.isfinite(got[3]).any() and not np.isfinite(got[17]).any()
+    rest = [i for i in range(20) if i not in (3, 17)]
+    assert np.array_equal(got[rest], want[rest], equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_strided_rows_and_buffers(dgq, dtype):
+    import torch
+    rng = np.random.default_rng(8)
+    O, C, group = 50, 200, 32
+    codes, words = ref.quantize(_layer(rng, O, C)[1], group)
+    w = _packed(dgq, codes, words, group, O, C)
+    wide = _up(rng.standard_normal((20, 333)).astype(np.float32), dtype)
+    x = wide[:, 9:209]
+    want = dgq.dgq_w4_matvec(x.contiguous(), w)
+    assert torch.equal(dgq.dgq_w4_matvec(x, w), want)
+    out = torch.full((22, O), 7.0, dtype=_type(dtype), device="cuda")
+    assert torch.equal(dgq.dgq_w4_matvec(x, w, out=out[1:21]), want)
+    assert torch.equal(out[1:21], want) and (out[0] == 7).all() and (out[21] == 7).all()
+    same = torch.as_strided(wide, (20, C), (0, 1))
+    assert torch.equal(dgq.dgq_w4_matvec(same, w), dgq.dgq_w4_matvec(same.contiguous(), w))
+    flat = torch.zeros(O * 3 + 1, device="cuda")[1:].view(3, O)  # an output at an odd place
+    assert torch.equal(dgq.dgq_w4_matvec(x[:3], w, out=flat), dgq.dgq_w4_matvec(x[:3], w, dtype=torch.float32))
+
+
+def test_rows_of_one_call_and_of_several(dgq):
+    """A row's product does not hang on what other rows hold."""
+    import torch
+    rng = np.random.default_rng(9)
+    O, C, group = 100, 640, 64
+    w = dgq.dgq_w4_pack(dgq.W4Weight.empty(O, C, group), _layer(rng, O, C)[0])
+    x = _up(rng.standard_normal((16, C)).astype(np.float32))
+    y = x.clone()
+    y[1:] = 1000
+    assert torch.equal(dgq.dgq_w4_matvec(x, w)[0], dgq.dgq_w4_matvec(y, w)[0])
+
+
+def test_weights_past_4_gib_of_values(dgq):
+    """Units beyond 2^31 weights: the last outputs of 131072 x 20480."""
+    import torch
+    O, C, group = 131072, 20480, 128
+    w = dgq.W4Weight.empty(O, C, group)
+    w.data.zero_()
+    n = O // 16 * (C // 128) * 1024
+    words = w.data[n:].view(torch.int32)
+    words.fill_(int(np.float32(1).view(np.int32)))      # values are the codes
+    w.data[n - 1024 * 160:n].fill_(0x11)                # ones for the last 16 outputs
+    x = torch.ones((2, C), device="cuda", dtype=torch.bfloat16)
+    y = dgq.dgq_w4_matvec(x, w, dtype=torch.float32)
+    torch.cuda.synchronize()
+    assert (y[:, :-16] == 0).all() and (y[:, -16:] == C).all()
+
+
+def test_captured_and_on_another_stream(dgq):
+    import torch
+    rng = np.random.default_rng(10)
+    O, C, group = 320, 1280, 64
+    t, _ = _layer(rng, O, C)
+    w = dgq.W4Weight.empty(O, C, group)
+    x = _up(rng.standard_normal((4, C)).astype(np.float32))
+    y, back = torch.empty((4, O), device="cuda"), torch.empty((O, C), device="cuda")
+    dgq.dgq_w4_pack(w, t)
+    want, want_back = dgq.dgq_w4_matvec(x, w, act=dgq.ACT_SILU), dgq.dgq_w4_unpack(w)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = dgq.dgq_w4_matvec(x, w, act=dgq.ACT_SILU, stream=side)
+    side.synchronize()
+    assert torch.equal(got, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            dgq.dgq_w4_pack(w, t)
+            dgq.dgq_w4_matvec(x, w, act=dgq.ACT_SILU, out=y)
+            dgq.dgq_w4_unpack(w, out=back)
+    for _ in range(4):
+        w.data.fill_(0), y.zero_(), back.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want) and torch.equal(back, want_back)
+        dgq.dgq_w4_matvec(x, w)
+
+
+def test_empty(dgq):
+    import torch
+    w = dgq.W4Weight.empty(5, 7, 32)
+    w.data.zero_()
+    assert dgq.dgq_w4_matvec(torch.empty((0, 7), device="cuda"), w).shape == (0, 5)
+
+
+def test_refusals(dgq):
+    import torch
+    f = lambda *s, **k: torch.zeros(s, device="cuda", **k)  # noqa: E731
+    with pytest.raises(ValueError, match="no such weights"):
+        dgq.W4Weight.empty(5, 7, 16)
+    w = dgq.W4Weight.empty(40, 70, 32)
+    short = dgq.W4Weight(w.data[:-1], 40, 70, 32)
+    odd = dgq.W4Weight(torch.zeros(w.data.numel() + 1, dtype=torch.uint8, device="cuda")[1:], 40, 70, 32)
+    bad = dgq.W4Weight(w.data, 40, 70, 48)
+    for call, error, text in [
+            (lambda: dgq.dgq_w4_pack(short, f(40, 70)), ValueError, "weight.data has"),
+            (lambda: dgq.dgq_w4_unpack(short), ValueError, "weight.data has"),
+            (lambda: dgq.dgq_w4_matvec(f(2, 70), short), ValueError, "weight.data has"),
+            (lambda: dgq.dgq_w4_pack(odd, f(40, 70)), dgq.DgqError, "16-byte"),
+            (lambda: dgq.dgq_w4_pack(bad, f(40, 70)), dgq.DgqError, "groups of 32"),
+            (lambda: dgq.dgq_w4_unpack(bad), dgq.DgqError, "groups of 32"),
+            (lambda: dgq.dgq_w4_matvec(f(2, 70), bad), dgq.DgqError, "groups of 32"),
+            (lambda: dgq.dgq_w4_pack(w, f(41, 70)), ValueError, "w must be"),
+            (lambda: dgq.dgq_w4_pack(w, f(70, 40).T), TypeError, "w must be"),
+            (lambda: dgq.dgq_w4_pack(w, f(40, 70).double()), TypeError, "w must be"),
+            (lambda: dgq.dgq_w4_pack(w, torch.zeros(40, 70)), TypeError, "w must be"),
+            (lambda: dgq.dgq_w4_unpack(w, dtype=torch.int8), ValueError, "dtype"),
+            (lambda: dgq.dgq_w4_unpack(w, out=f(40, 71)), ValueError, "out"),
+            (lambda: dgq.dgq_w4_matvec(f(2, 71), w), ValueError, "x must be"),
+            (lambda: dgq.dgq_w4_matvec(f(70), w), ValueError, "x must have 2"),
+            (lambda: dgq.dgq_w4_matvec(f(70, 2).T, w), TypeError, "x must be"),
+            (lambda: dgq.dgq_w4_matvec(f(2, 70), w, bias=f(41)), ValueError, "bias"),
+            (lambda: dgq.dgq_w4_matvec(f(2, 70), w, bias=f(40, dtype=torch.float16)), TypeError, "bias"),
+            (lambda: dgq.dgq_w4_matvec(f(2, 70), w, act=3), dgq.DgqError, "act"),
+            (lambda: dgq.dgq_w4_matvec(f(2, 70), w, dtype=torch.bfloat16), dgq.DgqError, "out_dtype"),
+            (lambda: dgq.dgq_w4_matvec(f(2, 70), w, out=f(3, 40)), ValueError, "out")]:
+        with pytest.raises(error, match=text):
+            call()
