@@ -124,11 +124,12 @@ __global__ __launch_bounds__(256) void k_w4_unpack(W4 m, T *__restrict__ w) {
 
 // ---- products --------------------------------------------------------------------------------------------------------
 //   y[m, o] = sum_g s (sum_{k in g} x[m, k] (code - zero))
-// on the matrix cores, 16 rows of x by 16 outputs by 32 inputs, in fp16.  A code becomes 1 + code / 16 by its place below the
-// exponent of 1 (two instructions for a pair), and less 1 + zero / 16 it is (code - zero) / 16, exactly.  Rows of fp16 are what
-// they are; those of bf16 and fp32 are taken a unit (128 inputs) at a time by a power of two that brings its largest to 2^14 .. 2^15,
-// bf16 as one fp16, fp32 as two (x = h + l, each rounded to nearest: off by 2^-23 x at most); what lies 2^29 below the unit's
-// largest loses bits, to 2^-39 of that.  The groups' sums meet in fp32 with their scales and those powers.
+// on the matrix cores, 16 rows of x by 16 outputs by 32 inputs, in fp16.  A nibble below the exponent of 1024 is 1024 + code (at
+// bits 0 .. 3) or 1024 + 16 code (at 4 .. 7), less 1024 + zero or times 1/16 less 64 + zero it is code - zero, exactly: nine
+// instructions for eight codes.  Rows of fp16 are what they are; those of bf16 and fp32 are taken a unit (128 inputs) at a time by
+// a power of two that brings its largest to 2^14 .. 2^15, bf16 as one fp16, fp32 as two (x = h + l, each rounded to nearest: off by
+// 2^-23 x at most); what lies 2^29 below the unit's largest loses bits, to 2^-39 of that.  The groups' sums meet in fp32 with
+// their scales and those powers.
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef float float2v __attribute__((ext_vector_type(2)));
@@ -143,130 +144,251 @@ union Piece {  // a lane's 8 numbers of an operand
 template <class T>
 constexpr int kPieces = sizeof(T) == 4 ? 2 : 1;
 
-// (code - zero) / 16 of a lane's eight codes; less: -(1 + zero / 16), twice
-__device__ Piece expand(uint32_t code, half2v less) {
-    Piece p;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        p.w[i] = ((i < 2 ? code << (6 - 4 * i) : code >> (4 * i - 6)) & 0x03c003c0u) | 0x3c003c00u;
-        p.p[i] += less;
-    }
-    return p;
-}
+// x & mask | bits in one instruction: both constants stay in registers (as literals they take two)
+__device__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t bits) { return (x & mask) | bits; }
 
-// One row's part of a unit for a lane (four times eight inputs), and what its sums are to be multiplied by.
+// code - zero of a lane's eight codes.  zero: of the group's word.
+struct Expand {
+    uint32_t nibble0 = 0x000f000fu, nibble1 = 0x00f000f0u, one = 0x64006400u;
+    union Pair {
+        uint32_t w;
+        half2v p;
+    };
+    struct Zero {
+        Pair low, high;  // -(1024 + zero), -(64 + zero), twice each
+    };
+    __device__ Expand() { asm("" : "+s"(nibble0), "+s"(nibble1), "+v"(one)); }
+    __device__ static Zero zero(uint32_t word) {
+        const uint32_t z = (word & 15) * 0x10001u;
+        Zero to;
+        to.low.w = z | 0xe400e400u, to.high.w = z << 4 | 0xd400d400u;
+        return to;
+    }
+    __device__ half8 operator()(uint32_t code, const Zero &zero) const {
+        const half2v part{(_Float16)(1.f / 16), (_Float16)(1.f / 16)};
+        Piece p;
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+            const uint32_t two = i ? code >> 8 : code;
+            p.w[i] = and_or(two, nibble0, one);
+            p.w[i + 1] = and_or(two, nibble1, one);
+            p.p[i] += zero.low.p;
+            p.p[i + 1] = __builtin_elementwise_fma(p.p[i + 1], part, zero.high.p);
+        }
+        return p.all;
+    }
+};
+
+// One row's part of a unit for a lane, four times eight inputs: as it is in memory,
 template <class T>
 struct RowPart {
-    Piece a[4][kPieces<T>];
-    float power;
+    T x[4][8];
     __device__ void load(const T *row, int k0, int C) {
-        if constexpr (std::is_same_v<T, _Float16>) {
-            power = 1.f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int k = k0 + 32 * j;
-                if (k + 8 <= C) a[j][0].all = *reinterpret_cast<const loose<T, 8> *>(row + k);
-                else
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) a[j][0].all[i] = k + i < C ? row[k + i] : (T)0.f;
-            }
-        } else {
-            float f[4][8], top = 0.f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) load_eight(row, k0 + 32 * j, C, f[j]);
+        if (k0 + 104 <= C) {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(f[j][i]));
+                for (int i = 0; i < 8; i += kVec<T>) {
+                    const loose<T, kVec<T>> v = *reinterpret_cast<const loose<T, kVec<T>> *>(row + k0 + 32 * j + i);
+#pragma unroll
+                    for (int e = 0; e < kVec<T>; ++e) x[j][i + e] = v[e];
+                }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[j][i] = k0 + 32 * j + i < C ? row[k0 + 32 * j + i] : (T)0.f;
+        }
+    }
+    // and as operands; returns what their sums are to be multiplied by.
+    __device__ float convert(Piece (&a)[4][kPieces<T>]) const {
+        if constexpr (std::is_same_v<T, _Float16>) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) a[j][0].all[i] = x[j][i];
+            return 1.f;
+        } else {
+            float top = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf((float)x[j][i]));
             const int e = max((int)(__float_as_uint(row_max(top)) >> 23), 15);  // 15: 2^-112
             const float down = __uint_as_float((uint32_t)(268 - e) << 23);     // 2^(14 - (e - 127)); e = 255 (infinity): 2^-114
-            power = __uint_as_float((uint32_t)(e - 14) << 23);
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    float2v v{f[j][2 * i] * down, f[j][2 * i + 1] * down};
+                    float2v v{(float)x[j][2 * i] * down, (float)x[j][2 * i + 1] * down};
 #pragma unroll
                     for (int n = 0; n < kPieces<T>; ++n) {
                         a[j][n].p[i] = __builtin_convertvector(v, half2v);
                         if (n + 1 < kPieces<T>) v -= __builtin_convertvector(a[j][n].p[i], float2v);
                     }
                 }
+            return __uint_as_float((uint32_t)(e - 14) << 23);
         }
     }
 };
 
-// A wavefront of a workgroup takes a share of the units of 16 NT outputs, for 16 RT rows; their sums meet in LDS.
-template <class T, class Y, int RT, int NT, int J>
-__global__ __launch_bounds__(512) void k_w4_matvec(const T *__restrict__ x, int64_t x_row, int32_t M, W4 m,
+// How a product is cut: a workgroup has `tiles` times `shares` wavefronts, one for each of its tiles of 16 outputs and each share
+// of the units (every shares-th), for 16 rows of x.  The rows of `chunk` units at a time are brought into fp16 by all of them and
+// wait in LDS, 1, 4 or 16 rows (1 << row_shift).
+struct Cut {
+    int32_t tiles, shares, chunk, row_shift;
+};
+
+// Bound by the bytes of the weights.  A wavefront's next kAhead units are on their way while it works on as many, and the rows of
+// the next chunk while all work on this one.
+constexpr int kAhead = 4;
+
+template <int J>
+struct Units {
+    uint4 code[kAhead];
+    uint32_t word[kAhead][4 / J];
+};
+
+template <class T, class Y, int J, int SHIFT>
+__global__ __launch_bounds__(512) void k_w4_matvec(const T *__restrict__ x, int64_t x_row, int32_t M, W4 m, Cut cut,
                                                    const float *__restrict__ bias, int32_t silu_on, Y *__restrict__ y) {
-    extern __shared__ float sums[];  // [waves][16 RT rows][16 NT]
-    const int tid = threadIdx.x, waves = blockDim.x >> 6, wave = tid >> 6;
+    constexpr int P = kPieces<T>;
+    constexpr bool kPowers = !std::is_same_v<T, _Float16>;
+    extern __shared__ uint4 lds[];  // [chunk][4 j][P][4 q][rows], then the powers [chunk][16]; later the sums
+    const unsigned tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
+    constexpr int shift = SHIFT, rows = 1 << shift;
+    float *powers = reinterpret_cast<float *>(lds + cut.chunk * 16 * P * rows);
     const Lane l;
-    const int tile0 = blockIdx.x * NT, row0 = blockIdx.y * 16 * RT;
-    const T *rows[RT];
-    int64_t unit0[NT];  // tiles behind the last are the last again, and not written
+    const int tile = wave % cut.tiles, share = wave / cut.tiles, row0 = blockIdx.y * 16;
+    const int64_t unit0 = (int64_t)min((int)blockIdx.x * cut.tiles + tile, m.R - 1) * m.T;  // behind the last: that again, not written
+    const uint4 *codes = reinterpret_cast<const uint4 *>(m.codes) + unit0 * 64;
+    const uint32_t *words = m.words() + unit0 * (64 / J);
+    const Expand expand;
+
+    // units first, first + shares, .. of a chunk that ends at `end` (its last again where there are no more)
+    auto fetch = [&](Units<J> &to, int first, int end) {
 #pragma unroll
-    for (int t = 0; t < RT; ++t) rows[t] = x + min(row0 + 16 * t + l.r, M - 1) * x_row;
+        for (int d = 0; d < kAhead; ++d) {
+            const int t = min(first + d * cut.shares, end - 1);
+            const uint4 *c = codes + (int64_t)t * 64;  // the same for all lanes
+            const uint32_t *w = words + (int64_t)t * (64 / J);
+            to.code[d] = c[lane];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) unit0[n] = (int64_t)min(tile0 + n, m.R - 1) * m.T;
-    float4v out[RT][NT] = {};
-    const int t0 = (int)((int64_t)m.T * wave / waves), t1 = (int)((int64_t)m.T * (wave + 1) / waves);
-    for (int t = t0; t < t1; ++t) {
-        uint32_t code[NT][4], word[NT][4 / J];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const uint4 c = reinterpret_cast<const uint4 *>(m.codes)[(unit0[n] + t) * 64 + (tid & 63)];
-            code[n][0] = c.x, code[n][1] = c.y, code[n][2] = c.z, code[n][3] = c.w;
-#pragma unroll
-            for (int g = 0; g < 4 / J; ++g) word[n][g] = m.words()[((unit0[n] + t) * 16 + l.r) * (4 / J) + g];
+            for (int g = 0; g < 4 / J; ++g) to.word[d][g] = w[l.r * (4 / J) + g];
         }
-        RowPart<T> part[RT];
-        float power[RT][4];  // of the rows 4 q .. 4 q + 3, as the products' results lie
+    };
+    Units<J> now, next;
+    fetch(now, share, min(cut.chunk, m.T));
+
+    // this lane's row, and its units of a chunk: first, first + step, ..
+    const int per = 16 >> shift, first = wave * per + (l.r >> shift), step = waves * per, row = l.r & (rows - 1);
+    const T *mine = x + min(row0 + row, M - 1) * x_row;
+    RowPart<T> part;
+    part.load(mine, min(first, m.T - 1) * kUnit + 8 * l.q, m.C);
+
+    float4v out{};
+    for (int t0 = 0; t0 < m.T; t0 += cut.chunk) {
+        const int end = min(t0 + cut.chunk, m.T);
+        if (t0) __syncthreads();
+        for (int u = first; t0 + u - (l.r >> shift) < end; u += step) {
+            if (u != first) part.load(mine, min(t0 + u, m.T - 1) * kUnit + 8 * l.q, m.C);
+            Piece a[4][P];
+            const float power = part.convert(a);
+            if (t0 + u >= end) continue;
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            part[rt].load(rows[rt], t * kUnit + 8 * l.q, m.C);
+            for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) power[rt][i] = std::is_same_v<T, _Float16> ? 1.f : __shfl(part[rt].power, 4 * l.q + i);
+                for (int p = 0; p < P; ++p)
+                    lds[((((u * 4 + j) * P + p) * 4 + l.q) << shift) + row] = *reinterpret_cast<uint4 *>(a[j][p].w);
+            if (kPowers && l.q == 0)
+                for (int i = row; i < 16; i += rows) powers[u * 16 + i] = power;
         }
+        __syncthreads();
+        if (end < m.T) part.load(mine, min(end + first, m.T - 1) * kUnit + 8 * l.q, m.C);
+
+        for (int t = t0 + share; t < end; t += kAhead * cut.shares) {
+            const bool same = t + kAhead * cut.shares < end;
+            fetch(next, same ? t + kAhead * cut.shares : min(end + share, m.T - 1), same ? end : min(end + cut.chunk, m.T));
+            __builtin_amdgcn_sched_barrier(0);  // they set out before the work below, not after it
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+            for (int d = 0; d < kAhead; ++d) {
+                const int u = t - t0 + d * cut.shares;
+                if (t0 + u >= end) break;
+                half8 a[4][P];
+                const uint4 *from = lds + (((u * 16 * P + l.q) << shift) + row);
 #pragma unroll
-            for (int g = 0; g < 4 / J; ++g) {
-                const _Float16 z = (_Float16)fmaf((float)(word[n][g] & 15), -1.f / 16, -1.f);
-                const float s = __uint_as_float(word[n][g] & ~15u);
-                float4v acc[RT] = {};
+                for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int j = g * J; j < g * J + J; ++j) {
-                    const Piece b = expand(code[n][j], half2v{z, z});
+                    for (int p = 0; p < P; ++p) a[j][p] = *reinterpret_cast<const half8 *>(from + ((4 * (j * P + p)) << shift));
+                float4v power;
+                if (kPowers) power = *reinterpret_cast<const float4v *>(powers + u * 16 + 4 * l.q);
+                const uint32_t c[4] = {now.code[d].x, now.code[d].y, now.code[d].z, now.code[d].w};
+                float4v sum{};
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt)
+                for (int g = 0; g < 4 / J; ++g) {
+                    float4v acc{};
+                    const Expand::Zero zero = Expand::zero(now.word[d][g]);
 #pragma unroll
-                        for (int p = 0; p < kPieces<T>; ++p)
-                            acc[rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(part[rt].a[j][p].all, b.all, acc[rt], 0, 0, 0);
+                    for (int j = g * J; j < g * J + J; ++j) {
+                        const half8 b = expand(c[j], zero);
+#pragma unroll
+                        for (int p = 0; p < P; ++p) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[j][p], b, acc, 0, 0, 0);
+                    }
+                    const float s = __uint_as_float(now.word[d][g] & ~15u);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sum[i] = g ? fmaf(s, acc[i], sum[i]) : s * acc[i];
                 }
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) out[rt][n][i] = fmaf(s * acc[rt][i], power[rt][i], out[rt][n][i]);
+                for (int i = 0; i < 4; ++i) out[i] = kPowers ? fmaf(sum[i], power[i], out[i]) : out[i] + sum[i];
             }
+            now = next;
+        }
     }
-    constexpr int W = 16 * NT, ALL = 16 * RT * W;
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sums[wave * ALL + (16 * rt + 4 * l.q + i) * W + 16 * n + l.r] = out[rt][n][i];
     __syncthreads();
-    for (int e = tid; e < ALL; e += blockDim.x) {
+    // [shares][16 rows][tiles][16]
+    float *sums = reinterpret_cast<float *>(lds);
+    const int wide = 16 * cut.tiles, all = 16 * wide;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sums[share * all + (4 * l.q + i) * wide + tile * 16 + l.r] = out[i];
+    __syncthreads();
+    const int have = min(16, M - row0);
+    for (int e = tid; e < have * wide; e += waves * 64) {
         float v = 0.f;
-        for (int w = 0; w < waves; ++w) v += sums[w * ALL + e];
-        const int row = row0 + e / W, o = tile0 * 16 + e % W;
-        if (row >= M || o >= m.O) continue;
-        v = bias ? fmaf(v, 16.f, bias[o]) : v * 16.f;
-        y[(int64_t)row * m.O + o] = (Y)(silu_on ? silu(v) : v);
+        for (int w = 0; w < cut.shares; ++w) v += sums[w * all + e];
+        const int o = blockIdx.x * wide + e % wide;
+        if (o >= m.O) continue;
+        if (bias) v += bias[o];
+        y[(int64_t)(row0 + e / wide) * m.O + o] = (Y)(silu_on ? silu(v) : v);
     }
+}
+
+// Bytes of LDS for a chunk, and for the sums behind it.
+template <class T>
+int lds_bytes(const Cut &c) {
+    return std::max(c.chunk * ((256 * kPieces<T> << c.row_shift) + 64), c.tiles * c.shares * 1024);
+}
+
+template <class T>
+Cut cut_of(int32_t M, const W4 &m, int tiles, int shares) {
+    Cut c{tiles, shares, 0, 0};
+    while (c.row_shift < 4 && (1 << c.row_shift) < M) c.row_shift += 2;
+    const int step = tiles * shares * (16 >> c.row_shift);  // units that the wavefronts bring at once
+    c.chunk = step;
+    // kAhead units to each share, if they fit
+    while (c.chunk < shares * kAhead && c.chunk < m.T && lds_bytes<T>({tiles, shares, c.chunk + step, c.row_shift}) <= 131072) c.chunk += step;
+    return c;
+}
+
+// Eight wavefronts: as many tiles as leave a workgroup for each of the 256 CUs (they share the rows' conversion), the units cut
+// among the rest; few units leave too little to a share (32 x 1280 -> 16640 fp32: 19 us with one share, 27 with two).
+template <class T>
+Cut cut_for(int32_t M, const W4 &m) {
+    int tiles = 4;
+    while (tiles > 1 && (int64_t)((m.R + tiles - 1) / tiles) * ((M + 15) / 16) < 256) tiles /= 2;
+    int shares = std::min(8 / tiles, m.T);
+    if (tiles == 4 && M > 4 && m.T < 16) shares = 1;
+    return cut_of<T>(M, m, tiles, shares);
 }
 
 template <class F>
@@ -297,23 +419,29 @@ hipError_t launch_w4_unpack(const W4 &m, int32_t dtype, void *w, hipStream_t st)
 }
 
 hipError_t launch_w4_matvec(const W4Product &p, const W4 &m, hipStream_t st) {
-    const int waves = std::min(m.T, 8);
+    hipError_t e = hipSuccess;
     by_dtype(p.dtype, [&](auto xt) {
         using T = decltype(xt);
+        const Cut c = cut_for<T>(p.M, m);
         by_output<T>(p.out_dtype, [&](auto yt) {
             using Y = decltype(yt);
             by_group(m.group, [&](auto j) {
-                auto go = [&](auto rt) {
-                    constexpr int RT = decltype(rt)::value, NT = 1;
-                    const dim3 grid((m.R + NT - 1) / NT, (p.M + 16 * RT - 1) / (16 * RT));
-                    k_w4_matvec<T, Y, RT, NT, decltype(j)::value><<<grid, 64 * waves, waves * RT * NT * 1024, st>>>(
-                        static_cast<const T *>(p.x), p.x_row, p.M, m, p.bias, p.act == DGQ_ACT_SILU, static_cast<Y *>(p.y));
+                constexpr int J = decltype(j)::value;
+                const dim3 grid((m.R + c.tiles - 1) / c.tiles, (p.M + 15) / 16);
+                auto go = [&](auto shift) {
+                    constexpr int S = decltype(shift)::value;
+                    e = DGQ_ENSURE_LDS((k_w4_matvec<T, Y, J, S>), lds_bytes<T>(c));
+                    if (e == hipSuccess)
+                        k_w4_matvec<T, Y, J, S><<<grid, 64 * c.tiles * c.shares, lds_bytes<T>(c), st>>>(
+                            static_cast<const T *>(p.x), p.x_row, p.M, m, c, p.bias, p.act == DGQ_ACT_SILU, static_cast<Y *>(p.y));
                 };
-                p.M <= 16 ? go(std::integral_constant<int, 1>{}) : go(std::integral_constant<int, 2>{});
+                c.row_shift == 0   ? go(std::integral_constant<int, 0>{})
+                : c.row_shift == 2 ? go(std::integral_constant<int, 2>{})
+                                   : go(std::integral_constant<int, 4>{});
             });
         });
     });
-    return hipGetLastError();
+    return e == hipSuccess ? hipGetLastError() : e;
 }
 
 }  // namespace dgq
