@@ -84,62 +84,156 @@ struct Shape {
 };
 
 // ---- sums ------------------------------------------------------------------------------------------------------------
+__device__ double2 sum_of(double2 a, double2 b) { return {a.x + b.x, a.y + b.y}; }
+// over `lanes` (a power of two) neighbouring lanes
+__device__ double2 lane_sums(double2 s, int lanes) {
+    for (int d = lanes >> 1; d; d >>= 1) s = sum_of(s, {__shfl_xor(s.x, d), __shfl_xor(s.y, d)});
+    return s;
+}
+
+// Sum of n entries, each lane's from `from` on and `stride` apart, eight reads at a time; over `lanes` neighbours.
+__device__ double2 strided_sum(const double2 *entries, int64_t n, int from, int stride, int lanes) {
+    double2 s{0, 0};
+    for (int64_t i = from; i < n; i += 8 * stride) {
+        double2 e[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) e[u] = i + u * stride < n ? entries[i + u * stride] : double2{0, 0};
+#pragma unroll
+        for (int u = 0; u < 8; ++u) s = sum_of(s, e[u]);
+    }
+    return lane_sums(s, lanes);
+}
+
+// A thread's n rows, `step` elements apart: f(index of the row, values).  kAhead loads are on their way while as many rows are
+// worked on.
+constexpr int kAhead = 4;
+template <class T>
+struct RowsOf {
+    static constexpr int V = kVec<T>;
+    using Vec = loose<T, V>;
+    const T *row;
+    int64_t step;
+    int n, have;
+    Vec now[kAhead];
+    __device__ RowsOf(const T *first, int64_t step_, int n_, int have_) : row(first), step(step_), n(n_), have(have_) {
+        if (have >= V) fetch(now, 0);
+    }
+    __device__ void fetch(Vec (&to)[kAhead], int i) const {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (i + u < n) to[u] = *reinterpret_cast<const Vec *>(row + (i + u) * step);
+    }
+    template <class F>
+    __device__ void each(F f) {
+        float x[V];
+        if (have >= V) {
+            for (int i = 0; i < n; i += kAhead) {
+                Vec next[kAhead];
+                fetch(next, i + kAhead);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u)
+                    if (i + u < n) {
+#pragma unroll
+                        for (int e = 0; e < V; ++e) x[e] = (float)now[u][e];
+                        f(i + u, x);
+                    }
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) now[u] = next[u];
+            }
+        } else {
+            for (int i = 0; i < n; ++i) {
+                load_vector(row + i * step, have, x);
+                f(i, x);
+            }
+        }
+    }
+};
+
 // Bound by the bytes of x.  sums: [G][parts][slices] double2.
 template <class T>
 __global__ __launch_bounds__(kMaxThreads) void k_gn_sums(const T *__restrict__ x, Images im, Rows xs, Chunks ch, Shape sh, int32_t C,
                                                          int32_t G, const float *__restrict__ add, int64_t add_row,
                                                          double2 *__restrict__ sums, int32_t parts) {
     constexpr int V = kVec<T>;
-    extern __shared__ double channel[];  // [high][width V]
-    const int tid = threadIdx.x, lane = tid & 63, high = sh.threads / sh.width, wide = sh.width * V;
+    extern __shared__ double2 entries[];  // [high][width] where vectors end with their groups, else [high][width V]
+    const int tid = threadIdx.x, high = sh.threads / sh.width, wide = sh.width * V;
     const int pr = tid / sh.width, c_slice = blockIdx.y * wide, c0 = c_slice + (tid - pr * sh.width) * V, have = min(V, C - c0);
     const bool on = pr < high && have > 0;
-    const int Cg = C / G, c_end = min(c_slice + wide, C);
+    const int Cg = C / G, c_end = min(c_slice + wide, C), each = Cg % V ? 1 : V;  // channels of an entry
+    // neighbouring lanes that share a group's entries
+    int lanes = 64;
+    while (lanes > 1 && lanes * G > sh.threads) lanes >>= 1;
     ch.each(im, blockIdx.x, [&](int32_t b, int32_t part, int64_t r0, int64_t r1) {
         double s[V] = {}, ss[V] = {};
-        int64_t n = 0;
         if (on) {
-            const T *row = x + xs.at(im, b, r0 + pr) + c0;
-            for (int64_t r = r0 + pr; r < r1; r += high, row += high * xs.row) {
-                float f[V];
-                load_vector(row, have, f);
+            const int n = (int)(r1 - r0 - pr + high - 1) / high;
+            RowsOf<T>(x + xs.at(im, b, r0 + pr) + c0, high * xs.row, n, have).each([&](int, const float (&f)[V]) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     s[i] += (double)f[i];
                     ss[i] = fma((double)f[i], (double)f[i], ss[i]);
                 }
-                ++n;
-            }
+            });
             if (add)
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const double d = i < have ? add[b * add_row + c0 + i] : 0.f;
-                    ss[i] += d * (2 * s[i] + n * d);
-                    s[i] += n * d;
+                for (int j = 0; j < V; ++j) {
+                    const double d = j < have ? add[b * add_row + c0 + j] : 0.f;
+                    ss[j] += d * (2 * s[j] + n * d);
+                    s[j] += n * d;
                 }
         }
-        double sum = 0;
-        for (int pass = 0; pass < 2; ++pass) {
-            __syncthreads();
-            if (pr < high)
+        __syncthreads();
+        if (pr < high) {
+            if (each == 1) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) channel[tid * V + i] = pass ? ss[i] : s[i];
-            __syncthreads();
-            // a wavefront per group
-            for (int g = tid >> 6; g < G; g += sh.threads >> 6) {
-                const int lo = max(g * Cg, c_slice), n_here = min((g + 1) * Cg, c_end) - lo;
-                sum = 0;
-                for (int e = lane; e < n_here * high; e += 64) sum += channel[e / n_here * wide + (lo - c_slice) + e % n_here];
+                for (int i = 0; i < V; ++i) entries[tid * V + i] = {s[i], ss[i]};
+            } else {
+                double2 sum{0, 0};
 #pragma unroll
-                for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-                if (lane == 0) {
-                    double *to = reinterpret_cast<double *>(sums + ((int64_t)g * parts + part) * sh.slices + blockIdx.y);
-                    to[pass] = sum;
-                }
+                for (int i = 0; i < V; ++i) sum = sum_of(sum, {s[i], ss[i]});
+                entries[tid] = sum;
             }
+        }
+        __syncthreads();
+        for (int g = tid / lanes; g < G; g += sh.threads / lanes) {
+            const int lo = (max(g * Cg, c_slice) - c_slice) / each, n_here = (min((g + 1) * Cg, c_end) - c_slice) / each - lo;
+            double2 sum{0, 0};
+            for (int p = 0; p < high; ++p)
+                for (int e = tid & (lanes - 1); e < n_here; e += lanes) sum = sum_of(sum, entries[p * (wide / each) + lo + e]);
+            sum = lane_sums(sum, lanes);
+            if ((tid & (lanes - 1)) == 0) sums[((int64_t)g * parts + part) * sh.slices + blockIdx.y] = sum;
         }
     });
 }
+
+// What an image's channel is given,
+struct Terms {
+    float weight, bias, add, scale, shift;
+    __device__ static Terms of(const NormTerms &t, const float *weight, const float *bias, int32_t b, int32_t c) {
+        return {weight ? weight[c] : 1.f, bias ? bias[c] : 0.f, t.add ? t.add[b * t.add_row + c] : 0.f,
+                t.scale ? t.scale[b * t.scale_row + c] : 0.f, t.shift ? t.shift[b * t.shift_row + c] : 0.f};
+    }
+};
+// and its line, from the sums over its group's n values.
+struct Line {
+    float p, a, q;
+};
+struct Group {
+    double m, r;
+    Group() = default;
+    __device__ Group(double2 s, double per, float eps) : m(s.x * per) {  // per: 1 / n
+        double v = s.y * per - m * m;
+        if (v < 0) v = 0;  // (not NaN)
+        r = rsqrt(v + (double)eps);
+    }
+    __device__ Line line(const Terms &t) const {
+        const double mean = m - (double)t.add;
+        const float p = (float)mean;
+        const double rw = r * (double)t.weight, one = 1 + (double)t.scale;
+        return {p, (float)(rw * one), (float)((((double)p - mean) * rw + (double)t.bias) * one + (double)t.shift)};
+    }
+};
 
 // ---- tables ----------------------------------------------------------------------------------------------------------
 // One workgroup per (group, image).  Bound by latency.  tables: fp32 [B][p, a, q][C].
@@ -149,74 +243,193 @@ __global__ __launch_bounds__(256) void k_gn_tables(const double2 *__restrict__ s
     __shared__ double2 wave_sums[4];
     const int g = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, Cg = C / G;
     const int64_t first = ((int64_t)g * parts + ch.first(im, b)) * slices, n_parts = (int64_t)ch.parts(im, b) * slices;
-    double2 s{0, 0};
-    for (int64_t i = tid; i < n_parts; i += 256) {
-        const double2 p = sums[first + i];
-        s.x += p.x, s.y += p.y;
-    }
-#pragma unroll
-    for (int d = 32; d; d >>= 1) s.x += __shfl_xor(s.x, d), s.y += __shfl_xor(s.y, d);
+    double2 s = strided_sum(sums + first, n_parts, tid, 256, 64);
     if ((tid & 63) == 0) wave_sums[tid >> 6] = s;
     __syncthreads();
     s = wave_sums[0];
 #pragma unroll
-    for (int w = 1; w < 4; ++w) s.x += wave_sums[w].x, s.y += wave_sums[w].y;
-    const double n = (double)(im.end(b) - im.start(b)) * Cg, m = s.x / n;
-    double v = s.y / n - m * m;
-    if (v < 0) v = 0;  // (not NaN)
-    const double r = 1 / sqrt(v + (double)eps);
+    for (int w = 1; w < 4; ++w) s = sum_of(s, wave_sums[w]);
+    const Group group(s, 1 / ((double)(im.end(b) - im.start(b)) * Cg), eps);
     for (int c = g * Cg + tid; c < (g + 1) * Cg; c += 256) {
-        const double mean = terms.add ? m - (double)terms.add[b * terms.add_row + c] : m;
-        const float p = (float)mean;
-        const double rw = weight ? r * (double)weight[c] : r, one = terms.scale ? 1 + (double)terms.scale[b * terms.scale_row + c] : 1.0;
-        const double q = (((double)p - mean) * rw + (bias ? (double)bias[c] : 0.0)) * one;
+        const Line line = group.line(Terms::of(terms, weight, bias, b, c));
         float *t = tables + (int64_t)b * 3 * C + c;
-        t[0] = p;
-        t[C] = (float)(rw * one);
-        t[2 * (int64_t)C] = (float)(terms.shift ? q + (double)terms.shift[b * terms.shift_row + c] : q);
+        t[0] = line.p;
+        t[C] = line.a;
+        t[2 * (int64_t)C] = line.q;
     }
 }
 
 // ---- values ----------------------------------------------------------------------------------------------------------
-// Bound by the bytes of x and y.  x and y may be one buffer: a thread writes what it alone has read.
-template <class T, class Y, bool SILU>
-__global__ __launch_bounds__(kMaxThreads) void k_gn_apply(const T *x, Images im, Rows xs, Chunks ch, Shape sh, int32_t C,
-                                                          const float *__restrict__ tables, Y *y) {
+// Bound by the bytes of x and y.  x and y may be one buffer: a thread writes what it alone has read.  tables null: every workgroup
+// adds up the sums of its image itself, which costs less than a launch that does it once, as long as they are few.
+template <class T, class Y>
+__global__ __launch_bounds__(kMaxThreads) void k_gn_apply(const T *x, Images im, Rows xs, Chunks ch, Shape sh, int32_t C, int32_t G,
+                                                          const float *__restrict__ tables, const double2 *__restrict__ sums,
+                                                          int32_t parts, const float *__restrict__ weight,
+                                                          const float *__restrict__ bias, float eps, NormTerms terms, int32_t silu_on,
+                                                          Y *y) {
     constexpr int V = kVec<T>;
-    const int tid = threadIdx.x, high = sh.threads / sh.width, pr = tid / sh.width;
-    const int c0 = (blockIdx.y * sh.width + tid - pr * sh.width) * V, have = min(V, C - c0);
-    if (pr >= high || have <= 0) return;
+    extern __shared__ float lines[];  // [p, a, q][width V], and in front of them the groups' m and r
+    const int tid = threadIdx.x, high = sh.threads / sh.width, pr = tid / sh.width, wide = sh.width * V, Cg = C / G;
+    const int c_slice = blockIdx.y * wide, c0 = c_slice + (tid - pr * sh.width) * V, have = min(V, C - c0);
+    int lanes = 64;
+    while (lanes > 1 && lanes * G > sh.threads) lanes >>= 1;
     ch.each(im, blockIdx.x, [&](int32_t b, int32_t, int64_t r0, int64_t r1) {
         float p[V], a[V], q[V];
-        const float *t = tables + (int64_t)b * 3 * C + c0;
+        const float *from;
+        int64_t stride;
+        const bool on = pr < high && have > 0;
+        RowsOf<T> rows(x + xs.at(im, b, r0 + pr) + c0, high * xs.row, on ? (int)(r1 - r0 - pr + high - 1) / high : 0, have);
+        if (tables) {
+            from = tables + (int64_t)b * 3 * C + c0;
+            stride = C;
+        } else {
+            Group *groups = reinterpret_cast<Group *>(lines);
+            float *to = lines + G * (sizeof(Group) / sizeof(float));
+            const int64_t first = ch.first(im, b), n_parts = (int64_t)ch.parts(im, b) * sh.slices;
+            const double per = 1 / ((double)(im.end(b) - im.start(b)) * Cg);
+            const int c_end = min(c_slice + wide, C);
+            Terms mine{};
+            if (c_slice + tid < c_end) mine = Terms::of(terms, weight, bias, b, c_slice + tid);
+            __syncthreads();
+            for (int g = tid / lanes; g < G; g += sh.threads / lanes) {
+                const double2 s = strided_sum(sums + ((int64_t)g * parts + first) * sh.slices, n_parts, tid & (lanes - 1), lanes, lanes);
+                if ((tid & (lanes - 1)) == 0) groups[g] = Group(s, per, eps);
+            }
+            __syncthreads();
+            for (int c = c_slice + tid; c < c_end; c += sh.threads) {
+                const Line line = groups[c / Cg].line(c == c_slice + tid ? mine : Terms::of(terms, weight, bias, b, c));
+                float *t = to + c - c_slice;
+                t[0] = line.p, t[wide] = line.a, t[2 * wide] = line.q;
+            }
+            __syncthreads();
+            from = to + c0 - c_slice;
+            stride = wide;
+        }
+        if (!on) return;
 #pragma unroll
         for (int i = 0; i < V; ++i)
-            if (i < have) p[i] = t[i], a[i] = t[C + i], q[i] = t[2 * (int64_t)C + i];
+            if (i < have) p[i] = from[i], a[i] = from[stride + i], q[i] = from[2 * stride + i];
             else p[i] = a[i] = q[i] = 0.f;
-        const T *from = x + xs.at(im, b, r0 + pr) + c0;
         Y *to = y + (r0 + pr) * C + c0;
-        for (int64_t r = r0 + pr; r < r1; r += high, from += high * xs.row, to += (int64_t)high * C) {
-            float f[V];
-            load_vector(from, have, f);
+        rows.each([&](int r, const float (&f)[V]) {
+            float v[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = fmaf(f[i] - p[i], a[i], q[i]);
+            if (silu_on)
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[i] = silu(v[i]);
+            store_vector(to + (int64_t)r * high * C, have, v);
+        });
+    });
+}
+
+// ---- all in one ------------------------------------------------------------------------------------------------------
+// One workgroup per (image, group) keeps its part of the map in registers, so that x crosses memory once: HELD vectors of a
+// thread, `width` threads side by side over the group's channels (the last vector ends with the group, and what it shares with
+// the one before counts there) and threads / width rows at a time.  Rows that do not fit are read twice.  A group is a stripe of
+// the rows, cut inside lines of memory: an XCD gets neighbouring groups, so that its cache puts the lines together.
+template <class T, class Y, int THREADS, int HELD>
+__global__ __launch_bounds__(THREADS) void k_gn_one(const T *x, Images im, Rows xs, int32_t C, int32_t G, int32_t width,
+                                                    const float *__restrict__ weight, const float *__restrict__ bias, float eps,
+                                                    NormTerms terms, int32_t silu_on, Y *y) {
+    constexpr int V = kVec<T>;
+    using Vec = loose<T, V>;
+    extern __shared__ float lines[];  // [p, a, q][C / G]
+    __shared__ double2 wave_sums[THREADS / 64];
+    const int n_all = im.B * G, each = (n_all + 7) / 8, id = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
+    if (id >= n_all || (int)(blockIdx.x >> 3) >= each) return;
+    // one size: the groups of an image on one XCD; packed: some groups of all images, whose sizes differ
+    const int b = im.offsets ? id % im.B : id / G, g = im.offsets ? id / im.B : id % G;
+    const int Cg = C / G, tid = threadIdx.x, pr = tid / width, v = tid - pr * width, high = THREADS / width;
+    const int c = min(v * V, Cg - V), again = v * V - c, c0 = g * Cg + c;  // again: values that the vector before has too
+    const int64_t r0 = im.start(b), r1 = im.end(b);
+    if (r1 <= r0) return;
+    const int n = pr < high ? max((int)(r1 - r0 - pr + high - 1) / high, 0) : 0;  // rows of this thread
+    const int64_t step = high * xs.row;
+    const T *from = x + xs.at(im, b, r0 + pr) + c0;
+    const double per = 1 / ((double)(r1 - r0) * Cg);
+
+    Vec held[HELD];
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+        if (i < n) held[i] = *reinterpret_cast<const Vec *>(from + i * step);
+    Terms mine{};
+    if (tid < Cg) mine = Terms::of(terms, weight, bias, b, g * Cg + tid);
+    double2 s{0, 0};
+    // first pass over a thread's rows; PLAIN: nothing is added, no value counts elsewhere
+    auto first = [&](auto plain) {
+        float shift[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) shift[i] = terms.add ? terms.add[b * terms.add_row + c0 + i] : 0.f;
+        auto count = [&](const Vec &w) {
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                f[i] = fmaf(f[i] - p[i], a[i], q[i]);
-                if (SILU) f[i] = silu(f[i]);
+                double d = (double)(float)w[i];
+                if constexpr (!decltype(plain)::value) {
+                    d += (double)shift[i];
+                    if (i < again) d = 0;
+                }
+                s.x += d;
+                s.y = fma(d, d, s.y);
             }
-            store_vector(to, have, f);
+        };
+#pragma unroll
+        for (int i = 0; i < HELD; ++i)
+            if (i < n) count(held[i]);
+        for (int i = HELD; i < n; ++i) count(*reinterpret_cast<const Vec *>(from + i * step));
+    };
+    if (!terms.add && Cg % V == 0) first(std::true_type{});
+    else first(std::false_type{});
+    s = lane_sums(s, 64);
+    if ((tid & 63) == 0) wave_sums[tid >> 6] = s;
+    __syncthreads();
+    s = wave_sums[0];
+#pragma unroll
+    for (int w = 1; w < THREADS / 64; ++w) s = sum_of(s, wave_sums[w]);
+    const Group group(s, per, eps);
+    for (int i = tid; i < Cg; i += THREADS) {
+        const Line l = group.line(i == tid ? mine : Terms::of(terms, weight, bias, b, g * Cg + i));
+        lines[i] = l.p, lines[Cg + i] = l.a, lines[2 * Cg + i] = l.q;
+    }
+    __syncthreads();
+    if (n == 0) return;
+    float p[V], a[V], q[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) p[e] = lines[c + e], a[e] = lines[Cg + c + e], q[e] = lines[2 * Cg + c + e];
+    Y *to = y + (r0 + pr) * C + c0;
+    auto value = [&](const Vec &w, float (&f)[V]) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) f[e] = fmaf((float)w[e] - p[e], a[e], q[e]);
+        if (silu_on)
+#pragma unroll
+            for (int e = 0; e < V; ++e) f[e] = silu(f[e]);
+    };
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+        if (i < n) {
+            float f[V];
+            value(held[i], f);
+            store_vector(to + (int64_t)i * high * C, V, f);
         }
-    });
+    for (int i = HELD; i < n; ++i) {  // y may be x: what two vectors share is written by the first, the second may have read it anew
+        float f[V];
+        value(*reinterpret_cast<const Vec *>(from + i * step), f);
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            if (e >= again) to[(int64_t)i * high * C + e] = (Y)f[e];
+    }
 }
 
 // ---- launches --------------------------------------------------------------------------------------------------------
 
-// Most threads that have a vector of their own, of workgroups of 4 to 8 wavefronts.
-Shape shape_for(int32_t C, int V) {
-    const int32_t vectors = (C + V - 1) / V, slices = (vectors + kMaxThreads - 1) / kMaxThreads, width = (vectors + slices - 1) / slices;
+// Of workgroups of half to all of `most` threads, the largest of those with most threads that have a vector of their own.
+Shape shape_for(int32_t C, int V, int32_t most) {
+    const int32_t vectors = (C + V - 1) / V, slices = (vectors + most - 1) / most, width = (vectors + slices - 1) / slices;
     int32_t best = 0, threads = 0;
-    for (int32_t t = 256; t <= kMaxThreads; t += 64) {
+    for (int32_t t = most / 2; t <= most; t += 64) {
         const int32_t used = 1024 * (t / width * width) / t;  // share in use
-        if (used > best) best = used, threads = t;
+        if (used >= best) best = used, threads = t;
     }
     return {threads, width, slices};
 }
@@ -231,19 +444,64 @@ Chunks chunks_for(const NormCall &n, const Shape &sh, int64_t most) {
     return {P, (int32_t)(per * n.B), (int32_t)per};
 }
 
-constexpr int64_t kChunks = 1024;
+// Workgroups of the two streaming kernels: one to a CU, two where an image then still has few parts to be added up by all (16 x
+// 4096 x 640 fp32 107 us, 110 with one; 1 x 1048576 x 128 fp16 175 and 171).
+int64_t chunk_count(int32_t B) { return B >= 8 ? 512 : 256; }
+constexpr int64_t kMaxFolded = 16384;  // sums of an image that every workgroup may read
+
+// Whether a workgroup can hold an image's group, and how: threads and vectors of each (0: it cannot, or is slower: long stripes
+// touch a line of memory in every row and need most CUs to keep up.  2 x 1024 x 1280 fp32 10.7 us, 14.9 with sums of chunks; 2 x
+// 4096 x 320 16.7 and 14.8, 8 x 4096 x 320 23.8 and 26.3).
+struct Hold {
+    int32_t threads = 0, held = 0, width = 0;
+};
+Hold hold_for(const NormCall &n) {
+    const int32_t V = n.dtype == DGQ_F32 ? 4 : 8, Cg = n.C / n.G, width = (Cg + V - 1) / V;
+    if (Cg < V || width > 256) return {};
+    const int64_t rows = n.offsets ? n.N / n.B * 3 / 2 : n.N;  // of a long image
+    if (rows > 2048 && (int64_t)n.B * n.G < 192) return {};
+    const Hold ways[] = {{256, 4, width}, {1024, 4, width}, {1024, 8, width}, {1024, 16, width}};
+    for (const Hold &h : ways)
+        if (rows <= (int64_t)h.held * (h.threads / width)) return h;
+    return {};
+}
 
 struct NormPlan {
+    Hold hold;
     Shape shape;
     Chunks chunks;
-    int32_t parts;
-    size_t sums_bytes, tables_bytes;
-    explicit NormPlan(const NormCall &n) : shape(shape_for(n.C, n.dtype == DGQ_F32 ? 4 : 8)), chunks(chunks_for(n, shape, kChunks)) {
+    int32_t parts = 0;
+    size_t sums_bytes = 0, tables_bytes = 0;  // tables_bytes 0: the last kernel makes them itself
+    explicit NormPlan(const NormCall &n) : hold(hold_for(n)), shape(shape_for(n.C, n.dtype == DGQ_F32 ? 4 : 8, kMaxThreads)), chunks(chunks_for(n, shape, chunk_count(n.B))) {
+        if (hold.held) return;
         parts = chunks.count + (n.offsets ? n.B : 0);
         sums_bytes = (size_t)n.G * parts * shape.slices * sizeof(double2);
-        tables_bytes = (size_t)n.B * 3 * n.C * sizeof(float);
+        if (n.G > 2048 || (int64_t)n.G * shape.slices * (n.offsets ? parts : chunks.per) > kMaxFolded) tables_bytes = (size_t)n.B * 3 * n.C * sizeof(float);
     }
 };
+
+template <class T, class Y>
+hipError_t launch_one(const NormCall &n, const Hold &h, const Images &im, const Rows &xs, hipStream_t st) {
+    const T *x = static_cast<const T *>(n.x);
+    Y *y = static_cast<Y *>(n.out);
+    const unsigned grid = 8 * (((int64_t)n.B * n.G + 7) / 8);
+    hipError_t e = hipSuccess;
+    auto go = [&](auto threads, auto held) {
+        constexpr int THREADS = decltype(threads)::value;
+        constexpr int HELD = decltype(held)::value;
+        const int bytes = 3 * (n.C / n.G) * (int)sizeof(float);
+        e = DGQ_ENSURE_LDS((k_gn_one<T, Y, THREADS, HELD>), bytes);
+        if (e == hipSuccess)
+            k_gn_one<T, Y, THREADS, HELD><<<grid, THREADS, bytes, st>>>(x, im, xs, n.C, n.G, h.width, n.weight, n.bias, n.eps,
+                                                                        n.terms, n.act == DGQ_ACT_SILU, y);
+    };
+    constexpr std::integral_constant<int, 1024> all{};
+    if (h.threads == 256) go(std::integral_constant<int, 256>{}, std::integral_constant<int, 4>{});
+    else if (h.held == 4) go(all, std::integral_constant<int, 4>{});
+    else if (h.held == 8) go(all, std::integral_constant<int, 8>{});
+    else go(all, std::integral_constant<int, 16>{});
+    return e;
+}
 
 }  // namespace
 
@@ -257,25 +515,37 @@ hipError_t launch_groupnorm(const NormCall &n, void *workspace, hipStream_t st) 
     const Images im{n.offsets, n.N, n.rows(), n.B};
     const Rows xs{n.x_batch, n.x_row};
     double2 *sums = static_cast<double2 *>(workspace);
-    float *tables = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + p.sums_bytes);
+    float *tables = p.tables_bytes ? reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + p.sums_bytes) : nullptr;
     const dim3 grid(p.chunks.count, p.shape.slices);
+    hipError_t e = hipSuccess;
     by_dtype(n.dtype, [&](auto xt) {
         using T = decltype(xt);
         const T *x = static_cast<const T *>(n.x);
-        k_gn_sums<T><<<grid, p.shape.threads, p.shape.threads * kVec<T> * sizeof(double), st>>>(
-            x, im, xs, p.chunks, p.shape, n.C, n.G, n.terms.add, n.terms.add_row, sums, p.parts);
-        k_gn_tables<<<dim3(n.G, n.B), 256, 0, st>>>(sums, p.parts, im, p.chunks, p.shape.slices, n.C, n.G, n.weight, n.bias, n.eps,
-                                                    n.terms, tables);
+        if (!p.hold.held) {
+            const int bytes = p.shape.threads * (int)sizeof(double2) * (n.C / n.G % kVec<T> ? kVec<T> : 1);
+            e = DGQ_ENSURE_LDS(k_gn_sums<T>, bytes);
+            if (e != hipSuccess) return;
+            k_gn_sums<T><<<grid, p.shape.threads, bytes, st>>>(x, im, xs, p.chunks, p.shape, n.C, n.G, n.terms.add, n.terms.add_row,
+                                                               sums, p.parts);
+            if (tables)
+                k_gn_tables<<<dim3(n.G, n.B), 256, 0, st>>>(sums, p.parts, im, p.chunks, p.shape.slices, n.C, n.G, n.weight, n.bias,
+                                                            n.eps, n.terms, tables);
+        }
         by_output<T>(n.out_dtype, [&](auto yt) {
             using Y = decltype(yt);
             Y *y = static_cast<Y *>(n.out);
-            if (n.act == DGQ_ACT_SILU)
-                k_gn_apply<T, Y, true><<<grid, p.shape.threads, 0, st>>>(x, im, xs, p.chunks, p.shape, n.C, tables, y);
-            else
-                k_gn_apply<T, Y, false><<<grid, p.shape.threads, 0, st>>>(x, im, xs, p.chunks, p.shape, n.C, tables, y);
+            if (p.hold.held) {
+                e = launch_one<T, Y>(n, p.hold, im, xs, st);
+                return;
+            }
+            const int bytes = tables ? 0 : n.G * (int)sizeof(Group) + 3 * p.shape.width * kVec<T> * (int)sizeof(float);
+            e = DGQ_ENSURE_LDS((k_gn_apply<T, Y>), bytes);
+            if (e == hipSuccess)
+                k_gn_apply<T, Y><<<grid, p.shape.threads, bytes, st>>>(x, im, xs, p.chunks, p.shape, n.C, n.G, tables, sums, p.parts,
+                                                                       n.weight, n.bias, n.eps, n.terms, n.act == DGQ_ACT_SILU, y);
         });
     });
-    return hipGetLastError();
+    return e == hipSuccess ? hipGetLastError() : e;
 }
 
 }  // namespace dgq

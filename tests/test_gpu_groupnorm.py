@@ -56,10 +56,11 @@ def _even(B, N):
 
 ALL = ("weight", "bias", "add", "scale", "shift")
 # B, N, C, G: single values, widths that fill no vector, groups that end inside one, one image of many rows, many of few, more
-# channels than one workgroup takes, a map that a workgroup holds, one just above
+# channels than one workgroup takes, maps that a workgroup holds in registers and larger ones, groups too many to be added up by all
 SIZES = [(1, 1, 1, 1), (1, 1, 32, 32), (3, 1, 40, 8), (2, 7, 30, 30), (2, 64, 37, 1), (1, 100, 90, 30), (5, 33, 129, 3),
          (2, 256, 320, 32), (2, 64, 1280, 32), (1, 4099, 128, 32), (300, 3, 24, 4), (2, 50, 2560, 32), (1, 9, 5000, 8),
-         (1, 5, 9001, 1), (4, 1024, 320, 32), (1, 20000, 16, 4)]
+         (1, 5, 9001, 1), (4, 1024, 320, 32), (1, 20000, 16, 4),
+         (1, 3000, 256, 256), (2, 6, 4096, 4096), (7, 600, 320, 32), (6, 2100, 320, 32), (3, 300, 516, 4), (9, 513, 264, 24)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -109,12 +110,31 @@ def test_packed(dgq, lengths, C, G, dtype):
     assert (out[:front] == 7).all() and (out[rows - behind:] == 7).all()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("C,G", [(80, 8), (96, 8)])
+def test_packed_with_one_long_image(dgq, C, G, in_place, dtype):
+    """An image far longer than the others, whose rows no workgroup holds, and groups that fill no vector."""
+    import torch
+    rng = np.random.default_rng(C)
+    lengths = [int(n) for n in rng.integers(0, 30, 40)]
+    lengths[17] = 9001
+    offsets = np.concatenate([[0], np.cumsum(lengths)])
+    x, xn = _map(rng, int(offsets[-1]), C, dtype)
+    t = _tables(rng, 40, C, ("weight", "add", "shift"))
+    out = dgq.dgq_groupnorm(x, G, act=dgq.ACT_SILU, offsets=_up(offsets.astype(np.int32)), out=x if in_place else torch.empty_like(x),
+                            **{k: _up(v) for k, v in t.items()})
+    _check(out, *ref.groupnorm(xn, offsets[:-1], offsets[1:], G, silu=True, out_type=dtype, **t))
+
+
 def test_packed_offsets_out_of_order_stay_inside(dgq):
     """Offsets below 0, above the rows and descending: wrong rows, but none outside the tensors."""
     import torch
     rng = np.random.default_rng(8)
-    rows, C, G = 500, 64, 8
-    for offsets in ([-5, 900, 20, 400, 10 ** 9], [400, 300, 200, 100, 0], [0, 500, 0, 500, 0], [-9, -8, -7, -6, -5]):
+    rows = 500
+    for G, offsets in ((g, o) for g in (8, 64) for o in ([-5, 900, 20, 400, 10 ** 9], [400, 300, 200, 100, 0], [0, 500, 0, 500, 0],
+                                                         [-9, -8, -7, -6, -5])):
+        C = 64
         around = torch.full((rows + 200, C), 3.0, device="cuda")
         out = around[100:100 + rows]
         dgq.dgq_groupnorm(_map(rng, rows, C, "fp32")[0], G, offsets=_up(np.array(offsets, np.int32)), out=out)
