@@ -22,71 +22,88 @@ struct Lane {
     __device__ Lane() : r(threadIdx.x & 15), q(threadIdx.x >> 4 & 3) {}
 };
 
-// Inputs k .. k + 7 of a row, those from C on 0.
+// One row's part of a unit for a lane, four times eight inputs; from C on 0.
 template <class T>
-__device__ void load_eight(const T *row, int k, int C, float (&f)[8]) {
-    constexpr int V = kVec<T>;
+struct RowPart {
+    T x[4][8];
+    __device__ void load(const T *row, int k0, int C) {
+        if (k0 + 104 <= C) {
 #pragma unroll
-    for (int v = 0; v < 8 / V; ++v) {
-        float part[V];
-        load_vector(row + k + v * V, C - k - v * V, part);
+            for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int i = 0; i < V; ++i) f[v * V + i] = part[i];
+                for (int i = 0; i < 8; i += kVec<T>) {
+                    const loose<T, kVec<T>> v = *reinterpret_cast<const loose<T, kVec<T>> *>(row + k0 + 32 * j + i);
+#pragma unroll
+                    for (int e = 0; e < kVec<T>; ++e) x[j][i + e] = v[e];
+                }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[j][i] = k0 + 32 * j + i < C ? row[k0 + 32 * j + i] : (T)0.f;
+        }
     }
-}
+};
 
 // nibble of input i (0 .. 7) of a lane's word
 __device__ constexpr int nibble(int i) { return i % 2 ? 4 + i / 2 : i / 2; }
 
 // over the lanes of a row
-__device__ float row_min(float x) { return x = fminf(x, __shfl_xor(x, 16)), fminf(x, __shfl_xor(x, 32)); }
-__device__ float row_max(float x) { return x = fmaxf(x, __shfl_xor(x, 16)), fmaxf(x, __shfl_xor(x, 32)); }
+__device__ float row_min(float x) {  // NaN if one is
+    x = __builtin_elementwise_minimum(x, __shfl_xor(x, 16));
+    return __builtin_elementwise_minimum(x, __shfl_xor(x, 32));
+}
+__device__ float row_max(float x) {
+    x = __builtin_elementwise_maximum(x, __shfl_xor(x, 16));
+    return __builtin_elementwise_maximum(x, __shfl_xor(x, 32));
+}
 
 // ---- packing ---------------------------------------------------------------------------------------------------------
-// A wavefront per unit.  Bound by the bytes of w.
+// A wavefront per unit, four neighbours of a row of units to a workgroup.  Bound by the bytes of w.
 template <class T, int J>  // J: words of 32 inputs in a group
 __global__ __launch_bounds__(256) void k_w4_pack(const T *__restrict__ w, int64_t w_row, W4 m) {
-    const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (unit >= m.units()) return;
+    const uint32_t wide = (m.T + 3) / 4, tile = blockIdx.x / wide;
+    const int t = (blockIdx.x - tile * wide) * 4 + (threadIdx.x >> 6);
+    if (t >= m.T) return;
+    const int64_t unit = (int64_t)tile * m.T + t;
     const Lane l;
-    const int o = (int)(unit / m.T) * 16 + l.r, k0 = (int)(unit % m.T) * kUnit + l.q * 8;
-    const T *row = w + o * w_row;
+    const int o = tile * 16 + l.r, k0 = t * kUnit + l.q * 8;
+    RowPart<T> part;
+    part.load(w + min(o, m.O - 1) * w_row, k0, o < m.O ? m.C : 0);
     float f[4][8];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        if (o < m.O) load_eight(row, k0 + 32 * j, m.C, f[j]);
-        else
+    for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[j][i] = 0.f;
-    }
+        for (int i = 0; i < 8; ++i) f[j][i] = (float)part.x[j][i];
     uint32_t code[4], word[4 / J];
 #pragma unroll
     for (int g = 0; g < 4 / J; ++g) {
-        float lo = 0.f, hi = 0.f, none = 0.f;  // none: NaN once a weight is not finite
+        float lo = 0.f, hi = 0.f;  // NaN once a weight is
 #pragma unroll
         for (int j = g * J; j < g * J + J; ++j)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                lo = fminf(lo, f[j][i]);
-                hi = fmaxf(hi, f[j][i]);
-                none = fmaf(f[j][i], 0.f, none);
+                lo = __builtin_elementwise_minimum(lo, f[j][i]);
+                hi = __builtin_elementwise_maximum(hi, f[j][i]);
             }
         lo = row_min(lo), hi = row_max(hi);
-        none += __shfl_xor(none, 16);
-        none += __shfl_xor(none, 32);
         const float all = hi - lo;
-        const bool bad = !(all <= 0x1.fffffep127f) || none != none;
+        const bool bad = !(all <= 0x1.fffffep127f);
         float s = __uint_as_float(__float_as_uint(all * (float)(1.0 / 15)) & ~15u);
         if (!(s >= kLeastScale)) s = 0.f;
         const float inv = s > 0.f ? 1.0f / s : 0.f, zero = fminf(fmaxf(rintf(-lo * inv), 0.f), 15.f);
         word[g] = bad ? kNaNWord : __float_as_uint(s) | (uint32_t)zero;
+        // w / s plus 3 2^22 has rne(w / s) in its lowest bits
+        const int from = (int)zero - __float_as_int(0x1.8p23f);
 #pragma unroll
         for (int j = g * J; j < g * J + J; ++j) {
             code[j] = 0;
-            if (bad) continue;
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                code[j] |= (uint32_t)fminf(fmaxf(rintf(f[j][i] * inv) + zero, 0.f), 15.f) << (4 * nibble(i));
+            for (int i = 0; i < 8; ++i) {
+                const int c = __float_as_int(f[j][i] * inv + 0x1.8p23f) + from;
+                code[j] |= (uint32_t)min(max(c, 0), 15) << (4 * nibble(i));
+            }
+            if (bad) code[j] = 0;
         }
     }
     reinterpret_cast<uint4 *>(m.codes)[unit * 64 + (threadIdx.x & 63)] = uint4{code[0], code[1], code[2], code[3]};
@@ -97,14 +114,17 @@ __global__ __launch_bounds__(256) void k_w4_pack(const T *__restrict__ w, int64_
 
 template <class T, int J>
 __global__ __launch_bounds__(256) void k_w4_unpack(W4 m, T *__restrict__ w) {
-    const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (unit >= m.units()) return;
+    const uint32_t wide = (m.T + 3) / 4, tile = blockIdx.x / wide;
+    const int t = (blockIdx.x - tile * wide) * 4 + (threadIdx.x >> 6);
+    if (t >= m.T) return;
+    const int64_t unit = (int64_t)tile * m.T + t;
     const Lane l;
-    const int o = (int)(unit / m.T) * 16 + l.r, k0 = (int)(unit % m.T) * kUnit + l.q * 8;
+    const int o = tile * 16 + l.r, k0 = t * kUnit + l.q * 8;
     if (o >= m.O) return;
     const uint4 all = reinterpret_cast<const uint4 *>(m.codes)[unit * 64 + (threadIdx.x & 63)];
     const uint32_t code[4] = {all.x, all.y, all.z, all.w};
     T *row = w + (int64_t)o * m.C;
+    const bool whole = k0 + 104 <= m.C;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const uint32_t word = m.words()[(unit * 16 + l.r) * (4 / J) + j / J];
@@ -117,7 +137,7 @@ __global__ __launch_bounds__(256) void k_w4_unpack(W4 m, T *__restrict__ w) {
 #pragma unroll
             for (int i = 0; i < V; ++i) f[i] = (float)((int)(code[j] >> (4 * nibble(v * V + i)) & 15) - zero) * s;
             const int k = k0 + 32 * j + v * V;
-            store_vector(row + k, m.C - k, f);
+            store_vector(row + k, whole ? V : m.C - k, f);
         }
     }
 }
@@ -179,58 +199,37 @@ struct Expand {
     }
 };
 
-// One row's part of a unit for a lane, four times eight inputs: as it is in memory,
+// Its inputs as operands; returns what their sums are to be multiplied by.
 template <class T>
-struct RowPart {
-    T x[4][8];
-    __device__ void load(const T *row, int k0, int C) {
-        if (k0 + 104 <= C) {
+__device__ float convert(const T (&x)[4][8], Piece (&a)[4][kPieces<T>]) {
+    if constexpr (std::is_same_v<T, _Float16>) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int i = 0; i < 8; i += kVec<T>) {
-                    const loose<T, kVec<T>> v = *reinterpret_cast<const loose<T, kVec<T>> *>(row + k0 + 32 * j + i);
+            for (int i = 0; i < 8; ++i) a[j][0].all[i] = x[j][i];
+        return 1.f;
+    } else {
+        float top = 0.f;
 #pragma unroll
-                    for (int e = 0; e < kVec<T>; ++e) x[j][i + e] = v[e];
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf((float)x[j][i]));
+        const int e = max((int)(__float_as_uint(row_max(top)) >> 23), 15);  // 15: 2^-112
+        const float down = __uint_as_float((uint32_t)(268 - e) << 23);     // 2^(14 - (e - 127)); e = 255 (infinity): 2^-114
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float2v v{(float)x[j][2 * i] * down, (float)x[j][2 * i + 1] * down};
+#pragma unroll
+                for (int n = 0; n < kPieces<T>; ++n) {
+                    a[j][n].p[i] = __builtin_convertvector(v, half2v);
+                    if (n + 1 < kPieces<T>) v -= __builtin_convertvector(a[j][n].p[i], float2v);
                 }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[j][i] = k0 + 32 * j + i < C ? row[k0 + 32 * j + i] : (T)0.f;
-        }
+            }
+        return __uint_as_float((uint32_t)(e - 14) << 23);
     }
-    // and as operands; returns what their sums are to be multiplied by.
-    __device__ float convert(Piece (&a)[4][kPieces<T>]) const {
-        if constexpr (std::is_same_v<T, _Float16>) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) a[j][0].all[i] = x[j][i];
-            return 1.f;
-        } else {
-            float top = 0.f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf((float)x[j][i]));
-            const int e = max((int)(__float_as_uint(row_max(top)) >> 23), 15);  // 15: 2^-112
-            const float down = __uint_as_float((uint32_t)(268 - e) << 23);     // 2^(14 - (e - 127)); e = 255 (infinity): 2^-114
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float2v v{(float)x[j][2 * i] * down, (float)x[j][2 * i + 1] * down};
-#pragma unroll
-                    for (int n = 0; n < kPieces<T>; ++n) {
-                        a[j][n].p[i] = __builtin_convertvector(v, half2v);
-                        if (n + 1 < kPieces<T>) v -= __builtin_convertvector(a[j][n].p[i], float2v);
-                    }
-                }
-            return __uint_as_float((uint32_t)(e - 14) << 23);
-        }
-    }
-};
+}
 
 // How a product is cut: a workgroup has `tiles` times `shares` wavefronts, one for each of its tiles of 16 outputs and each share
 // of the units (every shares-th), for 16 rows of x.  The rows of `chunk` units at a time are brought into fp16 by all of them and
@@ -250,7 +249,7 @@ struct Units {
 };
 
 template <class T, class Y, int J, int SHIFT>
-__global__ __launch_bounds__(512) void k_w4_matvec(const T *__restrict__ x, int64_t x_row, int32_t M, W4 m, Cut cut,
+__global__ __launch_bounds__(640) void k_w4_matvec(const T *__restrict__ x, int64_t x_row, int32_t M, W4 m, Cut cut,
                                                    const float *__restrict__ bias, int32_t silu_on, Y *__restrict__ y) {
     constexpr int P = kPieces<T>;
     constexpr bool kPowers = !std::is_same_v<T, _Float16>;
@@ -294,7 +293,7 @@ __global__ __launch_bounds__(512) void k_w4_matvec(const T *__restrict__ x, int6
         for (int u = first; t0 + u - (l.r >> shift) < end; u += step) {
             if (u != first) part.load(mine, min(t0 + u, m.T - 1) * kUnit + 8 * l.q, m.C);
             Piece a[4][P];
-            const float power = part.convert(a);
+            const float power = convert(part.x, a);
             if (t0 + u >= end) continue;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
@@ -380,14 +379,15 @@ Cut cut_of(int32_t M, const W4 &m, int tiles, int shares) {
     return c;
 }
 
-// Eight wavefronts: as many tiles as leave a workgroup for each of the 256 CUs (they share the rows' conversion), the units cut
-// among the rest; few units leave too little to a share (32 x 1280 -> 16640 fp32: 19 us with one share, 27 with two).
+// Up to ten wavefronts, which share the rows' conversion: as many tiles as leave one workgroup to each of the 256 CUs, in as few
+// rounds as ten tiles allow, and the units cut among what is left.
 template <class T>
 Cut cut_for(int32_t M, const W4 &m) {
-    int tiles = 4;
-    while (tiles > 1 && (int64_t)((m.R + tiles - 1) / tiles) * ((M + 15) / 16) < 256) tiles /= 2;
-    int shares = std::min(8 / tiles, m.T);
-    if (tiles == 4 && M > 4 && m.T < 16) shares = 1;
+    const int64_t blocks = (M + 15) / 16, all = m.R * blocks, rounds = (all + 2559) / 2560;
+    int tiles = (int)((all + 256 * rounds - 1) / (256 * rounds)), shares = 1;
+    while (shares * 2 * tiles <= 10 && shares * 2 <= m.T) shares *= 2;
+    // one conversion for all units, if ten wavefronts manage it
+    if (M > 4 && m.T <= 10 && tiles > 1 && tiles * shares < m.T) tiles = (m.T + shares - 1) / shares;
     return cut_of<T>(M, m, tiles, shares);
 }
 
@@ -402,7 +402,7 @@ hipError_t launch_w4_pack(const void *w, int32_t dtype, int64_t w_row, const W4 
     by_dtype(dtype, [&](auto t) {
         using T = decltype(t);
         by_group(m.group, [&](auto j) {
-            k_w4_pack<T, j.value><<<(unsigned)((m.units() + 3) / 4), 256, 0, st>>>(static_cast<const T *>(w), w_row, m);
+            k_w4_pack<T, j.value><<<(unsigned)m.R * ((m.T + 3) / 4), 256, 0, st>>>(static_cast<const T *>(w), w_row, m);
         });
     });
     return hipGetLastError();
@@ -412,7 +412,7 @@ hipError_t launch_w4_unpack(const W4 &m, int32_t dtype, void *w, hipStream_t st)
     by_dtype(dtype, [&](auto t) {
         using T = decltype(t);
         by_group(m.group, [&](auto j) {
-            k_w4_unpack<T, j.value><<<(unsigned)((m.units() + 3) / 4), 256, 0, st>>>(m, static_cast<T *>(w));
+            k_w4_unpack<T, j.value><<<(unsigned)m.R * ((m.T + 3) / 4), 256, 0, st>>>(m, static_cast<T *>(w));
         });
     });
     return hipGetLastError();
