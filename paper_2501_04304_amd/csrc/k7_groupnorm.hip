@@ -91,15 +91,16 @@ __device__ double2 lane_sums(double2 s, int lanes) {
     return s;
 }
 
-// Sum of n entries, each lane's from `from` on and `stride` apart, eight reads at a time; over `lanes` neighbours.
+// Sum of n entries, each lane's from `from` on and `stride` apart, sixteen reads at a time; over `lanes` neighbours.
 __device__ double2 strided_sum(const double2 *entries, int64_t n, int from, int stride, int lanes) {
+    constexpr int AT_ONCE = 16;
     double2 s{0, 0};
-    for (int64_t i = from; i < n; i += 8 * stride) {
-        double2 e[8];
+    for (int64_t i = from; i < n; i += AT_ONCE * stride) {
+        double2 e[AT_ONCE];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) e[u] = i + u * stride < n ? entries[i + u * stride] : double2{0, 0};
+        for (int u = 0; u < AT_ONCE; ++u) e[u] = i + u * stride < n ? entries[i + u * stride] : double2{0, 0};
 #pragma unroll
-        for (int u = 0; u < 8; ++u) s = sum_of(s, e[u]);
+        for (int u = 0; u < AT_ONCE; ++u) s = sum_of(s, e[u]);
     }
     return lane_sums(s, lanes);
 }
@@ -156,7 +157,7 @@ __global__ __launch_bounds__(kMaxThreads) void k_gn_sums(const T *__restrict__ x
                                                          int32_t G, const float *__restrict__ add, int64_t add_row,
                                                          double2 *__restrict__ sums, int32_t parts) {
     constexpr int V = kVec<T>;
-    extern __shared__ double2 entries[];  // [high][width] where vectors end with their groups, else [high][width V]
+    extern __shared__ double2 entries[];  // [values of a vector, or 1 where vectors end with their groups][high][width]
     const int tid = threadIdx.x, high = sh.threads / sh.width, wide = sh.width * V;
     const int pr = tid / sh.width, c_slice = blockIdx.y * wide, c0 = c_slice + (tid - pr * sh.width) * V, have = min(V, C - c0);
     const bool on = pr < high && have > 0;
@@ -184,23 +185,31 @@ __global__ __launch_bounds__(kMaxThreads) void k_gn_sums(const T *__restrict__ x
                 }
         }
         __syncthreads();
-        if (pr < high) {
-            if (each == 1) {
+        if (each == 1) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) entries[tid * V + i] = {s[i], ss[i]};
-            } else {
-                double2 sum{0, 0};
+            for (int i = 0; i < V; ++i) entries[i * sh.threads + tid] = {s[i], ss[i]};
+        } else {
+            double2 sum{0, 0};
 #pragma unroll
-                for (int i = 0; i < V; ++i) sum = sum_of(sum, {s[i], ss[i]});
-                entries[tid] = sum;
-            }
+            for (int i = 0; i < V; ++i) sum = sum_of(sum, {s[i], ss[i]});
+            entries[tid] = sum;
+        }
+        __syncthreads();
+        // over the rows, into the first of them
+        for (int e = tid; e < sh.width * (V / each); e += sh.threads) {
+            const int i = e / sh.width;
+            double2 *column = entries + i * sh.threads + (e - i * sh.width);
+            double2 sum = column[0];
+#pragma unroll 4
+            for (int p = 1; p < high; ++p) sum = sum_of(sum, column[p * sh.width]);
+            column[0] = sum;
         }
         __syncthreads();
         for (int g = tid / lanes; g < G; g += sh.threads / lanes) {
-            const int lo = (max(g * Cg, c_slice) - c_slice) / each, n_here = (min((g + 1) * Cg, c_end) - c_slice) / each - lo;
+            const int lo = (max(g * Cg, c_slice) - c_slice) / each, end = (min((g + 1) * Cg, c_end) - c_slice) / each;
             double2 sum{0, 0};
-            for (int p = 0; p < high; ++p)
-                for (int e = tid & (lanes - 1); e < n_here; e += lanes) sum = sum_of(sum, entries[p * (wide / each) + lo + e]);
+            for (int e = lo + (tid & (lanes - 1)); e < end; e += lanes)
+                sum = sum_of(sum, each == 1 ? entries[e % V * sh.threads + e / V] : entries[e]);
             sum = lane_sums(sum, lanes);
             if ((tid & (lanes - 1)) == 0) sums[((int64_t)g * parts + part) * sh.slices + blockIdx.y] = sum;
         }
@@ -423,13 +432,13 @@ __global__ __launch_bounds__(THREADS) void k_gn_one(const T *x, Images im, Rows 
 
 // ---- launches --------------------------------------------------------------------------------------------------------
 
-// Of workgroups of half to all of `most` threads, the largest of those with most threads that have a vector of their own.
+// Of workgroups of half to all of `most` threads, the one with most threads that have a vector of their own, as long as few idle.
 Shape shape_for(int32_t C, int V, int32_t most) {
     const int32_t vectors = (C + V - 1) / V, slices = (vectors + most - 1) / most, width = (vectors + slices - 1) / slices;
-    int32_t best = 0, threads = 0;
+    int32_t best = 0, threads = most;
     for (int32_t t = most / 2; t <= most; t += 64) {
-        const int32_t used = 1024 * (t / width * width) / t;  // share in use
-        if (used >= best) best = used, threads = t;
+        const int32_t used = t / width * width;
+        if (used > best && 8 * used >= 7 * t) best = used, threads = t;
     }
     return {threads, width, slices};
 }
@@ -444,9 +453,7 @@ Chunks chunks_for(const NormCall &n, const Shape &sh, int64_t most) {
     return {P, (int32_t)(per * n.B), (int32_t)per};
 }
 
-// Workgroups of the two streaming kernels: one to a CU, two where an image then still has few parts to be added up by all (16 x
-// 4096 x 640 fp32 107 us, 110 with one; 1 x 1048576 x 128 fp16 175 and 171).
-int64_t chunk_count(int32_t B) { return B >= 8 ? 512 : 256; }
+constexpr int64_t kChunks = 256;  // workgroups of the two streaming kernels, one to a CU: more add their own beginnings and ends
 constexpr int64_t kMaxFolded = 16384;  // sums of an image that every workgroup may read
 
 // Whether a workgroup can hold an image's group, and how: threads and vectors of each (0: it cannot, or is slower: long stripes
@@ -472,7 +479,7 @@ struct NormPlan {
     Chunks chunks;
     int32_t parts = 0;
     size_t sums_bytes = 0, tables_bytes = 0;  // tables_bytes 0: the last kernel makes them itself
-    explicit NormPlan(const NormCall &n) : hold(hold_for(n)), shape(shape_for(n.C, n.dtype == DGQ_F32 ? 4 : 8, kMaxThreads)), chunks(chunks_for(n, shape, chunk_count(n.B))) {
+    explicit NormPlan(const NormCall &n) : hold(hold_for(n)), shape(shape_for(n.C, n.dtype == DGQ_F32 ? 4 : 8, kMaxThreads)), chunks(chunks_for(n, shape, kChunks)) {
         if (hold.held) return;
         parts = chunks.count + (n.offsets ? n.B : 0);
         sums_bytes = (size_t)n.G * parts * shape.slices * sizeof(double2);
