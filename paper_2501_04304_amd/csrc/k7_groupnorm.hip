@@ -83,6 +83,26 @@ struct Shape {
     int32_t threads, width, slices;  // slices of `width` vectors over the channels (blockIdx.y)
 };
 
+// A thread's vector of a slice: channels c0 .. c0 + V - 1.  The last vector of all ends with the channels, and the first `again`
+// of its values are the vector before's; `have`: values of its own (0: no vector).  Fewer channels than V: `have` values, no more.
+template <class T>
+struct Place {
+    int pr, high, c_slice, wide, c0, again, have;
+    bool on;  // a row and a vector
+    __device__ Place(const Shape &sh, int32_t C) {
+        constexpr int V = kVec<T>;
+        const int tid = threadIdx.x;
+        high = sh.threads / sh.width, wide = sh.width * V;
+        pr = tid / sh.width;
+        c_slice = blockIdx.y * wide;
+        const int c = c_slice + (tid - pr * sh.width) * V;
+        have = max(min(V, C - c), 0);
+        again = C >= V && have > 0 ? V - have : 0;
+        c0 = c - again;
+        on = pr < high && have > 0;
+    }
+};
+
 // ---- sums ------------------------------------------------------------------------------------------------------------
 __device__ double2 sum_of(double2 a, double2 b) { return {a.x + b.x, a.y + b.y}; }
 // over `lanes` (a power of two) neighbouring lanes
@@ -114,10 +134,10 @@ struct RowsOf {
     using Vec = loose<T, V>;
     const T *row;
     int64_t step;
-    int n, have;
+    int n, few;  // few: values to a row, where they fill no vector
     Vec now[kAhead];
-    __device__ RowsOf(const T *first, int64_t step_, int n_, int have_) : row(first), step(step_), n(n_), have(have_) {
-        if (have >= V) fetch(now, 0);
+    __device__ RowsOf(const T *first, int64_t step_, int n_, int few_) : row(first), step(step_), n(n_), few(few_) {
+        if (!few) fetch(now, 0);
     }
     __device__ void fetch(Vec (&to)[kAhead], int i) const {
 #pragma unroll
@@ -127,7 +147,7 @@ struct RowsOf {
     template <class F>
     __device__ void each(F f) {
         float x[V];
-        if (have >= V) {
+        if (!few) {
             for (int i = 0; i < n; i += kAhead) {
                 Vec next[kAhead];
                 fetch(next, i + kAhead);
@@ -144,7 +164,7 @@ struct RowsOf {
             }
         } else {
             for (int i = 0; i < n; ++i) {
-                load_vector(row + i * step, have, x);
+                load_vector(row + i * step, few, x);
                 f(i, x);
             }
         }
@@ -158,18 +178,17 @@ __global__ __launch_bounds__(kMaxThreads) void k_gn_sums(const T *__restrict__ x
                                                          double2 *__restrict__ sums, int32_t parts) {
     constexpr int V = kVec<T>;
     extern __shared__ double2 entries[];  // [values of a vector, or 1 where vectors end with their groups][high][width]
-    const int tid = threadIdx.x, high = sh.threads / sh.width, wide = sh.width * V;
-    const int pr = tid / sh.width, c_slice = blockIdx.y * wide, c0 = c_slice + (tid - pr * sh.width) * V, have = min(V, C - c0);
-    const bool on = pr < high && have > 0;
-    const int Cg = C / G, c_end = min(c_slice + wide, C), each = Cg % V ? 1 : V;  // channels of an entry
+    const int tid = threadIdx.x;
+    const Place<T> at(sh, C);
+    const int high = at.high, c_slice = at.c_slice, c_end = min(c_slice + at.wide, C), Cg = C / G, each = Cg % V ? 1 : V;  // channels of an entry
     // neighbouring lanes that share a group's entries
     int lanes = 64;
     while (lanes > 1 && lanes * G > sh.threads) lanes >>= 1;
     ch.each(im, blockIdx.x, [&](int32_t b, int32_t part, int64_t r0, int64_t r1) {
         double s[V] = {}, ss[V] = {};
-        if (on) {
-            const int n = (int)(r1 - r0 - pr + high - 1) / high;
-            RowsOf<T>(x + xs.at(im, b, r0 + pr) + c0, high * xs.row, n, have).each([&](int, const float (&f)[V]) {
+        if (at.on) {
+            const int n = (int)(r1 - r0 - at.pr + high - 1) / high;
+            RowsOf<T>(x + xs.at(im, b, r0 + at.pr) + at.c0, high * xs.row, n, C < V ? at.have : 0).each([&](int, const float (&f)[V]) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     s[i] += (double)f[i];
@@ -179,7 +198,7 @@ __global__ __launch_bounds__(kMaxThreads) void k_gn_sums(const T *__restrict__ x
             if (add)
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    const double d = j < have ? add[b * add_row + c0 + j] : 0.f;
+                    const double d = j < at.again + at.have ? add[b * add_row + at.c0 + j] : 0.f;
                     ss[j] += d * (2 * s[j] + n * d);
                     s[j] += n * d;
                 }
@@ -187,7 +206,8 @@ __global__ __launch_bounds__(kMaxThreads) void k_gn_sums(const T *__restrict__ x
         __syncthreads();
         if (each == 1) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) entries[i * sh.threads + tid] = {s[i], ss[i]};
+            for (int i = 0; i < V; ++i)
+                if (i >= at.again) entries[(i - at.again) * sh.threads + tid] = {s[i], ss[i]};  // (none reads what that leaves out)
         } else {
             double2 sum{0, 0};
 #pragma unroll
@@ -269,7 +289,7 @@ __global__ __launch_bounds__(256) void k_gn_tables(const double2 *__restrict__ s
 }
 
 // ---- values ----------------------------------------------------------------------------------------------------------
-// Bound by the bytes of x and y.  x and y may be one buffer: a thread writes what it alone has read.  tables null: every workgroup
+// Bound by the bytes of x and y.  x and y may be one buffer.  tables null: every workgroup
 // adds up the sums of its image itself, which costs less than a launch that does it once, as long as they are few.
 template <class T, class Y>
 __global__ __launch_bounds__(kMaxThreads) void k_gn_apply(const T *x, Images im, Rows xs, Chunks ch, Shape sh, int32_t C, int32_t G,
@@ -278,49 +298,52 @@ __global__ __launch_bounds__(kMaxThreads) void k_gn_apply(const T *x, Images im,
                                                           const float *__restrict__ bias, float eps, NormTerms terms, int32_t silu_on,
                                                           Y *y) {
     constexpr int V = kVec<T>;
-    extern __shared__ float lines[];  // [p, a, q][width V], and in front of them the groups' m and r
-    const int tid = threadIdx.x, high = sh.threads / sh.width, pr = tid / sh.width, wide = sh.width * V, Cg = C / G;
-    const int c_slice = blockIdx.y * wide, c0 = c_slice + (tid - pr * sh.width) * V, have = min(V, C - c0);
+    extern __shared__ float lines[];  // the groups' m and r, [p, a, q][width V + V]
+    const int tid = threadIdx.x, Cg = C / G;
+    const Place<T> at(sh, C);
+    const int high = at.high, c_slice = at.c_slice, wide = at.wide;
+    const bool same = static_cast<const void *>(x) == y;
     int lanes = 64;
     while (lanes > 1 && lanes * G > sh.threads) lanes >>= 1;
     ch.each(im, blockIdx.x, [&](int32_t b, int32_t, int64_t r0, int64_t r1) {
         float p[V], a[V], q[V];
         const float *from;
         int64_t stride;
-        const bool on = pr < high && have > 0;
-        RowsOf<T> rows(x + xs.at(im, b, r0 + pr) + c0, high * xs.row, on ? (int)(r1 - r0 - pr + high - 1) / high : 0, have);
+        RowsOf<T> rows(x + xs.at(im, b, r0 + at.pr) + at.c0, high * xs.row, at.on ? (int)(r1 - r0 - at.pr + high - 1) / high : 0,
+                       C < V ? at.have : 0);
         if (tables) {
-            from = tables + (int64_t)b * 3 * C + c0;
+            from = tables + (int64_t)b * 3 * C + at.c0;
             stride = C;
         } else {
             Group *groups = reinterpret_cast<Group *>(lines);
             float *to = lines + G * (sizeof(Group) / sizeof(float));
             const int64_t first = ch.first(im, b), n_parts = (int64_t)ch.parts(im, b) * sh.slices;
             const double per = 1 / ((double)(im.end(b) - im.start(b)) * Cg);
-            const int c_end = min(c_slice + wide, C);
+            // (the last vector of all may begin in front of its slice)
+            const int c_first = max(c_slice - V, 0), c_end = min(c_slice + wide, C), room = wide + V;
             Terms mine{};
-            if (c_slice + tid < c_end) mine = Terms::of(terms, weight, bias, b, c_slice + tid);
+            if (c_first + tid < c_end) mine = Terms::of(terms, weight, bias, b, c_first + tid);
             __syncthreads();
             for (int g = tid / lanes; g < G; g += sh.threads / lanes) {
                 const double2 s = strided_sum(sums + ((int64_t)g * parts + first) * sh.slices, n_parts, tid & (lanes - 1), lanes, lanes);
                 if ((tid & (lanes - 1)) == 0) groups[g] = Group(s, per, eps);
             }
             __syncthreads();
-            for (int c = c_slice + tid; c < c_end; c += sh.threads) {
-                const Line line = groups[c / Cg].line(c == c_slice + tid ? mine : Terms::of(terms, weight, bias, b, c));
-                float *t = to + c - c_slice;
-                t[0] = line.p, t[wide] = line.a, t[2 * wide] = line.q;
+            for (int c = c_first + tid; c < c_end; c += sh.threads) {
+                const Line line = groups[c / Cg].line(c == c_first + tid ? mine : Terms::of(terms, weight, bias, b, c));
+                float *t = to + c - c_first;
+                t[0] = line.p, t[room] = line.a, t[2 * room] = line.q;
             }
             __syncthreads();
-            from = to + c0 - c_slice;
-            stride = wide;
+            from = to + at.c0 - c_first;
+            stride = room;
         }
-        if (!on) return;
+        if (!at.on) return;
 #pragma unroll
         for (int i = 0; i < V; ++i)
-            if (i < have) p[i] = from[i], a[i] = from[stride + i], q[i] = from[2 * stride + i];
+            if (i < at.again + at.have) p[i] = from[i], a[i] = from[stride + i], q[i] = from[2 * stride + i];
             else p[i] = a[i] = q[i] = 0.f;
-        Y *to = y + (r0 + pr) * C + c0;
+        Y *to = y + (r0 + at.pr) * C + at.c0;
         rows.each([&](int r, const float (&f)[V]) {
             float v[V];
 #pragma unroll
@@ -328,7 +351,14 @@ __global__ __launch_bounds__(kMaxThreads) void k_gn_apply(const T *x, Images im,
             if (silu_on)
 #pragma unroll
                 for (int i = 0; i < V; ++i) v[i] = silu(v[i]);
-            store_vector(to + (int64_t)r * high * C, have, v);
+            Y *row = to + (int64_t)r * high * C;
+            if (same && at.again) {  // what two vectors share is written by the first; the second may have read it anew
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (i >= at.again) row[i] = (Y)v[i];
+            } else {
+                store_vector(row, at.again + at.have, v);
+            }
         });
     });
 }
@@ -443,22 +473,32 @@ Shape shape_for(int32_t C, int V, int32_t most) {
     return {threads, width, slices};
 }
 
-Chunks chunks_for(const NormCall &n, const Shape &sh, int64_t most) {
+constexpr int64_t kChunks = 256;  // workgroups of the two streaming kernels, one to a CU: more add their own beginnings and ends
+Chunks chunks_for(const NormCall &n, const Shape &sh) {
     const int64_t rows = n.rows(), high = sh.threads / sh.width;
-    int64_t P = (rows + most - 1) / most;
-    P = (P + high - 1) / high * high;
-    if (n.offsets) return {P, (int32_t)((rows + P - 1) / P), 0};
-    const int64_t per = (n.N + P - 1) / P;
-    P = ((n.N + per - 1) / per + high - 1) / high * high;  // the chunks of an image alike
+    auto up = [&](int64_t r) { return (r + high - 1) / high * high; };
+    if (n.offsets) {
+        const int64_t P = up((rows + kChunks - 1) / kChunks);
+        return {P, (int32_t)((rows + P - 1) / P), 0};
+    }
+    // chunks of an image alike, in the number of rounds that costs least: a round takes its rows and some 5 us, 100 KB of them
+    const int64_t extra = 100000 / ((int64_t)n.C * (n.dtype == DGQ_F32 ? 4 : 2));
+    int64_t per = 1, least = INT64_MAX;
+    for (int64_t rounds = 1; rounds <= 4; ++rounds) {
+        const int64_t p = std::min(std::max<int64_t>(kChunks * rounds / n.B, 1), (n.N + high - 1) / high);
+        const int64_t cost = (p * n.B + kChunks - 1) / kChunks * (up((n.N + p - 1) / p) + extra);
+        if (cost < least) least = cost, per = p;
+    }
+    const int64_t P = up((n.N + per - 1) / per);
+    per = (n.N + P - 1) / P;
     return {P, (int32_t)(per * n.B), (int32_t)per};
 }
 
-constexpr int64_t kChunks = 256;  // workgroups of the two streaming kernels, one to a CU: more add their own beginnings and ends
 constexpr int64_t kMaxFolded = 16384;  // sums of an image that every workgroup may read
 
 // Whether a workgroup can hold an image's group, and how: threads and vectors of each (0: it cannot, or is slower: long stripes
-// touch a line of memory in every row and need most CUs to keep up.  2 x 1024 x 1280 fp32 10.7 us, 14.9 with sums of chunks; 2 x
-// 4096 x 320 16.7 and 14.8, 8 x 4096 x 320 23.8 and 26.3).
+// touch a line of memory in every row, many values keep its vector pipes busy, and both need most CUs to keep up.  2 x 1024 x 1280
+// fp32 10.7 us, 14.9 with sums of chunks; 2 x 4096 x 320 16.7 and 14.8, 8 x 4096 x 320 23.8 and 26.3).
 struct Hold {
     int32_t threads = 0, held = 0, width = 0;
 };
@@ -466,7 +506,7 @@ Hold hold_for(const NormCall &n) {
     const int32_t V = n.dtype == DGQ_F32 ? 4 : 8, Cg = n.C / n.G, width = (Cg + V - 1) / V;
     if (Cg < V || width > 256) return {};
     const int64_t rows = n.offsets ? n.N / n.B * 3 / 2 : n.N;  // of a long image
-    if (rows > 2048 && (int64_t)n.B * n.G < 192) return {};
+    if ((rows > 2048 || rows * Cg > 65536) && (int64_t)n.B * n.G < 192) return {};
     const Hold ways[] = {{256, 4, width}, {1024, 4, width}, {1024, 8, width}, {1024, 16, width}};
     for (const Hold &h : ways)
         if (rows <= (int64_t)h.held * (h.threads / width)) return h;
@@ -479,7 +519,7 @@ struct NormPlan {
     Chunks chunks;
     int32_t parts = 0;
     size_t sums_bytes = 0, tables_bytes = 0;  // tables_bytes 0: the last kernel makes them itself
-    explicit NormPlan(const NormCall &n) : hold(hold_for(n)), shape(shape_for(n.C, n.dtype == DGQ_F32 ? 4 : 8, kMaxThreads)), chunks(chunks_for(n, shape, kChunks)) {
+    explicit NormPlan(const NormCall &n) : hold(hold_for(n)), shape(shape_for(n.C, n.dtype == DGQ_F32 ? 4 : 8, kMaxThreads)), chunks(chunks_for(n, shape)) {
         if (hold.held) return;
         parts = chunks.count + (n.offsets ? n.B : 0);
         sums_bytes = (size_t)n.G * parts * shape.slices * sizeof(double2);
@@ -545,7 +585,7 @@ hipError_t launch_groupnorm(const NormCall &n, void *workspace, hipStream_t st) 
                 e = launch_one<T, Y>(n, p.hold, im, xs, st);
                 return;
             }
-            const int bytes = tables ? 0 : n.G * (int)sizeof(Group) + 3 * p.shape.width * kVec<T> * (int)sizeof(float);
+            const int bytes = tables ? 0 : n.G * (int)sizeof(Group) + 3 * (p.shape.width + 1) * kVec<T> * (int)sizeof(float);
             e = DGQ_ENSURE_LDS((k_gn_apply<T, Y>), bytes);
             if (e == hipSuccess)
                 k_gn_apply<T, Y><<<grid, p.shape.threads, bytes, st>>>(x, im, xs, p.chunks, p.shape, n.C, n.G, tables, sums, p.parts,

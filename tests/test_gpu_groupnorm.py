@@ -60,7 +60,8 @@ ALL = ("weight", "bias", "add", "scale", "shift")
 SIZES = [(1, 1, 1, 1), (1, 1, 32, 32), (3, 1, 40, 8), (2, 7, 30, 30), (2, 64, 37, 1), (1, 100, 90, 30), (5, 33, 129, 3),
          (2, 256, 320, 32), (2, 64, 1280, 32), (1, 4099, 128, 32), (300, 3, 24, 4), (2, 50, 2560, 32), (1, 9, 5000, 8),
          (1, 5, 9001, 1), (4, 1024, 320, 32), (1, 20000, 16, 4),
-         (1, 3000, 256, 256), (2, 6, 4096, 4096), (7, 600, 320, 32), (6, 2100, 320, 32), (3, 300, 516, 4), (9, 513, 264, 24)]
+         (1, 3000, 256, 256), (2, 6, 4096, 4096), (7, 600, 320, 32), (6, 2100, 320, 32), (3, 300, 516, 4), (9, 513, 264, 24),
+         (2, 700, 999, 3), (1, 900, 4099, 1), (40, 300, 259, 7), (12, 64, 1926, 1)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -165,11 +166,11 @@ def test_strides(dgq, N, dtype):
     _check(out, *ref.groupnorm(np.concatenate([on] * 3), *_even(3, N), G, add=np.stack([emb[0, :C]] * 3), out_type=dtype))
 
 
-@pytest.mark.parametrize("N", [64, 6000])
-def test_in_place_and_workspace(dgq, N):
+@pytest.mark.parametrize("N,C", [(64, 320), (6000, 320), (50, 333), (3000, 333)])
+def test_in_place_and_workspace(dgq, N, C):
     import torch
     rng = np.random.default_rng(10)
-    B, C, G = 2, 320, 32
+    B, G = 2, C // 10 if C == 320 else 9
     x, xn = _map(rng, B * N, C, "fp16")
     x = x.view(B, N, C)
     other = dgq.dgq_groupnorm(x, G)
@@ -178,7 +179,7 @@ def test_in_place_and_workspace(dgq, N):
     assert torch.equal(x, other)
     assert (ws[-16:] == 255).all()
     with pytest.raises(dgq.DgqError, match="workspace"):
-        dgq.dgq_groupnorm(torch.zeros((2, 9000, 320), device="cuda"), G, workspace=ws[:16])
+        dgq.dgq_groupnorm(torch.zeros((2, 9000, C), device="cuda"), G, workspace=ws[:16])
 
 
 @pytest.mark.parametrize("N", [64, 5000])
