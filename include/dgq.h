@@ -731,18 +731,22 @@ int dgq_w4_unpack(const void *data, int32_t O, int32_t C, int32_t group, int32_t
 
 /*
  * Products with such weights: y[m, o] = act(sum_k x[m, k] s (code[o, k] - zero) + bias[o]).  For few rows, whose time is the
- * weights' bytes; any number is taken (64 rows at a time, which read the weights anew).
+ * weights' bytes; any number is taken (16 rows at a time, which read the weights anew).
  *   x     [M, C] of `dtype`, inputs contiguous, rows x_row_stride elements apart, aligned to an element
  *   bias  fp32 [O], or NULL
  *   y     [M, O] of out_dtype (dtype or fp32), contiguous
+ *   workspace dgq_w4_matvec_workspace_bytes(...) bytes, 16-byte aligned (0 bytes: NULL): few outputs of many inputs are cut
+ *         over the chip along the inputs and joined by a second kernel
  * fp32 rows count with 23 bits, fp16 and bf16 ones with all of theirs (bf16 and fp32: elements 2^29 below the largest of their
  * 128 inputs: to 2^-39 of that); codes less zeros are exact, sums are fp32 and rounded once to y.  NaN or infinity in a row of x
  * makes that row not finite, no other.
  * The same call gives the same bits; the order of the sums goes by the sizes.  Enqueues on `stream`; neither synchronises nor
  * allocates.
  */
+size_t dgq_w4_matvec_workspace_bytes(int32_t M, int32_t O, int32_t C);
 int dgq_w4_matvec(const void *x, int32_t dtype, int64_t x_row_stride, int32_t M, const void *data, int32_t O, int32_t C,
-                  int32_t group, const float *bias, int32_t act, void *y, int32_t out_dtype, void *stream);
+                  int32_t group, const float *bias, int32_t act, void *y, int32_t out_dtype, void *workspace,
+                  size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

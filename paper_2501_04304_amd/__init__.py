@@ -114,7 +114,9 @@ def lib():
         L.dgq_w4_bytes.restype = sz
         L.dgq_w4_pack.argtypes = [vp, i32, i64, i32, i32, i32, vp, vp]
         L.dgq_w4_unpack.argtypes = [vp, i32, i32, i32, i32, vp, vp]
-        L.dgq_w4_matvec.argtypes = [vp, i32, i64, i32, vp, i32, i32, i32, vp, i32, vp, i32, vp]
+        L.dgq_w4_matvec_workspace_bytes.argtypes = [i32, i32, i32]
+        L.dgq_w4_matvec_workspace_bytes.restype = sz
+        L.dgq_w4_matvec.argtypes = [vp, i32, i64, i32, vp, i32, i32, i32, vp, i32, vp, i32, vp, sz, vp]
         L.dgq_last_error.restype = C.c_char_p
         L.dgq_version.restype = C.c_int
         _lib = L
@@ -593,8 +595,12 @@ def dgq_w4_unpack(weight: W4Weight, dtype=None, out=None, stream=None):
     return (_hot or _load_hot()).w4_unpack(weight.data, weight.out_channels, weight.in_channels, weight.group, dtype, out, stream)
 
 
-def dgq_w4_matvec(x, weight: W4Weight, bias=None, act: int = ACT_NONE, dtype=None, out=None, stream=None):
+def dgq_w4_matvec_workspace_bytes(rows: int, out_channels: int, in_channels: int) -> int:
+    return int(lib().dgq_w4_matvec_workspace_bytes(rows, out_channels, in_channels))
+
+
+def dgq_w4_matvec(x, weight: W4Weight, bias=None, act: int = ACT_NONE, dtype=None, out=None, workspace=None, stream=None):
     """act(x W^T + bias) for the few rows of x [rows, in_channels] (fp32, fp16 or bf16, inputs contiguous): [rows,
     out_channels] of `dtype` (x's type, or float32).  bias: fp32 [out_channels]."""
     return (_hot or _load_hot()).w4_matvec(x, weight.data, weight.out_channels, weight.in_channels, weight.group, bias, act, dtype,
-                                           out, stream)
+                                           out, workspace, stream)

@@ -1509,8 +1509,14 @@ int dgq_w4_unpack(const void *data, int32_t O, int32_t C, int32_t group, int32_t
     return DGQ_OK;
 }
 
+size_t dgq_w4_matvec_workspace_bytes(int32_t M, int32_t O, int32_t C) {
+    if (M < 1 || M > kMaxChannels || !w4_sizes_ok(O, C, 128)) return 0;
+    return w4_matvec_workspace_bytes(M, W4{nullptr, O, C, 128, (O + 15) / 16, (C + 127) / 128});
+}
+
 int dgq_w4_matvec(const void *x, int32_t dtype, int64_t x_row_stride, int32_t M, const void *data, int32_t O, int32_t C,
-                  int32_t group, const float *bias, int32_t act, void *y, int32_t out_dtype, void *stream) {
+                  int32_t group, const float *bias, int32_t act, void *y, int32_t out_dtype, void *workspace,
+                  size_t workspace_bytes, void *stream) {
     W4 m;
     if (const int rc = w4_of("dgq_w4_matvec", data, O, C, group, &m)) return rc;
     if (!kv_dtype_ok(dtype)) return fail(DGQ_EINVAL, "dgq_w4_matvec: bad dtype");
@@ -1522,7 +1528,10 @@ int dgq_w4_matvec(const void *x, int32_t dtype, int64_t x_row_stride, int32_t M,
     if (M > kMaxChannels) return fail(DGQ_EUNSUPPORTED, "dgq_w4_matvec: more than 2^20 rows");
     if (!aligned_to(x, dtype) || !aligned_to(y, out_dtype) || !aligned_to(bias, DGQ_F32))
         return fail(DGQ_EALIGN, "dgq_w4_matvec: tensor not aligned to its elements");
-    DGQ_HIP(launch_w4_matvec({x, dtype, x_row_stride, M, bias, act, y, out_dtype}, m, static_cast<hipStream_t>(stream)));
+    const size_t need = w4_matvec_workspace_bytes(M, m);
+    if (need && (!workspace || workspace_bytes < need || !aligned16(workspace)))
+        return fail(DGQ_EWORKSPACE, "dgq_w4_matvec: workspace missing, too small or misaligned");
+    DGQ_HIP(launch_w4_matvec({x, dtype, x_row_stride, M, bias, act, y, out_dtype}, m, workspace, static_cast<hipStream_t>(stream)));
     return DGQ_OK;
 }
 

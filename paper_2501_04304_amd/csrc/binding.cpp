@@ -853,10 +853,10 @@ PyObject *w4_unpack(Args a) {
     return one(a[5], out);
 }
 
-// (x, data, out_channels, in_channels, group, bias, act, dtype, out, stream)
+// (x, data, out_channels, in_channels, group, bias, act, dtype, out, workspace, stream)
 PyObject *w4_matvec(Args a) {
     const W4In m(a + 1);
-    const Place place(a[9], m.data);
+    const Place place(a[10], m.data);
     const at::Tensor &x = floats(a[0], "x", 2);
     if (x.size(1) != m.C) raise_value("x must be [rows, in_channels] of the weight");
     if (x.size(0) > INT32_MAX) raise_value("x is too large");
@@ -864,11 +864,19 @@ PyObject *w4_matvec(Args a) {
     const int32_t M = (int32_t)x.size(0), act = integer32(a[6]);
     const float *bp = vector_of(a[5], "bias", m.O, place);
     const at::Tensor out = output(a[8], a[7], x.scalar_type(), {M, m.O}, x, place, "out");
+    at::Tensor ws;
+    if (given(a[9])) {
+        ws = tensor(a[9], at::kByte, "workspace");
+        place.same(ws, "workspace");
+    } else if (const size_t need = dgq_w4_matvec_workspace_bytes(M, m.O, m.C)) {
+        ws = empty({(int64_t)need}, at::kByte, x);
+    }
     const void *xp = x.data_ptr(), *dp = m.data.data_ptr();
-    void *yp = out.data_ptr();
+    void *yp = out.data_ptr(), *wp = ws.defined() ? ws.data_ptr() : nullptr;
+    const size_t wb = ws.defined() ? (size_t)ws.numel() : 0;
     enqueue([&] {
         return dgq_w4_matvec(xp, kv_dtype(x.scalar_type()), step(x, 0), M, dp, m.O, m.C, m.group, bp, act, yp,
-                             kv_dtype(out.scalar_type()), place.stream());
+                             kv_dtype(out.scalar_type()), wp, wb, place.stream());
     });
     return one(a[8], out);
 }
@@ -914,7 +922,7 @@ PyMethodDef kMethods[] = {
     DGQ_METHOD(groupnorm, 14),
     DGQ_METHOD(w4_pack, 6),
     DGQ_METHOD(w4_unpack, 7),
-    DGQ_METHOD(w4_matvec, 10),
+    DGQ_METHOD(w4_matvec, 11),
     {"set_error_class", set_error_class, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };

@@ -303,7 +303,8 @@ struct W4Product {
 };
 hipError_t launch_w4_pack(const void *w, int32_t dtype, int64_t w_row, const W4 &m, hipStream_t st);
 hipError_t launch_w4_unpack(const W4 &m, int32_t dtype, void *w, hipStream_t st);
-hipError_t launch_w4_matvec(const W4Product &p, const W4 &m, hipStream_t st);
+size_t w4_matvec_workspace_bytes(int32_t M, const W4 &m);
+hipError_t launch_w4_matvec(const W4Product &p, const W4 &m, void *workspace, hipStream_t st);
 
 size_t xattn_workspace_bytes(int32_t B, int32_t N, int32_t H, int32_t d, int32_t nk);
 // the least the attention can work with (the row statistics alone; its maximum then goes

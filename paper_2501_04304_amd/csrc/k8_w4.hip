@@ -233,9 +233,10 @@ __device__ float convert(const T (&x)[4][8], Piece (&a)[4][kPieces<T>]) {
 
 // How a product is cut: a workgroup has `tiles` times `shares` wavefronts, one for each of its tiles of 16 outputs and each share
 // of the units (every shares-th), for 16 rows of x.  The rows of `chunk` units at a time are brought into fp16 by all of them and
-// wait in LDS, 1, 4 or 16 rows (1 << row_shift).
+// wait in LDS, 1, 4 or 16 rows (1 << row_shift).  splits: workgroups (blockIdx.z) that have a part of the units each, where there
+// are few outputs and many inputs; their sums meet in a second kernel.
 struct Cut {
-    int32_t tiles, shares, chunk, row_shift;
+    int32_t tiles, shares, splits, chunk, row_shift;
 };
 
 // Bound by the bytes of the weights.  A wavefront's next kAhead units are on their way while it works on as many, and the rows of
@@ -250,7 +251,8 @@ struct Units {
 
 template <class T, class Y, int J, int SHIFT>
 __global__ __launch_bounds__(640) void k_w4_matvec(const T *__restrict__ x, int64_t x_row, int32_t M, W4 m, Cut cut,
-                                                   const float *__restrict__ bias, int32_t silu_on, Y *__restrict__ y) {
+                                                   const float *__restrict__ bias, int32_t silu_on, Y *__restrict__ y,
+                                                   float *__restrict__ parts) {
     constexpr int P = kPieces<T>;
     constexpr bool kPowers = !std::is_same_v<T, _Float16>;
     extern __shared__ uint4 lds[];  // [chunk][4 j][P][4 q][rows], then the powers [chunk][16]; later the sums
@@ -277,21 +279,22 @@ __global__ __launch_bounds__(640) void k_w4_matvec(const T *__restrict__ x, int6
             for (int g = 0; g < 4 / J; ++g) to.word[d][g] = w[l.r * (4 / J) + g];
         }
     };
+    const int begin = (int)((int64_t)m.T * blockIdx.z / cut.splits), stop = (int)((int64_t)m.T * (blockIdx.z + 1) / cut.splits);
     Units<J> now, next;
-    fetch(now, share, min(cut.chunk, m.T));
+    fetch(now, begin + share, min(begin + cut.chunk, stop));
 
     // this lane's row, and its units of a chunk: first, first + step, ..
     const int per = 16 >> shift, first = wave * per + (l.r >> shift), step = waves * per, row = l.r & (rows - 1);
     const T *mine = x + min(row0 + row, M - 1) * x_row;
     RowPart<T> part;
-    part.load(mine, min(first, m.T - 1) * kUnit + 8 * l.q, m.C);
+    part.load(mine, min(begin + first, stop - 1) * kUnit + 8 * l.q, m.C);
 
     float4v out{};
-    for (int t0 = 0; t0 < m.T; t0 += cut.chunk) {
-        const int end = min(t0 + cut.chunk, m.T);
-        if (t0) __syncthreads();
+    for (int t0 = begin; t0 < stop; t0 += cut.chunk) {
+        const int end = min(t0 + cut.chunk, stop);
+        if (t0 > begin) __syncthreads();
         for (int u = first; t0 + u - (l.r >> shift) < end; u += step) {
-            if (u != first) part.load(mine, min(t0 + u, m.T - 1) * kUnit + 8 * l.q, m.C);
+            if (u != first) part.load(mine, min(t0 + u, stop - 1) * kUnit + 8 * l.q, m.C);
             Piece a[4][P];
             const float power = convert(part.x, a);
             if (t0 + u >= end) continue;
@@ -304,11 +307,11 @@ __global__ __launch_bounds__(640) void k_w4_matvec(const T *__restrict__ x, int6
                 for (int i = row; i < 16; i += rows) powers[u * 16 + i] = power;
         }
         __syncthreads();
-        if (end < m.T) part.load(mine, min(end + first, m.T - 1) * kUnit + 8 * l.q, m.C);
+        if (end < stop) part.load(mine, min(end + first, stop - 1) * kUnit + 8 * l.q, m.C);
 
         for (int t = t0 + share; t < end; t += kAhead * cut.shares) {
             const bool same = t + kAhead * cut.shares < end;
-            fetch(next, same ? t + kAhead * cut.shares : min(end + share, m.T - 1), same ? end : min(end + cut.chunk, m.T));
+            fetch(next, same ? t + kAhead * cut.shares : min(end + share, stop - 1), same ? end : min(end + cut.chunk, stop));
             __builtin_amdgcn_sched_barrier(0);  // they set out before the work below, not after it
 #pragma unroll
             for (int d = 0; d < kAhead; ++d) {
@@ -357,9 +360,27 @@ __global__ __launch_bounds__(640) void k_w4_matvec(const T *__restrict__ x, int6
         for (int w = 0; w < cut.shares; ++w) v += sums[w * all + e];
         const int o = blockIdx.x * wide + e % wide;
         if (o >= m.O) continue;
+        const int64_t to = (int64_t)(row0 + e / wide) * m.O + o;
+        if (cut.splits > 1) {
+            parts[(int64_t)blockIdx.z * M * m.O + to] = v;
+            continue;
+        }
         if (bias) v += bias[o];
-        y[(int64_t)(row0 + e / wide) * m.O + o] = (Y)(silu_on ? silu(v) : v);
+        y[to] = (Y)(silu_on ? silu(v) : v);
     }
+}
+
+// The splits' sums, in their order.
+template <class Y>
+__global__ __launch_bounds__(256) void k_w4_join(const float *__restrict__ parts, int32_t splits, int32_t M, int32_t O,
+                                                 const float *__restrict__ bias, int32_t silu_on, Y *__restrict__ y) {
+    const int n = M * O, e = blockIdx.x * 256 + threadIdx.x;
+    if (e >= n) return;
+    float v = 0.f;
+#pragma unroll 8
+    for (int i = 0; i < splits; ++i) v += parts[(int64_t)i * n + e];
+    if (bias) v += bias[e % O];
+    y[e] = (Y)(silu_on ? silu(v) : v);
 }
 
 // Bytes of LDS for a chunk, and for the sums behind it.
@@ -369,26 +390,35 @@ int lds_bytes(const Cut &c) {
 }
 
 template <class T>
-Cut cut_of(int32_t M, const W4 &m, int tiles, int shares) {
-    Cut c{tiles, shares, 0, 0};
+Cut cut_of(int32_t M, const W4 &m, int tiles, int shares, int splits) {
+    Cut c{tiles, shares, splits, 0, 0};
     while (c.row_shift < 4 && (1 << c.row_shift) < M) c.row_shift += 2;
-    const int step = tiles * shares * (16 >> c.row_shift);  // units that the wavefronts bring at once
+    const int step = tiles * shares * (16 >> c.row_shift), units = (m.T + splits - 1) / splits;  // step: units that the wavefronts bring at once
     c.chunk = step;
     // kAhead units to each share, if they fit
-    while (c.chunk < shares * kAhead && c.chunk < m.T && lds_bytes<T>({tiles, shares, c.chunk + step, c.row_shift}) <= 131072) c.chunk += step;
+    auto fits = [&](int chunk) { return lds_bytes<T>({tiles, shares, splits, chunk, c.row_shift}) <= 131072; };
+    while (c.chunk < shares * kAhead && c.chunk < units && fits(c.chunk + step)) c.chunk += step;
     return c;
 }
 
 // Up to ten wavefronts, which share the rows' conversion: as many tiles as leave one workgroup to each of the 256 CUs, in as few
-// rounds as ten tiles allow, and the units cut among what is left.
-template <class T>
-Cut cut_for(int32_t M, const W4 &m) {
-    const int64_t blocks = (M + 15) / 16, all = m.R * blocks, rounds = (all + 2559) / 2560;
-    int tiles = (int)((all + 256 * rounds - 1) / (256 * rounds)), shares = 1;
-    while (shares * 2 * tiles <= 10 && shares * 2 <= m.T) shares *= 2;
-    // one conversion for all units, if ten wavefronts manage it
-    if (M > 4 && m.T <= 10 && tiles > 1 && tiles * shares < m.T) tiles = (m.T + shares - 1) / shares;
-    return cut_of<T>(M, m, tiles, shares);
+// rounds as ten tiles allow, and the units cut among what is left.  Where that leaves more than half of the CUs without work and
+// units enough to pay for a second kernel, every tile's units are split among workgroups (29 x 6477 -> 103 fp32 23 us in one
+// part, 8 in eight; 2 x 19840 -> 30 bf16 18 and 7; at 24 units they are level): 6 to a part, which take one conversion, or 10 of
+// few rows.
+struct Ways {
+    int tiles, shares, splits;
+};
+Ways ways_for(int32_t M, int32_t R, int32_t T) {
+    const int64_t blocks = (M + 15) / 16, all = R * blocks, rounds = (all + 2559) / 2560;
+    int tiles = (int)((all + 256 * rounds - 1) / (256 * rounds)), shares = 1, splits = 1;
+    while (shares * 2 * tiles <= 10 && shares * 2 <= T) shares *= 2;
+    if (M > 4 && T <= 10 && tiles > 1 && tiles * shares < T) tiles = (T + shares - 1) / shares;  // one conversion for all units
+    if (all < 128 && T >= (M > 4 ? 32 : 48)) {
+        splits = (int)(M > 4 ? std::min<int64_t>(512 / all, T / 6) : std::min<int64_t>(256 / all, T / 10));
+        for (shares = 1; shares * 2 <= (M > 4 ? 4 : 8) && shares * 2 * splits <= T;) shares *= 2;
+    }
+    return {tiles, shares, splits};
 }
 
 template <class F>
@@ -418,27 +448,37 @@ hipError_t launch_w4_unpack(const W4 &m, int32_t dtype, void *w, hipStream_t st)
     return hipGetLastError();
 }
 
-hipError_t launch_w4_matvec(const W4Product &p, const W4 &m, hipStream_t st) {
+size_t w4_matvec_workspace_bytes(int32_t M, const W4 &m) {
+    const Ways w = ways_for(M, m.R, m.T);
+    return w.splits > 1 ? (size_t)w.splits * M * m.O * sizeof(float) : 0;
+}
+
+hipError_t launch_w4_matvec(const W4Product &p, const W4 &m, void *workspace, hipStream_t st) {
     hipError_t e = hipSuccess;
+    const Ways w = ways_for(p.M, m.R, m.T);
+    float *parts = static_cast<float *>(workspace);
     by_dtype(p.dtype, [&](auto xt) {
         using T = decltype(xt);
-        const Cut c = cut_for<T>(p.M, m);
+        const Cut c = cut_of<T>(p.M, m, w.tiles, w.shares, w.splits);
         by_output<T>(p.out_dtype, [&](auto yt) {
             using Y = decltype(yt);
+            Y *y = static_cast<Y *>(p.y);
             by_group(m.group, [&](auto j) {
                 constexpr int J = decltype(j)::value;
-                const dim3 grid((m.R + c.tiles - 1) / c.tiles, (p.M + 15) / 16);
+                const dim3 grid((m.R + c.tiles - 1) / c.tiles, (p.M + 15) / 16, c.splits);
                 auto go = [&](auto shift) {
                     constexpr int S = decltype(shift)::value;
                     e = DGQ_ENSURE_LDS((k_w4_matvec<T, Y, J, S>), lds_bytes<T>(c));
                     if (e == hipSuccess)
                         k_w4_matvec<T, Y, J, S><<<grid, 64 * c.tiles * c.shares, lds_bytes<T>(c), st>>>(
-                            static_cast<const T *>(p.x), p.x_row, p.M, m, c, p.bias, p.act == DGQ_ACT_SILU, static_cast<Y *>(p.y));
+                            static_cast<const T *>(p.x), p.x_row, p.M, m, c, p.bias, p.act == DGQ_ACT_SILU, y, parts);
                 };
                 c.row_shift == 0   ? go(std::integral_constant<int, 0>{})
                 : c.row_shift == 2 ? go(std::integral_constant<int, 2>{})
                                    : go(std::integral_constant<int, 4>{});
             });
+            if (e == hipSuccess && c.splits > 1)
+                k_w4_join<Y><<<(p.M * m.O + 255) / 256, 256, 0, st>>>(parts, c.splits, p.M, m.O, p.bias, p.act == DGQ_ACT_SILU, y);
         });
     });
     return e == hipSuccess ? hipGetLastError() : e;

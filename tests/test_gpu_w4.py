@@ -126,7 +126,7 @@ ROWS = [1, 2, 5, 16, 17, 32, 33, 64, 100]
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("group", GROUPS)
-@pytest.mark.parametrize("O,C", SIZES + [(64, 1280), (1030, 300), (33, 4000)])
+@pytest.mark.parametrize("O,C", SIZES + [(64, 1280), (1030, 300), (33, 4000), (40, 9999), (2500, 700), (7000, 90)])
 def test_products_of_small_integers(dgq, O, C, group, dtype):
     """Integers and scales of powers of two: every sum is a number of fp32, so every bit has to be right, and so is each place."""
     rng = np.random.default_rng(O + 3 * C)
@@ -148,7 +148,8 @@ def test_products_of_small_integers(dgq, O, C, group, dtype):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("group", GROUPS)
-@pytest.mark.parametrize("M,C,O", [(1, 320, 1280), (2, 2051, 103), (16, 1280, 64), (40, 700, 48), (3, 5000, 20), (70, 130, 33)])
+@pytest.mark.parametrize("M,C,O", [(1, 320, 1280), (2, 2051, 103), (16, 1280, 64), (40, 700, 48), (3, 5000, 20), (70, 130, 33), (5, 20000, 17),
+                                   (30, 15001, 100)])
 def test_products(dgq, M, C, O, group, dtype):
     rng = np.random.default_rng(M + C)
     _, wn = _layer(rng, O, C)
@@ -233,6 +234,21 @@ def test_strided_rows_and_buffers(dgq, dtype):
     assert torch.equal(dgq.dgq_w4_matvec(same, w), dgq.dgq_w4_matvec(same.contiguous(), w))
     flat = torch.zeros(O * 3 + 1, device="cuda")[1:].view(3, O)  # an output at an odd place
     assert torch.equal(dgq.dgq_w4_matvec(x[:3], w, out=flat), dgq.dgq_w4_matvec(x[:3], w, dtype=torch.float32))
+
+
+def test_workspace(dgq):
+    import torch
+    rng = np.random.default_rng(17)
+    M, O, C = 5, 30, 9000
+    w = dgq.dgq_w4_pack(dgq.W4Weight.empty(O, C, 64), _layer(rng, O, C)[0])
+    x = _up(rng.standard_normal((M, C)).astype(np.float32))
+    need = dgq.dgq_w4_matvec_workspace_bytes(M, O, C)
+    assert need > 0
+    ws = torch.full((need + 16,), 255, dtype=torch.uint8, device="cuda")
+    assert torch.equal(dgq.dgq_w4_matvec(x, w, workspace=ws), dgq.dgq_w4_matvec(x, w))
+    assert (ws[-16:] == 255).all()
+    with pytest.raises(dgq.DgqError, match="workspace"):
+        dgq.dgq_w4_matvec(x, w, workspace=ws[:16])
 
 
 def test_rows_of_one_call_and_of_several(dgq):

@@ -82,16 +82,26 @@ def test_w4_pack_and_unpack(lib, kw, code):
 @pytest.mark.parametrize("kw,code", [
     (dict(x=None), EINVAL), (dict(y=None), EINVAL), (dict(data=None), EINVAL), (dict(dtype=4), EINVAL), (dict(out_dtype=1), EINVAL),
     (dict(dtype=1, out_dtype=2), EINVAL), (dict(M=-1), EINVAL), (dict(row=-1), EINVAL), (dict(act=2), EINVAL), (dict(group=1), EUNSUPPORTED),
-    (dict(M=(1 << 20) + 1), EUNSUPPORTED), (dict(x=P + 2), EALIGN), (dict(y=P + 2), EALIGN), (dict(bias=P + 2), EALIGN), (dict(data=P + 4), EALIGN)])
+    (dict(M=(1 << 20) + 1), EUNSUPPORTED), (dict(x=P + 2), EALIGN), (dict(y=P + 2), EALIGN), (dict(bias=P + 2), EALIGN), (dict(data=P + 4), EALIGN),
+    (dict(C=20000), EWORKSPACE), (dict(C=20000, ws=P, ws_bytes=8), EWORKSPACE), (dict(C=20000, ws=P + 4, ws_bytes=1 << 30), EWORKSPACE)])
 def test_w4_matvec(lib, kw, code):
-    a = dict(x=P, dtype=0, row=8, M=1, data=P, O=8, C=8, group=32, bias=None, act=0, y=P, out_dtype=0, stream=None)
+    a = dict(x=P, dtype=0, row=8, M=1, data=P, O=8, C=8, group=32, bias=None, act=0, y=P, out_dtype=0, ws=None,
+             ws_bytes=0, stream=None)
     a.update(kw)
     assert lib.dgq_w4_matvec(*a.values()) == code
     assert b"dgq_w4_matvec" in lib.dgq_last_error()
 
 
+def test_w4_matvec_workspace(lib):
+    size = lib.dgq_w4_matvec_workspace_bytes
+    assert size(3, 40, 20000) % (3 * 40 * 4) == 0 and size(3, 40, 20000) > 0  # some parts of [3, 40] fp32
+    assert size(3, 40, 128) == 0 and size(1, 16384, 4096) == 0
+    for bad in ((0, 40, 20000), (3, 0, 20000), (3, 40, 0), (3, 40, (1 << 20) + 1)):
+        assert size(*bad) == 0
+
+
 def test_w4_matvec_of_no_rows_is_no_work(lib):
-    assert lib.dgq_w4_matvec(None, 0, 8, 0, P, 8, 8, 32, None, 0, None, 0, None) == 0
+    assert lib.dgq_w4_matvec(None, 0, 8, 0, P, 8, 8, 32, None, 0, None, 0, None, 0, None) == 0
 
 
 # ---- the references themselves ----
