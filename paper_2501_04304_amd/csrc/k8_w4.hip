@@ -242,6 +242,9 @@ struct Cut {
 // Bound by the bytes of the weights.  A wavefront's next kAhead units are on their way while it works on as many, and the rows of
 // the next chunk while all work on this one.
 constexpr int kAhead = 4;
+// Wavefronts of a workgroup, as many as registers allow.
+template <class T>
+constexpr int kMaxWaves = sizeof(T) == 4 ? 10 : 16;
 
 template <int J>
 struct Units {
@@ -250,7 +253,7 @@ struct Units {
 };
 
 template <class T, class Y, int J, int SHIFT>
-__global__ __launch_bounds__(640) void k_w4_matvec(const T *__restrict__ x, int64_t x_row, int32_t M, W4 m, Cut cut,
+__global__ __launch_bounds__(64 * kMaxWaves<T>) void k_w4_matvec(const T *__restrict__ x, int64_t x_row, int32_t M, W4 m, Cut cut,
                                                    const float *__restrict__ bias, int32_t silu_on, Y *__restrict__ y,
                                                    float *__restrict__ parts) {
     constexpr int P = kPieces<T>;
@@ -313,10 +316,8 @@ __global__ __launch_bounds__(640) void k_w4_matvec(const T *__restrict__ x, int6
             const bool same = t + kAhead * cut.shares < end;
             fetch(next, same ? t + kAhead * cut.shares : min(end + share, stop - 1), same ? end : min(end + cut.chunk, stop));
             __builtin_amdgcn_sched_barrier(0);  // they set out before the work below, not after it
-#pragma unroll
-            for (int d = 0; d < kAhead; ++d) {
+            auto unit = [&](int d) {
                 const int u = t - t0 + d * cut.shares;
-                if (t0 + u >= end) break;
                 half8 a[4][P];
                 const uint4 *from = lds + (((u * 16 * P + l.q) << shift) + row);
 #pragma unroll
@@ -343,6 +344,11 @@ __global__ __launch_bounds__(640) void k_w4_matvec(const T *__restrict__ x, int6
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) out[i] = kPowers ? fmaf(sum[i], power[i], out[i]) : out[i] + sum[i];
+            };
+#pragma unroll
+            for (int d = 0; d < kAhead; ++d) {
+                if (t + d * cut.shares >= end) break;
+                unit(d);
             }
             now = next;
         }
@@ -394,25 +400,28 @@ Cut cut_of(int32_t M, const W4 &m, int tiles, int shares, int splits) {
     Cut c{tiles, shares, splits, 0, 0};
     while (c.row_shift < 4 && (1 << c.row_shift) < M) c.row_shift += 2;
     const int step = tiles * shares * (16 >> c.row_shift), units = (m.T + splits - 1) / splits;  // step: units that the wavefronts bring at once
-    c.chunk = step;
-    // kAhead units to each share, if they fit
-    auto fits = [&](int chunk) { return lds_bytes<T>({tiles, shares, splits, chunk, c.row_shift}) <= 131072; };
-    while (c.chunk < shares * kAhead && c.chunk < units && fits(c.chunk + step)) c.chunk += step;
+    // as many times that as fit, in parts alike: one workgroup to a CU may have most of its LDS
+    const int64_t groups = (int64_t)((m.R + tiles - 1) / tiles) * ((M + 15) / 16) * splits;
+    const int most = std::max((groups <= 256 ? 131072 : 65536) / lds_bytes<T>({tiles, shares, splits, step, c.row_shift}), 1);
+    const int parts = (units + most * step - 1) / (most * step), each = (units + parts - 1) / parts;
+    c.chunk = (each + step - 1) / step * step;
     return c;
 }
 
-// Up to ten wavefronts, which share the rows' conversion: as many tiles as leave one workgroup to each of the 256 CUs, in as few
-// rounds as ten tiles allow, and the units cut among what is left.  Where that leaves more than half of the CUs without work and
+// Wavefronts share the rows' conversion: as many tiles as leave one workgroup to each of the 256 CUs, in as few rounds as `most`
+// tiles allow (64 x 8192 -> 28672 bf16 129 us with ten, 98 with sixteen), and the units cut among what is left
+// (of ten for few rows, whose wavefronts wait for memory alone: 1 x 4096 -> 16384 bf16 9.5 us with eight, 11 with sixteen; 8 x 4096
+// -> 11000 14 and 12).  Where that leaves more than half of the CUs without work and
 // units enough to pay for a second kernel, every tile's units are split among workgroups (29 x 6477 -> 103 fp32 23 us in one
 // part, 8 in eight; 2 x 19840 -> 30 bf16 18 and 7; at 24 units they are level): 6 to a part, which take one conversion, or 10 of
 // few rows.
 struct Ways {
     int tiles, shares, splits;
 };
-Ways ways_for(int32_t M, int32_t R, int32_t T) {
-    const int64_t blocks = (M + 15) / 16, all = R * blocks, rounds = (all + 2559) / 2560;
+Ways ways_for(int32_t M, int32_t R, int32_t T, int most) {
+    const int64_t blocks = (M + 15) / 16, all = R * blocks, rounds = (all + 256 * most - 1) / (256 * most);
     int tiles = (int)((all + 256 * rounds - 1) / (256 * rounds)), shares = 1, splits = 1;
-    while (shares * 2 * tiles <= 10 && shares * 2 <= T) shares *= 2;
+    while (shares * 2 * tiles <= (M > 4 ? most : 10) && shares * 2 <= T) shares *= 2;
     if (M > 4 && T <= 10 && tiles > 1 && tiles * shares < T) tiles = (T + shares - 1) / shares;  // one conversion for all units
     if (all < 128 && T >= (M > 4 ? 32 : 48)) {
         splits = (int)(M > 4 ? std::min<int64_t>(512 / all, T / 6) : std::min<int64_t>(256 / all, T / 10));
@@ -449,16 +458,16 @@ hipError_t launch_w4_unpack(const W4 &m, int32_t dtype, void *w, hipStream_t st)
 }
 
 size_t w4_matvec_workspace_bytes(int32_t M, const W4 &m) {
-    const Ways w = ways_for(M, m.R, m.T);
+    const Ways w = ways_for(M, m.R, m.T, 10);  // (splits are for few tiles, whatever the type)
     return w.splits > 1 ? (size_t)w.splits * M * m.O * sizeof(float) : 0;
 }
 
 hipError_t launch_w4_matvec(const W4Product &p, const W4 &m, void *workspace, hipStream_t st) {
     hipError_t e = hipSuccess;
-    const Ways w = ways_for(p.M, m.R, m.T);
     float *parts = static_cast<float *>(workspace);
     by_dtype(p.dtype, [&](auto xt) {
         using T = decltype(xt);
+        const Ways w = ways_for(p.M, m.R, m.T, kMaxWaves<T>);
         const Cut c = cut_of<T>(p.M, m, w.tiles, w.shares, w.splits);
         by_output<T>(p.out_dtype, [&](auto yt) {
             using Y = decltype(yt);
