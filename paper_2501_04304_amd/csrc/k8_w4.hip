@@ -421,7 +421,7 @@ struct Ways {
 Ways ways_for(int32_t M, int32_t R, int32_t T, int most) {
     const int64_t blocks = (M + 15) / 16, all = R * blocks, rounds = (all + 256 * most - 1) / (256 * most);
     int tiles = (int)((all + 256 * rounds - 1) / (256 * rounds)), shares = 1, splits = 1;
-    while (shares * 2 * tiles <= (M > 4 ? most : 10) && shares * 2 <= T) shares *= 2;
+    while (shares * 2 * tiles <= (M > 4 ? most : 10) && shares * 2 <= std::min(T, 8)) shares *= 2;
     if (M > 4 && T <= 10 && tiles > 1 && tiles * shares < T) tiles = (T + shares - 1) / shares;  // one conversion for all units
     if (all < 128 && T >= (M > 4 ? 32 : 48)) {
         splits = (int)(M > 4 ? std::min<int64_t>(512 / all, T / 6) : std::min<int64_t>(256 / all, T / 10));
