@@ -731,7 +731,7 @@ int dgq_w4_unpack(const void *data, int32_t O, int32_t C, int32_t group, int32_t
 
 /*
  * Products with such weights: y[m, o] = act(sum_k x[m, k] s (code[o, k] - zero) + bias[o]).  For few rows, whose time is the
- * weights' bytes; any number is taken (16 rows at a time, which read the weights anew).
+ * weights' bytes; up to 2^19 are taken (16 at a time, which read the weights anew).
  *   x     [M, C] of `dtype`, inputs contiguous, rows x_row_stride elements apart, aligned to an element
  *   bias  fp32 [O], or NULL
  *   y     [M, O] of out_dtype (dtype or fp32), contiguous

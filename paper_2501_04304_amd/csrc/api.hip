@@ -1417,7 +1417,7 @@ bool act_ok(int32_t a) { return a == DGQ_ACT_NONE || a == DGQ_ACT_SILU; }
 bool out_dtype_ok(int32_t out, int32_t in) { return out == in || out == DGQ_F32; }
 bool aligned_to(const void *p, int32_t dtype) { return (reinterpret_cast<uintptr_t>(p) & (dtype == DGQ_F32 ? 3u : 1u)) == 0; }
 
-constexpr int32_t kMaxChannels = 1 << 20, kMaxOutputs = 1 << 24;
+constexpr int32_t kMaxChannels = 1 << 20, kMaxOutputs = 1 << 24, kMaxFewRows = 1 << 19;
 
 // Sizes of a group norm's call; an error names it.
 int norm_sizes(const char *who, int32_t B, int64_t N, bool packed, int32_t C, int32_t G, int32_t dtype) {
@@ -1510,7 +1510,7 @@ int dgq_w4_unpack(const void *data, int32_t O, int32_t C, int32_t group, int32_t
 }
 
 size_t dgq_w4_matvec_workspace_bytes(int32_t M, int32_t O, int32_t C) {
-    if (M < 1 || M > kMaxChannels || !w4_sizes_ok(O, C, 128)) return 0;
+    if (M < 1 || M > kMaxFewRows || !w4_sizes_ok(O, C, 128)) return 0;
     return w4_matvec_workspace_bytes(M, W4{nullptr, O, C, 128, (O + 15) / 16, (C + 127) / 128});
 }
 
@@ -1525,7 +1525,7 @@ int dgq_w4_matvec(const void *x, int32_t dtype, int64_t x_row_stride, int32_t M,
     if (M < 0 || x_row_stride < 0) return fail(DGQ_EINVAL, "dgq_w4_matvec: rows or stride below 0");
     if (M == 0) return DGQ_OK;
     if (!x || !y) return fail(DGQ_EINVAL, "dgq_w4_matvec: null pointer");
-    if (M > kMaxChannels) return fail(DGQ_EUNSUPPORTED, "dgq_w4_matvec: more than 2^20 rows");
+    if (M > kMaxFewRows) return fail(DGQ_EUNSUPPORTED, "dgq_w4_matvec: more than 2^19 rows");
     if (!aligned_to(x, dtype) || !aligned_to(y, out_dtype) || !aligned_to(bias, DGQ_F32))
         return fail(DGQ_EALIGN, "dgq_w4_matvec: tensor not aligned to its elements");
     const size_t need = w4_matvec_workspace_bytes(M, m);

@@ -187,7 +187,7 @@ __global__ __launch_bounds__(kMaxThreads) void k_gn_sums(const T *__restrict__ x
     ch.each(im, blockIdx.x, [&](int32_t b, int32_t part, int64_t r0, int64_t r1) {
         double s[V] = {}, ss[V] = {};
         if (at.on) {
-            const int n = (int)(r1 - r0 - at.pr + high - 1) / high;
+            const int n = (int)((r1 - r0 - at.pr + high - 1) / high);
             RowsOf<T>(x + xs.at(im, b, r0 + at.pr) + at.c0, high * xs.row, n, C < V ? at.have : 0).each([&](int, const float (&f)[V]) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
@@ -309,7 +309,7 @@ __global__ __launch_bounds__(kMaxThreads) void k_gn_apply(const T *x, Images im,
         float p[V], a[V], q[V];
         const float *from;
         int64_t stride;
-        RowsOf<T> rows(x + xs.at(im, b, r0 + at.pr) + at.c0, high * xs.row, at.on ? (int)(r1 - r0 - at.pr + high - 1) / high : 0,
+        RowsOf<T> rows(x + xs.at(im, b, r0 + at.pr) + at.c0, high * xs.row, at.on ? (int)((r1 - r0 - at.pr + high - 1) / high) : 0,
                        C < V ? at.have : 0);
         if (tables) {
             from = tables + (int64_t)b * 3 * C + at.c0;
@@ -384,7 +384,7 @@ __global__ __launch_bounds__(THREADS) void k_gn_one(const T *x, Images im, Rows 
     const int c = min(v * V, Cg - V), again = v * V - c, c0 = g * Cg + c;  // again: values that the vector before has too
     const int64_t r0 = im.start(b), r1 = im.end(b);
     if (r1 <= r0) return;
-    const int n = pr < high ? max((int)(r1 - r0 - pr + high - 1) / high, 0) : 0;  // rows of this thread
+    const int n = pr < high ? max((int)((r1 - r0 - pr + high - 1) / high), 0) : 0;  // rows of this thread
     const int64_t step = high * xs.row;
     const T *from = x + xs.at(im, b, r0 + pr) + c0;
     const double per = 1 / ((double)(r1 - r0) * Cg);
@@ -504,7 +504,7 @@ struct Hold {
 };
 Hold hold_for(const NormCall &n) {
     const int32_t V = n.dtype == DGQ_F32 ? 4 : 8, Cg = n.C / n.G, width = (Cg + V - 1) / V;
-    if (Cg < V || width > 256) return {};
+    if (Cg < V || width > 256 || (int64_t)n.B * n.G > 1 << 24) return {};
     const int64_t rows = n.offsets ? n.N / n.B * 3 / 2 : n.N;  // of a long image
     if ((rows > 2048 || rows * Cg > 65536) && (int64_t)n.B * n.G < 192) return {};
     const Hold ways[] = {{256, 4, width}, {1024, 4, width}, {1024, 8, width}, {1024, 16, width}};

@@ -82,7 +82,7 @@ def test_w4_pack_and_unpack(lib, kw, code):
 @pytest.mark.parametrize("kw,code", [
     (dict(x=None), EINVAL), (dict(y=None), EINVAL), (dict(data=None), EINVAL), (dict(dtype=4), EINVAL), (dict(out_dtype=1), EINVAL),
     (dict(dtype=1, out_dtype=2), EINVAL), (dict(M=-1), EINVAL), (dict(row=-1), EINVAL), (dict(act=2), EINVAL), (dict(group=1), EUNSUPPORTED),
-    (dict(M=(1 << 20) + 1), EUNSUPPORTED), (dict(x=P + 2), EALIGN), (dict(y=P + 2), EALIGN), (dict(bias=P + 2), EALIGN), (dict(data=P + 4), EALIGN),
+    (dict(M=(1 << 19) + 1), EUNSUPPORTED), (dict(x=P + 2), EALIGN), (dict(y=P + 2), EALIGN), (dict(bias=P + 2), EALIGN), (dict(data=P + 4), EALIGN),
     (dict(C=20000), EWORKSPACE), (dict(C=20000, ws=P, ws_bytes=8), EWORKSPACE), (dict(C=20000, ws=P + 4, ws_bytes=1 << 30), EWORKSPACE)])
 def test_w4_matvec(lib, kw, code):
     a = dict(x=P, dtype=0, row=8, M=1, data=P, O=8, C=8, group=32, bias=None, act=0, y=P, out_dtype=0, ws=None,
