@@ -42,7 +42,7 @@ def build_binding(verbose: bool = False) -> str:
     cmd += ["-o", HOT, os.path.join(CSRC, "binding.cpp")]
     for d in cpp_extension.library_paths("cuda"):
         cmd += ["-L" + d]
-    cmd += ["-L" + HERE, "-Wl,-rpath,$ORIGIN", "-l:libdgq.so", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_hip"]
+    cmd += ["-L" + HERE, "-Wl,-rpath,$ORIGIN", "-l:libdgq.so", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-ltorch_hip", "-lc10", "-lc10_hip"]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.check_call(cmd)
