@@ -6,6 +6,7 @@
 // a lane's 16 bytes are its part of four operands of the 16 x 16 x 32 matrix instructions, and behind all codes one word for each
 // group, its scale with the zero in the 4 lowest bits.
 #include <algorithm>
+#include <cmath>
 
 #include "vectors.h"
 
@@ -170,30 +171,24 @@ __device__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t bits) { return (x
 // code - zero of a lane's eight codes.  zero: of the group's word.
 struct Expand {
     uint32_t nibble0 = 0x000f000fu, nibble1 = 0x00f000f0u, one = 0x64006400u;
-    union Pair {
-        uint32_t w;
-        half2v p;
-    };
     struct Zero {
-        Pair low, high;  // -(1024 + zero), -(64 + zero), twice each
+        _Float16 low, high;  // -(1024 + zero), -(64 + zero)
     };
     __device__ Expand() { asm("" : "+s"(nibble0), "+s"(nibble1), "+v"(one)); }
     __device__ static Zero zero(uint32_t word) {
-        const uint32_t z = (word & 15) * 0x10001u;
-        Zero to;
-        to.low.w = z | 0xe400e400u, to.high.w = z << 4 | 0xd400d400u;
-        return to;
+        const uint16_t low = 0xe400u | (word & 15), high = 0xd400u | (word & 15) << 4;
+        return {__builtin_bit_cast(_Float16, low), __builtin_bit_cast(_Float16, high)};
     }
     __device__ half8 operator()(uint32_t code, const Zero &zero) const {
-        const half2v part{(_Float16)(1.f / 16), (_Float16)(1.f / 16)};
+        const half2v part{(_Float16)(1.f / 16), (_Float16)(1.f / 16)}, low{zero.low, zero.low}, high{zero.high, zero.high};
         Piece p;
 #pragma unroll
         for (int i = 0; i < 4; i += 2) {
             const uint32_t two = i ? code >> 8 : code;
             p.w[i] = and_or(two, nibble0, one);
             p.w[i + 1] = and_or(two, nibble1, one);
-            p.p[i] += zero.low.p;
-            p.p[i + 1] = __builtin_elementwise_fma(p.p[i + 1], part, zero.high.p);
+            p.p[i] += low;
+            p.p[i + 1] = __builtin_elementwise_fma(p.p[i + 1], part, high);
         }
         return p.all;
     }
@@ -241,22 +236,23 @@ struct Cut {
 
 // Bound by the bytes of the weights.  A wavefront's next kAhead units are on their way while it works on as many, and the rows of
 // the next chunk while all work on this one.
-constexpr int kAhead = 4;
+template <int J>
+constexpr int kAhead = J == 1 ? 3 : 4;  // (four words to a unit: registers)
 // Wavefronts of a workgroup, as many as registers allow.
 template <class T>
-constexpr int kMaxWaves = sizeof(T) == 4 ? 10 : 16;
+constexpr int kMaxWaves = sizeof(T) == 4 ? 10 : 12;
 
 template <int J>
 struct Units {
-    uint4 code[kAhead];
-    uint32_t word[kAhead][4 / J];
+    uint4 code[kAhead<J>];
+    uint32_t word[kAhead<J>][4 / J];
 };
 
 template <class T, class Y, int J, int SHIFT>
 __global__ __launch_bounds__(64 * kMaxWaves<T>) void k_w4_matvec(const T *__restrict__ x, int64_t x_row, int32_t M, W4 m, Cut cut,
                                                    const float *__restrict__ bias, int32_t silu_on, Y *__restrict__ y,
                                                    float *__restrict__ parts) {
-    constexpr int P = kPieces<T>;
+    constexpr int P = kPieces<T>, AHEAD = kAhead<J>;
     constexpr bool kPowers = !std::is_same_v<T, _Float16>;
     extern __shared__ uint4 lds[];  // [chunk][4 j][P][4 q][rows], then the powers [chunk][16]; later the sums
     const unsigned tid = threadIdx.x, lane = tid & 63;
@@ -266,20 +262,19 @@ __global__ __launch_bounds__(64 * kMaxWaves<T>) void k_w4_matvec(const T *__rest
     const Lane l;
     const int tile = wave % cut.tiles, share = wave / cut.tiles, row0 = blockIdx.y * 16;
     const int64_t unit0 = (int64_t)min((int)blockIdx.x * cut.tiles + tile, m.R - 1) * m.T;  // behind the last: that again, not written
-    const uint4 *codes = reinterpret_cast<const uint4 *>(m.codes) + unit0 * 64;
-    const uint32_t *words = m.words() + unit0 * (64 / J);
+    const char *codes = reinterpret_cast<const char *>(m.codes) + unit0 * 1024;  // the tile's, the same for all lanes
+    const char *words = reinterpret_cast<const char *>(m.words() + unit0 * (64 / J));
     const Expand expand;
 
     // units first, first + shares, .. of a chunk that ends at `end` (its last again where there are no more)
     auto fetch = [&](Units<J> &to, int first, int end) {
 #pragma unroll
-        for (int d = 0; d < kAhead; ++d) {
+        for (int d = 0; d < AHEAD; ++d) {
             const int t = min(first + d * cut.shares, end - 1);
-            const uint4 *c = codes + (int64_t)t * 64;  // the same for all lanes
-            const uint32_t *w = words + (int64_t)t * (64 / J);
-            to.code[d] = c[lane];
+            to.code[d] = *reinterpret_cast<const uint4 *>(codes + (uint32_t)(t * 1024 + lane * 16));  // (a tile has less than 2^24 bytes)
+            const uint32_t *w = reinterpret_cast<const uint32_t *>(words + (uint32_t)(t * (256 / J) + l.r * (16 / J)));
 #pragma unroll
-            for (int g = 0; g < 4 / J; ++g) to.word[d][g] = w[l.r * (4 / J) + g];
+            for (int g = 0; g < 4 / J; ++g) to.word[d][g] = w[g];
         }
     };
     const int begin = (int)((int64_t)m.T * blockIdx.z / cut.splits), stop = (int)((int64_t)m.T * (blockIdx.z + 1) / cut.splits);
@@ -312,11 +307,14 @@ __global__ __launch_bounds__(64 * kMaxWaves<T>) void k_w4_matvec(const T *__rest
         __syncthreads();
         if (end < stop) part.load(mine, min(end + first, stop - 1) * kUnit + 8 * l.q, m.C);
 
-        for (int t = t0 + share; t < end; t += kAhead * cut.shares) {
-            const bool same = t + kAhead * cut.shares < end;
-            fetch(next, same ? t + kAhead * cut.shares : min(end + share, stop - 1), same ? end : min(end + cut.chunk, stop));
+        // a batch of units from t on with what is there, the next one on its way
+        auto batch = [&](int t, const Units<J> &with, Units<J> &next) {
+            const bool same = t + AHEAD * cut.shares < end;
+            fetch(next, same ? t + AHEAD * cut.shares : min(end + share, stop - 1), same ? end : min(end + cut.chunk, stop));
             __builtin_amdgcn_sched_barrier(0);  // they set out before the work below, not after it
-            auto unit = [&](int d) {
+#pragma unroll
+            for (int d = 0; d < AHEAD; ++d) {
+                if (t + d * cut.shares >= end) break;
                 const int u = t - t0 + d * cut.shares;
                 half8 a[4][P];
                 const uint4 *from = lds + (((u * 16 * P + l.q) << shift) + row);
@@ -326,31 +324,34 @@ __global__ __launch_bounds__(64 * kMaxWaves<T>) void k_w4_matvec(const T *__rest
                     for (int p = 0; p < P; ++p) a[j][p] = *reinterpret_cast<const half8 *>(from + ((4 * (j * P + p)) << shift));
                 float4v power;
                 if (kPowers) power = *reinterpret_cast<const float4v *>(powers + u * 16 + 4 * l.q);
-                const uint32_t c[4] = {now.code[d].x, now.code[d].y, now.code[d].z, now.code[d].w};
+                const uint32_t c[4] = {with.code[d].x, with.code[d].y, with.code[d].z, with.code[d].w};
                 float4v sum{};
 #pragma unroll
                 for (int g = 0; g < 4 / J; ++g) {
                     float4v acc{};
-                    const Expand::Zero zero = Expand::zero(now.word[d][g]);
+                    const Expand::Zero zero = Expand::zero(with.word[d][g]);
 #pragma unroll
                     for (int j = g * J; j < g * J + J; ++j) {
                         const half8 b = expand(c[j], zero);
 #pragma unroll
                         for (int p = 0; p < P; ++p) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[j][p], b, acc, 0, 0, 0);
                     }
-                    const float s = __uint_as_float(now.word[d][g] & ~15u);
+                    const float s = __uint_as_float(with.word[d][g] & ~15u);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) sum[i] = g ? fmaf(s, acc[i], sum[i]) : s * acc[i];
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) out[i] = kPowers ? fmaf(sum[i], power[i], out[i]) : out[i] + sum[i];
-            };
-#pragma unroll
-            for (int d = 0; d < kAhead; ++d) {
-                if (t + d * cut.shares >= end) break;
-                unit(d);
             }
-            now = next;
+        };
+        for (int t = t0 + share; t < end; t += AHEAD * cut.shares) {
+            batch(t, now, next);
+            t += AHEAD * cut.shares;
+            if (t >= end) {
+                now = next;
+                break;
+            }
+            batch(t, next, now);
         }
     }
     __syncthreads();
@@ -400,30 +401,36 @@ Cut cut_of(int32_t M, const W4 &m, int tiles, int shares, int splits) {
     Cut c{tiles, shares, splits, 0, 0};
     while (c.row_shift < 4 && (1 << c.row_shift) < M) c.row_shift += 2;
     const int step = tiles * shares * (16 >> c.row_shift), units = (m.T + splits - 1) / splits;  // step: units that the wavefronts bring at once
-    // as many times that as fit, in parts alike: one workgroup to a CU may have most of its LDS
+    // as many times that as fit, in parts alike: what is alone on a CU, by its number or by its registers, may have most of the LDS
     const int64_t groups = (int64_t)((m.R + tiles - 1) / tiles) * ((M + 15) / 16) * splits;
-    const int most = std::max((groups <= 256 ? 131072 : 65536) / lds_bytes<T>({tiles, shares, splits, step, c.row_shift}), 1);
+    const int most = std::max((groups <= 256 || tiles * shares > 6 ? 131072 : 65536) / lds_bytes<T>({tiles, shares, splits, step, c.row_shift}), 1);
     const int parts = (units + most * step - 1) / (most * step), each = (units + parts - 1) / parts;
     c.chunk = (each + step - 1) / step * step;
     return c;
 }
 
-// Wavefronts share the rows' conversion: as many tiles as leave one workgroup to each of the 256 CUs, in as few rounds as `most`
-// tiles allow (64 x 8192 -> 28672 bf16 129 us with ten, 98 with sixteen), and the units cut among what is left
-// (of ten for few rows, whose wavefronts wait for memory alone: 1 x 4096 -> 16384 bf16 9.5 us with eight, 11 with sixteen; 8 x 4096
-// -> 11000 14 and 12).  Where that leaves more than half of the CUs without work and
-// units enough to pay for a second kernel, every tile's units are split among workgroups (29 x 6477 -> 103 fp32 23 us in one
-// part, 8 in eight; 2 x 19840 -> 30 bf16 18 and 7; at 24 units they are level): 6 to a part, which take one conversion, or 10 of
-// few rows.
+// Wavefronts share the rows' conversion: tiles such that workgroups fill the 256 CUs in few rounds and wavefronts the four SIMDs
+// of each alike (64 x 8192 -> 28672 bf16 118 us with twelve tiles, 129 with eight), and the units cut among what is
+// left (of ten for few rows, whose wavefronts wait for memory alone: 1 x 4096 -> 16384 bf16 9.5 us with eight, 11 with sixteen).
+// Where that leaves more than half of the CUs without work and units enough to pay for a second kernel, every tile's units are
+// split among workgroups (29 x 6477 -> 103 fp32 23 us in one part, 8 in eight; 2 x 19840 -> 30 bf16 18 and 7; at 20 units they are
+// level): 6 to a part, which take one conversion, or 10 of few rows.
 struct Ways {
     int tiles, shares, splits;
 };
 Ways ways_for(int32_t M, int32_t R, int32_t T, int most) {
-    const int64_t blocks = (M + 15) / 16, all = R * blocks, rounds = (all + 256 * most - 1) / (256 * most);
-    int tiles = (int)((all + 256 * rounds - 1) / (256 * rounds)), shares = 1, splits = 1;
+    const int64_t blocks = (M + 15) / 16, all = R * blocks;
+    int tiles = 1, shares = 1, splits = 1;
+    double least = 1e30;
+    for (int t = 1; t <= most; ++t) {
+        // rounds of the CUs (many even out), times a tile's work on a SIMD and the rows' conversion, as long for 16 rows
+        const double groups = (double)((R + t - 1) / t * blocks) / 256, rounds = groups > 2 ? groups : std::ceil(groups);
+        const double cost = rounds * ((t + 3) / 4 + (M > 4 ? 1 : 0.25)) + 1e-3 * rounds;  // of equals the fewest rounds
+        if (cost < least) least = cost, tiles = t;
+    }
     while (shares * 2 * tiles <= (M > 4 ? most : 10) && shares * 2 <= std::min(T, 8)) shares *= 2;
     if (M > 4 && T <= 10 && tiles > 1 && tiles * shares < T) tiles = (T + shares - 1) / shares;  // one conversion for all units
-    if (all < 128 && T >= (M > 4 ? 32 : 48)) {
+    if (all < 128 && T >= (M > 4 ? 20 : 48)) {
         splits = (int)(M > 4 ? std::min<int64_t>(512 / all, T / 6) : std::min<int64_t>(256 / all, T / 10));
         for (shares = 1; shares * 2 <= (M > 4 ? 4 : 8) && shares * 2 * splits <= T;) shares *= 2;
     }
