@@ -690,7 +690,8 @@ typedef enum dgq_act { DGQ_ACT_NONE = 0, DGQ_ACT_SILU = 1 } dgq_act;  /* SiLU: t
  *   dtype, out_dtype   dgq_dtype of x and out; out has x's type or fp32
  *   weight, bias       fp32 [C], or NULL for 1 and 0
  *   add, scale, shift  fp32 [B, C], channels contiguous, rows `stride` elements apart, or NULL for none
- *   workspace dgq_groupnorm_workspace_bytes(...) bytes, 16-byte aligned: sums and tables, written before they are read
+ *   workspace dgq_groupnorm_workspace_bytes(...) bytes, 16-byte aligned (0 bytes: NULL): sums and tables, written before they are
+ *             read; this call's alone until it is done
  * Sums are in 64 bits and in an order of the call's sizes, x' - m is taken before it is rounded: the same call gives the same bits,
  * and a map whose mean is thousands of times its deviation loses nothing to that.  NaN or infinity stays in its image and
  * group, all of whose values become NaN.  A group of one value, or of equal ones, gives its bias (eps above 0).
@@ -736,10 +737,10 @@ int dgq_w4_unpack(const void *data, int32_t O, int32_t C, int32_t group, int32_t
  *   bias  fp32 [O], or NULL
  *   y     [M, O] of out_dtype (dtype or fp32), contiguous
  *   workspace dgq_w4_matvec_workspace_bytes(...) bytes, 16-byte aligned (0 bytes: NULL): few outputs of many inputs are cut
- *         over the chip along the inputs and joined by a second kernel
+ *         over the chip along the inputs and joined by a second kernel; this call's alone until it is done
  * fp32 rows count with 23 bits, fp16 and bf16 ones with all of theirs (bf16 and fp32: elements 2^29 below the largest of their
  * 128 inputs: to 2^-39 of that); codes less zeros are exact, sums are fp32 and rounded once to y.  NaN or infinity in a row of x
- * makes that row not finite, no other.
+ * makes that row not finite, no other.  Scales of 2^100 and more may overflow in a group's sum.
  * The same call gives the same bits; the order of the sums goes by the sizes.  Enqueues on `stream`; neither synchronises nor
  * allocates.
  */

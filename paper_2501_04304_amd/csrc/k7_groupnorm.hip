@@ -4,13 +4,18 @@
 //   m = mean x',  v = mean (x' - m)^2,  r = 1 / sqrt(v + eps)
 //   t = ((x' - m) r w[c] + beta[c]) (1 + scale[b, c]) + shift[b, c],   y = t  or  t / (1 + exp(-t))
 //
-// Three launches.  k_gn_sums: sum and sum of squares of every group over chunks of rows.  k_gn_tables: an image's chunks summed in
-// order, and for every channel three numbers of fp32,
+// For every channel of an image three numbers of fp32,
 //   p = (m - add) rounded,  a = r w (1 + scale),  q = ((p - (m - add)) r w + beta) (1 + scale) + shift,
-// so that t = (x - p) a + q: x - p loses nothing where x is near the mean, however far that is from 0.  k_gn_apply: that line and
-// the activation for every value.  Sums and tables are in 64 bits: x and x^2 of 32-bit numbers are exact there (but for the
-// sums' own last bits), so E[x^2] - m^2 keeps fp32's accuracy up to means of some thousand standard deviations, and partial sums
-// combine by plain addition.  add enters the sums per channel: sum x' = sum x + n add, sum x'^2 = sum x^2 + 2 add sum x + n add^2.
+// so that t = (x - p) a + q: x - p loses nothing where x is near the mean, however far that is from 0.  Sums, m, r and these three
+// are computed in 64 bits: x and x^2 of 32-bit numbers are exact there (but for the sums' own last bits), so E[x^2] - m^2 keeps
+// fp32's accuracy up to means of some thousand deviations, and partial sums combine by plain addition, in an order of the sizes
+// alone.  (The three instructions a value hide behind its bytes: a read of 168 MB takes 28.8 us with 64-bit sums and 28.2 with
+// 32-bit ones.)
+//
+// Maps whose groups fit a workgroup's registers: k_gn_one, x crosses memory once.  Others: k_gn_sums over chunks of rows, then
+// k_gn_apply, whose workgroups first add up their image's chunks (or k_gn_tables between the two, where those are many); x is
+// read twice.  2 x 64 x 1280 fp32 takes 5.1 us, 2 x 4096 x 320 15, 16 x 4096 x 640 107 and 1048576 x 128 fp16 164 (3.2 TB/s of its
+// bytes once, 4.9 of what it moves: plain loops that read a map of that size and then copy it take 168).
 #include <algorithm>
 
 #include "vectors.h"
@@ -171,7 +176,9 @@ struct RowsOf {
     }
 };
 
-// Bound by the bytes of x.  sums: [G][parts][slices] double2.
+// Bound by the bytes of x, and for small maps by the way from the kernel's arguments over x and LDS to the sums (4.7 us for 2 x
+// 4096 x 320, of which the rows take 2.5).  add enters per channel: sum x' = sum x + n add, sum x'^2 = sum x^2 + 2 add sum x + n add^2.
+// 16 x 4096 x 640 fp32: 47 us behind the last call's 168 MB on their way to memory.  sums: [G][parts][slices] double2.
 template <class T>
 __global__ __launch_bounds__(kMaxThreads) void k_gn_sums(const T *__restrict__ x, Images im, Rows xs, Chunks ch, Shape sh, int32_t C,
                                                          int32_t G, const float *__restrict__ add, int64_t add_row,
@@ -265,7 +272,8 @@ struct Group {
 };
 
 // ---- tables ----------------------------------------------------------------------------------------------------------
-// One workgroup per (group, image).  Bound by latency.  tables: fp32 [B][p, a, q][C].
+// One workgroup per (group, image), where an image has too many sums for all to add up.  Bound by latency (5 us).  tables: fp32
+// [B][p, a, q][C].
 __global__ __launch_bounds__(256) void k_gn_tables(const double2 *__restrict__ sums, int32_t parts, Images im, Chunks ch, int32_t slices,
                                                    int32_t C, int32_t G, const float *__restrict__ weight, const float *__restrict__ bias,
                                                    float eps, NormTerms terms, float *__restrict__ tables) {
@@ -289,8 +297,8 @@ __global__ __launch_bounds__(256) void k_gn_tables(const double2 *__restrict__ s
 }
 
 // ---- values ----------------------------------------------------------------------------------------------------------
-// Bound by the bytes of x and y.  x and y may be one buffer.  tables null: every workgroup
-// adds up the sums of its image itself, which costs less than a launch that does it once, as long as they are few.
+// Bound by the bytes of x and y (16 x 4096 x 640 fp32: 60 us, 5.6 TB/s).  x and y may be one buffer.  tables null: every workgroup
+// adds up its image's sums itself, its first rows on their way meanwhile: 2.7 us at 128 sums of 32 groups, and a launch less.
 template <class T, class Y>
 __global__ __launch_bounds__(kMaxThreads) void k_gn_apply(const T *x, Images im, Rows xs, Chunks ch, Shape sh, int32_t C, int32_t G,
                                                           const float *__restrict__ tables, const double2 *__restrict__ sums,
@@ -368,6 +376,8 @@ __global__ __launch_bounds__(kMaxThreads) void k_gn_apply(const T *x, Images im,
 // thread, `width` threads side by side over the group's channels (the last vector ends with the group, and what it shares with
 // the one before counts there) and threads / width rows at a time.  Rows that do not fit are read twice.  A group is a stripe of
 // the rows, cut inside lines of memory: an XCD gets neighbouring groups, so that its cache puts the lines together.
+// Bound by latency where maps are small (2 x 64 x 1280 fp32 4 us on the GPU), by the longest image's 32 workgroups in 8 packed
+// images of up to 4096 x 960 bf16 (36.5 us; a copy of the bytes 18), by lines that two XCDs write (25 % more than there are) above.
 template <class T, class Y, int THREADS, int HELD>
 __global__ __launch_bounds__(THREADS) void k_gn_one(const T *x, Images im, Rows xs, int32_t C, int32_t G, int32_t width,
                                                     const float *__restrict__ weight, const float *__restrict__ bias, float eps,

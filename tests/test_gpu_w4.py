@@ -263,20 +263,35 @@ def test_rows_of_one_call_and_of_several(dgq):
     assert torch.equal(dgq.dgq_w4_matvec(x, w)[0], dgq.dgq_w4_matvec(y, w)[0])
 
 
-def test_weights_past_4_gib_of_values(dgq):
-    """Units beyond 2^31 weights: the last outputs of 131072 x 20480."""
+def test_codes_past_4_gib(dgq):
+    """The last outputs of 262144 x 40960 weights, whose codes take 5 GiB."""
     import torch
-    O, C, group = 131072, 20480, 128
+    O, C, group = 262144, 40960, 128
     w = dgq.W4Weight.empty(O, C, group)
     w.data.zero_()
     n = O // 16 * (C // 128) * 1024
-    words = w.data[n:].view(torch.int32)
-    words.fill_(int(np.float32(1).view(np.int32)))      # values are the codes
-    w.data[n - 1024 * 160:n].fill_(0x11)                # ones for the last 16 outputs
-    x = torch.ones((2, C), device="cuda", dtype=torch.bfloat16)
-    y = dgq.dgq_w4_matvec(x, w, dtype=torch.float32)
-    torch.cuda.synchronize()
-    assert (y[:, :-16] == 0).all() and (y[:, -16:] == C).all()
+    assert n > 2 ** 32
+    w.data[n:].view(torch.int32).fill_(int(np.float32(1).view(np.int32)))  # values are the codes
+    w.data[n - 1024 * (C // 128):n].fill_(0x11)                            # ones for the last 16 outputs
+    for M in (1, 2, 5):
+        y = dgq.dgq_w4_matvec(torch.ones((M, C), device="cuda", dtype=torch.bfloat16), w, dtype=torch.float32)
+        assert (y[:, :-16] == 0).all() and (y[:, -16:] == C).all()
+
+
+def test_pack_of_more_than_2_to_31_weights(dgq):
+    import torch
+    O, C, group = 70003, 32768, 64
+    t = torch.zeros((O, C), dtype=torch.float16, device="cuda")
+    rng = np.random.default_rng(18)
+    rows = rng.standard_normal((3, C)).astype(np.float16)
+    t[-3:] = torch.from_numpy(rows).cuda()
+    w = dgq.dgq_w4_pack(dgq.W4Weight.empty(O, C, group), t)
+    t.fill_(1)
+    assert dgq.dgq_w4_unpack(w, out=t) is t
+    codes, words = ref.quantize(rows.astype(np.float32), group)
+    want = ref.values(codes, words, group, 3, C).astype(np.float32)
+    assert torch.equal(t[-3:].cpu(), torch.from_numpy(want).half())
+    assert (t[:-3].view(-1)[::997] == 0).all() and (t[-4] == 0).all()
 
 
 def test_captured_and_on_another_stream(dgq):
