@@ -1417,6 +1417,13 @@ bool act_ok(int32_t a) { return a == DGQ_ACT_NONE || a == DGQ_ACT_SILU; }
 bool out_dtype_ok(int32_t out, int32_t in) { return out == in || out == DGQ_F32; }
 bool aligned_to(const void *p, int32_t dtype) { return (reinterpret_cast<uintptr_t>(p) & (dtype == DGQ_F32 ? 3u : 1u)) == 0; }
 
+// Bytes of the values of a tensor of `dtype` whose last one lies `last` elements behind its first, in numbers that no stride passes.
+__int128 span(__int128 last, int32_t dtype) { return (last + 1) * (dtype == DGQ_F32 ? 4 : 2); }
+bool overlap(const void *a, __int128 a_bytes, const void *b, __int128 b_bytes) {
+    const __int128 p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
+    return p < q + b_bytes && q < p + a_bytes;
+}
+
 constexpr int32_t kMaxChannels = 1 << 20, kMaxOutputs = 1 << 24, kMaxFewRows = 1 << 19;
 
 // Sizes of a group norm's call; an error names it.
@@ -1476,6 +1483,11 @@ int dgq_groupnorm(const void *x, int32_t dtype, int64_t x_batch_stride, int64_t 
     const size_t need = groupnorm_workspace_bytes(n);
     if (need && (!workspace || workspace_bytes < need || !aligned16(workspace)))
         return fail(DGQ_EWORKSPACE, "dgq_groupnorm: workspace missing, too small or misaligned");
+    const int32_t images = offsets ? 1 : B;
+    const bool same = x == out && dtype == out_dtype && (N == 1 || x_row_stride == C) && (images == 1 || x_batch_stride == N * C);
+    const __int128 last = (__int128)(images - 1) * x_batch_stride + (__int128)(N - 1) * x_row_stride + C - 1;
+    if (!same && overlap(x, span(last, dtype), out, span((__int128)images * N * C - 1, out_dtype)))
+        return fail(DGQ_EINVAL, "dgq_groupnorm: out overlaps x and is not x, contiguous and of one type");
     DGQ_HIP(launch_groupnorm(n, workspace, static_cast<hipStream_t>(stream)));
     return DGQ_OK;
 }
@@ -1531,6 +1543,8 @@ int dgq_w4_matvec(const void *x, int32_t dtype, int64_t x_row_stride, int32_t M,
     const size_t need = w4_matvec_workspace_bytes(M, m);
     if (need && (!workspace || workspace_bytes < need || !aligned16(workspace)))
         return fail(DGQ_EWORKSPACE, "dgq_w4_matvec: workspace missing, too small or misaligned");
+    if (overlap(x, span((__int128)(M - 1) * x_row_stride + C - 1, dtype), y, span((__int128)M * O - 1, out_dtype)))
+        return fail(DGQ_EINVAL, "dgq_w4_matvec: y overlaps x");
     DGQ_HIP(launch_w4_matvec({x, dtype, x_row_stride, M, bias, act, y, out_dtype}, m, workspace, static_cast<hipStream_t>(stream)));
     return DGQ_OK;
 }

@@ -39,6 +39,8 @@ def _norm(lib, **kw):
     (dict(row=-8), EINVAL), (dict(batch=-8), EINVAL), (dict(add=P, add_s=-1), EINVAL), (dict(scale=P, scale_s=-1), EINVAL),
     (dict(shift=P, shift_s=-1), EINVAL), (dict(x=P + 2), EALIGN), (dict(x=P + 1, dtype=1), EALIGN), (dict(out=P + 2), EALIGN),
     (dict(weight=P + 2), EALIGN), (dict(bias=P + 1), EALIGN), (dict(add=P + 2), EALIGN), (dict(offsets=P + 2), EALIGN),
+    (dict(row=16), EINVAL), (dict(out=P + 32), EINVAL), (dict(out=P - 32), EINVAL), (dict(dtype=1, out_dtype=0, G=1), EINVAL),
+    (dict(B=2, batch=0), EINVAL), (dict(row=0), EINVAL), (dict(row=1 << 62, out=P + 512), EINVAL),
     (dict(N=100000), EWORKSPACE), (dict(N=100000, ws=P, ws_bytes=16), EWORKSPACE), (dict(N=100000, ws=P + 8, ws_bytes=1 << 30), EWORKSPACE)])
 def test_groupnorm(lib, kw, code):
     assert _norm(lib, **kw) == code
@@ -83,6 +85,7 @@ def test_w4_pack_and_unpack(lib, kw, code):
     (dict(x=None), EINVAL), (dict(y=None), EINVAL), (dict(data=None), EINVAL), (dict(dtype=4), EINVAL), (dict(out_dtype=1), EINVAL),
     (dict(dtype=1, out_dtype=2), EINVAL), (dict(M=-1), EINVAL), (dict(row=-1), EINVAL), (dict(act=2), EINVAL), (dict(group=1), EUNSUPPORTED),
     (dict(M=(1 << 19) + 1), EUNSUPPORTED), (dict(x=P + 2), EALIGN), (dict(y=P + 2), EALIGN), (dict(bias=P + 2), EALIGN), (dict(data=P + 4), EALIGN),
+    (dict(), EINVAL), (dict(y=P + 28), EINVAL), (dict(y=P - 28), EINVAL), (dict(M=3, row=1 << 61, y=P + 512), EINVAL),
     (dict(C=20000), EWORKSPACE), (dict(C=20000, ws=P, ws_bytes=8), EWORKSPACE), (dict(C=20000, ws=P + 4, ws_bytes=1 << 30), EWORKSPACE)])
 def test_w4_matvec(lib, kw, code):
     a = dict(x=P, dtype=0, row=8, M=1, data=P, O=8, C=8, group=32, bias=None, act=0, y=P, out_dtype=0, ws=None,
