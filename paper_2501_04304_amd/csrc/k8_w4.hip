@@ -235,7 +235,7 @@ struct Cut {
     int32_t tiles, shares, splits, chunk, row_shift;
 };
 
-// Bound by the bytes of the weights (1 x 8192 -> 28672 bf16 25.9 us, 4.8 TB/s; a read of as many bytes takes 21) and, from 16 rows
+// Bound by the bytes of the weights (1 x 8192 -> 28672 bf16 23.8 us, 5.2 TB/s; a read of as many bytes takes 21) and, from 16 rows
 // on, by the vector pipes: 55 instructions to a unit of one tile beside four matrix instructions (eight for fp32), 130 (bf16) or
 // 230 (fp32) to bring 16 rows of a unit into fp16, once for all tiles of a workgroup.  A wavefront's next kAhead units are on
 // their way while it works on as many, and the rows of the next chunk while all work on this one.  Small products are bound by
@@ -253,7 +253,16 @@ struct Units {
     uint32_t word[kAhead<J>][4 / J];
 };
 
-template <class T, class Y, int J, int SHIFT>
+// Codes, or codes that no cache need keep.
+template <bool ONCE>
+__device__ uint4 read_codes(const char *p) {
+    typedef uint32_t words __attribute__((ext_vector_type(4)));
+    if constexpr (!ONCE) return *reinterpret_cast<const uint4 *>(p);
+    const words v = __builtin_nontemporal_load(reinterpret_cast<const words *>(p));
+    return {v.x, v.y, v.z, v.w};
+}
+
+template <class T, class Y, int J, int SHIFT, bool ONCE>
 __global__ __launch_bounds__(64 * kMaxWaves<T>) void k_w4_matvec(const T *__restrict__ x, int64_t x_row, int32_t M, W4 m, Cut cut,
                                                    const float *__restrict__ bias, int32_t silu_on, Y *__restrict__ y,
                                                    float *__restrict__ parts) {
@@ -276,7 +285,7 @@ __global__ __launch_bounds__(64 * kMaxWaves<T>) void k_w4_matvec(const T *__rest
 #pragma unroll
         for (int d = 0; d < AHEAD; ++d) {
             const int t = min(first + d * cut.shares, end - 1);
-            to.code[d] = *reinterpret_cast<const uint4 *>(codes + (uint32_t)(t * 1024 + lane * 16));  // (a tile has less than 2^24 bytes)
+            to.code[d] = read_codes<ONCE>(codes + (uint32_t)(t * 1024 + lane * 16));  // (a tile has less than 2^24 bytes)
             const uint32_t *w = reinterpret_cast<const uint32_t *>(words + (uint32_t)(t * (256 / J) + l.r * (16 / J)));
 #pragma unroll
             for (int g = 0; g < 4 / J; ++g) to.word[d][g] = w[g];
@@ -442,6 +451,12 @@ Ways ways_for(int32_t M, int32_t R, int32_t T, int most) {
     return {tiles, shares, splits};
 }
 
+// Whether the codes go past the caches.  The 256 MB next to memory seldom hold weights of 100 MB until their next use, and reads
+// that leave no lines there are faster: bf16 1 x 8192 -> 28672 23.8 us against 26.2, four rows 26.7 and 27.8, 131072 outputs 100 and
+// 106.  Smaller weights that are used again at once lose (1 x 8192 -> 16384 16.2 and 15.4), more than 16 rows read them several
+// times, and fp32 rows are not bound by them (30.8 and 29.0).
+bool read_once(int32_t M, const W4 &m) { return M <= 16 && m.units() >= 100000000 / 1024; }
+
 template <class F>
 void by_group(int32_t group, F f) {
     group == 32 ? f(std::integral_constant<int, 1>{}) : group == 64 ? f(std::integral_constant<int, 2>{}) : f(std::integral_constant<int, 4>{});
@@ -487,16 +502,23 @@ hipError_t launch_w4_matvec(const W4Product &p, const W4 &m, void *workspace, hi
             by_group(m.group, [&](auto j) {
                 constexpr int J = decltype(j)::value;
                 const dim3 grid((m.R + c.tiles - 1) / c.tiles, (p.M + 15) / 16, c.splits);
-                auto go = [&](auto shift) {
+                auto go = [&](auto shift, auto once) {
                     constexpr int S = decltype(shift)::value;
-                    e = DGQ_ENSURE_LDS((k_w4_matvec<T, Y, J, S>), lds_bytes<T>(c));
+                    constexpr bool ONCE = decltype(once)::value;
+                    e = DGQ_ENSURE_LDS((k_w4_matvec<T, Y, J, S, ONCE>), lds_bytes<T>(c));
                     if (e == hipSuccess)
-                        k_w4_matvec<T, Y, J, S><<<grid, 64 * c.tiles * c.shares, lds_bytes<T>(c), st>>>(
+                        k_w4_matvec<T, Y, J, S, ONCE><<<grid, 64 * c.tiles * c.shares, lds_bytes<T>(c), st>>>(
                             static_cast<const T *>(p.x), p.x_row, p.M, m, c, p.bias, p.act == DGQ_ACT_SILU, y, parts);
                 };
-                c.row_shift == 0   ? go(std::integral_constant<int, 0>{})
-                : c.row_shift == 2 ? go(std::integral_constant<int, 2>{})
-                                   : go(std::integral_constant<int, 4>{});
+                auto by_rows = [&](auto once) {
+                    c.row_shift == 0   ? go(std::integral_constant<int, 0>{}, once)
+                    : c.row_shift == 2 ? go(std::integral_constant<int, 2>{}, once)
+                                       : go(std::integral_constant<int, 4>{}, once);
+                };
+                if constexpr (sizeof(T) == 2) {
+                    if (read_once(p.M, m)) return by_rows(std::true_type{});
+                }
+                by_rows(std::false_type{});
             });
             if (e == hipSuccess && c.splits > 1)
                 k_w4_join<Y><<<(p.M * m.O + 255) / 256, 256, 0, st>>>(parts, c.splits, p.M, m.O, p.bias, p.act == DGQ_ACT_SILU, y);

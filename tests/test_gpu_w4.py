@@ -263,6 +263,30 @@ def test_rows_of_one_call_and_of_several(dgq):
     assert torch.equal(dgq.dgq_w4_matvec(x, w)[0], dgq.dgq_w4_matvec(y, w)[0])
 
 
+@pytest.mark.parametrize("group", GROUPS)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_codes_of_100_mb(dgq, dtype, group):
+    """Three tiles of weights 509 times over: every copy's outputs are the first one's to the bit."""
+    import torch
+    rng = np.random.default_rng(19)
+    C, copies = 8192, 509
+    O = 48 * copies
+    w, n = _layer(rng, 48, C)
+    small = dgq.dgq_w4_pack(dgq.W4Weight.empty(48, C, group), w)
+    codes, words = _bytes_equal(dgq, small, n, group)
+    big = dgq.W4Weight.empty(O, C, group)
+    part = 3 * (C // 128) * 1024
+    assert part * copies > 100000000 // 1024 * 1024
+    big.data[:part * copies].view(copies, part).copy_(small.data[:part].expand(copies, -1))
+    big.data[part * copies:].view(copies, -1).copy_(small.data[part:].expand(copies, -1))
+    for M in (1, 3, 16, 17):
+        x = _up(rng.standard_normal((M, C)).astype(np.float32), dtype)
+        y = dgq.dgq_w4_matvec(x, big, dtype=torch.float32).view(M, copies, 48)
+        assert torch.equal(y, y[:, :1].expand(-1, copies, -1))
+        want, tol = ref.matvec(x.float().cpu().numpy(), codes, words, group, 48, pieces=2 if dtype == "fp32" else 1)
+        assert (np.abs(y[:, 0].double().cpu().numpy() - want) <= tol).all()
+
+
 def test_codes_past_4_gib(dgq):
     """The last outputs of 262144 x 40960 weights, whose codes take 5 GiB."""
     import torch
