@@ -90,12 +90,11 @@ struct Shape {
 
 // A thread's vector of a slice: channels c0 .. c0 + V - 1.  The last vector of all ends with the channels, and the first `again`
 // of its values are the vector before's; `have`: values of its own (0: no vector).  Fewer channels than V: `have` values, no more.
-template <class T>
+template <int V>
 struct Place {
     int pr, high, c_slice, wide, c0, again, have;
     bool on;  // a row and a vector
     __device__ Place(const Shape &sh, int32_t C) {
-        constexpr int V = kVec<T>;
         const int tid = threadIdx.x;
         high = sh.threads / sh.width, wide = sh.width * V;
         pr = tid / sh.width;
@@ -131,11 +130,10 @@ __device__ double2 strided_sum(const double2 *entries, int64_t n, int from, int 
 }
 
 // A thread's n rows, `step` elements apart: f(index of the row, values).  kAhead loads are on their way while as many rows are
-// worked on.
-constexpr int kAhead = 4;
-template <class T>
+// worked on (64 bytes of them).  PAST: past the caches.
+template <class T, int V, bool PAST>
 struct RowsOf {
-    static constexpr int V = kVec<T>;
+    static constexpr int kAhead = 4 * kVec<T> / V;
     using Vec = loose<T, V>;
     const T *row;
     int64_t step;
@@ -147,7 +145,10 @@ struct RowsOf {
     __device__ void fetch(Vec (&to)[kAhead], int i) const {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
-            if (i + u < n) to[u] = *reinterpret_cast<const Vec *>(row + (i + u) * step);
+            if (i + u < n) {
+                const Vec *from = reinterpret_cast<const Vec *>(row + (i + u) * step);
+                to[u] = PAST ? load_past(from) : *from;
+            }
     }
     template <class F>
     __device__ void each(F f) {
@@ -186,7 +187,7 @@ __global__ __launch_bounds__(kMaxThreads) void k_gn_sums(const T *__restrict__ x
     constexpr int V = kVec<T>;
     extern __shared__ double2 entries[];  // [values of a vector, or 1 where vectors end with their groups][high][width]
     const int tid = threadIdx.x;
-    const Place<T> at(sh, C);
+    const Place<V> at(sh, C);
     const int high = at.high, c_slice = at.c_slice, c_end = min(c_slice + at.wide, C), Cg = C / G, each = Cg % V ? 1 : V;  // channels of an entry
     // neighbouring lanes that share a group's entries
     int lanes = 64;
@@ -195,7 +196,7 @@ __global__ __launch_bounds__(kMaxThreads) void k_gn_sums(const T *__restrict__ x
         double s[V] = {}, ss[V] = {};
         if (at.on) {
             const int n = (int)((r1 - r0 - at.pr + high - 1) / high);
-            RowsOf<T>(x + xs.at(im, b, r0 + at.pr) + at.c0, high * xs.row, n, C < V ? at.have : 0).each([&](int, const float (&f)[V]) {
+            RowsOf<T, V, false>(x + xs.at(im, b, r0 + at.pr) + at.c0, high * xs.row, n, C < V ? at.have : 0).each([&](int, const float (&f)[V]) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     s[i] += (double)f[i];
@@ -297,18 +298,21 @@ __global__ __launch_bounds__(256) void k_gn_tables(const double2 *__restrict__ s
 }
 
 // ---- values ----------------------------------------------------------------------------------------------------------
-// Bound by the bytes of x and y (16 x 4096 x 640 fp32: 60 us, 5.6 TB/s).  x and y may be one buffer.  tables null: every workgroup
-// adds up its image's sums itself, its first rows on their way meanwhile: 2.7 us at 128 sums of 32 groups, and a launch less.
+// Bound by the bytes of x and y.  x and y may be one buffer.  tables null: every workgroup adds up its image's sums itself, its
+// first rows on their way meanwhile: 2.7 us at 128 sums of 32 groups, and a launch less.  The second read of x and the writes of y
+// go past the caches, so that more of x is still there: 16 x 4096 x 640 fp32 82 us for both kernels, 93 with writes alone, 108 with
+// neither, and 113, 115 and 123 with a kernel behind that reads y.  Such a write wants whole lines: a vector is 16 bytes of y (8 bf16
+// values to 32 bytes of fp32, 16 x up to 4096 x 640 packed: 62, by the 4 here 47).
 template <class T, class Y>
 __global__ __launch_bounds__(kMaxThreads) void k_gn_apply(const T *x, Images im, Rows xs, Chunks ch, Shape sh, int32_t C, int32_t G,
                                                           const float *__restrict__ tables, const double2 *__restrict__ sums,
-                                                          int32_t parts, const float *__restrict__ weight,
+                                                          int32_t parts, int32_t slices, const float *__restrict__ weight,
                                                           const float *__restrict__ bias, float eps, NormTerms terms, int32_t silu_on,
                                                           Y *y) {
-    constexpr int V = kVec<T>;
+    constexpr int V = kVec<Y>;
     extern __shared__ float lines[];  // the groups' m and r, [p, a, q][width V + V]
     const int tid = threadIdx.x, Cg = C / G;
-    const Place<T> at(sh, C);
+    const Place<V> at(sh, C);
     const int high = at.high, c_slice = at.c_slice, wide = at.wide;
     const bool same = static_cast<const void *>(x) == y;
     int lanes = 64;
@@ -317,7 +321,7 @@ __global__ __launch_bounds__(kMaxThreads) void k_gn_apply(const T *x, Images im,
         float p[V], a[V], q[V];
         const float *from;
         int64_t stride;
-        RowsOf<T> rows(x + xs.at(im, b, r0 + at.pr) + at.c0, high * xs.row, at.on ? (int)((r1 - r0 - at.pr + high - 1) / high) : 0,
+        RowsOf<T, V, true> rows(x + xs.at(im, b, r0 + at.pr) + at.c0, high * xs.row, at.on ? (int)((r1 - r0 - at.pr + high - 1) / high) : 0,
                        C < V ? at.have : 0);
         if (tables) {
             from = tables + (int64_t)b * 3 * C + at.c0;
@@ -325,7 +329,7 @@ __global__ __launch_bounds__(kMaxThreads) void k_gn_apply(const T *x, Images im,
         } else {
             Group *groups = reinterpret_cast<Group *>(lines);
             float *to = lines + G * (sizeof(Group) / sizeof(float));
-            const int64_t first = ch.first(im, b), n_parts = (int64_t)ch.parts(im, b) * sh.slices;
+            const int64_t first = ch.first(im, b), n_parts = (int64_t)ch.parts(im, b) * slices;
             const double per = 1 / ((double)(im.end(b) - im.start(b)) * Cg);
             // (the last vector of all may begin in front of its slice)
             const int c_first = max(c_slice - V, 0), c_end = min(c_slice + wide, C), room = wide + V;
@@ -333,7 +337,7 @@ __global__ __launch_bounds__(kMaxThreads) void k_gn_apply(const T *x, Images im,
             if (c_first + tid < c_end) mine = Terms::of(terms, weight, bias, b, c_first + tid);
             __syncthreads();
             for (int g = tid / lanes; g < G; g += sh.threads / lanes) {
-                const double2 s = strided_sum(sums + ((int64_t)g * parts + first) * sh.slices, n_parts, tid & (lanes - 1), lanes, lanes);
+                const double2 s = strided_sum(sums + ((int64_t)g * parts + first) * slices, n_parts, tid & (lanes - 1), lanes, lanes);
                 if ((tid & (lanes - 1)) == 0) groups[g] = Group(s, per, eps);
             }
             __syncthreads();
@@ -365,7 +369,7 @@ __global__ __launch_bounds__(kMaxThreads) void k_gn_apply(const T *x, Images im,
                 for (int i = 0; i < V; ++i)
                     if (i >= at.again) row[i] = (Y)v[i];
             } else {
-                store_vector(row, at.again + at.have, v);
+                store_past(row, at.again + at.have, v);
             }
         });
     });
@@ -506,9 +510,12 @@ Chunks chunks_for(const NormCall &n, const Shape &sh) {
 
 constexpr int64_t kMaxFolded = 16384;  // sums of an image that every workgroup may read
 
-// Whether a workgroup can hold an image's group, and how: threads and vectors of each (0: it cannot, or is slower: long stripes
-// touch a line of memory in every row, many values keep its vector pipes busy, and both need most CUs to keep up.  2 x 1024 x 1280
-// fp32 10.7 us, 14.9 with sums of chunks; 2 x 4096 x 320 16.7 and 14.8, 8 x 4096 x 320 23.8 and 26.3).
+// Whether a workgroup can hold an image's group, and how: threads and vectors of each (0: it cannot, or is slower).  Many values
+// keep its vector pipes busy and need most CUs to keep up: 2 x 1024 x 1280 fp32 10.7 us, 14.1 with sums of chunks, but 2 x 4096 x
+// 320 16.7 and 13.9, 4 x 4096 x 320 18.3 and 16.8.  A group's stripe of the rows touches lines of memory that others touch too,
+// and no access of it can go past the caches: large maps of stripes below a line or two are faster in chunks (16 x 4096 x 320 fp32 63
+// and 44, 16 x 4096 x 640 bf16 67 and 49, 32 x 1024 x 320 bf16 22.8 and 19.7; 16 x 1024 x 640 fp32 22 and 25, 32 x 1024 x 1280 83
+// and 90).
 struct Hold {
     int32_t threads = 0, held = 0, width = 0;
 };
@@ -517,6 +524,8 @@ Hold hold_for(const NormCall &n) {
     if (Cg < V || width > 256 || (int64_t)n.B * n.G > 1 << 24) return {};
     const int64_t rows = n.offsets ? n.N / n.B * 3 / 2 : n.N;  // of a long image
     if ((rows > 2048 || rows * Cg > 65536) && (int64_t)n.B * n.G < 192) return {};
+    const int64_t stripe = Cg * (16 / V), bytes = n.rows() * n.C * (16 / V);
+    if ((stripe < 128 && bytes >= 44000000) || (stripe < 32 && bytes >= 20000000)) return {};
     const Hold ways[] = {{256, 4, width}, {1024, 4, width}, {1024, 8, width}, {1024, 16, width}};
     for (const Hold &h : ways)
         if (rows <= (int64_t)h.held * (h.threads / width)) return h;
@@ -595,11 +604,13 @@ hipError_t launch_groupnorm(const NormCall &n, void *workspace, hipStream_t st) 
                 e = launch_one<T, Y>(n, p.hold, im, xs, st);
                 return;
             }
-            const int bytes = tables ? 0 : n.G * (int)sizeof(Group) + 3 * (p.shape.width + 1) * kVec<T> * (int)sizeof(float);
+            const Shape shape = shape_for(n.C, kVec<Y>, kMaxThreads);
+            const int bytes = tables ? 0 : n.G * (int)sizeof(Group) + 3 * (shape.width + 1) * kVec<Y> * (int)sizeof(float);
             e = DGQ_ENSURE_LDS((k_gn_apply<T, Y>), bytes);
             if (e == hipSuccess)
-                k_gn_apply<T, Y><<<grid, p.shape.threads, bytes, st>>>(x, im, xs, p.chunks, p.shape, n.C, n.G, tables, sums, p.parts,
-                                                                       n.weight, n.bias, n.eps, n.terms, n.act == DGQ_ACT_SILU, y);
+                k_gn_apply<T, Y><<<dim3(p.chunks.count, shape.slices), shape.threads, bytes, st>>>(
+                    x, im, xs, p.chunks, shape, n.C, n.G, tables, sums, p.parts, p.shape.slices, n.weight, n.bias, n.eps, n.terms,
+                    n.act == DGQ_ACT_SILU, y);
         });
     });
     return e == hipSuccess ? hipGetLastError() : e;

@@ -13,9 +13,8 @@ template <class T, int N>
 using loose [[gnu::aligned(alignof(T))]] = T __attribute__((ext_vector_type(N)));
 
 // The first `have` of a vector's elements, the others 0.
-template <class T>
-__device__ inline void load_vector(const T *from, int have, float (&f)[kVec<T>]) {
-    constexpr int V = kVec<T>;
+template <class T, int V>
+__device__ inline void load_vector(const T *from, int have, float (&f)[V]) {
     if (have >= V) {
         const loose<T, V> x = *reinterpret_cast<const loose<T, V> *>(from);
 #pragma unroll
@@ -37,6 +36,20 @@ __device__ inline void store_vector(T *to, int have, const float (&f)[V]) {
         for (int i = 0; i < V; ++i)
             if (i < have) to[i] = (T)f[i];
     }
+}
+
+// The same for what no cache need keep (nontemporal): whole vectors.
+template <class V>
+__device__ inline V load_past(const V *from) {
+    return __builtin_nontemporal_load(from);
+}
+template <class T, int V>
+__device__ inline void store_past(T *to, int have, const float (&f)[V]) {
+    if (have < V) return store_vector(to, have, f);
+    loose<T, V> x;
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = (T)f[i];
+    __builtin_nontemporal_store(x, reinterpret_cast<loose<T, V> *>(to));
 }
 
 // t / (1 + exp(-t)) with the hardware's 2^x and 1 / x, good to one unit in the last place each; the exponent's own rounding adds
