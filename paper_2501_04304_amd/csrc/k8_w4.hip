@@ -61,7 +61,7 @@ __device__ float row_max(float x) {
 
 // ---- packing ---------------------------------------------------------------------------------------------------------
 // A wavefront per unit, four neighbours of a row of units to a workgroup: a lane reads what its 16 bytes of codes stand for, lines
-// of memory meet in four loads.  Bound by the bytes of w (8192 x 8192 bf16: 38 us there, 27 back, 5.2 TB/s over both, a copy 5.3).
+// of memory meet in four loads.  Bound by the bytes of w (8192 x 8192 bf16 31.5 us, 5.4 TB/s).
 template <class T, int J>  // J: words of 32 inputs in a group
 __global__ __launch_bounds__(256) void k_w4_pack(const T *__restrict__ w, int64_t w_row, W4 m) {
     const uint32_t wide = (m.T + 3) / 4, tile = blockIdx.x / wide;
@@ -114,33 +114,34 @@ __global__ __launch_bounds__(256) void k_w4_pack(const T *__restrict__ w, int64_
         for (int g = 0; g < 4 / J; ++g) m.words()[(unit * 16 + l.r) * (4 / J) + g] = word[g];
 }
 
+// A wavefront per unit: its stores are whole rows of the unit, one next to the other, whose lanes pick their codes' words.  past:
+// the values are whole lines of memory and go past the caches (8192 x 8192 bf16 25.5 us, 6.6 TB/s, and 33 without; behind k_w4_pack
+// 57 for both and 65).  Rows that begin inside a line lose by that (8191 x 8191 fp16 behind its packing 103 and 89).
 template <class T, int J>
-__global__ __launch_bounds__(256) void k_w4_unpack(W4 m, T *__restrict__ w) {
+__global__ __launch_bounds__(256) void k_w4_unpack(W4 m, T *__restrict__ w, bool past) {
+    constexpr int V = kVec<T>, kLanes = kUnit / V, kRows = 64 / kLanes;  // lanes to a row, rows at a time
     const uint32_t wide = (m.T + 3) / 4, tile = blockIdx.x / wide;
     const int t = (blockIdx.x - tile * wide) * 4 + (threadIdx.x >> 6);
     if (t >= m.T) return;
     const int64_t unit = (int64_t)tile * m.T + t;
-    const Lane l;
-    const int o = tile * 16 + l.r, k0 = t * kUnit + l.q * 8;
-    if (o >= m.O) return;
-    const uint4 all = reinterpret_cast<const uint4 *>(m.codes)[unit * 64 + (threadIdx.x & 63)];
-    const uint32_t code[4] = {all.x, all.y, all.z, all.w};
-    T *row = w + (int64_t)o * m.C;
-    const bool whole = k0 + 104 <= m.C;
+    const int lane = threadIdx.x & 63, at = lane % kLanes * V, up = lane / kLanes, j = at / 32, q = at / 8 % 4, k = t * kUnit + at;
+    const uint32_t *codes = reinterpret_cast<const uint32_t *>(m.codes) + unit * 256 + 64 * q + j;
+    const uint32_t *words = m.words() + unit * (64 / J) + j / J;
+    uint32_t code[16 / kRows], word[16 / kRows];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const uint32_t word = m.words()[(unit * 16 + l.r) * (4 / J) + j / J];
-        const float s = __uint_as_float(word & ~15u);
-        constexpr int V = kVec<T>;
-        const int zero = word & 15;
+    for (int n = 0; n < 16 / kRows; ++n) code[n] = codes[4 * (n * kRows + up)], word[n] = words[(n * kRows + up) * (4 / J)];
 #pragma unroll
-        for (int v = 0; v < 8 / V; ++v) {
-            float f[V];
+    for (int n = 0; n < 16 / kRows; ++n) {
+        const int o = tile * 16 + n * kRows + up;
+        if (o >= m.O) return;
+        const float s = __uint_as_float(word[n] & ~15u);
+        const int zero = word[n] & 15;
+        const uint32_t own = code[n] >> at % 8 * 2;  // (the nibbles of 4 .. 7 lie two above those of 0 .. 3)
+        float f[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) f[i] = (float)((int)(code[j] >> (4 * nibble(v * V + i)) & 15) - zero) * s;
-            const int k = k0 + 32 * j + v * V;
-            store_vector(row + k, whole ? V : m.C - k, f);
-        }
+        for (int i = 0; i < V; ++i) f[i] = (float)((int)(own >> (4 * nibble(i)) & 15) - zero) * s;
+        T *to = w + (int64_t)o * m.C + k;
+        past ? store_past(to, m.C - k, f) : store_vector(to, m.C - k, f);
     }
 }
 
@@ -477,8 +478,9 @@ hipError_t launch_w4_pack(const void *w, int32_t dtype, int64_t w_row, const W4 
 hipError_t launch_w4_unpack(const W4 &m, int32_t dtype, void *w, hipStream_t st) {
     by_dtype(dtype, [&](auto t) {
         using T = decltype(t);
+        const bool past = (reinterpret_cast<uintptr_t>(w) | (uint64_t)m.C * sizeof(T)) % 128 == 0;
         by_group(m.group, [&](auto j) {
-            k_w4_unpack<T, j.value><<<(unsigned)m.R * ((m.T + 3) / 4), 256, 0, st>>>(m, static_cast<T *>(w));
+            k_w4_unpack<T, j.value><<<(unsigned)m.R * ((m.T + 3) / 4), 256, 0, st>>>(m, static_cast<T *>(w), past);
         });
     });
     return hipGetLastError();
