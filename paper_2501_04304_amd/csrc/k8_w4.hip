@@ -242,16 +242,17 @@ struct Cut {
 // their way while it works on as many, and the rows of the next chunk while all work on this one.  Small products are bound by
 // latency: 2 x 320 -> 1280 5.2 us, 32 x 1280 -> 16640 fp32 12 (rows 2, their conversion 2, ten units a wavefront 3.5, the slowest
 // SIMD 2.6, the sums 1).
-template <int J>
-constexpr int kAhead = J == 1 ? 3 : 4;  // (four words to a unit: registers)
+// kAhead: 8 x 4096 -> 11000 bf16 11.3 us with two, 11.8 with three, 12.4 with four; 1 x 8192 -> 28672 fp16 23.6, 22.5 and 22.6.
+template <int J, bool ONCE>
+constexpr int kAhead = ONCE && J > 1 ? 3 : 2;
 // Wavefronts of a workgroup, as many as registers allow.
 template <class T>
-constexpr int kMaxWaves = sizeof(T) == 4 ? 10 : 12;
+constexpr int kMaxWaves = sizeof(T) == 4 ? 12 : 16;
 
-template <int J>
+template <int J, int AHEAD>
 struct Units {
-    uint4 code[kAhead<J>];
-    uint32_t word[kAhead<J>][4 / J];
+    uint4 code[AHEAD];
+    uint32_t word[AHEAD][4 / J];
 };
 
 // Codes, or codes that no cache need keep.
@@ -267,7 +268,7 @@ template <class T, class Y, int J, int SHIFT, bool ONCE>
 __global__ __launch_bounds__(64 * kMaxWaves<T>) void k_w4_matvec(const T *__restrict__ x, int64_t x_row, int32_t M, W4 m, Cut cut,
                                                    const float *__restrict__ bias, int32_t silu_on, Y *__restrict__ y,
                                                    float *__restrict__ parts) {
-    constexpr int P = kPieces<T>, AHEAD = kAhead<J>;
+    constexpr int P = kPieces<T>, AHEAD = kAhead<J, ONCE>;
     constexpr bool kPowers = !std::is_same_v<T, _Float16>;
     extern __shared__ uint4 lds[];  // [chunk][4 j][P][4 q][rows], then the powers [chunk][16]; later the sums
     const unsigned tid = threadIdx.x, lane = tid & 63;
@@ -282,7 +283,7 @@ __global__ __launch_bounds__(64 * kMaxWaves<T>) void k_w4_matvec(const T *__rest
     const Expand expand;
 
     // units first, first + shares, .. of a chunk that ends at `end` (its last again where there are no more)
-    auto fetch = [&](Units<J> &to, int first, int end) {
+    auto fetch = [&](Units<J, AHEAD> &to, int first, int end) {
 #pragma unroll
         for (int d = 0; d < AHEAD; ++d) {
             const int t = min(first + d * cut.shares, end - 1);
@@ -293,7 +294,7 @@ __global__ __launch_bounds__(64 * kMaxWaves<T>) void k_w4_matvec(const T *__rest
         }
     };
     const int begin = (int)((int64_t)m.T * blockIdx.z / cut.splits), stop = (int)((int64_t)m.T * (blockIdx.z + 1) / cut.splits);
-    Units<J> now, next;
+    Units<J, AHEAD> now, next;
     fetch(now, begin + share, min(begin + cut.chunk, stop));
 
     // this lane's row, and its units of a chunk: first, first + step, ..
@@ -323,7 +324,7 @@ __global__ __launch_bounds__(64 * kMaxWaves<T>) void k_w4_matvec(const T *__rest
         if (end < stop) part.load(mine, min(end + first, stop - 1) * kUnit + 8 * l.q, m.C);
 
         // a batch of units from t on with what is there, the next one on its way
-        auto batch = [&](int t, const Units<J> &with, Units<J> &next) {
+        auto batch = [&](int t, const Units<J, AHEAD> &with, Units<J, AHEAD> &next) {
             const bool same = t + AHEAD * cut.shares < end;
             fetch(next, same ? t + AHEAD * cut.shares : min(end + share, stop - 1), same ? end : min(end + cut.chunk, stop));
             __builtin_amdgcn_sched_barrier(0);  // they set out before the work below, not after it
@@ -425,8 +426,9 @@ Cut cut_of(int32_t M, const W4 &m, int tiles, int shares, int splits) {
 }
 
 // Wavefronts share the rows' conversion: tiles such that workgroups fill the 256 CUs in few rounds and wavefronts the four SIMDs
-// of each alike (64 x 8192 -> 28672 bf16 118 us with twelve tiles, 129 with eight), and the units cut among what is
-// left (of ten for few rows, whose wavefronts wait for memory alone: 1 x 4096 -> 16384 bf16 9.5 us with eight, 11 with sixteen).
+// of each alike (64 x 8192 -> 28672 bf16 a twelfth less with twelve tiles than with eight), and the units cut among what is left:
+// of twelve for few rows (3 x 7997 -> 22282 bf16 28 us with six wavefronts, 22 with twelve; 1 x 4096 -> 16384 9.5 with eight, 11 with
+// sixteen), in at most four parts where they take several chunks (35 x 9158 -> 1901 bf16 19 in four, 22 in eight).
 // Where that leaves more than half of the CUs without work and units enough to pay for a second kernel, every tile's units are
 // split among workgroups (29 x 6477 -> 103 fp32 23 us in one part, 8 in eight; 2 x 19840 -> 30 bf16 18 and 7; at 20 units they are
 // level): 6 to a part, which take one conversion, or 10 of few rows.
@@ -443,7 +445,7 @@ Ways ways_for(int32_t M, int32_t R, int32_t T, int most) {
         const double cost = rounds * ((t + 3) / 4 + (M > 4 ? 1 : 0.25)) + 1e-3 * rounds;  // of equals the fewest rounds
         if (cost < least) least = cost, tiles = t;
     }
-    while (shares * 2 * tiles <= (M > 4 ? most : 10) && shares * 2 <= std::min(T, 8)) shares *= 2;
+    while (shares * 2 * tiles <= (M > 4 ? most : 12) && shares * 2 <= std::min(T, M > 4 && T > 24 ? 4 : 8)) shares *= 2;
     if (M > 4 && T <= 10 && tiles > 1 && tiles * shares < T) tiles = (T + shares - 1) / shares;  // one conversion for all units
     if (all < 128 && T >= (M > 4 ? 20 : 48)) {
         splits = (int)(M > 4 ? std::min<int64_t>(512 / all, T / 6) : std::min<int64_t>(256 / all, T / 10));
