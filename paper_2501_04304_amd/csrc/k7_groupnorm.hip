@@ -14,8 +14,8 @@
 //
 // Maps whose groups fit a workgroup's registers: k_gn_one, x crosses memory once.  Others: k_gn_sums over chunks of rows, then
 // k_gn_apply, whose workgroups first add up their image's chunks (or k_gn_tables between the two, where those are many); x is
-// read twice.  2 x 64 x 1280 fp32 takes 5.1 us, 2 x 4096 x 320 15, 16 x 4096 x 640 107 and 1048576 x 128 fp16 164 (3.2 TB/s of its
-// bytes once, 4.9 of what it moves: plain loops that read a map of that size and then copy it take 168).
+// read twice.  2 x 64 x 1280 fp32 takes 5.1 us, 2 x 4096 x 320 13.8, 16 x 4096 x 640 82 (a copy of it 63) and 1048576 x 128 fp16 135
+// (101).
 #include <algorithm>
 
 #include "vectors.h"
@@ -179,7 +179,7 @@ struct RowsOf {
 
 // Bound by the bytes of x, and for small maps by the way from the kernel's arguments over x and LDS to the sums (4.7 us for 2 x
 // 4096 x 320, of which the rows take 2.5).  add enters per channel: sum x' = sum x + n add, sum x'^2 = sum x^2 + 2 add sum x + n add^2.
-// 16 x 4096 x 640 fp32: 47 us behind the last call's 168 MB on their way to memory.  sums: [G][parts][slices] double2.
+// 16 x 4096 x 640 fp32: 30 us, 5.6 TB/s.  sums: [G][parts][slices] double2.
 template <class T>
 __global__ __launch_bounds__(kMaxThreads) void k_gn_sums(const T *__restrict__ x, Images im, Rows xs, Chunks ch, Shape sh, int32_t C,
                                                          int32_t G, const float *__restrict__ add, int64_t add_row,
@@ -381,7 +381,8 @@ __global__ __launch_bounds__(kMaxThreads) void k_gn_apply(const T *x, Images im,
 // the one before counts there) and threads / width rows at a time.  Rows that do not fit are read twice.  A group is a stripe of
 // the rows, cut inside lines of memory: an XCD gets neighbouring groups, so that its cache puts the lines together.
 // Bound by latency where maps are small (2 x 64 x 1280 fp32 4 us on the GPU), by the longest image's 32 workgroups in 8 packed
-// images of up to 4096 x 960 bf16 (36.5 us; a copy of the bytes 18), by lines that two XCDs write (25 % more than there are) above.
+// images of up to 4096 x 960 bf16 (37.5 us; a copy of the bytes 18), by lines that two XCDs write (25 % more than there are) above.
+// Its stripes share lines, whose parts must meet in the caches: past them 16 x 4096 x 320 fp32 takes 120 us instead of 63.
 template <class T, class Y, int THREADS, int HELD>
 __global__ __launch_bounds__(THREADS) void k_gn_one(const T *x, Images im, Rows xs, int32_t C, int32_t G, int32_t width,
                                                     const float *__restrict__ weight, const float *__restrict__ bias, float eps,

@@ -240,7 +240,7 @@ struct Cut {
 // on, by the vector pipes: 55 instructions to a unit of one tile beside four matrix instructions (eight for fp32), 130 (bf16) or
 // 230 (fp32) to bring 16 rows of a unit into fp16, once for all tiles of a workgroup.  A wavefront's next kAhead units are on
 // their way while it works on as many, and the rows of the next chunk while all work on this one.  Small products are bound by
-// latency: 2 x 320 -> 1280 5.2 us, 32 x 1280 -> 16640 fp32 12 (rows 2, their conversion 2, ten units a wavefront 3.5, the slowest
+// latency: 2 x 320 -> 1280 5.1 us, 32 x 1280 -> 16640 fp32 11.5 (rows 2, their conversion 2, ten units a wavefront 3.5, the slowest
 // SIMD 2.6, the sums 1).
 // kAhead: 8 x 4096 -> 11000 bf16 11.3 us with two, 11.8 with three, 12.4 with four; 1 x 8192 -> 28672 fp16 23.6, 22.5 and 22.6.
 template <int J, bool ONCE>
