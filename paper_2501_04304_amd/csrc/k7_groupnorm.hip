@@ -33,7 +33,27 @@ struct Images {
     __device__ int64_t at(int32_t i) const { return min(max((int64_t)offsets[i], (int64_t)0), rows); }
     __device__ int64_t start(int32_t b) const { return offsets ? at(b) : b * n; }
     __device__ int64_t end(int32_t b) const { return offsets ? at(b + 1) : (b + 1) * n; }
+    // The first packed image that ends behind row r, B if none does: a wavefront tests 64 at a time, so that a search is one or
+    // two reads after one another (three above 4096 images).
+    __device__ int32_t image(int64_t r) const {
+        int32_t lo = 0, n = B;
+        for (;;) {
+            const int32_t step = (n + 63) >> 6;
+            const uint64_t behind = __ballot(at(lo + min(((int32_t)(threadIdx.x & 63) + 1) * step, n)) > r);
+            if (!behind) return lo + n;
+            const int32_t f = __builtin_ctzll(behind) * step;
+            lo += f;
+            if (step == 1) return lo;
+            n = min(step, n - f);
+        }
+    }
 };
+
+// Rows pr, pr + high, .. of those from r0 on and below r1 (of all maps there are less than 2^31).
+__device__ int rows_of(int64_t r0, int64_t r1, int pr, int high) {
+    const int32_t left = (int32_t)(r1 - r0) - pr;
+    return left > 0 ? (int)(((uint32_t)left + high - 1) / (uint32_t)high) : 0;
+}
 
 // Chunks of P rows, one to a workgroup.  Images of one size are cut one by one (`per` chunks each); packed ones are cut across, so
 // that ragged ones keep all workgroups busy, and a chunk that several images meet in is worked on image by image.  Image b's part
@@ -41,11 +61,11 @@ struct Images {
 struct Chunks {
     int64_t P;
     int32_t count, per;
-    __device__ int32_t first(const Images &im, int32_t b) const { return im.offsets ? (int32_t)(im.start(b) / P) + b : b * per; }
+    __device__ int32_t first(const Images &im, int32_t b) const { return im.offsets ? (int32_t)((uint32_t)im.start(b) / (uint32_t)P) + b : b * per; }
     __device__ int32_t parts(const Images &im, int32_t b) const {
         if (!im.offsets) return per;
         const int64_t s = im.start(b), e = im.end(b);
-        return e > s ? (int32_t)((e - 1) / P - s / P) + 1 : 0;
+        return e > s ? (int32_t)((uint32_t)(e - 1) / (uint32_t)P - (uint32_t)s / (uint32_t)P) + 1 : 0;
     }
     // f(image, part, first row, row behind the last) for the images of chunk c.  (Offsets that do not ascend give wrong rows, but
     // rows of x, images below B and parts below count + B.)
@@ -60,12 +80,8 @@ struct Chunks {
         int64_t r = c * P;
         const int64_t r1 = min(r + P, im.rows);
         while (r < r1) {
-            int32_t lo = 0, hi = im.B;
-            while (lo < hi) {
-                const int32_t mid = (lo + hi) >> 1;
-                if (im.at(mid + 1) > r) hi = mid; else lo = mid + 1;
-            }
-            if (lo == im.B) return;
+            const int32_t lo = im.image(r);
+            if (lo >= im.B) return;
             const int64_t from = max(r, im.start(lo)), to = min(im.end(lo), r1);
             if (to > from) f(lo, c + lo, from, to);
             const int64_t next = max(from, to);
@@ -195,7 +211,7 @@ __global__ __launch_bounds__(kMaxThreads) void k_gn_sums(const T *__restrict__ x
     ch.each(im, blockIdx.x, [&](int32_t b, int32_t part, int64_t r0, int64_t r1) {
         double s[V] = {}, ss[V] = {};
         if (at.on) {
-            const int n = (int)((r1 - r0 - at.pr + high - 1) / high);
+            const int n = rows_of(r0, r1, at.pr, high);
             RowsOf<T, V, false>(x + xs.at(im, b, r0 + at.pr) + at.c0, high * xs.row, n, C < V ? at.have : 0).each([&](int, const float (&f)[V]) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
@@ -321,7 +337,7 @@ __global__ __launch_bounds__(kMaxThreads) void k_gn_apply(const T *x, Images im,
         float p[V], a[V], q[V];
         const float *from;
         int64_t stride;
-        RowsOf<T, V, true> rows(x + xs.at(im, b, r0 + at.pr) + at.c0, high * xs.row, at.on ? (int)((r1 - r0 - at.pr + high - 1) / high) : 0,
+        RowsOf<T, V, true> rows(x + xs.at(im, b, r0 + at.pr) + at.c0, high * xs.row, at.on ? rows_of(r0, r1, at.pr, high) : 0,
                        C < V ? at.have : 0);
         if (tables) {
             from = tables + (int64_t)b * 3 * C + at.c0;
@@ -399,7 +415,7 @@ __global__ __launch_bounds__(THREADS) void k_gn_one(const T *x, Images im, Rows 
     const int c = min(v * V, Cg - V), again = v * V - c, c0 = g * Cg + c;  // again: values that the vector before has too
     const int64_t r0 = im.start(b), r1 = im.end(b);
     if (r1 <= r0) return;
-    const int n = pr < high ? max((int)((r1 - r0 - pr + high - 1) / high), 0) : 0;  // rows of this thread
+    const int n = pr < high ? rows_of(r0, r1, pr, high) : 0;  // rows of this thread
     const int64_t step = high * xs.row;
     const T *from = x + xs.at(im, b, r0 + pr) + c0;
     const double per = 1 / ((double)(r1 - r0) * Cg);

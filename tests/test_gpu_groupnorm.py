@@ -128,6 +128,22 @@ def test_packed_with_one_long_image(dgq, C, G, in_place, dtype):
     _check(out, *ref.groupnorm(xn, offsets[:-1], offsets[1:], G, silu=True, out_type=dtype, **t))
 
 
+@pytest.mark.parametrize("B", [63, 64, 65, 130, 4097, 9000])
+def test_packed_of_many_images(dgq, B):
+    """Images of 0 to 3 rows, of which a chunk holds many: the search among them takes one to three steps."""
+    import torch
+    rng = np.random.default_rng(B)
+    C, G = 40, 20  # groups below a vector
+    offsets = 3 + np.concatenate([[0], np.cumsum(rng.integers(0, 4, B))])
+    rows = int(offsets[-1]) + 2
+    x, xn = _map(rng, rows, C, "fp32")
+    t = _tables(rng, B, C, ("weight", "add"))
+    out = torch.full((rows, C), 7.0, device="cuda")
+    assert dgq.dgq_groupnorm(x, G, offsets=_up(offsets.astype(np.int32)), out=out, **{k: _up(v) for k, v in t.items()}) is out
+    _check(out, *ref.groupnorm(xn, offsets[:-1], offsets[1:], G, **t))
+    assert (out[:3] == 7).all() and (out[-2:] == 7).all()
+
+
 def test_packed_offsets_out_of_order_stay_inside(dgq):
     """Offsets below 0, above the rows and descending: wrong rows, but none outside the tensors."""
     import torch
