@@ -210,19 +210,19 @@ __device__ float convert(const T (&x)[4][8], Piece (&a)[4][kPieces<T>]) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf((float)x[j][i]));
-        const int e = max((int)(__float_as_uint(row_max(top)) >> 23), 15);  // 15: 2^-112
+            for (int i = 0; i < 8; ++i) top = __builtin_elementwise_maximum(top, fabsf((float)x[j][i]));
+        const int e = max((int)(__float_as_uint(row_max(top)) >> 23 & 255), 15);  // 15: 2^-112
         const float down = __uint_as_float((uint32_t)(268 - e) << 23);     // 2^(14 - (e - 127)); e = 255 (infinity): 2^-114
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                float2v v{(float)x[j][2 * i] * down, (float)x[j][2 * i + 1] * down};
-#pragma unroll
-                for (int n = 0; n < kPieces<T>; ++n) {
-                    a[j][n].p[i] = __builtin_convertvector(v, half2v);
-                    if (n + 1 < kPieces<T>) v -= __builtin_convertvector(a[j][n].p[i], float2v);
-                }
+                // (the second piece in one instruction: the rest of a product with a power of two is exact)
+                const float x0 = (float)x[j][2 * i], x1 = (float)x[j][2 * i + 1];
+                const half2v h = __builtin_convertvector((float2v{x0 * down, x1 * down}), half2v);
+                a[j][0].p[i] = h;
+                if constexpr (kPieces<T> > 1)
+                    a[j][1].p[i] = __builtin_convertvector((float2v{fmaf(x0, down, -(float)h[0]), fmaf(x1, down, -(float)h[1])}), half2v);
             }
         return __uint_as_float((uint32_t)(e - 14) << 23);
     }
@@ -238,7 +238,7 @@ struct Cut {
 
 // Bound by the bytes of the weights (1 x 8192 -> 28672 bf16 23.8 us, 5.2 TB/s; a read of as many bytes takes 21) and, from 16 rows
 // on, by the vector pipes: 55 instructions to a unit of one tile beside four matrix instructions (eight for fp32), 130 (bf16) or
-// 230 (fp32) to bring 16 rows of a unit into fp16, once for all tiles of a workgroup.  A wavefront's next kAhead units are on
+// 200 (fp32) to bring 16 rows of a unit into fp16, once for all tiles of a workgroup.  A wavefront's next kAhead units are on
 // their way while it works on as many, and the rows of the next chunk while all work on this one.  Small products are bound by
 // latency: 2 x 320 -> 1280 5.1 us, 32 x 1280 -> 16640 fp32 11.5 (rows 2, their conversion 2, ten units a wavefront 3.5, the slowest
 // SIMD 2.6, the sums 1).
