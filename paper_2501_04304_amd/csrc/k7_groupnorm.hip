@@ -532,20 +532,22 @@ constexpr int64_t kMaxFolded = 16384;  // sums of an image that every workgroup 
 // 320 16.7 and 13.9, 4 x 4096 x 320 18.3 and 16.8.  A group's stripe of the rows touches lines of memory that others touch too,
 // and no access of it can go past the caches: large maps of stripes below a line or two are faster in chunks (16 x 4096 x 320 fp32 63
 // and 44, 16 x 4096 x 640 bf16 67 and 49, 32 x 1024 x 320 bf16 22.8 and 19.7; 16 x 1024 x 640 fp32 22 and 25, 32 x 1024 x 1280 83
-// and 90).
+// and 90).  A launch has fewer than 2^32 threads: what needs more (2^24 groups of 256 threads, 2^22 of 1024) is cut in chunks too.
 struct Hold {
     int32_t threads = 0, held = 0, width = 0;
 };
+int64_t one_grid(const NormCall &n) { return 8 * (((int64_t)n.B * n.G + 7) / 8); }  // workgroups: as many to every XCD
 Hold hold_for(const NormCall &n) {
     const int32_t V = n.dtype == DGQ_F32 ? 4 : 8, Cg = n.C / n.G, width = (Cg + V - 1) / V;
-    if (Cg < V || width > 256 || (int64_t)n.B * n.G > 1 << 24) return {};
+    if (Cg < V || width > 256) return {};
     const int64_t rows = n.offsets ? n.N / n.B * 3 / 2 : n.N;  // of a long image
     if ((rows > 2048 || rows * Cg > 65536) && (int64_t)n.B * n.G < 192) return {};
     const int64_t stripe = Cg * (16 / V), bytes = n.rows() * n.C * (16 / V);
     if ((stripe < 128 && bytes >= 44000000) || (stripe < 32 && bytes >= 20000000)) return {};
     const Hold ways[] = {{256, 4, width}, {1024, 4, width}, {1024, 8, width}, {1024, 16, width}};
     for (const Hold &h : ways)
-        if (rows <= (int64_t)h.held * (h.threads / width)) return h;
+        if (rows <= (int64_t)h.held * (h.threads / width))
+            return one_grid(n) * h.threads <= (int64_t)UINT32_MAX ? h : Hold{};  // (wider ways ask for more)
     return {};
 }
 
@@ -567,7 +569,7 @@ template <class T, class Y>
 hipError_t launch_one(const NormCall &n, const Hold &h, const Images &im, const Rows &xs, hipStream_t st) {
     const T *x = static_cast<const T *>(n.x);
     Y *y = static_cast<Y *>(n.out);
-    const unsigned grid = 8 * (((int64_t)n.B * n.G + 7) / 8);
+    const unsigned grid = (unsigned)one_grid(n);
     hipError_t e = hipSuccess;
     auto go = [&](auto threads, auto held) {
         constexpr int THREADS = decltype(threads)::value;

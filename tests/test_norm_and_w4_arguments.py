@@ -58,6 +58,17 @@ def test_groupnorm_workspace(lib):
         assert size(*bad) == 0
 
 
+@pytest.mark.parametrize("B,N,C,G,dtype", [(16384, 1, 32768, 1024, 0), (65535, 1, 32768, 512, 0), (16384, 1, 65536, 1024, 2),
+                                           (4097, 129, 32768, 1024, 0), (4096, 129, 65536, 1024, 1)])
+def test_groupnorm_of_more_groups_than_a_launch_takes(lib, B, N, C, G, dtype):
+    """A workgroup to every group, of 256 threads or (129 rows) of 1024, would be 2^32 threads and more: such calls go through
+    sums of chunks, which need a workspace.  Just below that a workgroup takes each."""
+    size = lib.dgq_groupnorm_workspace_bytes
+    assert size(B, N, 0, C, G, dtype) > 0
+    below = B // 2 if N == 1 else 2000
+    assert size(below, N, 0, C, G, dtype) == 0
+
+
 def test_w4_bytes(lib):
     size = lib.dgq_w4_bytes
     assert size(16, 128, 128) == 1024 + 64 and size(16, 128, 32) == 1024 + 256
