@@ -739,8 +739,8 @@ int dgq_w4_unpack(const void *data, int32_t O, int32_t C, int32_t group, int32_t
  *   y     [M, O] of out_dtype (dtype or fp32), contiguous, outside x's first to last value (DGQ_EINVAL)
  *   workspace dgq_w4_matvec_workspace_bytes(...) bytes, 16-byte aligned (0 bytes: NULL): few outputs of many inputs are cut
  *         over the chip along the inputs and joined by a second kernel; this call's alone until it is done
- * fp32 rows count with 23 bits, fp16 and bf16 ones with all of theirs (bf16 and fp32: elements 2^29 below the largest of their
- * 128 inputs: to 2^-39 of that); codes less zeros are exact, sums are fp32 and rounded once to y.  NaN or infinity in a row of x
+ * fp32 rows count with 23 bits, fp16 and bf16 ones with all of theirs (elements 2^28 below the largest of their 128 inputs: fp32 to
+ * 2^-51 of that, bf16 to 2^-39); codes less zeros are exact, sums are fp32 and rounded once to y.  NaN or infinity in a row of x
  * makes that row not finite, no other.  Scales of 2^100 and more may overflow in a group's sum.
  * The same call gives the same bits; the order of the sums goes by the sizes.  Enqueues on `stream`; neither synchronises nor
  * allocates.

@@ -151,8 +151,9 @@ __global__ __launch_bounds__(256) void k_w4_unpack(W4 m, T *__restrict__ w, bool
 // bits 0 .. 3) or 1024 + 16 code (at 4 .. 7), less 1024 + zero or times 1/16 less 64 + zero it is code - zero, exactly: nine
 // instructions for eight codes.  Rows of fp16 are what they are; those of bf16 and fp32 are taken a unit (128 inputs) at a time by
 // a power of two that brings its largest to 2^14 .. 2^15, bf16 as one fp16, fp32 as two (x = h + l, each rounded to nearest: off by
-// 2^-23 x at most); what lies 2^29 below the unit's largest loses bits, to 2^-39 of that.  The groups' sums meet in fp32 with
-// their scales and those powers.
+// 2^-23 x at most).  l is kept 2^12 times as large, which brings it up to 2^15 too, and has sums of its own: at h's scale it would
+// leave fp16's normal numbers 2^16 below the unit's largest (2 % of the time, 5 % at groups of 32).  What lies more than 2^28
+// below that loses bits, fp32 to 2^-51 of it, bf16 to 2^-39.  The groups' sums meet in fp32 with their scales and those powers.
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef float float2v __attribute__((ext_vector_type(2)));
@@ -166,6 +167,7 @@ union Piece {  // a lane's 8 numbers of an operand
 
 template <class T>
 constexpr int kPieces = sizeof(T) == 4 ? 2 : 1;
+constexpr float kSecond = 0x1p12f;  // the second piece's own power
 
 // x & mask | bits in one instruction: both constants stay in registers (as literals they take two)
 __device__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t bits) { return (x & mask) | bits; }
@@ -217,12 +219,12 @@ __device__ float convert(const T (&x)[4][8], Piece (&a)[4][kPieces<T>]) {
         for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                // (the second piece in one instruction: the rest of a product with a power of two is exact)
                 const float x0 = (float)x[j][2 * i], x1 = (float)x[j][2 * i + 1];
                 const half2v h = __builtin_convertvector((float2v{x0 * down, x1 * down}), half2v);
                 a[j][0].p[i] = h;
-                if constexpr (kPieces<T> > 1)
-                    a[j][1].p[i] = __builtin_convertvector((float2v{fmaf(x0, down, -(float)h[0]), fmaf(x1, down, -(float)h[1])}), half2v);
+                if constexpr (kPieces<T> > 1)  // what h leaves is exact, and so are products with powers of two: l is rounded once
+                    a[j][1].p[i] = __builtin_convertvector(
+                        (float2v{fmaf(x0, down, -(float)h[0]) * kSecond, fmaf(x1, down, -(float)h[1]) * kSecond}), half2v);
             }
         return __uint_as_float((uint32_t)(e - 14) << 23);
     }
@@ -344,17 +346,20 @@ __global__ __launch_bounds__(64 * kMaxWaves<T>) void k_w4_matvec(const T *__rest
                 float4v sum{};
 #pragma unroll
                 for (int g = 0; g < 4 / J; ++g) {
-                    float4v acc{};
+                    float4v acc[P] = {};
                     const Expand::Zero zero = Expand::zero(with.word[d][g]);
 #pragma unroll
                     for (int j = g * J; j < g * J + J; ++j) {
                         const half8 b = expand(c[j], zero);
 #pragma unroll
-                        for (int p = 0; p < P; ++p) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[j][p], b, acc, 0, 0, 0);
+                        for (int p = 0; p < P; ++p) acc[p] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[j][p], b, acc[p], 0, 0, 0);
                     }
                     const float s = __uint_as_float(with.word[d][g] & ~15u);
+                    if constexpr (P > 1)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) sum[i] = g ? fmaf(s, acc[i], sum[i]) : s * acc[i];
+                        for (int i = 0; i < 4; ++i) acc[0][i] = fmaf(acc[1][i], 1 / kSecond, acc[0][i]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sum[i] = g ? fmaf(s, acc[0][i], sum[i]) : s * acc[0][i];
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) out[i] = kPowers ? fmaf(sum[i], power[i], out[i]) : out[i] + sum[i];

@@ -184,6 +184,38 @@ def test_single_inputs_at_any_size(dgq, dtype):
     assert (np.abs(got - x) <= np.abs(x) * (2.0 ** -23 if dtype == "fp32" else 0)).all()
 
 
+@pytest.mark.parametrize("group", GROUPS)
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("M", [1, 3, 20, 40])
+def test_small_inputs_beside_a_large_one(dgq, M, dtype, group):
+    """A large input whose codes are its group's zero, and an input for every output up to 2^45 below it: the product is the
+    small input itself.  fp32 is two numbers of 11 bits, the second 2^12 times what the first leaves: off by 2^-23 of the input
+    down to 2^28 below the largest (a first piece of 2^-14 of fp16's range and more), by half a step of fp16, 2^-25, times 2^-12
+    where the largest is 2^14 and more, 2^-51 of that, below; bf16 is one number, exact there and off by 2^-25 / 2^14 below.
+    Both pieces are multiples of one step of fp32 of their sum, scales are 1: nothing else is rounded."""
+    rng = np.random.default_rng(20 + M)
+    O, C = 48, 3 * 128
+    zero = rng.integers(0, 15, (48, C // group))
+    codes = np.repeat(zero, group, axis=1)
+    at = 128 * np.arange(3)[:, None] + np.arange(16)  # outputs of a unit each
+    codes[np.arange(48), at.reshape(-1)] += 1
+    words = np.full(zero.shape, np.float32(1).view(np.uint32)) | zero.astype(np.uint32)
+    w = _packed(dgq, codes, words, group, O, C)
+    for e in (-130, -100, -60, 0, 100, 126):
+        x = np.zeros((M, C))
+        x[:, at.reshape(-1)] = (1 + rng.random((M, 48))) * 2.0 ** (e - rng.integers(0, 46, (M, 48))) * rng.choice([-1, 1], (M, 48))
+        x[:, 100::128] = (1 + rng.random((M, 3))) * 2.0 ** e
+        t = _up(x.astype(np.float32), dtype)
+        x = t.double().cpu().numpy()
+        got = dgq.dgq_w4_matvec(t, w, dtype=_type("fp32")).double().cpu().numpy()
+        top = np.repeat(np.abs(x.reshape(M, 3, 128)).max(2), 16, axis=1)
+        want = x[:, at.reshape(-1)]
+        near = np.abs(want) >= 2.0 ** -28 * top
+        tol = np.where(near, 2.0 ** -23 * np.abs(want), 2.0 ** -51 * top) if dtype == "fp32" else np.where(near, 0, 2.0 ** -39 * top)
+        off = np.abs(got - want) > tol + 2.0 ** -150  # (fp32's own least step)
+        assert not off.any(), (e, np.log2(np.abs(got - want)[off] / np.abs(want)[off]).max())
+
+
 def test_rows_of_far_exponents(dgq):
     """Elements 2^20 and 2^60 apart in one unit and in different ones."""
     rng = np.random.default_rng(16)
