@@ -103,9 +103,16 @@ void *stream_of(PyObject *o) {
     return p;
 }
 
-// (straight from the allocator: the dispatcher's way there takes 0.5 us; a new tensor has no gradient)
-at::Tensor empty(at::IntArrayRef sizes, at::ScalarType t, const at::Tensor &like) {
-    return at::detail::empty_cuda(sizes, t, like.device(), std::nullopt);
+// A new tensor, straight from the allocator (the dispatcher's way there takes 0.5 us; a new tensor has no gradient).  Where torch is
+// to fill what nobody writes (torch.use_deterministic_algorithms), it does so on the stream that the call enqueues on.
+at::Tensor empty(at::IntArrayRef sizes, at::ScalarType t, const at::Tensor &like, PyObject *stream = Py_None) {
+    const at::Context &torch = at::globalContext();
+    if (!torch.deterministicAlgorithms() || !torch.deterministicFillUninitializedMemory())
+        return at::detail::empty_cuda(sizes, t, like.device(), std::nullopt);
+    std::optional<c10::hip::HIPStreamGuard> on;
+    if (given(stream)) on.emplace(c10::hip::getStreamFromExternal(static_cast<hipStream_t>(stream_of(stream)), like.device().index()));
+    at::AutoDispatchBelowADInplaceOrView below;
+    return at::empty(sizes, like.options().dtype(t).requires_grad(false));
 }
 
 dgq_groups_info_t info_of(const dgq_groups_t *g) {
@@ -193,8 +200,8 @@ PyObject *quantize_act(Args a) {
         throw Raised();
     }
     const CodesShape shape(g, rows);
-    const at::Tensor codes = given(a[2]) ? tensor(a[2], at::kChar, "codes") : empty(shape.sizes(), at::kChar, x);
-    const at::Tensor cls = given(a[3]) ? tensor(a[3], at::kByte, "row_class") : empty({rows}, at::kByte, x);
+    const at::Tensor codes = given(a[2]) ? tensor(a[2], at::kChar, "codes") : empty(shape.sizes(), at::kChar, x, a[4]);
+    const at::Tensor cls = given(a[3]) ? tensor(a[3], at::kByte, "row_class") : empty({rows}, at::kByte, x, a[4]);
     if (!shape.is(codes) || cls.numel() != rows) raise_value("codes / row_class have the wrong shape");
     void *st = stream_of(a[4]);
     const float *xp = pointer<float>(x);
@@ -220,7 +227,7 @@ struct LinearIn {
 PyObject *linear(Args a) {
     const LinearIn in(a[0], a[1], a[2], a[3]);
     const int64_t O = out_channels_of(a[1]);
-    const at::Tensor y = given(a[4]) ? tensor(a[4], at::kFloat, "y") : empty({in.rows, O}, at::kFloat, in.codes);
+    const at::Tensor y = given(a[4]) ? tensor(a[4], at::kFloat, "y") : empty({in.rows, O}, at::kFloat, in.codes, a[6]);
     if (!shape_is(y, {in.rows, O})) raise_value("y has the wrong shape");
     int32_t *dump = nullptr;
     if (given(a[5])) {
@@ -247,7 +254,7 @@ PyObject *linear(Args a) {
 PyObject *linear_geglu(Args a) {
     const LinearIn in(a[0], a[1], a[2], a[3]);
     const int64_t oh = out_channels_of(a[1]) / 2;
-    const at::Tensor y = given(a[4]) ? tensor(a[4], at::kFloat, "y") : empty({in.rows, oh}, at::kFloat, in.codes);
+    const at::Tensor y = given(a[4]) ? tensor(a[4], at::kFloat, "y") : empty({in.rows, oh}, at::kFloat, in.codes, a[5]);
     if (!shape_is(y, {in.rows, oh})) raise_value("y has the wrong shape");
     void *st = stream_of(a[5]);
     const int8_t *cp = pointer<int8_t>(in.codes);
@@ -261,8 +268,8 @@ PyObject *linear_geglu(Args a) {
 PyObject *linear_geglu_requant(Args a) {
     const LinearIn in(a[0], a[1], a[2], a[3]);
     const CodesShape shape(groups_of(a[4]), in.rows);
-    const at::Tensor codes2 = given(a[5]) ? tensor(a[5], at::kChar, "codes_next") : empty(shape.sizes(), at::kChar, in.codes);
-    const at::Tensor cls2 = given(a[6]) ? tensor(a[6], at::kByte, "row_class_next") : empty({in.rows}, at::kByte, in.codes);
+    const at::Tensor codes2 = given(a[5]) ? tensor(a[5], at::kChar, "codes_next") : empty(shape.sizes(), at::kChar, in.codes, a[7]);
+    const at::Tensor cls2 = given(a[6]) ? tensor(a[6], at::kByte, "row_class_next") : empty({in.rows}, at::kByte, in.codes, a[7]);
     if (!shape.is(codes2) || cls2.numel() != in.rows) raise_value("codes_next / row_class_next have the wrong shape");
     void *st = stream_of(a[7]);
     const int8_t *cp = pointer<int8_t>(in.codes);
@@ -281,7 +288,7 @@ PyObject *conv3x3_codes(Args a) {
     const CodesShape shape(g9, (int64_t)B * H * W);
     if (codes.numel() * 9 != shape.n[0] * shape.n[1] * shape.n[2])
         raise_value("codes do not belong to a [B*H*W, C] map of this layer");
-    const at::Tensor out = given(a[5]) ? tensor(a[5], at::kChar, "codes9") : empty(shape.sizes(), at::kChar, codes);
+    const at::Tensor out = given(a[5]) ? tensor(a[5], at::kChar, "codes9") : empty(shape.sizes(), at::kChar, codes, a[6]);
     if (!shape.is(out)) raise_value("codes9 has the wrong shape");
     void *st = stream_of(a[6]);
     const int8_t *cp = pointer<int8_t>(codes);
@@ -298,8 +305,8 @@ PyObject *quantize_act_conv3x3(Args a) {
     const int64_t rows = (int64_t)B * H * W;
     if (g && !shape_is(x, {rows, info_of(g).channels})) raise_value("x must be [B*H*W, C]");
     const int64_t nbytes = (int64_t)dgq_conv3x3_codes3_bytes(g9, B, H, W);
-    const at::Tensor codes3 = given(a[6]) ? tensor(a[6], at::kChar, "codes3") : empty({nbytes}, at::kChar, x);
-    const at::Tensor cls = given(a[7]) ? tensor(a[7], at::kByte, "row_class") : empty({rows}, at::kByte, x);
+    const at::Tensor codes3 = given(a[6]) ? tensor(a[6], at::kChar, "codes3") : empty({nbytes}, at::kChar, x, a[8]);
+    const at::Tensor cls = given(a[7]) ? tensor(a[7], at::kByte, "row_class") : empty({rows}, at::kByte, x, a[8]);
     if (codes3.numel() != nbytes || cls.numel() != rows) raise_value("codes3 / row_class have the wrong size");
     void *st = stream_of(a[8]);
     const float *xp = pointer<float>(x);
@@ -318,7 +325,7 @@ PyObject *linear_conv3x3(Args a) {
     const int64_t rows = (int64_t)B * H * W, O = out_channels_of(a[1]);
     holds(codes3, (int64_t)dgq_conv3x3_codes3_bytes(g9, B, H, W), "codes3");
     holds(cls, rows, "row_class");
-    const at::Tensor y = given(a[7]) ? tensor(a[7], at::kFloat, "y") : empty({rows, O}, at::kFloat, codes3);
+    const at::Tensor y = given(a[7]) ? tensor(a[7], at::kFloat, "y") : empty({rows, O}, at::kFloat, codes3, a[8]);
     if (!shape_is(y, {rows, O})) raise_value("y has the wrong shape");
     void *st = stream_of(a[8]);
     const int8_t *cp = pointer<int8_t>(codes3);
@@ -348,9 +355,9 @@ PyObject *xattn_logq(Args a) {
         raise_value("k / v have the wrong shape");
     if (kb && THPVariable_Unpack(a[3]).numel() != nk) raise_value("key_bias has the wrong shape");
     const int32_t bits = integer32(a[4]);
-    const at::Tensor out = given(a[5]) ? tensor(a[5], at::kFloat, "out") : empty(q.sizes(), at::kFloat, q);
+    const at::Tensor out = given(a[5]) ? tensor(a[5], at::kFloat, "out") : empty(q.sizes(), at::kFloat, q, a[9]);
     holds(out, q.numel(), "out");
-    const at::Tensor scale = given(a[6]) ? tensor(a[6], at::kFloat, "scale_out") : empty({s.B}, at::kFloat, q);
+    const at::Tensor scale = given(a[6]) ? tensor(a[6], at::kFloat, "scale_out") : empty({s.B}, at::kFloat, q, a[9]);
     holds(scale, s.B, "scale_out");
     uint8_t *dump = optional<uint8_t>(a[7], at::kByte, "codes_dump");
     if (dump && !shape_is(THPVariable_Unpack(a[7]), {s.B, s.H, s.N, nk - 1})) raise_value("codes_dump has the wrong shape");
@@ -359,7 +366,7 @@ PyObject *xattn_logq(Args a) {
         if (!THPVariable_Check(a[8])) raise(PyExc_TypeError, "workspace must be a tensor");
         ws = THPVariable_Unpack(a[8]);
     } else if (const size_t need = dgq_xattn_workspace_bytes((int32_t)s.B, (int32_t)s.N, (int32_t)s.H, (int32_t)s.d, (int32_t)nk)) {
-        ws = empty({(int64_t)need}, at::kByte, q);
+        ws = empty({(int64_t)need}, at::kByte, q, a[9]);
     }
     void *wp = ws.defined() ? ws.data_ptr() : nullptr;
     const size_t wb = ws.defined() ? (size_t)ws.numel() * ws.element_size() : 0;
@@ -385,7 +392,7 @@ PyObject *xattn_logq_static(Args a) {
     holds_if_given(a[3], nk, "key_bias");
     holds(sin, s.B, "scale_in");
     const int32_t bits = integer32(a[4]);
-    const at::Tensor out = given(a[6]) ? tensor(a[6], at::kFloat, "out") : empty(q.sizes(), at::kFloat, q);
+    const at::Tensor out = given(a[6]) ? tensor(a[6], at::kFloat, "out") : empty(q.sizes(), at::kFloat, q, a[9]);
     holds(out, q.numel(), "out");
     float *so = optional<float>(a[7], at::kFloat, "scale_out");
     holds_if_given(a[7], s.B, "scale_out");
@@ -413,7 +420,7 @@ PyObject *selfattn_logq(Args a) {
     if (k.sizes() != q.sizes() || v.sizes() != q.sizes() || sin.numel() != s.B)
         raise_value("q, k, v must share one shape [B,N,H,d] and scale_in have B entries");
     const int32_t bits = integer32(a[3]);
-    const at::Tensor out = given(a[5]) ? tensor(a[5], at::kFloat, "out") : empty(q.sizes(), at::kFloat, q);
+    const at::Tensor out = given(a[5]) ? tensor(a[5], at::kFloat, "out") : empty(q.sizes(), at::kFloat, q, a[9]);
     holds(out, q.numel(), "out");
     float *so = optional<float>(a[6], at::kFloat, "scale_out");
     holds_if_given(a[6], s.B, "scale_out");
@@ -425,7 +432,7 @@ PyObject *selfattn_logq(Args a) {
         ws = THPVariable_Unpack(a[8]);
     } else {
         const size_t need = dgq_selfattn_workspace_bytes((int32_t)s.B, (int32_t)s.N, (int32_t)s.H, (int32_t)s.d);
-        ws = empty({(int64_t)(need > 16 ? need : 16)}, at::kByte, q);
+        ws = empty({(int64_t)(need > 16 ? need : 16)}, at::kByte, q, a[9]);
     }
     void *wp = ws.data_ptr(), *st = stream_of(a[9]);
     const size_t wb = (size_t)ws.numel();
