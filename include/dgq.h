@@ -722,13 +722,14 @@ size_t dgq_w4_bytes(int32_t O, int32_t C, int32_t group);
  *   zero = clamp(rne(-lo * (1/s)), 0, 15),   code = clamp(rne(w * (1/s)) + zero, 0, 15)
  * (s = 0: all codes 0).  A group with NaN, infinity or hi - lo above fp32 gets the scale NaN.
  *   w     [O, C] of `dtype`, inputs contiguous, rows w_row_stride elements apart, aligned to an element
- *   data  dgq_w4_bytes(...) bytes, 16-byte aligned, all of them written
+ *   data  dgq_w4_bytes(...) bytes, 16-byte aligned, all of them written; outside w's first to last value (DGQ_EINVAL)
  * Enqueues on `stream`; neither synchronises nor allocates.
  */
 int dgq_w4_pack(const void *w, int32_t dtype, int64_t w_row_stride, int32_t O, int32_t C, int32_t group, void *data,
                 void *stream);
 
-/* The values: w [O, C] of `dtype`, contiguous, each rounded once.  Enqueues on `stream`; neither synchronises nor allocates. */
+/* The values: w [O, C] of `dtype`, contiguous, outside data (DGQ_EINVAL), each rounded once.  Enqueues on `stream`; neither
+ * synchronises nor allocates. */
 int dgq_w4_unpack(const void *data, int32_t O, int32_t C, int32_t group, int32_t dtype, void *w, void *stream);
 
 /*

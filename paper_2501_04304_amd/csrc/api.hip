@@ -1506,6 +1506,8 @@ int dgq_w4_pack(const void *w, int32_t dtype, int64_t w_row_stride, int32_t O, i
     if (w_row_stride < 0) return fail(DGQ_EINVAL, "dgq_w4_pack: stride below 0");
     if (!aligned_to(w, dtype)) return fail(DGQ_EALIGN, "dgq_w4_pack: tensor not aligned to its elements");
     if ((int64_t)m.R * ((m.T + 3) / 4) > kMaxGroups) return fail(DGQ_EUNSUPPORTED, "dgq_w4_pack: more than 2^24 units of 16 x 512 weights");
+    if (overlap(w, span((__int128)(O - 1) * w_row_stride + C - 1, dtype), data, dgq_w4_bytes(O, C, group)))
+        return fail(DGQ_EINVAL, "dgq_w4_pack: w overlaps data");
     DGQ_HIP(launch_w4_pack(w, dtype, w_row_stride, m, static_cast<hipStream_t>(stream)));
     return DGQ_OK;
 }
@@ -1517,6 +1519,8 @@ int dgq_w4_unpack(const void *data, int32_t O, int32_t C, int32_t group, int32_t
     if (!w) return fail(DGQ_EINVAL, "dgq_w4_unpack: null pointer");
     if (!aligned_to(w, dtype)) return fail(DGQ_EALIGN, "dgq_w4_unpack: tensor not aligned to its elements");
     if ((int64_t)m.R * ((m.T + 3) / 4) > kMaxGroups) return fail(DGQ_EUNSUPPORTED, "dgq_w4_unpack: more than 2^24 units of 16 x 512 weights");
+    if (overlap(w, span((__int128)O * C - 1, dtype), data, dgq_w4_bytes(O, C, group)))
+        return fail(DGQ_EINVAL, "dgq_w4_unpack: w overlaps data");
     DGQ_HIP(launch_w4_unpack(m, dtype, w, static_cast<hipStream_t>(stream)));
     return DGQ_OK;
 }

@@ -92,6 +92,20 @@ def test_w4_pack_and_unpack(lib, kw, code):
         assert b"dgq_w4_unpack" in lib.dgq_last_error()
 
 
+@pytest.mark.parametrize("at", [0, 64, 1276, -252])
+def test_w4_pack_and_unpack_into_what_they_read(lib, at):
+    """8 x 8 fp32 values are 256 bytes, packed 1280: values that begin inside the packed ones, end there, or whose rows lie around
+    them."""
+    assert lib.dgq_w4_bytes(8, 8, 32) == 1280
+    big = (C.c_float * 2048)()
+    data = (C.addressof(big) + 1024 + 15) & ~15
+    assert lib.dgq_w4_pack(data + at, 0, 8, 8, 8, 32, data, None) == EINVAL
+    assert b"dgq_w4_pack: w overlaps data" in lib.dgq_last_error()
+    assert lib.dgq_w4_unpack(data, 8, 8, 32, 0, data + at, None) == EINVAL
+    assert b"dgq_w4_unpack: w overlaps data" in lib.dgq_last_error()
+    assert lib.dgq_w4_pack(data - 32 - abs(at), 0, 1 << 20, 8, 8, 32, data, None) == EINVAL
+
+
 @pytest.mark.parametrize("kw,code", [
     (dict(x=None), EINVAL), (dict(y=None), EINVAL), (dict(data=None), EINVAL), (dict(dtype=4), EINVAL), (dict(out_dtype=1), EINVAL),
     (dict(dtype=1, out_dtype=2), EINVAL), (dict(M=-1), EINVAL), (dict(row=-1), EINVAL), (dict(act=2), EINVAL), (dict(group=1), EUNSUPPORTED),
