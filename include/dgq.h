@@ -687,7 +687,7 @@ typedef enum dgq_act { DGQ_ACT_NONE = 0, DGQ_ACT_SILU = 1 } dgq_act;  /* SiLU: t
  *             offsets[b] .. offsets[b + 1] - 1, none of them allowed; rows of no image keep what out held.  x: channels
  *             contiguous, batch and row strides in elements, not negative; out: contiguous.  Aligned to an element;
  *             16 bytes, as all widths here are that are a multiple of 8, are read fastest.  out may be x (contiguous, same
- *             type) and lies outside its first to last value otherwise (DGQ_EINVAL)
+ *             type) and lies outside its first to last value otherwise, and outside the tables and offsets (DGQ_EINVAL)
  *   dtype, out_dtype   dgq_dtype of x and out; out has x's type or fp32
  *   weight, bias       fp32 [C], or NULL for 1 and 0
  *   add, scale, shift  fp32 [B, C], channels contiguous, rows `stride` elements apart, or NULL for none
@@ -737,7 +737,7 @@ int dgq_w4_unpack(const void *data, int32_t O, int32_t C, int32_t group, int32_t
  * weights' bytes; up to 2^19 are taken (16 at a time, which read the weights anew).
  *   x     [M, C] of `dtype`, inputs contiguous, rows x_row_stride elements apart, aligned to an element
  *   bias  fp32 [O], or NULL
- *   y     [M, O] of out_dtype (dtype or fp32), contiguous, outside x's first to last value (DGQ_EINVAL)
+ *   y     [M, O] of out_dtype (dtype or fp32), contiguous, outside x's first to last value, data and bias (DGQ_EINVAL)
  *   workspace dgq_w4_matvec_workspace_bytes(...) bytes, 16-byte aligned (0 bytes: NULL): few outputs of many inputs are cut
  *         over the chip along the inputs and joined by a second kernel; this call's alone until it is done
  * fp32 rows count with 23 bits, fp16 and bf16 ones with all of theirs (elements 2^28 below the largest of their 128 inputs: fp32 to

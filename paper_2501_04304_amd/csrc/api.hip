@@ -1488,6 +1488,15 @@ int dgq_groupnorm(const void *x, int32_t dtype, int64_t x_batch_stride, int64_t 
     const __int128 last = (__int128)(images - 1) * x_batch_stride + (__int128)(N - 1) * x_row_stride + C - 1;
     if (!same && overlap(x, span(last, dtype), out, span((__int128)images * N * C - 1, out_dtype)))
         return fail(DGQ_EINVAL, "dgq_groupnorm: out overlaps x and is not x, contiguous and of one type");
+    const struct {
+        const void *data;
+        __int128 last;
+        const char *name;
+    } read[] = {{weight, C - 1, "weight"}, {bias, C - 1, "bias"}, {offsets, B, "offsets"}, {add, (__int128)(B - 1) * add_stride + C - 1, "add"},
+                {scale, (__int128)(B - 1) * scale_stride + C - 1, "scale"}, {shift, (__int128)(B - 1) * shift_stride + C - 1, "shift"}};
+    for (const auto &r : read)
+        if (r.data && overlap(r.data, span(r.last, DGQ_F32), out, span((__int128)images * N * C - 1, out_dtype)))
+            return fail(DGQ_EINVAL, std::string("dgq_groupnorm: out overlaps ") + r.name);
     DGQ_HIP(launch_groupnorm(n, workspace, static_cast<hipStream_t>(stream)));
     return DGQ_OK;
 }
@@ -1549,6 +1558,10 @@ int dgq_w4_matvec(const void *x, int32_t dtype, int64_t x_row_stride, int32_t M,
         return fail(DGQ_EWORKSPACE, "dgq_w4_matvec: workspace missing, too small or misaligned");
     if (overlap(x, span((__int128)(M - 1) * x_row_stride + C - 1, dtype), y, span((__int128)M * O - 1, out_dtype)))
         return fail(DGQ_EINVAL, "dgq_w4_matvec: y overlaps x");
+    if (overlap(data, dgq_w4_bytes(O, C, group), y, span((__int128)M * O - 1, out_dtype)))
+        return fail(DGQ_EINVAL, "dgq_w4_matvec: y overlaps data");
+    if (bias && overlap(bias, span(O - 1, DGQ_F32), y, span((__int128)M * O - 1, out_dtype)))
+        return fail(DGQ_EINVAL, "dgq_w4_matvec: y overlaps bias");
     DGQ_HIP(launch_w4_matvec({x, dtype, x_row_stride, M, bias, act, y, out_dtype}, m, workspace, static_cast<hipStream_t>(stream)));
     return DGQ_OK;
 }

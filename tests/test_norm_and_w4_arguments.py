@@ -47,6 +47,26 @@ def test_groupnorm(lib, kw, code):
     assert b"dgq_groupnorm" in lib.dgq_last_error()
 
 
+BIG = (C.c_float * 4096)()
+Q = (C.addressof(BIG) + 8192 + 15) & ~15
+
+
+@pytest.mark.parametrize("name,at", [(n, a) for n in ("weight", "bias", "add", "scale", "shift", "offsets") for a in (0, 252, -4)])
+def test_groupnorm_into_what_it_reads(lib, name, at):
+    """out has 8 rows of 8 fp32 channels: tables that begin inside it and (vectors, offsets) ones that end there."""
+    size = {"weight": 32, "bias": 32, "add": 32, "scale": 32, "shift": 32, "offsets": 8}[name]
+    kw = {name: Q + (at if at >= 0 else 4 - size)}
+    assert _norm(lib, x=Q - 4096, out=Q, **kw) == EINVAL
+    assert b"dgq_groupnorm: out overlaps " + name.encode() in lib.dgq_last_error()
+
+
+def test_groupnorm_into_rows_of_a_table(lib):
+    """Two images' rows of a table, 1024 floats apart, out in the second of them and between them."""
+    for at in (4096, 2048):
+        assert _norm(lib, x=Q - 4096, out=Q, B=2, batch=64, scale=Q - at, scale_s=1024) == EINVAL
+        assert b"dgq_groupnorm: out overlaps scale" in lib.dgq_last_error()
+
+
 def test_groupnorm_of_no_rows_is_no_work(lib):
     assert _norm(lib, N=0, x=None, out=None) == 0
 
@@ -118,6 +138,16 @@ def test_w4_matvec(lib, kw, code):
     a.update(kw)
     assert lib.dgq_w4_matvec(*a.values()) == code
     assert b"dgq_w4_matvec" in lib.dgq_last_error()
+
+
+@pytest.mark.parametrize("name,at", [("data", 0), ("data", 28), ("data", -1264), ("bias", 0), ("bias", 28), ("bias", -28)])
+def test_w4_matvec_into_what_it_reads(lib, name, at):
+    """y has 8 fp32 values; 8 x 8 weights take 1280 bytes."""
+    kw = dict(data=Q - 2048, bias=None)
+    y = Q + at if name == "data" and at >= 0 else Q
+    kw[name] = Q if name == "data" and at >= 0 else Q - 1264 if name == "data" else Q + at
+    assert lib.dgq_w4_matvec(Q + 4096, 0, 8, 1, kw["data"], 8, 8, 32, kw["bias"], 0, y, 0, None, 0, None) == EINVAL
+    assert b"dgq_w4_matvec: y overlaps " + name.encode() in lib.dgq_last_error()
 
 
 def test_w4_matvec_workspace(lib):
