@@ -195,19 +195,21 @@ struct RowsOf {
 
 // Bound by the bytes of x, and for small maps by the way from the kernel's arguments over x and LDS to the sums (4.7 us for 2 x
 // 4096 x 320, of which the rows take 2.5).  add enters per channel: sum x' = sum x + n add, sum x'^2 = sum x^2 + 2 add sum x + n add^2.
-// 16 x 4096 x 640 fp32: 30 us, 5.6 TB/s.  sums: [G][parts][slices] double2.
+// 16 x 4096 x 640 fp32: 30 us, 5.6 TB/s.  sums: [G][parts][met] double2, met: slices that a group's channels may lie in, that of its first
+// channel first, 0 for those that they do not.
 template <class T>
 __global__ __launch_bounds__(kMaxThreads) void k_gn_sums(const T *__restrict__ x, Images im, Rows xs, Chunks ch, Shape sh, int32_t C,
                                                          int32_t G, const float *__restrict__ add, int64_t add_row,
-                                                         double2 *__restrict__ sums, int32_t parts) {
+                                                         double2 *__restrict__ sums, int32_t parts, int32_t met) {
     constexpr int V = kVec<T>;
     extern __shared__ double2 entries[];  // [values of a vector, or 1 where vectors end with their groups][high][width]
     const int tid = threadIdx.x;
     const Place<V> at(sh, C);
     const int high = at.high, c_slice = at.c_slice, c_end = min(c_slice + at.wide, C), Cg = C / G, each = Cg % V ? 1 : V;  // channels of an entry
+    const int g_first = sh.slices > 1 ? c_slice / Cg : 0, g_end = sh.slices > 1 ? (c_end - 1) / Cg + 1 : G;  // groups of the slice
     // neighbouring lanes that share a group's entries
     int lanes = 64;
-    while (lanes > 1 && lanes * G > sh.threads) lanes >>= 1;
+    while (lanes > 1 && lanes * (g_end - g_first) > sh.threads) lanes >>= 1;
     ch.each(im, blockIdx.x, [&](int32_t b, int32_t part, int64_t r0, int64_t r1) {
         double s[V] = {}, ss[V] = {};
         if (at.on) {
@@ -249,13 +251,22 @@ __global__ __launch_bounds__(kMaxThreads) void k_gn_sums(const T *__restrict__ x
             column[0] = sum;
         }
         __syncthreads();
-        for (int g = tid / lanes; g < G; g += sh.threads / lanes) {
+        for (int g = g_first + tid / lanes; g < g_end; g += sh.threads / lanes) {
             const int lo = (max(g * Cg, c_slice) - c_slice) / each, end = (min((g + 1) * Cg, c_end) - c_slice) / each;
             double2 sum{0, 0};
             for (int e = lo + (tid & (lanes - 1)); e < end; e += lanes)
                 sum = sum_of(sum, each == 1 ? entries[e % V * sh.threads + e / V] : entries[e]);
             sum = lane_sums(sum, lanes);
-            if ((tid & (lanes - 1)) == 0) sums[((int64_t)g * parts + part) * sh.slices + blockIdx.y] = sum;
+            if ((tid & (lanes - 1)) == 0) {
+                double2 *to = sums + ((int64_t)g * parts + part) * met;
+                if (met > 1) {
+                    const int from = g * Cg / at.wide, n = ((g + 1) * Cg - 1) / at.wide + 1 - from;
+                    if ((int)blockIdx.y == from)
+                        for (int i = n; i < met; ++i) to[i] = {0, 0};
+                    to += (int)blockIdx.y - from;
+                }
+                *to = sum;
+            }
         }
     });
 }
@@ -291,12 +302,12 @@ struct Group {
 // ---- tables ----------------------------------------------------------------------------------------------------------
 // One workgroup per (group, image), where an image has too many sums for all to add up.  Bound by latency (5 us).  tables: fp32
 // [B][p, a, q][C].
-__global__ __launch_bounds__(256) void k_gn_tables(const double2 *__restrict__ sums, int32_t parts, Images im, Chunks ch, int32_t slices,
+__global__ __launch_bounds__(256) void k_gn_tables(const double2 *__restrict__ sums, int32_t parts, Images im, Chunks ch, int32_t met,
                                                    int32_t C, int32_t G, const float *__restrict__ weight, const float *__restrict__ bias,
                                                    float eps, NormTerms terms, float *__restrict__ tables) {
     __shared__ double2 wave_sums[4];
     const int g = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, Cg = C / G;
-    const int64_t first = ((int64_t)g * parts + ch.first(im, b)) * slices, n_parts = (int64_t)ch.parts(im, b) * slices;
+    const int64_t first = ((int64_t)g * parts + ch.first(im, b)) * met, n_parts = (int64_t)ch.parts(im, b) * met;
     double2 s = strided_sum(sums + first, n_parts, tid, 256, 64);
     if ((tid & 63) == 0) wave_sums[tid >> 6] = s;
     __syncthreads();
@@ -322,7 +333,7 @@ __global__ __launch_bounds__(256) void k_gn_tables(const double2 *__restrict__ s
 template <class T, class Y>
 __global__ __launch_bounds__(kMaxThreads) void k_gn_apply(const T *x, Images im, Rows xs, Chunks ch, Shape sh, int32_t C, int32_t G,
                                                           const float *__restrict__ tables, const double2 *__restrict__ sums,
-                                                          int32_t parts, int32_t slices, const float *__restrict__ weight,
+                                                          int32_t parts, int32_t met, const float *__restrict__ weight,
                                                           const float *__restrict__ bias, float eps, NormTerms terms, int32_t silu_on,
                                                           Y *y) {
     constexpr int V = kVec<Y>;
@@ -345,7 +356,7 @@ __global__ __launch_bounds__(kMaxThreads) void k_gn_apply(const T *x, Images im,
         } else {
             Group *groups = reinterpret_cast<Group *>(lines);
             float *to = lines + G * (sizeof(Group) / sizeof(float));
-            const int64_t first = ch.first(im, b), n_parts = (int64_t)ch.parts(im, b) * slices;
+            const int64_t first = ch.first(im, b), n_parts = (int64_t)ch.parts(im, b) * met;
             const double per = 1 / ((double)(im.end(b) - im.start(b)) * Cg);
             // (the last vector of all may begin in front of its slice)
             const int c_first = max(c_slice - V, 0), c_end = min(c_slice + wide, C), room = wide + V;
@@ -353,7 +364,7 @@ __global__ __launch_bounds__(kMaxThreads) void k_gn_apply(const T *x, Images im,
             if (c_first + tid < c_end) mine = Terms::of(terms, weight, bias, b, c_first + tid);
             __syncthreads();
             for (int g = tid / lanes; g < G; g += sh.threads / lanes) {
-                const double2 s = strided_sum(sums + ((int64_t)g * parts + first) * slices, n_parts, tid & (lanes - 1), lanes, lanes);
+                const double2 s = strided_sum(sums + ((int64_t)g * parts + first) * met, n_parts, tid & (lanes - 1), lanes, lanes);
                 if ((tid & (lanes - 1)) == 0) groups[g] = Group(s, per, eps);
             }
             __syncthreads();
@@ -555,12 +566,14 @@ struct NormPlan {
     Hold hold;
     Shape shape;
     Chunks chunks;
-    int32_t parts = 0;
+    int32_t parts = 0, met = 1;  // met: slices that a group's channels may lie in
     size_t sums_bytes = 0, tables_bytes = 0;  // tables_bytes 0: the last kernel makes them itself
     explicit NormPlan(const NormCall &n) : hold(hold_for(n)), shape(shape_for(n.C, n.dtype == DGQ_F32 ? 4 : 8, kMaxThreads)), chunks(chunks_for(n, shape)) {
         if (hold.held) return;
         parts = chunks.count + (n.offsets ? n.B : 0);
-        sums_bytes = (size_t)n.G * parts * shape.slices * sizeof(double2);
+        const int32_t Cg = n.C / n.G, wide = shape.width * (n.dtype == DGQ_F32 ? 4 : 8);
+        if (wide % Cg) met = std::min(shape.slices, Cg % wide ? (Cg - 1) / wide + 2 : Cg / wide);
+        sums_bytes = (size_t)n.G * parts * met * sizeof(double2);
         if (n.G > 2048 || (int64_t)n.G * shape.slices * (n.offsets ? parts : chunks.per) > kMaxFolded) tables_bytes = (size_t)n.B * 3 * n.C * sizeof(float);
     }
 };
@@ -611,9 +624,9 @@ hipError_t launch_groupnorm(const NormCall &n, void *workspace, hipStream_t st) 
             e = DGQ_ENSURE_LDS(k_gn_sums<T>, bytes);
             if (e != hipSuccess) return;
             k_gn_sums<T><<<grid, p.shape.threads, bytes, st>>>(x, im, xs, p.chunks, p.shape, n.C, n.G, n.terms.add, n.terms.add_row,
-                                                               sums, p.parts);
+                                                               sums, p.parts, p.met);
             if (tables)
-                k_gn_tables<<<dim3(n.G, n.B), 256, 0, st>>>(sums, p.parts, im, p.chunks, p.shape.slices, n.C, n.G, n.weight, n.bias,
+                k_gn_tables<<<dim3(n.G, n.B), 256, 0, st>>>(sums, p.parts, im, p.chunks, p.met, n.C, n.G, n.weight, n.bias,
                                                             n.eps, n.terms, tables);
         }
         by_output<T>(n.out_dtype, [&](auto yt) {
@@ -628,7 +641,7 @@ hipError_t launch_groupnorm(const NormCall &n, void *workspace, hipStream_t st) 
             e = DGQ_ENSURE_LDS((k_gn_apply<T, Y>), bytes);
             if (e == hipSuccess)
                 k_gn_apply<T, Y><<<dim3(p.chunks.count, shape.slices), shape.threads, bytes, st>>>(
-                    x, im, xs, p.chunks, shape, n.C, n.G, tables, sums, p.parts, p.shape.slices, n.weight, n.bias, n.eps, n.terms,
+                    x, im, xs, p.chunks, shape, n.C, n.G, tables, sums, p.parts, p.met, n.weight, n.bias, n.eps, n.terms,
                     n.act == DGQ_ACT_SILU, y);
         });
     });

@@ -78,6 +78,41 @@ def test_sizes(dgq, B, N, C, G, dtype):
     _check(out, *ref.groupnorm(xn, *_even(B, N), G))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,N,C,G", [(1, 700, 7000, 28), (2, 300, 9000, 3), (2, 40, 10007, 10007), (1, 700, 6000, 24), (3, 90, 8200, 4100),
+                                     (1, 700, 20002, 73), (1, 700, 8192, 1)])
+def test_groups_in_several_slices_of_the_channels(dgq, B, N, C, G, dtype):
+    """More channels than a workgroup takes: groups that lie in one slice of them, that some slices cut, that cover slices; out
+    of a workspace that held NaN, so that every sum that is read was written."""
+    import torch
+    assert C % G == 0
+    rng = np.random.default_rng(C + G)
+    x, xn = _map(rng, B * N, C, dtype)
+    t = _tables(rng, B, C, ("weight", "add", "shift"))
+    need = dgq.dgq_groupnorm_workspace_bytes(B, N, False, C, G, x.dtype)
+    assert need > 0
+    ws = torch.full((need + 16,), 255, dtype=torch.uint8, device="cuda")
+    for to in {dtype, "fp32"}:
+        out = dgq.dgq_groupnorm(x.view(B, N, C), G, dtype=_type(to), workspace=ws, **{k: _up(v) for k, v in t.items()})
+        _check(out, *ref.groupnorm(xn, *_even(B, N), G, out_type=to, **t))
+    assert (ws[-16:] == 255).all()
+
+
+def test_more_groups_than_a_launch_takes(dgq):
+    """2^24 groups of 32 values, through sums of chunks: 16384 images of one row and 32768 channels."""
+    import torch
+    B, C, G = 16384, 32768, 1024
+    x = torch.empty((B, 1, C), device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x.normal_(generator=g)
+    out = dgq.dgq_groupnorm(x, G)
+    for b in (0, 1, 4095, 8192, B - 2, B - 1):
+        xn = x[b].cpu().numpy()
+        _check(out[b], *ref.groupnorm(xn, [0], [1], G), "image %d" % b)
+    m = out.view(B, G, 32).double().mean(2)
+    assert m.abs().max() < 1e-5  # every group of every image; 32 values of 2^-24 of 5 each
+
+
 @pytest.mark.parametrize("names", [(), ("weight",), ("bias",), ("add",), ("scale",), ("shift",), ("add", "scale"),
                                    ("weight", "bias", "shift")])
 @pytest.mark.parametrize("B,N,C,G", [(2, 40, 320, 32), (2, 3000, 80, 8)])

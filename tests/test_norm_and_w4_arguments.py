@@ -89,6 +89,14 @@ def test_groupnorm_of_more_groups_than_a_launch_takes(lib, B, N, C, G, dtype):
     assert size(below, N, 0, C, G, dtype) == 0
 
 
+@pytest.mark.parametrize("B,N,C,G,dtype,most", [(1, 1, 1 << 20, 1 << 20, 0, 16 + 12), (1, 4096, 65536, 8192, 0, 34), (1, 4096, 65536, 8192, 1, 34),
+                                                (2, 500, 40000, 40, 0, 2), (1, 256, 1 << 20, 1, 0, 24), (16384, 1, 32768, 1024, 0, 257)])
+def test_groupnorm_workspace_of_wide_maps(lib, B, N, C, G, dtype, most):
+    """A group's channels lie in one slice of a workgroup's, or in a few neighbours: 16 bytes for each of these and each chunk of
+    rows, and 12 a channel of an image where the sums are many.  most: MiB."""
+    assert 0 < lib.dgq_groupnorm_workspace_bytes(B, N, 0, C, G, dtype) <= most << 20
+
+
 def test_w4_bytes(lib):
     size = lib.dgq_w4_bytes
     assert size(16, 128, 128) == 1024 + 64 and size(16, 128, 32) == 1024 + 256
