@@ -696,7 +696,7 @@ typedef enum dgq_act { DGQ_ACT_NONE = 0, DGQ_ACT_SILU = 1 } dgq_act;  /* SiLU: t
  * Sums are in 64 bits and in an order of the call's sizes, x' - m is taken before it is rounded: the same call gives the same bits,
  * and a map whose mean is thousands of times its deviation loses nothing to that.  NaN or infinity stays in its image and
  * group, all of whose values become NaN.  A group of one value, or of equal ones, gives its bias (eps above 0).
- * C a multiple of G, at most 2^20; B at most 65535.  Enqueues on `stream`; neither synchronises nor allocates.
+ * C a multiple of G, at most 2^20; B 1 to 65535.  Enqueues on `stream`; neither synchronises nor allocates.
  */
 size_t dgq_groupnorm_workspace_bytes(int32_t B, int64_t N, int32_t packed, int32_t C, int32_t G, int32_t dtype);
 int dgq_groupnorm(const void *x, int32_t dtype, int64_t x_batch_stride, int64_t x_row_stride, const int32_t *offsets,

@@ -556,8 +556,8 @@ def dgq_groupnorm(x, num_groups: int, weight=None, bias=None, eps: float = 1e-5,
     """Group norm of x [B, N, C], or of packed x [rows, C] with offsets int32 [B + 1], over each image's rows and the C /
     num_groups channels of a group: act((norm(x + add) * weight + bias) * (1 + scale) + shift).  x: fp32,
     fp16 or bf16, channels contiguous; weight, bias fp32 [C]; add, scale, shift fp32 [B, C], columns of a wider tensor if they
-    are.  Returns out, contiguous, of x's shape and of `dtype` (x's type, or float32); it may be x.  Packed rows of no image
-    keep what it held."""
+    are.  Returns out, contiguous, of x's shape and of `dtype` (x's type, or float32); it may be x, and overlaps nothing else that
+    is read.  Packed rows of no image keep what it held (anything, if it is not passed)."""
     return (_hot or _load_hot()).groupnorm(x, num_groups, weight, bias, eps, act, add, scale, shift, offsets, dtype, out,
                                            workspace, stream)
 

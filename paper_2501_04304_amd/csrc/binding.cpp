@@ -803,7 +803,8 @@ PyObject *groupnorm(Args a) {
         place.same(offsets, "offsets");
         op = pointer<int32_t>(offsets), B = offsets.numel() - 1;
     }
-    const int64_t N = x.size(packed ? 0 : 1), channels = x.size(-1);
+    int64_t N = x.size(packed ? 0 : 1);
+    const int64_t channels = x.size(-1);
     if (B > INT32_MAX || channels > INT32_MAX) raise_value("x is too large");
     const int32_t C = (int32_t)channels, G = integer32(a[1]), act = integer32(a[5]), type = kv_dtype(x.scalar_type());
     const double eps = PyFloat_AsDouble(a[4]);
@@ -811,6 +812,7 @@ PyObject *groupnorm(Args a) {
     const float *wp = vector_of(a[2], "weight", C, place), *bp = vector_of(a[3], "bias", C, place);
     const Rows add(a[6], "add", B, C, place), scale(a[7], "scale", B, C, place), shift(a[8], "shift", B, C, place);
     const at::Tensor out = output(a[11], a[10], x.scalar_type(), x.sizes(), x, place, "out");
+    if (!packed && B == 0) B = 1, N = 0;  // no images are no work, like images of no rows
     at::Tensor ws;
     if (given(a[12])) {
         ws = tensor(a[12], at::kByte, "workspace");

@@ -349,6 +349,20 @@ def test_empty(dgq):
     assert dgq.dgq_groupnorm(torch.empty((0, 64), device="cuda"), 8, offsets=off).shape == (0, 64)
 
 
+@pytest.mark.parametrize("N", [0, 1, 5000])
+def test_no_images(dgq, N):
+    """No images are no work, as images of no rows are; what is wrong with the call is still refused."""
+    import torch
+    x, row = torch.empty((0, N, 64), dtype=torch.float16, device="cuda"), torch.empty((0, 64), device="cuda")
+    out = dgq.dgq_groupnorm(x, 8, torch.ones(64, device="cuda"), add=row, scale=row, dtype=torch.float32)
+    assert out.shape == (0, N, 64) and out.dtype == torch.float32
+    assert dgq.dgq_groupnorm(x, 8, out=x) is x
+    with pytest.raises(dgq.DgqError, match="multiple of G"):
+        dgq.dgq_groupnorm(x, 7)
+    with pytest.raises(ValueError, match="add"):
+        dgq.dgq_groupnorm(x, 8, add=torch.zeros((1, 64), device="cuda"))
+
+
 def test_refusals(dgq):
     import torch
     f = lambda *s, **k: torch.zeros(s, device="cuda", **k)  # noqa: E731
