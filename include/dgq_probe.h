@@ -68,6 +68,13 @@ int dgq_probe_xattn_kv_kernel(int32_t B, int64_t N, int32_t packed, int32_t Hq, 
 int dgq_probe_xattn_kv_rows(int32_t B, int64_t N, int32_t packed, int32_t Hq, int32_t H, int32_t d, int32_t width,
                             int32_t block_size);
 
+/*
+ * The kernels that dgq_groupnorm takes for these arguments (as of dgq_groupnorm_workspace_bytes; host only, for tests that mean to
+ * reach one of them): 0 sums of chunks and values, 1 those and tables between them; 10, 11, 12, 13 a workgroup to every image's
+ * group, of 256 threads with 4 vectors each or 1024 with 4, 8, 16.  DGQ_EINVAL for what is not a call.
+ */
+int dgq_probe_groupnorm_kernel(int32_t B, int64_t N, int32_t packed, int32_t C, int32_t G, int32_t dtype);
+
 #ifdef __cplusplus
 }
 #endif

@@ -282,6 +282,7 @@ struct NormCall {
     int64_t rows() const { return offsets ? N : B * N; }
 };
 size_t groupnorm_workspace_bytes(const NormCall &n);
+int groupnorm_kernel(const NormCall &n);  // as dgq_probe_groupnorm_kernel names them
 hipError_t launch_groupnorm(const NormCall &n, void *workspace, hipStream_t st);
 
 // ---- weights in 4 bits (layout in include/dgq.h, dgq_w4_bytes; k8_w4.hip) ----------------------------

@@ -608,6 +608,12 @@ size_t groupnorm_workspace_bytes(const NormCall &n) {
     return p.sums_bytes + p.tables_bytes;
 }
 
+int groupnorm_kernel(const NormCall &n) {
+    const NormPlan p(n);
+    if (!p.hold.held) return p.tables_bytes ? 1 : 0;
+    return p.hold.threads == 256 ? 10 : p.hold.held == 4 ? 11 : p.hold.held == 8 ? 12 : 13;
+}
+
 hipError_t launch_groupnorm(const NormCall &n, void *workspace, hipStream_t st) {
     const NormPlan p(n);
     const Images im{n.offsets, n.N, n.rows(), n.B};

@@ -162,4 +162,15 @@ int dgq_probe_xattn_kv_rows(int32_t B, int64_t N, int32_t packed, int32_t Hq, in
     return xattn_kv_rows(B, packed ? N : (int64_t)B * N, packed != 0, Hq, H, d, (int64_t)width * block_size);
 }
 
+int dgq_probe_groupnorm_kernel(int32_t B, int64_t N, int32_t packed, int32_t C, int32_t G, int32_t dtype) {
+    if (B < 1 || N < 1 || C < 1 || G < 1 || C % G || dtype < DGQ_F32 || dtype > DGQ_BF16) {
+        set_error("dgq_probe_groupnorm_kernel: not a call");
+        return DGQ_EINVAL;
+    }
+    static const int32_t some = 0;
+    NormCall n{};
+    n.dtype = dtype, n.offsets = packed ? &some : nullptr, n.B = B, n.N = N, n.C = C, n.G = G;
+    return groupnorm_kernel(n);
+}
+
 }  // extern "C"

@@ -98,6 +98,47 @@ def test_groups_in_several_slices_of_the_channels(dgq, B, N, C, G, dtype):
     assert (ws[-16:] == 255).all()
 
 
+# many rows that workgroups of 1024 threads just hold, in groups that end inside a vector and that do not
+HELD = [(6, 4500, 320, 32), (8, 2500, 480, 30), (192, 1500, 48, 1)]
+# packed: lengths and channels
+HELD_PACKED = [([2000, 1800, 0, 2500, 4100, 1, 900, 2700], 960, 32), ([30, 8200, 6000, 3500, 1, 0], 640, 40)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,N,C,G", HELD)
+def test_many_rows_that_a_workgroup_holds(dgq, B, N, C, G, dtype):
+    rng = np.random.default_rng(B + N)
+    x, xn = _map(rng, B * N, C, dtype)
+    t = _tables(rng, B, C, ("bias", "add", "scale"))
+    for to in sorted({dtype, "fp32"}):
+        out = dgq.dgq_groupnorm(x.view(B, N, C), G, dtype=_type(to), act=dgq.ACT_SILU, **{k: _up(v) for k, v in t.items()})
+        _check(out, *ref.groupnorm(xn, *_even(B, N), G, silu=True, out_type=to, **t))
+    kept = dgq.dgq_groupnorm(x.view(B, N, C), G)
+    assert dgq.dgq_groupnorm(x.view(B, N, C), G, out=x.view(B, N, C)).equal(kept)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lengths,C,G", HELD_PACKED)
+def test_packed_rows_of_which_a_workgroup_holds_most(dgq, lengths, C, G, dtype):
+    """Images of as many rows as a workgroup holds, fewer and more; in place and not, of x's type and fp32."""
+    import torch
+    rng = np.random.default_rng(sum(lengths))
+    B, front, behind = len(lengths), 2, 3
+    offsets = front + np.concatenate([[0], np.cumsum(lengths)])
+    rows = int(offsets[-1]) + behind
+    x, xn = _map(rng, rows, C, dtype)
+    t = _tables(rng, B, C, ("weight", "add", "shift"))
+    kw = dict(offsets=_up(offsets.astype(np.int32)), **{k: _up(v) for k, v in t.items()})
+    want = {to: ref.groupnorm(xn, offsets[:-1], offsets[1:], G, out_type=to, **t) for to in {dtype, "fp32"}}
+    for to in want:
+        out = torch.full((rows, C), 7.0, dtype=_type(to), device="cuda")
+        _check(dgq.dgq_groupnorm(x, G, out=out, **kw), *want[to])
+        assert (out[:front] == 7).all() and (out[rows - behind:] == 7).all()
+    kept = x.clone()
+    _check(dgq.dgq_groupnorm(x, G, out=x, **kw), *want[dtype])
+    assert torch.equal(x[:front], kept[:front]) and torch.equal(x[rows - behind:], kept[rows - behind:])
+
+
 def test_more_groups_than_a_launch_takes(dgq):
     """2^24 groups of 32 values, through sums of chunks: 16384 images of one row and 32768 channels."""
     import torch
