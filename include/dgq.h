@@ -693,10 +693,11 @@ typedef enum dgq_act { DGQ_ACT_NONE = 0, DGQ_ACT_SILU = 1 } dgq_act;  /* SiLU: t
  *   add, scale, shift  fp32 [B, C], channels contiguous, rows `stride` elements apart, or NULL for none
  *   workspace dgq_groupnorm_workspace_bytes(...) bytes, 16-byte aligned (0 bytes: NULL): sums and tables, written before they are
  *             read; this call's alone until it is done
- * Sums are in 64 bits and in an order of the call's sizes, x' - m is taken before it is rounded: the same call gives the same bits,
- * and a map whose mean is thousands of times its deviation loses nothing to that.  NaN or infinity stays in its image and
- * group, all of whose values become NaN.  A group of one value, or of equal ones, gives its bias (eps above 0).
- * C a multiple of G, at most 2^20; B 1 to 65535.  Enqueues on `stream`; neither synchronises nor allocates.
+ * Sums are in 64 bits and in an order of the call's sizes, x' - m is taken before it is rounded: the same call gives the same
+ * bits, and a map whose mean is thousands of times its deviation loses nothing to that.  NaN or infinity stays in its image and
+ * group, all of whose values become NaN.  A group of one value, or of equal ones, gives its bias (eps above 0). Packed images may
+ * differ in length, and are fastest if they do not differ by far: one that holds nearly all rows of many takes several times as
+ * long as even ones.  C a multiple of G, at most 2^20; B 1 to 65535.  Enqueues on `stream`; neither synchronises nor allocates.
  */
 size_t dgq_groupnorm_workspace_bytes(int32_t B, int64_t N, int32_t packed, int32_t C, int32_t G, int32_t dtype);
 int dgq_groupnorm(const void *x, int32_t dtype, int64_t x_batch_stride, int64_t x_row_stride, const int32_t *offsets,

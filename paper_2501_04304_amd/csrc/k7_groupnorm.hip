@@ -194,9 +194,9 @@ struct RowsOf {
 };
 
 // Bound by the bytes of x, and for small maps by the way from the kernel's arguments over x and LDS to the sums (4.7 us for 2 x
-// 4096 x 320, of which the rows take 2.5).  add enters per channel: sum x' = sum x + n add, sum x'^2 = sum x^2 + 2 add sum x + n add^2.
-// 16 x 4096 x 640 fp32: 30 us, 5.6 TB/s.  sums: [G][parts][met] double2, met: slices that a group's channels may lie in, that of its first
-// channel first, 0 for those that they do not.
+// 4096 x 320, of which the rows take 2.5).  add enters per channel: sum x' = sum x + n add, sum x'^2 = sum x^2 + 2 add sum x + n
+// add^2. 16 x 4096 x 640 fp32: 30 us, 5.6 TB/s.  sums: [G][parts][met] double2, met: slices that a group's channels may lie in,
+// that of its first channel first, 0 for those that they do not.
 template <class T>
 __global__ __launch_bounds__(kMaxThreads) void k_gn_sums(const T *__restrict__ x, Images im, Rows xs, Chunks ch, Shape sh, int32_t C,
                                                          int32_t G, const float *__restrict__ add, int64_t add_row,
@@ -539,11 +539,15 @@ Chunks chunks_for(const NormCall &n, const Shape &sh) {
 constexpr int64_t kMaxFolded = 16384;  // sums of an image that every workgroup may read
 
 // Whether a workgroup can hold an image's group, and how: threads and vectors of each (0: it cannot, or is slower).  Many values
-// keep its vector pipes busy and need most CUs to keep up: 2 x 1024 x 1280 fp32 10.7 us, 14.1 with sums of chunks, but 2 x 4096 x
-// 320 16.7 and 13.9, 4 x 4096 x 320 18.3 and 16.8.  A group's stripe of the rows touches lines of memory that others touch too,
-// and no access of it can go past the caches: large maps of stripes below a line or two are faster in chunks (16 x 4096 x 320 fp32 63
-// and 44, 16 x 4096 x 640 bf16 67 and 49, 32 x 1024 x 320 bf16 22.8 and 19.7; 16 x 1024 x 640 fp32 22 and 25, 32 x 1024 x 1280 83
-// and 90).  A launch has fewer than 2^32 threads: what needs more (2^24 groups of 256 threads, 2^22 of 1024) is cut in chunks too.
+// keep its vector pipes busy and need most CUs to keep up: 2 x 1024 x 1280 fp32 10.7 us, 14.1 with sums of chunks, but 2 x 4096
+// x 320 16.7 and 13.9, 4 x 4096 x 320 18.3 and 16.8.  A group's stripe of the rows touches lines of memory that others touch
+// too, and no access of it can go past the caches: large maps of stripes below a line or two are faster in chunks (16 x 4096 x
+// 320 fp32 63 and 44, 16 x 4096 x 640 bf16 67 and 49, 32 x 1024 x 320 bf16 22.8 and 19.7; 16 x 1024 x 640 fp32 22 and 25, 32 x
+// 1024 x 1280 83 and 90).  Of packed images the host knows the rows of all, so a long one is taken to have 1.5 times the mean's;
+// what a thread does not hold it reads twice, and a much longer image keeps 32 workgroups busy while the others are done (8
+// images x 960 bf16, 16384 rows: even ones 37.5 us, nearly all in one 298; in chunks 39 and 60.  But chunks take some 10 us for
+// every image in them: 16 x 1024 x 1280 fp32 40 and 52, 65535 images x 16 rows x 64 channels in one group 183 and 1794).  A
+// launch has fewer than 2^32 threads: what needs more (2^24 groups of 256 threads, 2^22 of 1024) is cut in chunks too.
 struct Hold {
     int32_t threads = 0, held = 0, width = 0;
 };

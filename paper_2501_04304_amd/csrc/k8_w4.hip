@@ -149,11 +149,12 @@ __global__ __launch_bounds__(256) void k_w4_unpack(W4 m, T *__restrict__ w, bool
 //   y[m, o] = sum_g s (sum_{k in g} x[m, k] (code - zero))
 // on the matrix cores, 16 rows of x by 16 outputs by 32 inputs, in fp16.  A nibble below the exponent of 1024 is 1024 + code (at
 // bits 0 .. 3) or 1024 + 16 code (at 4 .. 7), less 1024 + zero or times 1/16 less 64 + zero it is code - zero, exactly: nine
-// instructions for eight codes.  Rows of fp16 are what they are; those of bf16 and fp32 are taken a unit (128 inputs) at a time by
-// a power of two that brings its largest to 2^14 .. 2^15, bf16 as one fp16, fp32 as two (x = h + l, each rounded to nearest: off by
-// 2^-23 x at most).  l is kept 2^12 times as large, which brings it up to 2^15 too, and has sums of its own: at h's scale it would
-// leave fp16's normal numbers 2^16 below the unit's largest (2 % of the time, 5 % at groups of 32).  What lies more than 2^28
-// below that loses bits, fp32 to 2^-51 of it, bf16 to 2^-39.  The groups' sums meet in fp32 with their scales and those powers.
+// instructions for eight codes (Kim et al., arXiv 2211.10017, with the zeros folded in).  Rows of fp16 are what they are; those
+// of bf16 and fp32 are taken a unit (128 inputs) at a time by a power of two that brings its largest to 2^14 .. 2^15, bf16 as
+// one fp16, fp32 as two (x = h + l, each rounded to nearest: off by 2^-23 x at most).  l is kept 2^12 times as large, which
+// brings it up to 2^15 too, and has sums of its own: at h's scale it would leave fp16's normal numbers 2^16 below the unit's
+// largest (2 % of the time, 5 % at groups of 32).  What lies more than 2^28 below that loses bits, fp32 to 2^-51 of it, bf16 to
+// 2^-39.  The groups' sums meet in fp32 with their scales and those powers.
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef float float2v __attribute__((ext_vector_type(2)));
@@ -238,12 +239,12 @@ struct Cut {
     int32_t tiles, shares, splits, chunk, row_shift;
 };
 
-// Bound by the bytes of the weights (1 x 8192 -> 28672 bf16 23.8 us, 5.2 TB/s; a read of as many bytes takes 21) and, from 16 rows
-// on, by the vector pipes: 55 instructions to a unit of one tile beside four matrix instructions (eight for fp32), 130 (bf16) or
-// 200 (fp32) to bring 16 rows of a unit into fp16, once for all tiles of a workgroup.  A wavefront's next kAhead units are on
-// their way while it works on as many, and the rows of the next chunk while all work on this one.  Small products are bound by
-// latency: 2 x 320 -> 1280 5.1 us, 32 x 1280 -> 16640 fp32 11.5 (rows 2, their conversion 2, ten units a wavefront 3.5, the slowest
-// SIMD 2.6, the sums 1).
+// Bound by the bytes of the weights (1 x 8192 -> 28672 bf16 23.8 us, 5.2 TB/s; a read of as many bytes takes 21) and, from 16
+// rows on, by the vector pipes: 55 instructions to a unit of one tile beside four matrix instructions (fp32: 4 more a group, and
+// eight), 130 (bf16) or 230 (fp32) to bring 16 rows of a unit into fp16, once for all tiles of a workgroup.  A wavefront's next
+// kAhead units are on their way while it works on as many, and the rows of the next chunk while all work on this one.  Small
+// products are bound by latency: 2 x 320 -> 1280 5.1 us, 32 x 1280 -> 16640 fp32 11.8 (rows 2, their conversion 2, ten units a
+// wavefront 3.8, the slowest SIMD 2.6, the sums 1).
 // kAhead: 8 x 4096 -> 11000 bf16 11.3 us with two, 11.8 with three, 12.4 with four; 1 x 8192 -> 28672 fp16 23.6, 22.5 and 22.6.
 template <int J, bool ONCE>
 constexpr int kAhead = ONCE && J > 1 ? 3 : 2;
@@ -451,7 +452,8 @@ Ways ways_for(int32_t M, int32_t R, int32_t T, int most) {
         if (cost < least) least = cost, tiles = t;
     }
     while (shares * 2 * tiles <= (M > 4 ? most : 12) && shares * 2 <= std::min(T, M > 4 && T > 24 ? 4 : 8)) shares *= 2;
-    if (M > 4 && T <= 10 && tiles > 1 && tiles * shares < T) tiles = (T + shares - 1) / shares;  // one conversion for all units
+    // one conversion for all units (10: the most that was measured)
+    if (M > 4 && T <= 10 && tiles > 1 && tiles * shares < T) tiles = (T + shares - 1) / shares;
     if (all < 128 && T >= (M > 4 ? 20 : 48)) {
         splits = (int)(M > 4 ? std::min<int64_t>(512 / all, T / 6) : std::min<int64_t>(256 / all, T / 10));
         for (shares = 1; shares * 2 <= (M > 4 ? 4 : 8) && shares * 2 * splits <= T;) shares *= 2;

@@ -53,7 +53,7 @@ __device__ inline void store_past(T *to, int have, const float (&f)[V]) {
 }
 
 // t / (1 + exp(-t)) with the hardware's 2^x and 1 / x, good to one unit in the last place each; the exponent's own rounding adds
-// |t| 2^-24.
+// |t| 2^-24.  Below -87.3, where 1 / x would be below 2^-126, it may be 0 for what is there up to 10^-36.
 __device__ inline float silu(float t) {
     return t * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t * -1.44269504088896341f));
 }
